@@ -223,6 +223,114 @@ typedef struct {
 int ftp_profile(ftp_plan_t* plan, int32_t enable);
 int ftp_profile_read(ftp_plan_t* plan, ftp_kernel_time* out, int32_t capacity, int32_t* count);
 
+/* ---- operators of a token block ------------------------------------------------------------------------------------
+ * What follows the early layers when their output map's pixels become the tokens of an attention block, and what keeps
+ * such a block's training in little memory: layer norm, softmax attention whose backward pass recomputes the
+ * probabilities, activations kept in 8 bits between the forward and the backward pass.
+ *
+ * No plan: a call takes a description of its shape (host), device pointers and the stream.  Strides are in elements.
+ * The calls allocate nothing, are asynchronous on `stream`, start no other stream and never wait, so they can be captured
+ * into a HIP graph; scratch comes from the caller (the _workspace queries, bytes; 256-byte aligned; its contents need not
+ * be kept or cleared).  Outputs must not overlap inputs unless stated.  Every sum runs in 32 bits and in a fixed order:
+ * equal calls give equal bits.  Sizes of zero are valid where stated and launch nothing that reads. */
+
+/* Layer norm over the channels of outer x inner tokens: mean and biased variance of each token's channels,
+ * y = (x - mean) * rstd * gamma + beta, rstd = 1 / sqrt(variance + eps).  Element (o, i, c) of x lies at
+ * x_stride[0] * o + x_stride[1] * i + x_stride[2] * c, so token rows and NCHW maps (outer = images, inner = pixels,
+ * stride 1 along the pixels) both are read and written as they lie; from map to rows too.  outer or inner may be 0;
+ * outer * inner is at most 2^31 - 1. */
+typedef struct {
+    int64_t outer, inner;
+    int32_t channels;              /* >= 1; at most 4096 unless all tensors of a pass have channel stride 1 */
+    int32_t dtype;                 /* ftp_dtype of x, y, gamma, beta, dy, dx */
+    float eps;
+    int32_t reserved;
+    int64_t x_stride[3], y_stride[3];     /* outer, inner, channel; 0: broadcast (inputs only) */
+    int64_t dy_stride[3], dx_stride[3];   /* backward pass only (y_stride is not used there) */
+} ftp_norm_shape;
+
+/* gamma, beta: [channels] or null (1 and 0).  mean, rstd: fp32 [outer][inner], or null if no backward pass follows. */
+int ftp_norm_forward(const ftp_norm_shape* shape, const void* x, const void* gamma, const void* beta, void* y,
+                     float* mean, float* rstd, void* stream);
+
+/* Bytes of scratch of ftp_norm_backward. */
+int ftp_norm_workspace(const ftp_norm_shape* shape, size_t* bytes);
+
+/* dx (may be dy itself, with the same strides), dgamma and dbeta (fp32 [channels], both or neither null).
+ * x is given either as itself (codes = exponents = null) or as an 8-bit checkpoint of its tokens (x = null; codes
+ * [outer * inner][channels] with blocks of `block` channels, see ftp_checkpoint_pack; x_stride is not used, and dy and dx have
+ * channel stride 1).  mean, rstd as the forward pass left them. */
+int ftp_norm_backward(const ftp_norm_shape* shape, const void* dy, const void* x, const int8_t* codes,
+                      const int8_t* exponents, int32_t block, const void* gamma, const float* mean, const float* rstd,
+                      void* dx, float* dgamma, float* dbeta, void* workspace, void* stream);
+
+/* Activations in 8 bits.  A row of `cols` values is cut into blocks of `block` neighbours (the last one may be shorter);
+ * a block has one exponent e, the smallest whole number >= -126 with |x| <= 127 * 2^e for all its values, and each value the
+ * code q = x / 2^e rounded to the nearest whole number, ties to even; it stands for q * 2^e, which fp32 and bfloat hold
+ * exactly.  (At e = 122 codes stop at +-63, so that none stands for more than the largest finite number.)  A block that
+ * holds an infinity or a NaN has e = 127 and codes 0 and stands for NaN in all its places.  rows may be 0. */
+typedef struct {
+    int64_t rows;
+    int64_t cols;                  /* 1 .. 2^30 */
+    int64_t stride;                /* elements between rows of the caller's tensors (x, dy, dx), >= cols */
+    int32_t block;                 /* 32, 64, 128 or 256 */
+    int32_t dtype;                 /* ftp_dtype of the caller's tensors */
+} ftp_checkpoint_shape;
+
+typedef enum { FTP_ACT_NONE = 0, FTP_ACT_LEAKY = 1, FTP_ACT_GELU = 2, FTP_ACT_SILU = 3 } ftp_act;
+
+/* codes: [rows][cols] contiguous; exponents: [rows][ceil(cols / block)]. */
+int ftp_checkpoint_pack(const ftp_checkpoint_shape* shape, const void* x, int8_t* codes, int8_t* exponents, void* stream);
+
+/* out = act(value): leaky ReLU with `slope`, GELU x * Phi(x), SiLU x / (1 + exp(-x)). */
+int ftp_checkpoint_unpack(const ftp_checkpoint_shape* shape, const int8_t* codes, const int8_t* exponents, int32_t act,
+                          float slope, void* out, void* stream);
+
+/* dx = dy * act'(value); dx may be dy itself. */
+int ftp_checkpoint_act_backward(const ftp_checkpoint_shape* shape, const int8_t* codes, const int8_t* exponents,
+                                int32_t act, float slope, const void* dy, void* dx, void* stream);
+
+/* Bytes of scratch of ftp_checkpoint_wgrad for `outputs` columns of dy. */
+int ftp_checkpoint_workspace(const ftp_checkpoint_shape* shape, int32_t outputs, size_t* bytes);
+
+/* dw[n][k] = sum over rows of dy[row][n] * value[row][k], fp32 [outputs][cols]: the weight gradient of a linear layer whose
+ * input was kept.  dy: [rows][outputs] with `dy_stride` elements between rows (shape->stride is not used). */
+int ftp_checkpoint_wgrad(const ftp_checkpoint_shape* shape, const int8_t* codes, const int8_t* exponents, const void* dy,
+                         int64_t dy_stride, int32_t outputs, float* dw, void* workspace, void* stream);
+
+/* Softmax attention: out[i] = sum over the keys j that query i sees of softmax_j(scale * q[i] . k[j]) v[j], for `heads` heads that
+ * share the keys and values of heads / kv_heads neighbours.  Image b has q_lens[b] queries and kv_lens[b] keys (null: q_len, kv_len; values outside
+ * 0 .. q_len / kv_len are cut to that); query i sees the keys j < kv_lens[b], and with `causal` only
+ * j <= i + kv_lens[b] - q_lens[b] (the last query sees the last key).  A query that sees no key, and one beyond
+ * q_lens[b], has out = 0, lse = -infinity and dq = 0; a key that no query sees has dk = dv = 0.  Keys, values and queries
+ * that are not seen do not reach any result, whatever they hold.
+ * Element (b, t, h, c) of q lies at q_stride[0] * b + q_stride[1] * t + q_stride[2] * h + c; likewise the others.  Inputs may
+ * be broadcast (stride 0); gradients then come out unsummed, in buffers of their own.  q_len and kv_len may be 0. */
+typedef struct {
+    int32_t batch, heads, kv_heads;     /* kv_heads divides heads */
+    int32_t q_len, kv_len;
+    int32_t head_dim;                   /* 1 .. 128 */
+    int32_t dtype;                      /* ftp_dtype of all tensors but lse */
+    int32_t causal;
+    float scale;                        /* finite */
+    int32_t reserved;
+    int64_t q_stride[3], k_stride[3], v_stride[3], out_stride[3];          /* image, token, head */
+    int64_t dout_stride[3], dq_stride[3], dk_stride[3], dv_stride[3];      /* backward pass only */
+} ftp_attention_shape;
+
+/* Bytes of scratch of the two passes (either pointer may be null). */
+int ftp_attention_workspace(const ftp_attention_shape* shape, size_t* forward_bytes, size_t* backward_bytes);
+
+/* lse: fp32 [batch][heads][q_len], the logarithm of the sum of the exponentials; null if no backward pass follows. */
+int ftp_attention_forward(const ftp_attention_shape* shape, const void* q, const void* k, const void* v,
+                          const int32_t* q_lens, const int32_t* kv_lens, void* out, float* lse, void* workspace,
+                          void* stream);
+
+/* out, lse: as the forward pass left them.  The probabilities are computed again from q, k and lse. */
+int ftp_attention_backward(const ftp_attention_shape* shape, const void* dout, const void* q, const void* k, const void* v,
+                           const int32_t* q_lens, const int32_t* kv_lens, const void* out, const float* lse,
+                           void* dq, void* dk, void* dv, void* workspace, void* stream);
+
 const char* ftp_strerror(int code);
 
 /* hipError_t value of the last failed HIP call on this thread (0 if none). */

@@ -31,6 +31,28 @@ class ftp_kernel_time(ctypes.Structure):
                 ("executed_flops_per_launch", ctypes.c_double)]
 
 
+FTP_ACT_NONE, FTP_ACT_LEAKY, FTP_ACT_GELU, FTP_ACT_SILU = 0, 1, 2, 3
+
+_I64x3 = ctypes.c_int64 * 3
+
+
+class ftp_norm_shape(ctypes.Structure):
+    _fields_ = [("outer", ctypes.c_int64), ("inner", ctypes.c_int64), ("channels", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("eps", ctypes.c_float), ("reserved", ctypes.c_int32), ("x_stride", _I64x3), ("y_stride", _I64x3),
+                ("dy_stride", _I64x3), ("dx_stride", _I64x3)]
+
+
+class ftp_checkpoint_shape(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("stride", ctypes.c_int64), ("block", ctypes.c_int32),
+                ("dtype", ctypes.c_int32)]
+
+
+class ftp_attention_shape(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("batch", "heads", "kv_heads", "q_len", "kv_len", "head_dim", "dtype", "causal")] + [
+        ("scale", ctypes.c_float), ("reserved", ctypes.c_int32)] + [
+        (n + "_stride", _I64x3) for n in ("q", "k", "v", "out", "dout", "dq", "dk", "dv")]
+
+
 PASS_NAMES = {0: "conv_fwd", 1: "conv_bwd_data", 2: "wgrad", 3: "reduce", 4: "pool_fwd", 5: "pool_bwd", 6: "scale_dy", 7: "update", 8: "wgrad_sum"}
 
 
@@ -41,6 +63,11 @@ class FtpError(RuntimeError):
         if code == FTP_EHIP:
             msg += " (hipError %d)" % _lib.ftp_last_hip_error()
         super().__init__("%s: %s [%d]" % (where, msg, code))
+
+
+TOKEN_EXPORTS = ("ftp_norm_forward", "ftp_norm_workspace", "ftp_norm_backward", "ftp_checkpoint_pack", "ftp_checkpoint_unpack",
+                 "ftp_checkpoint_act_backward", "ftp_checkpoint_workspace", "ftp_checkpoint_wgrad", "ftp_attention_workspace",
+                 "ftp_attention_forward", "ftp_attention_backward")
 
 
 def _load():
@@ -80,12 +107,24 @@ def _load():
     lib.ftp_profile.argtypes = [vp, i32]
     lib.ftp_set_overlap.argtypes = [vp, i32]
     lib.ftp_profile_read.argtypes = [vp, ctypes.POINTER(ftp_kernel_time), i32, ctypes.POINTER(i32)]
+    ns, cs, ats, psz = (ctypes.POINTER(t) for t in (ftp_norm_shape, ftp_checkpoint_shape, ftp_attention_shape, sz))
+    lib.ftp_norm_forward.argtypes = [ns] + [vp] * 7
+    lib.ftp_norm_workspace.argtypes = [ns, psz]
+    lib.ftp_norm_backward.argtypes = [ns, vp, vp, vp, vp, i32] + [vp] * 8
+    lib.ftp_checkpoint_pack.argtypes = [cs, vp, vp, vp, vp]
+    lib.ftp_checkpoint_unpack.argtypes = [cs, vp, vp, i32, ctypes.c_float, vp, vp]
+    lib.ftp_checkpoint_act_backward.argtypes = [cs, vp, vp, i32, ctypes.c_float, vp, vp, vp]
+    lib.ftp_checkpoint_workspace.argtypes = [cs, i32, psz]
+    lib.ftp_checkpoint_wgrad.argtypes = [cs, vp, vp, vp, ctypes.c_int64, i32, vp, vp, vp]
+    lib.ftp_attention_workspace.argtypes = [ats, psz, psz]
+    lib.ftp_attention_forward.argtypes = [ats] + [vp] * 9
+    lib.ftp_attention_backward.argtypes = [ats] + [vp] * 13
     lib.ftp_strerror.argtypes = [ctypes.c_int]
     lib.ftp_strerror.restype = ctypes.c_char_p
     lib.ftp_last_hip_error.restype = ctypes.c_int
     lib.ftp_joint_launches.restype = ctypes.c_longlong
     for f in ("ftp_profile", "ftp_profile_read", "ftp_set_overlap", "ftp_plan_buffer", "ftp_plan_rect", "ftp_plan_map_shape", "ftp_plan_sizes", "ftp_plan_work", "ftp_forward",
-              "ftp_forward_static", "ftp_backward", "ftp_reduce_wgrad", "ftp_sgd_step"):
+              "ftp_forward_static", "ftp_backward", "ftp_reduce_wgrad", "ftp_sgd_step") + TOKEN_EXPORTS:
         getattr(lib, f).restype = ctypes.c_int
     return lib
 
@@ -94,7 +133,7 @@ _lib = _load()
 
 EXPORTS = ("ftp_profile", "ftp_profile_read", "ftp_set_overlap", "ftp_plan", "ftp_plan_destroy", "ftp_plan_buffer", "ftp_plan_rect", "ftp_plan_map_shape", "ftp_plan_sizes", "ftp_plan_work",
            "ftp_forward", "ftp_forward_static", "ftp_backward", "ftp_reduce_wgrad", "ftp_sgd_step", "ftp_strerror", "ftp_last_hip_error",
-           "ftp_joint_launches")
+           "ftp_joint_launches") + TOKEN_EXPORTS
 
 
 def _check(rc, where):
@@ -211,6 +250,59 @@ def ftp_profile_read(plan, capacity=256):
              "flops_per_launch": r.flops_per_launch, "bytes_per_launch": r.bytes_per_launch,
              "kernel": r.kernel.decode(), "executed_flops_per_launch": r.executed_flops_per_launch}
             for r in out[:min(n.value, capacity)]]
+
+
+# ---- operators of a token block; `shape` is the structure of the same name, device pointers and the stream are integers ----
+def ftp_norm_forward(shape, x, gamma, beta, y, mean=0, rstd=0, stream=0):
+    _check(_lib.ftp_norm_forward(shape, x, gamma, beta, y, mean, rstd, stream), "ftp_norm_forward")
+
+
+def ftp_norm_workspace(shape):
+    n = ctypes.c_size_t()
+    _check(_lib.ftp_norm_workspace(shape, n), "ftp_norm_workspace")
+    return n.value
+
+
+def ftp_norm_backward(shape, dy, x, codes, exponents, block, gamma, mean, rstd, dx, dgamma, dbeta, workspace, stream=0):
+    _check(_lib.ftp_norm_backward(shape, dy, x, codes, exponents, block, gamma, mean, rstd, dx, dgamma, dbeta, workspace, stream),
+           "ftp_norm_backward")
+
+
+def ftp_checkpoint_pack(shape, x, codes, exponents, stream=0):
+    _check(_lib.ftp_checkpoint_pack(shape, x, codes, exponents, stream), "ftp_checkpoint_pack")
+
+
+def ftp_checkpoint_unpack(shape, codes, exponents, act, slope, out, stream=0):
+    _check(_lib.ftp_checkpoint_unpack(shape, codes, exponents, act, slope, out, stream), "ftp_checkpoint_unpack")
+
+
+def ftp_checkpoint_act_backward(shape, codes, exponents, act, slope, dy, dx, stream=0):
+    _check(_lib.ftp_checkpoint_act_backward(shape, codes, exponents, act, slope, dy, dx, stream), "ftp_checkpoint_act_backward")
+
+
+def ftp_checkpoint_workspace(shape, outputs):
+    n = ctypes.c_size_t()
+    _check(_lib.ftp_checkpoint_workspace(shape, outputs, n), "ftp_checkpoint_workspace")
+    return n.value
+
+
+def ftp_checkpoint_wgrad(shape, codes, exponents, dy, dy_stride, outputs, dw, workspace, stream=0):
+    _check(_lib.ftp_checkpoint_wgrad(shape, codes, exponents, dy, dy_stride, outputs, dw, workspace, stream), "ftp_checkpoint_wgrad")
+
+
+def ftp_attention_workspace(shape):
+    f, b = ctypes.c_size_t(), ctypes.c_size_t()
+    _check(_lib.ftp_attention_workspace(shape, f, b), "ftp_attention_workspace")
+    return f.value, b.value
+
+
+def ftp_attention_forward(shape, q, k, v, q_lens, kv_lens, out, lse, workspace, stream=0):
+    _check(_lib.ftp_attention_forward(shape, q, k, v, q_lens, kv_lens, out, lse, workspace, stream), "ftp_attention_forward")
+
+
+def ftp_attention_backward(shape, dout, q, k, v, q_lens, kv_lens, out, lse, dq, dk, dv, workspace, stream=0):
+    _check(_lib.ftp_attention_backward(shape, dout, q, k, v, q_lens, kv_lens, out, lse, dq, dk, dv, workspace, stream),
+           "ftp_attention_backward")
 
 
 def ftp_strerror(code):

@@ -2,6 +2,7 @@
 #include "ftp.h"
 #include "ftp_plan.h"
 #include "ftp_launch.h"
+#include "ftp_tokens.h"
 
 #include <algorithm>
 #include <cstdlib>
@@ -673,6 +674,14 @@ long long ftp_joint_launches(void) { return g_joint_launches; }
 namespace ftp {
 
 thread_local const char* g_kernel_label = "";
+
+int launched()
+{
+    const hipError_t e = hipGetLastError();
+    if (e == hipSuccess) return FTP_OK;
+    g_last_hip = (int)e;
+    return FTP_EHIP;
+}
 
 Profiler::event_t Profiler::get()
 {

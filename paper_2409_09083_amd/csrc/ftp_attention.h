@@ -1,0 +1,278 @@
+// What the attention kernels share: operands of the matrix cores from LDS and registers, staging of tiles, which query sees which key.
+//
+// The queries of the heads that share a key head are rows of one list: row r is query r / group of head r % group of those.  A tile of keys is
+// then read once for the whole group, gradients of shared keys need no sum over heads, and one query of a long cache still fills rows.
+//
+// All products run on 32x32 blocks: bfloats 16 deep (v_mfma_f32_32x32x16_bf16), fp32 numbers 2 deep (v_mfma_f32_32x32x2_f32, eight of them in the bfloat one's place).  A lane holds of
+// an operand the 8 values (index lane % 32; contraction 8 h + j, h = lane / 32, j < 8), and of a result column lane % 32 and rows 8 (i / 4) + 4 h + i % 4, i < 16.
+// The contraction may run over any order that both operands share.  So a result is the next product's operand as it lies: its registers 8 s .. 8 s + 7 are the operand
+// (index lane % 32; contraction 16 s + 8 (j / 4) + 4 h + j % 4), and the other operand is loaded in that order.  No probability passes through LDS.
+#pragma once
+#include "ftp_tokens.h"
+#include "ftp_order.h"
+
+namespace ftp {
+
+typedef __bf16 b16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x8 __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+template <typename T> struct FragOf { typedef b16x8 type; };
+template <> struct FragOf<float> { typedef f32x8 type; };
+
+__device__ __forceinline__ f32x16 mma(b16x8 a, b16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x16 mma(f32x8 a, f32x8 b, f32x16 c)
+{
+#pragma unroll
+    for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b[j], c, 0, 0, 0);
+    return c;
+}
+
+// Registers 8 s .. 8 s + 7 of a result as an operand: rounded to bfloats where the operands are bfloats (the probabilities and their gradients lose
+// what the inputs have lost already; sums stay fp32).
+template <typename T>
+__device__ __forceinline__ typename FragOf<T>::type operand(const f32x16& v, int s)
+{
+    if constexpr (sizeof(T) == 4) {
+        f32x8 r;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) r[j] = v[8 * s + j];
+        return r;
+    } else {
+        u32x4 r;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) r[j] = pack_bf16(v[8 * s + 2 * j], v[8 * s + 2 * j + 1]);
+        return __builtin_bit_cast(b16x8, r);
+    }
+}
+
+// A tile of rows of D channels in LDS, in chunks of 16 bytes.  Chunks are exchanged within a row by the row's low bits, so that neither 16 rows of one chunk (operand along the channels) nor the
+// transposing load's 4 rows x 64 bytes meet on the 64 banks.
+template <typename T, int D>
+struct Tile {
+    static constexpr int kEl = 16 / (int)sizeof(T), kChunks = D / kEl, kRow = D * (int)sizeof(T);
+    static __device__ __forceinline__ int mix(int row)
+    {
+        if constexpr (sizeof(T) == 4) return D == 32 ? (row >> 1) & 7 : row & 15;
+        else return D == 32 ? (row >> 2) & 3 : D == 64 ? ((row & 2) << 1) | ((row >> 2) & 3) : ((row & 3) << 2) | ((row >> 2) & 3);
+    }
+    static __device__ __forceinline__ int at(int row, int chunk) { return row * kRow + ((chunk ^ mix(row)) << 4); }
+
+    // operand (index: row row0 + lane % 32; contraction: channels 16 s + 8 h + j)
+    static __device__ __forceinline__ typename FragOf<T>::type along(const char* t, int row0, int s)
+    {
+        const int l = threadIdx.x & 63, row = row0 + (l & 31), h = l >> 5;
+        if constexpr (sizeof(T) == 4) {
+            const f32x4 a = *(const f32x4*)(t + at(row, 4 * s + 2 * h)), b = *(const f32x4*)(t + at(row, 4 * s + 2 * h + 1));
+            return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+        } else {
+            return *(const b16x8*)(t + at(row, 2 * s + h));
+        }
+    }
+    // operand (index: channel d0 + lane % 32; contraction: rows row0 + 8 (j / 4) + 4 h + j % 4)
+    static __device__ __forceinline__ typename FragOf<T>::type across(const char* t, int row0, int d0)
+    {
+        const int l = threadIdx.x & 63, h = l >> 5;
+        if constexpr (sizeof(T) == 4) {
+            const int d = d0 + (l & 31);
+            f32x8 r;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) r[j] = *(const float*)(t + at(row0 + 8 * (j >> 2) + 4 * h + (j & 3), d >> 2) + (d & 3) * 4);
+            return r;
+        } else {
+            // each 16 lanes: 4 rows x 16 channels, lane i brings 8 bytes of row i / 4 and takes channel i of the four rows
+            const int i = l & 15, col = d0 + (l & 16) + (i & 3) * 4;
+            s16x4 v[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+                v[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                    (s16x4 __attribute__((address_space(3)))*)(t + at(row0 + 8 * j + 4 * h + (i >> 2), col >> 3) + (col & 7) * 2));
+            return __builtin_bit_cast(b16x8, __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7));
+        }
+    }
+};
+
+// The 16 bytes of channels [d0, d0 + 16 / sizeof(T)) of a row; zero past channel d.  vec: addresses allow one load (and d is whole chunks).
+template <typename T>
+__device__ __forceinline__ u32x4 chunk_of(const T* row, int d0, int d, bool vec)
+{
+    constexpr int E = 16 / (int)sizeof(T);
+    u32x4 r = {0, 0, 0, 0};
+    if (vec) {
+        if (d0 < d) r = *(const u32x4*)(row + d0);
+        return r;
+    }
+#pragma unroll
+    for (int j = 0; j < E; ++j) {
+        if (d0 + j >= d) continue;
+        if constexpr (sizeof(T) == 4) r[j] = __float_as_uint(row[d0 + j]);
+        else r[j >> 1] |= (uint32_t)row[d0 + j] << (16 * (j & 1));
+    }
+    return r;
+}
+
+// Part of a tile of ROWS rows on its way through the registers of the workgroup's 256 threads.  row(i): address of row i, or null: zeros.
+template <typename T, int D, int ROWS>
+struct Staged {
+    typedef Tile<T, D> L;
+    static constexpr int kAll = ROWS * L::kChunks, kEach = (kAll + 255) / 256;
+    static_assert(kAll % 256 == 0 || kEach == 1, "whole chunks a thread");
+    u32x4 r[kEach];
+    template <class Row>
+    __device__ __forceinline__ void fetch(Row row, int d, bool vec)
+    {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int u = threadIdx.x + 256 * i;
+            const T* p = kAll < 256 && u >= kAll ? nullptr : row(u / L::kChunks);
+            r[i] = u32x4{0, 0, 0, 0};
+            if (p) r[i] = chunk_of(p, (u % L::kChunks) * L::kEl, d, vec);
+        }
+    }
+    __device__ __forceinline__ void put(char* t) const
+    {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int u = threadIdx.x + 256 * i;
+            if (kAll < 256 && u >= kAll) continue;
+            *(u32x4*)(t + L::at(u / L::kChunks, u % L::kChunks)) = r[i];
+        }
+    }
+};
+
+// Operands (index: this lane's row; contraction: channels 16 s + 8 h + j) straight from memory; row null: zeros.
+template <typename T, int D>
+__device__ __forceinline__ void row_operands(typename FragOf<T>::type (&f)[D / 16], const T* row, int d, bool vec, bool negate)
+{
+    const int h = (threadIdx.x >> 5) & 1;
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s) {
+        u32x4 w[sizeof(T) / 2];
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
+            w[i] = u32x4{0, 0, 0, 0};
+            if (row) w[i] = chunk_of(row, 16 * s + 8 * h + 4 * i, d, vec);
+            if (negate) w[i] ^= sizeof(T) == 4 ? 0x80000000u : 0x80008000u;
+        }
+        __builtin_memcpy(&f[s], w, sizeof(f[s]));
+    }
+}
+
+// v of the other half's lane with the same lane % 32, combined with f: both halves get the result.
+template <class F>
+__device__ __forceinline__ float across_halves(float v, F f)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return f(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float both_sum(float v) { return across_halves(v, [](float a, float b) { return a + b; }); }
+__device__ __forceinline__ float both_max(float v) { return across_halves(v, [](float a, float b) { return fmaxf(a, b); }); }
+
+// Four neighbouring channels d0 .. d0 + 3 of a row, those below d.
+template <typename T>
+__device__ __forceinline__ void store4(T* row, int d0, int d, bool vec, float a, float b, float c, float e)
+{
+    if (vec) {
+        if (d0 >= d) return;
+        if constexpr (sizeof(T) == 4) *(f32x4*)(row + d0) = f32x4{a, b, c, e};
+        else *(uint2*)(row + d0) = uint2{pack_bf16(a, b), pack_bf16(c, e)};
+        return;
+    }
+    if (d0 < d) st(row + d0, a);
+    if (d0 + 1 < d) st(row + d0 + 1, b);
+    if (d0 + 2 < d) st(row + d0 + 2, c);
+    if (d0 + 3 < d) st(row + d0 + 3, e);
+}
+
+struct AttentionArgs {
+    const void* q; const void* k; const void* v; const int* q_lens; const int* kv_lens;
+    void* out; float* lse; float* ws;
+    const void* dout; void* dq; void* dk; void* dv; float* delta;
+    long long qs[3], ks[3], vs[3], os[3], gs[3], dqs[3], dks[3], dvs[3];
+    int batch, heads, kv, group, q_len, kv_len, d, causal, vec;
+    int blocks, splits, groups, by_xcd;             // workgroups: blocks of rows (keys) x splits of the other axis x (image, key head)
+    float scale, c;                                 // c = |scale| * log2(e): exponentials are powers of 2 here
+};
+
+// Lengths of an image, and what a row of it sees.
+struct Lengths {
+    int q, k, off;                                  // off: a causal query i sees keys up to i + off
+    __device__ __forceinline__ Lengths(const AttentionArgs& a, int b)
+    {
+        q = a.q_lens ? min(max(a.q_lens[b], 0), a.q_len) : a.q_len;
+        k = a.kv_lens ? min(max(a.kv_lens[b], 0), a.kv_len) : a.kv_len;
+        off = k - q;
+    }
+    // number of keys that query i sees
+    __device__ __forceinline__ int seen(const AttentionArgs& a, int i) const { return i >= q ? 0 : a.causal ? min(max(i + off + 1, 0), k) : k; }
+};
+
+__device__ __forceinline__ int query_of(const AttentionArgs& a, int row) { return a.group == 1 ? row : (int)((uint32_t)row / (uint32_t)a.group); }
+
+// Which block, split, image and key head a workgroup has; false: none.  Blocks of one (image, key head) read the same keys (queries) and run on one XCD where
+// the groups are many enough to load all eight.
+__device__ __forceinline__ bool place_of(const AttentionArgs& a, int& block, int& split, int& b, int& kvh)
+{
+    int g;
+    const int index = (int)blockIdx.x;
+    if (a.by_xcd) {
+        if (!xcd_order(index, a.groups, a.blocks, g, block)) return false;
+    } else {
+        g = index / a.blocks;
+        block = index - g * a.blocks;
+    }
+    split = g % a.splits;
+    g /= a.splits;
+    b = g / a.kv;
+    kvh = g - b * a.kv;
+    return true;
+}
+inline unsigned place_groups(AttentionArgs& a)
+{
+    a.groups = a.batch * a.kv * a.splits;
+    a.by_xcd = a.groups % 8 == 0 || a.groups >= 48;
+    return a.by_xcd ? xcd_grid(a.groups, a.blocks) : (unsigned)(a.groups * a.blocks);
+}
+
+// Hidden keys and rows are multiplied by 0 inside a block, which makes NaN of what is not finite there.  A wavefront that ends with such a result computes the rows (keys)
+// concerned once more, one seen pair after the other; only causal calls have hidden values in a block (rows past the lengths are zeros).
+template <int DT>
+__device__ __forceinline__ bool not_finite(const f32x16 (&v)[DT])
+{
+    bool bad = false;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) bad = bad || !(fabsf(v[d][r]) < INFINITY);
+    return bad;
+}
+template <typename T>
+__device__ __forceinline__ float dot_of(const T* x, const T* y, int d)
+{
+    float s = 0;
+    for (int c = 0; c < d; ++c) s = fmaf(ld(x + c), ld(y + c), s);
+    return s;
+}
+// v[channel] += f * row[channel] for the channels that this lane holds of a result
+template <typename T, int DT>
+__device__ __forceinline__ void add_row(f32x16 (&v)[DT], float f, const T* row, int d)
+{
+    const int h = (threadIdx.x >> 5) & 1;
+#pragma unroll
+    for (int k = 0; k < DT; ++k)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const int c = 32 * k + 8 * (r >> 2) + 4 * h + (r & 3);
+            if (c < d) v[k][r] = fmaf(f, ld(row + c), v[k][r]);
+        }
+}
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+AttentionArgs attention_args(const ftp_attention_shape& s);
+
+}  // namespace ftp

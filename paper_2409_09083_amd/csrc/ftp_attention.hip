@@ -1,0 +1,242 @@
+// Softmax attention, forward: out = softmax(scale q k^T) v over the keys a query sees, one pass over the keys with the running maximum and sum of each row.
+//
+// A workgroup is 128 rows (32 a wavefront) against tiles of keys, staged in LDS with the next tile's loads in flight.  S^T = K Q^T puts a row's scores into one lane pair
+// (lane % 32), so maximum, sum and rescaling are per lane; P^T is then the operand of O^T = V^T P^T as it lies (ftp_attention.h).  Few rows (single tokens): the keys are
+// split over workgroups, whose unnormalised rows a second kernel joins.
+#include "ftp_attention.h"
+
+#include <algorithm>
+#include <cmath>
+
+namespace ftp {
+namespace {
+
+constexpr int kWaves = 4;
+template <typename T> constexpr int kKeys = sizeof(T) == 4 ? 32 : 64;
+
+template <typename T, int D>
+__global__ __launch_bounds__(256) void k_attention(const AttentionArgs a)
+{
+    typedef Tile<T, D> L;
+    typedef typename FragOf<T>::type Frag;
+    constexpr int BN = kKeys<T>, SUB = BN / 32, DT = D / 32, kTile = BN * L::kRow;
+    __shared__ __align__(16) char lds[2][2][kTile];
+    int block, split, b, kvh;
+    if (!place_of(a, block, split, b, kvh)) return;
+    if (a.causal) block = a.blocks - 1 - block;     // the longest ones first
+    const Lengths len(a, b);
+    const int rows = a.q_len * a.group;
+    const int wave = threadIdx.x >> 6, l = threadIdx.x & 63, h = l >> 5;
+    const int first = block * 32 * kWaves, row = first + wave * 32 + (l & 31);
+    const int i = query_of(a, row), head = kvh * a.group + row - i * a.group;
+    const bool inside = row < rows;
+    const int seen = inside ? len.seen(a, i) : 0;
+    // keys that some row of the workgroup sees, and those that all its rows inside the lengths see
+    const int last = query_of(a, min(first + 32 * kWaves, rows) - 1), i0 = query_of(a, first);
+    const int end = i0 < len.q ? len.seen(a, min(last, len.q - 1)) : 0, common = len.seen(a, i0);
+    const int tiles = (end + BN - 1) / BN, lo = (int)((long long)tiles * split / a.splits), hi = (int)((long long)tiles * (split + 1) / a.splits);
+    const bool busy = first + wave * 32 < rows;     // the wavefront has rows
+
+    Frag q[D / 16];
+    row_operands<T, D>(q, seen ? (const T*)a.q + b * a.qs[0] + i * a.qs[1] + head * a.qs[2] : nullptr, a.d, a.vec, a.scale < 0);
+    const T* kp = (const T*)a.k + b * a.ks[0] + kvh * a.ks[2];
+    const T* vp = (const T*)a.v + b * a.vs[0] + kvh * a.vs[2];
+    Staged<T, D, BN> sk, sv;
+    const auto fetch = [&](int t) {
+        sk.fetch([&](int r) { const int key = t * BN + r; return key < len.k ? kp + key * a.ks[1] : nullptr; }, a.d, a.vec);
+        sv.fetch([&](int r) { const int key = t * BN + r; return key < len.k ? vp + key * a.vs[1] : nullptr; }, a.d, a.vec);
+    };
+
+    f32x16 o[DT] = {};
+    float m = -INFINITY, sum = 0;
+    if (lo < hi) {
+        fetch(lo);
+        sk.put(lds[0][0]);
+        sv.put(lds[0][1]);
+        __syncthreads();
+    }
+    for (int t = lo; t < hi; ++t) {
+        const char* tk = lds[(t - lo) & 1][0];
+        const char* tv = lds[(t - lo) & 1][1];
+        if (t + 1 < hi) fetch(t + 1);
+        if (busy) {
+            f32x16 s[SUB] = {};
+#pragma unroll
+            for (int u = 0; u < SUB; ++u)
+#pragma unroll
+                for (int k = 0; k < D / 16; ++k) s[u] = mma(L::along(tk, 32 * u, k), q[k], s[u]);
+            if ((t + 1) * BN > common) {
+#pragma unroll
+                for (int u = 0; u < SUB; ++u)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        if (t * BN + 32 * u + 8 * (r >> 2) + 4 * h + (r & 3) >= seen) s[u][r] = -INFINITY;
+            }
+            float top = s[0][0];
+#pragma unroll
+            for (int u = 0; u < SUB; ++u)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) top = fmaxf(top, s[u][r]);
+            top = fmaxf(m, both_max(top) * a.c);
+            if (__any(top > m)) {
+                const float f = __builtin_amdgcn_exp2f(m == -INFINITY ? 0.0f : m - top);
+                sum *= f;
+#pragma unroll
+                for (int d = 0; d < DT; ++d)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) o[d][r] *= f;
+                m = top;
+            }
+            const float base = m == -INFINITY ? 0.0f : m;           // (no key seen so far)
+#pragma unroll
+            for (int u = 0; u < SUB; ++u)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    s[u][r] = __builtin_amdgcn_exp2f(fmaf(s[u][r], a.c, -base));
+                    sum += s[u][r];
+                }
+#pragma unroll
+            for (int u = 0; u < SUB; ++u)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const Frag p = operand<T>(s[u], k);
+#pragma unroll
+                    for (int d = 0; d < DT; ++d) o[d] = mma(L::across(tv, 32 * u + 16 * k, 32 * d), p, o[d]);
+                }
+        }
+        if (t + 1 < hi) {
+            sk.put(lds[(t + 1 - lo) & 1][0]);
+            sv.put(lds[(t + 1 - lo) & 1][1]);
+        }
+        __syncthreads();
+    }
+    if (!inside) return;
+    if (a.causal && __any(not_finite(o))) {
+        const bool redo = both_max(not_finite(o) ? 1.0f : 0.0f) > 0;
+        const T* qr = (const T*)a.q + b * a.qs[0] + i * a.qs[1] + head * a.qs[2];
+        if (redo) {
+#pragma unroll
+            for (int d = 0; d < DT; ++d) o[d] = f32x16{};
+            for (int key = lo * BN; key < min(hi * BN, seen); ++key) {
+                const float s = dot_of(qr, kp + key * a.ks[1], a.d);
+                add_row<T, DT>(o, __builtin_amdgcn_exp2f(fmaf(a.scale < 0 ? -s : s, a.c, -m)), vp + key * a.vs[1], a.d);
+            }
+        }
+    }
+    sum = both_sum(sum);
+    if (a.splits > 1) {
+        // [split][image][key head][row][D], and the rows' maxima and sums behind
+        const long long at = (((long long)split * a.batch + b) * a.kv + kvh) * rows + row, n = (long long)a.splits * a.batch * a.kv * rows;
+        float* p = a.ws + at * D;
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4)
+                *(f32x4*)(p + 32 * d + 8 * (r >> 2) + 4 * h) = f32x4{o[d][r], o[d][r + 1], o[d][r + 2], o[d][r + 3]};
+        if (h == 0) { a.ws[n * D + 2 * at] = m; a.ws[n * D + 2 * at + 1] = sum; }
+        return;
+    }
+    const float inv = seen ? 1.0f / sum : 0.0f;
+    T* p = (T*)a.out + b * a.os[0] + i * a.os[1] + head * a.os[2];
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+            const f32x4 v = seen ? f32x4{o[d][r] * inv, o[d][r + 1] * inv, o[d][r + 2] * inv, o[d][r + 3] * inv} : f32x4{0, 0, 0, 0};
+            store4(p, 32 * d + 8 * (r >> 2) + 4 * h, a.d, a.vec, v[0], v[1], v[2], v[3]);
+        }
+    if (h == 0 && a.lse) a.lse[((long long)b * a.heads + head) * a.q_len + i] = seen ? fmaf(m, kLn2, logf(sum)) : -INFINITY;
+}
+
+// Joins the splits of a row: D / 4 lanes a row, four channels each.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void k_attention_join(const AttentionArgs a)
+{
+    constexpr int LANES = D / 4;
+    const int rows = a.q_len * a.group;
+    const long long per = (long long)a.batch * a.kv * rows, at = (long long)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
+    if (at >= per) return;
+    const int d0 = (threadIdx.x % LANES) * 4;
+    const int row = (int)(at % rows), i = query_of(a, row);
+    const int kvh = (int)(at / rows % a.kv), b = (int)(at / rows / a.kv), head = kvh * a.group + row - i * a.group;
+    const float* ms = a.ws + per * a.splits * D;
+    float m = -INFINITY;
+    for (int s = 0; s < a.splits; ++s) m = fmaxf(m, ms[2 * (s * per + at)]);
+    f32x4 o = {0, 0, 0, 0};
+    float sum = 0;
+#pragma unroll 4
+    for (int s = 0; s < a.splits; ++s) {
+        const float ps = ms[2 * (s * per + at)], f = ps == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ps - m);
+        sum = fmaf(ms[2 * (s * per + at) + 1], f, sum);
+        o += *(const f32x4*)(a.ws + (s * per + at) * D + d0) * f;
+    }
+    const bool any = Lengths(a, b).seen(a, i) > 0;
+    o = any ? o * (1.0f / sum) : f32x4{0, 0, 0, 0};
+    store4((T*)a.out + b * a.os[0] + i * a.os[1] + head * a.os[2], d0, a.d, a.vec, o[0], o[1], o[2], o[3]);
+    if (d0 == 0 && a.lse) a.lse[((long long)b * a.heads + head) * a.q_len + i] = any ? fmaf(m, kLn2, logf(sum)) : -INFINITY;
+}
+
+// Splits of the keys: none where the blocks of rows give every CU a workgroup; else as many as do, of at least 4 tiles.
+int forward_splits(const ftp_attention_shape& s)
+{
+    const long long blocks = ceil_div((long long)s.q_len * (s.heads / s.kv_heads), 32 * kWaves) * s.batch * s.kv_heads;
+    const long long tiles = ceil_div(s.kv_len, s.dtype == FTP_BF16 ? 64 : 32);
+    if (blocks == 0 || blocks >= 256) return 1;
+    return (int)std::max(1ll, std::min({512 / blocks, tiles / 4, 128ll}));
+}
+
+template <typename T, int D>
+void run(const AttentionArgs& a, unsigned grid, hipStream_t st)
+{
+    k_attention<T, D><<<grid, 256, 0, st>>>(a);
+    if (a.splits > 1) {
+        const long long rows = (long long)a.batch * a.kv * a.q_len * a.group;
+        k_attention_join<T, D><<<(unsigned)ceil_div(rows, 1024 / D), 256, 0, st>>>(a);
+    }
+}
+
+}  // namespace
+
+AttentionArgs attention_args(const ftp_attention_shape& s)
+{
+    AttentionArgs a = {};
+    for (int i = 0; i < 3; ++i) {
+        a.qs[i] = s.q_stride[i]; a.ks[i] = s.k_stride[i]; a.vs[i] = s.v_stride[i]; a.os[i] = s.out_stride[i];
+        a.gs[i] = s.dout_stride[i]; a.dqs[i] = s.dq_stride[i]; a.dks[i] = s.dk_stride[i]; a.dvs[i] = s.dv_stride[i];
+    }
+    a.batch = s.batch; a.heads = s.heads; a.kv = s.kv_heads; a.group = s.heads / s.kv_heads;
+    a.q_len = s.q_len; a.kv_len = s.kv_len; a.d = s.head_dim; a.causal = s.causal;
+    a.scale = s.scale;
+    a.c = std::max(std::fabs(s.scale) * kLog2e, 1e-30f);             // (0 would make NaN of a hidden score, -infinity)
+    return a;
+}
+
+size_t attention_forward_workspace(const ftp_attention_shape& s)
+{
+    const int splits = forward_splits(s), D = s.head_dim <= 32 ? 32 : s.head_dim <= 64 ? 64 : 128;
+    return splits > 1 ? (size_t)splits * s.batch * s.heads * s.q_len * (D + 2) * sizeof(float) : 0;
+}
+
+void attention_forward(const ftp_attention_shape& s, const void* q, const void* k, const void* v, const int* q_lens, const int* kv_lens, void* out, float* lse,
+                       float* ws, hipStream_t st)
+{
+    AttentionArgs a = attention_args(s);
+    a.q = q; a.k = k; a.v = v; a.q_lens = q_lens; a.kv_lens = kv_lens; a.out = out; a.lse = lse; a.ws = ws;
+    const int el = s.dtype == FTP_BF16 ? 8 : 4;
+    a.vec = s.head_dim % el == 0 && aligned(q, 16) && aligned(k, 16) && aligned(v, 16) && aligned(out, 16);
+    for (int i = 0; i < 3; ++i) a.vec = a.vec && a.qs[i] % el == 0 && a.ks[i] % el == 0 && a.vs[i] % el == 0 && a.os[i] % el == 0;
+    a.blocks = (int)ceil_div((long long)a.q_len * a.group, 32 * kWaves);
+    a.splits = forward_splits(s);
+    const unsigned grid = place_groups(a);
+    if (s.dtype == FTP_BF16) {
+        if (a.d <= 32) run<bf16_t, 32>(a, grid, st);
+        else if (a.d <= 64) run<bf16_t, 64>(a, grid, st);
+        else run<bf16_t, 128>(a, grid, st);
+    } else {
+        if (a.d <= 32) run<float, 32>(a, grid, st);
+        else if (a.d <= 64) run<float, 64>(a, grid, st);
+        else run<float, 128>(a, grid, st);
+    }
+}
+
+}  // namespace ftp
