@@ -11,6 +11,9 @@
 #include "ftp_tokens.h"
 #include "ftp_order.h"
 
+#include <type_traits>
+#include <utility>
+
 namespace ftp {
 
 typedef __bf16 b16x8 __attribute__((ext_vector_type(8)));
@@ -62,10 +65,12 @@ struct Tile {
     }
     static __device__ __forceinline__ int at(int row, int chunk) { return row * kRow + ((chunk ^ mix(row)) << 4); }
 
+    // (mix() goes by a row's low four bits: row0, a multiple of 16, only moves the address)
     // operand (index: row row0 + lane % 32; contraction: channels 16 s + 8 h + j)
     static __device__ __forceinline__ typename FragOf<T>::type along(const char* t, int row0, int s)
     {
-        const int l = threadIdx.x & 63, row = row0 + (l & 31), h = l >> 5;
+        const int l = threadIdx.x & 63, row = l & 31, h = l >> 5;
+        t += row0 * kRow;
         if constexpr (sizeof(T) == 4) {
             const f32x4 a = *(const f32x4*)(t + at(row, 4 * s + 2 * h)), b = *(const f32x4*)(t + at(row, 4 * s + 2 * h + 1));
             return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
@@ -77,11 +82,12 @@ struct Tile {
     static __device__ __forceinline__ typename FragOf<T>::type across(const char* t, int row0, int d0)
     {
         const int l = threadIdx.x & 63, h = l >> 5;
+        t += row0 * kRow;
         if constexpr (sizeof(T) == 4) {
             const int d = d0 + (l & 31);
             f32x8 r;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) r[j] = *(const float*)(t + at(row0 + 8 * (j >> 2) + 4 * h + (j & 3), d >> 2) + (d & 3) * 4);
+            for (int j = 0; j < 8; ++j) r[j] = *(const float*)(t + at(8 * (j >> 2) + 4 * h + (j & 3), d >> 2) + (d & 3) * 4);
             return r;
         } else {
             // each 16 lanes: 4 rows x 16 channels, lane i brings 8 bytes of row i / 4 and takes channel i of the four rows
@@ -90,7 +96,7 @@ struct Tile {
 #pragma unroll
             for (int j = 0; j < 2; ++j)
                 v[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                    (s16x4 __attribute__((address_space(3)))*)(t + at(row0 + 8 * j + 4 * h + (i >> 2), col >> 3) + (col & 7) * 2));
+                    (s16x4 __attribute__((address_space(3)))*)(t + at(8 * j + 4 * h + (i >> 2), col >> 3) + (col & 7) * 2));
             return __builtin_bit_cast(b16x8, __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7));
         }
     }
@@ -115,34 +121,122 @@ __device__ __forceinline__ u32x4 chunk_of(const T* row, int d0, int d, bool vec)
     return r;
 }
 
-// Part of a tile of ROWS rows on its way through the registers of the workgroup's 256 threads.  row(i): address of row i, or null: zeros.
-template <typename T, int D, int ROWS>
+// Rows of a tile on their way from memory to LDS, for the workgroup's 256 threads.  VEC: straight into LDS (buffer loads whose lanes fill 16 bytes each, one
+// after the other; what is out of the resource's range arrives as zeros), landed once wait_tiles() returns.  Else, where addresses or the head size do not allow
+// 16 bytes at once: through registers, written by put().  Where a row lies in its tile is the same for all tiles and is worked out once: offset(r), bytes from
+// the tile's base (wavefront-uniform).
+template <typename T, int D, int ROWS, bool VEC>
 struct Staged {
     typedef Tile<T, D> L;
-    static constexpr int kAll = ROWS * L::kChunks, kEach = (kAll + 255) / 256;
+    typedef typename std::conditional<VEC, int, long long>::type Bytes;
+    static constexpr int kAll = ROWS * L::kChunks, kEach = (kAll + 255) / 256, kNone = -1;
     static_assert(kAll % 256 == 0 || kEach == 1, "whole chunks a thread");
-    u32x4 r[kEach];
-    template <class Row>
-    __device__ __forceinline__ void fetch(Row row, int d, bool vec)
+    Bytes at[kEach];
+    u32x4 r[VEC ? 1 : kEach];
+    int d;
+    template <class Offset>
+    __device__ __forceinline__ void init(Offset offset, int d_)
     {
+        d = d_;
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
-            const int u = threadIdx.x + 256 * i;
-            const T* p = kAll < 256 && u >= kAll ? nullptr : row(u / L::kChunks);
-            r[i] = u32x4{0, 0, 0, 0};
-            if (p) r[i] = chunk_of(p, (u % L::kChunks) * L::kEl, d, vec);
+            const int u = threadIdx.x + 256 * i, row = u / L::kChunks, chunk = (u % L::kChunks) ^ (VEC ? L::mix(row) : 0);       // (the chunk that lies here)
+            at[i] = (kAll < 256 && u >= kAll) || chunk * L::kEl >= d ? (Bytes)kNone : offset(row) + chunk * 16;
         }
     }
-    __device__ __forceinline__ void put(char* t) const
+    // `rows`: how many rows there are, the others are zeros
+    __device__ __forceinline__ void fetch(char* tile, const T* base, int rows)
     {
+        if constexpr (VEC) {
+            const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)base, (short)0, (int)0x80000000u, 0x00020000);
+            if (rows >= ROWS) {
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-            const int u = threadIdx.x + 256 * i;
-            if (kAll < 256 && u >= kAll) continue;
-            *(u32x4*)(t + L::at(u / L::kChunks, u % L::kChunks)) = r[i];
+                for (int i = 0; i < kEach; ++i) load(tile, rsrc, i, at[i]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < kEach; ++i) load(tile, rsrc, i, (int)(threadIdx.x + 256 * i) / L::kChunks < rows ? at[i] : kNone);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) {
+                const int u = threadIdx.x + 256 * i, chunk = u % L::kChunks;
+                r[i] = u32x4{0, 0, 0, 0};
+                if (u / L::kChunks < rows && at[i] >= 0) r[i] = chunk_of((const T*)((const char*)base + (at[i] - chunk * 16)), chunk * L::kEl, d, false);
+            }
+        }
+    }
+    __device__ __forceinline__ void put(char* tile) const
+    {
+        if constexpr (!VEC) {
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) {
+                const int u = threadIdx.x + 256 * i;
+                if (kAll < 256 && u >= kAll) continue;
+                *(u32x4*)(tile + L::at(u / L::kChunks, u % L::kChunks)) = r[i];
+            }
+        }
+    }
+private:
+    static __device__ __forceinline__ void load(char* tile, __amdgpu_buffer_rsrc_t rsrc, int i, int offset)
+    {
+        const int first = __builtin_amdgcn_readfirstlane(threadIdx.x & ~63) + 256 * i;
+        if (kAll < 256 && first >= kAll) return;
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)(tile + first * 16), 16, offset, 0, 0, 0);
+    }
+};
+// This wavefront's loads have landed (vmcnt(0)); a barrier behind it makes it everybody's.
+__device__ __forceinline__ void wait_tiles() { __builtin_amdgcn_s_waitcnt(0x0F70); }
+
+// f(0), f(1), .. f(N - 1) with constants
+template <class F, int... I>
+__device__ __forceinline__ void unrolled(F f, std::integer_sequence<int, I...>) { (f(std::integral_constant<int, I>{}), ...); }
+template <int N, class F>
+__device__ __forceinline__ void unrolled(F f) { unrolled(f, std::make_integer_sequence<int, N>{}); }
+
+// The work of one unit (32 x 32 pairs) in the order in which it keeps matrix cores and vector units busy at once: NA products of the next unit's scores with the first half of this
+// unit's exponentials (valu(0 .. 3), two registers each), NC products of that half's probabilities with the second half of the exponentials, and the other half's products.
+// Operands are read from LDS two slots ahead.  The order is fixed (sched_barrier): left to itself the compiler puts all matrix instructions behind each other, where the
+// vector unit waits for them.
+template <int NA, int NC, class LoadA, class MmaA, class Valu, class LoadC, class MmaC>
+__device__ __forceinline__ void overlap(LoadA load_a, MmaA mma_a, Valu valu, LoadC load_c, MmaC mma_c)
+{
+    constexpr int PA = (NA + 3) / 4, PC = (NC + 3) / 4;
+    const auto loads = [&](auto s) __attribute__((always_inline)) {
+        if constexpr (s < 4) unrolled<PA>([&](auto i) __attribute__((always_inline)) { if constexpr (s * PA + i < NA) load_a(s * PA + i); });
+        else if constexpr (s < 12) unrolled<PC>([&](auto i) __attribute__((always_inline)) { if constexpr ((s & 3) * PC + i < NC) load_c((s - 4) / 4, (s & 3) * PC + i); });
+    };
+    loads(std::integral_constant<int, 0>{});
+    loads(std::integral_constant<int, 1>{});
+    __builtin_amdgcn_sched_barrier(0);
+    unrolled<12>([&](auto s) __attribute__((always_inline)) {
+        loads(std::integral_constant<int, s + 2>{});
+        if constexpr (s < 4) unrolled<PA>([&](auto i) __attribute__((always_inline)) { if constexpr (s * PA + i < NA) mma_a(s * PA + i); });
+        else unrolled<PC>([&](auto i) __attribute__((always_inline)) { if constexpr ((s & 3) * PC + i < NC) mma_c((s - 4) / 4, (s & 3) * PC + i); });
+        if constexpr (s < 8) valu((int)s);
+        __builtin_amdgcn_sched_barrier(0);
+    });
+}
+
+// Scores of hidden pairs start from this instead of 0: their exponential is 0, whatever is added.
+constexpr float kHidden = -3e38f;
+
+// Operand words of two neighbouring registers of a result as they become known (see operand()).
+template <typename T>
+struct Words {
+    typename FragOf<T>::type f[2];
+    __device__ __forceinline__ void set(int pair, float a, float b)
+    {
+        if constexpr (sizeof(T) == 4) { f[pair >> 2][2 * (pair & 3)] = a; f[pair >> 2][2 * (pair & 3) + 1] = b; }
+        else {
+            u32x4 w = __builtin_bit_cast(u32x4, f[pair >> 2]);
+            w[pair & 3] = pack_bf16(a, b);
+            f[pair >> 2] = __builtin_bit_cast(b16x8, w);
         }
     }
 };
+
+// Workgroups a CU that the register budget is set for: two (all sums and operands in 256 registers) where they fit.
+template <typename T, int D> constexpr int kPerCu = sizeof(T) == 4 && D == 128 ? 1 : 2;
 
 // Operands (index: this lane's row; contraction: channels 16 s + 8 h + j) straight from memory; row null: zeros.
 template <typename T, int D>
@@ -240,6 +334,8 @@ inline unsigned place_groups(AttentionArgs& a)
 
 // Hidden keys and rows are multiplied by 0 inside a block, which makes NaN of what is not finite there.  A wavefront that ends with such a result computes the rows (keys)
 // concerned once more, one seen pair after the other; only causal calls have hidden values in a block (rows past the lengths are zeros).
+// v, as if it were not known from before: what is computed from it is computed here
+__device__ __forceinline__ int again(int v) { asm volatile("" : "+v"(v)); return v; }
 template <int DT>
 __device__ __forceinline__ bool not_finite(const f32x16 (&v)[DT])
 {
@@ -274,5 +370,8 @@ __device__ __forceinline__ void add_row(f32x16 (&v)[DT], float f, const T* row, 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 AttentionArgs attention_args(const ftp_attention_shape& s);
+
+// Offsets within a tile (at most 64 such strides) stay below 2^30 bytes.
+inline bool near_rows(long long stride) { return stride < (1ll << 21); }
 
 }  // namespace ftp

@@ -12,21 +12,22 @@ namespace ftp {
 namespace {
 
 constexpr int kWaves = 4;
-template <typename T> constexpr int kKeys = sizeof(T) == 4 ? 32 : 64;
+template <typename T, int D> constexpr int kKeys = sizeof(T) == 4 ? 32 : 64;       // keys of a tile
 
-template <typename T, int D>
-__global__ __launch_bounds__(256) void k_attention(const AttentionArgs a)
+template <typename T, int D, bool VEC>
+__global__ __launch_bounds__(256, (kPerCu<T, D>)) void k_attention(const AttentionArgs a)
 {
     typedef Tile<T, D> L;
     typedef typename FragOf<T>::type Frag;
-    constexpr int BN = kKeys<T>, SUB = BN / 32, DT = D / 32, kTile = BN * L::kRow;
-    __shared__ __align__(16) char lds[2][2][kTile];
+    constexpr int BN = kKeys<T, D>, UNITS = BN / 32, KS = D / 16, DT = D / 32, kTile = BN * L::kRow;
+    struct Keys { char tile[2][kTile]; };           // a tile of keys and values
+    __shared__ __align__(16) Keys even, odd;        // (apart, so that reads of one need not wait for loads of the other)
     int block, split, b, kvh;
     if (!place_of(a, block, split, b, kvh)) return;
     if (a.causal) block = a.blocks - 1 - block;     // the longest ones first
     const Lengths len(a, b);
     const int rows = a.q_len * a.group;
-    const int wave = threadIdx.x >> 6, l = threadIdx.x & 63, h = l >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, h = l >> 5;
     const int first = block * 32 * kWaves, row = first + wave * 32 + (l & 31);
     const int i = query_of(a, row), head = kvh * a.group + row - i * a.group;
     const bool inside = row < rows;
@@ -35,91 +36,98 @@ __global__ __launch_bounds__(256) void k_attention(const AttentionArgs a)
     const int last = query_of(a, min(first + 32 * kWaves, rows) - 1), i0 = query_of(a, first);
     const int end = i0 < len.q ? len.seen(a, min(last, len.q - 1)) : 0, common = len.seen(a, i0);
     const int tiles = (end + BN - 1) / BN, lo = (int)((long long)tiles * split / a.splits), hi = (int)((long long)tiles * (split + 1) / a.splits);
-    const bool busy = first + wave * 32 < rows;     // the wavefront has rows
 
     Frag q[D / 16];
-    row_operands<T, D>(q, seen ? (const T*)a.q + b * a.qs[0] + i * a.qs[1] + head * a.qs[2] : nullptr, a.d, a.vec, a.scale < 0);
+    row_operands<T, D>(q, seen ? (const T*)a.q + b * a.qs[0] + i * a.qs[1] + head * a.qs[2] : nullptr, a.d, VEC, a.scale < 0);
     const T* kp = (const T*)a.k + b * a.ks[0] + kvh * a.ks[2];
     const T* vp = (const T*)a.v + b * a.vs[0] + kvh * a.vs[2];
-    Staged<T, D, BN> sk, sv;
-    const auto fetch = [&](int t) {
-        sk.fetch([&](int r) { const int key = t * BN + r; return key < len.k ? kp + key * a.ks[1] : nullptr; }, a.d, a.vec);
-        sv.fetch([&](int r) { const int key = t * BN + r; return key < len.k ? vp + key * a.vs[1] : nullptr; }, a.d, a.vec);
+    Staged<T, D, BN, VEC> sk, sv;
+    typedef typename Staged<T, D, BN, VEC>::Bytes Bytes;
+    sk.init([&](int r) { return r * (Bytes)a.ks[1] * (Bytes)sizeof(T); }, a.d);
+    sv.init([&](int r) { return r * (Bytes)a.vs[1] * (Bytes)sizeof(T); }, a.d);
+    const auto fetch = [&](int t, Keys& to) __attribute__((always_inline)) {
+        sk.fetch(to.tile[0], kp + (long long)t * BN * a.ks[1], len.k - t * BN);
+        sv.fetch(to.tile[1], vp + (long long)t * BN * a.vs[1], len.k - t * BN);
+    };
+    const auto land = [&](Keys& to) __attribute__((always_inline)) {
+        sk.put(to.tile[0]);
+        sv.put(to.tile[1]);
+        wait_tiles();
+        __syncthreads();
     };
 
     f32x16 o[DT] = {};
-    float m = -INFINITY, sum = 0;
+    const float nothing = -1e30f * a.c;             // the reference of a row that has seen no key
+    float m = nothing, sum = 0;
+    const auto step = [&](int t, Keys& now, Keys& next) __attribute__((always_inline)) {
+        if (t + 1 < hi) fetch(t + 1, next);
+        f32x16 s[UNITS] = {};
+        if ((t + 1) * BN > common) {
+            const int left = seen - t * BN - 4 * h; // keys of the tile that the row sees, counted from this lane's first
+#pragma unroll
+            for (int u = 0; u < UNITS; ++u)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[u][r] = 32 * u + 8 * (r >> 2) + (r & 3) >= left ? kHidden : 0.0f;
+        }
+        float top = kHidden;
+#pragma unroll
+        for (int u = 0; u < UNITS; ++u) {
+#pragma unroll
+            for (int c = 0; c < KS; ++c) s[u] = mma(L::along(now.tile[0], 32 * u, c), q[c], s[u]);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) top = fmaxf(top, s[u][r]);
+        }
+        top = both_max(top) * a.c;
+        // the reference only has to keep the powers in range: it follows the maximum once that is 2^8 ahead (exact all the same: sums and rows share it)
+        if (__any(top > m + 8.0f)) {
+            top = fmaxf(m, top);
+            const float f = __builtin_amdgcn_exp2f(m - top);
+            sum *= f;
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) o[d][r] *= f;
+            m = top;
+        }
+#pragma unroll
+        for (int u = 0; u < UNITS; ++u) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                s[u][r] = __builtin_amdgcn_exp2f(fmaf(s[u][r], a.c, -m));
+                sum += s[u][r];
+            }
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                const Frag p = operand<T>(s[u], c);
+#pragma unroll
+                for (int d = 0; d < DT; ++d) o[d] = mma(L::across(now.tile[1], 32 * u + 16 * c, 32 * d), p, o[d]);
+            }
+        }
+        if (t + 1 < hi) land(next);
+    };
     if (lo < hi) {
-        fetch(lo);
-        sk.put(lds[0][0]);
-        sv.put(lds[0][1]);
-        __syncthreads();
+        fetch(lo, even);
+        land(even);
     }
-    for (int t = lo; t < hi; ++t) {
-        const char* tk = lds[(t - lo) & 1][0];
-        const char* tv = lds[(t - lo) & 1][1];
-        if (t + 1 < hi) fetch(t + 1);
-        if (busy) {
-            f32x16 s[SUB] = {};
-#pragma unroll
-            for (int u = 0; u < SUB; ++u)
-#pragma unroll
-                for (int k = 0; k < D / 16; ++k) s[u] = mma(L::along(tk, 32 * u, k), q[k], s[u]);
-            if ((t + 1) * BN > common) {
-#pragma unroll
-                for (int u = 0; u < SUB; ++u)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        if (t * BN + 32 * u + 8 * (r >> 2) + 4 * h + (r & 3) >= seen) s[u][r] = -INFINITY;
-            }
-            float top = s[0][0];
-#pragma unroll
-            for (int u = 0; u < SUB; ++u)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) top = fmaxf(top, s[u][r]);
-            top = fmaxf(m, both_max(top) * a.c);
-            if (__any(top > m)) {
-                const float f = __builtin_amdgcn_exp2f(m == -INFINITY ? 0.0f : m - top);
-                sum *= f;
-#pragma unroll
-                for (int d = 0; d < DT; ++d)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) o[d][r] *= f;
-                m = top;
-            }
-            const float base = m == -INFINITY ? 0.0f : m;           // (no key seen so far)
-#pragma unroll
-            for (int u = 0; u < SUB; ++u)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    s[u][r] = __builtin_amdgcn_exp2f(fmaf(s[u][r], a.c, -base));
-                    sum += s[u][r];
-                }
-#pragma unroll
-            for (int u = 0; u < SUB; ++u)
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const Frag p = operand<T>(s[u], k);
-#pragma unroll
-                    for (int d = 0; d < DT; ++d) o[d] = mma(L::across(tv, 32 * u + 16 * k, 32 * d), p, o[d]);
-                }
-        }
-        if (t + 1 < hi) {
-            sk.put(lds[(t + 1 - lo) & 1][0]);
-            sv.put(lds[(t + 1 - lo) & 1][1]);
-        }
-        __syncthreads();
+    for (int t = lo; t < hi; t += 2) {
+        step(t, even, odd);
+        if (t + 1 < hi) step(t + 1, odd, even);
     }
     if (!inside) return;
-    if (a.causal && __any(not_finite(o))) {
-        const bool redo = both_max(not_finite(o) ? 1.0f : 0.0f) > 0;
+    if (a.causal && __any(not_finite(o) || !(sum < INFINITY))) {
+        const int row = again(first + wave * 32 + (l & 31)), i = query_of(a, row), head = kvh * a.group + row - i * a.group;      // (not worth registers before)
         const T* qr = (const T*)a.q + b * a.qs[0] + i * a.qs[1] + head * a.qs[2];
-        if (redo) {
+        if (both_max(not_finite(o) || !(sum < INFINITY) ? 1.0f : 0.0f) > 0) {
+            const auto score = [&](int key) { const float s = dot_of(qr, kp + key * a.ks[1], a.d); return (a.scale < 0 ? -s : s) * a.c; };
 #pragma unroll
             for (int d = 0; d < DT; ++d) o[d] = f32x16{};
+            m = nothing;
+            sum = 0;
+            for (int key = lo * BN; key < min(hi * BN, seen); ++key) m = fmaxf(m, score(key));
             for (int key = lo * BN; key < min(hi * BN, seen); ++key) {
-                const float s = dot_of(qr, kp + key * a.ks[1], a.d);
-                add_row<T, DT>(o, __builtin_amdgcn_exp2f(fmaf(a.scale < 0 ? -s : s, a.c, -m)), vp + key * a.vs[1], a.d);
+                const float p = __builtin_amdgcn_exp2f(score(key) - m);
+                add_row<T, DT>(o, p, vp + key * a.vs[1], a.d);
+                sum += h ? 0.0f : p;
             }
         }
     }
@@ -148,7 +156,7 @@ __global__ __launch_bounds__(256) void k_attention(const AttentionArgs a)
     if (h == 0 && a.lse) a.lse[((long long)b * a.heads + head) * a.q_len + i] = seen ? fmaf(m, kLn2, logf(sum)) : -INFINITY;
 }
 
-// Joins the splits of a row: D / 4 lanes a row, four channels each.
+// Joins the splits of a row: D / 4 lanes a row, four channels each; the lanes work out the splits' weights side by side.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void k_attention_join(const AttentionArgs a)
 {
@@ -156,20 +164,29 @@ __global__ __launch_bounds__(256) void k_attention_join(const AttentionArgs a)
     const int rows = a.q_len * a.group;
     const long long per = (long long)a.batch * a.kv * rows, at = (long long)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
     if (at >= per) return;
-    const int d0 = (threadIdx.x % LANES) * 4;
+    const int lane = threadIdx.x % LANES, d0 = lane * 4;
     const int row = (int)(at % rows), i = query_of(a, row);
     const int kvh = (int)(at / rows % a.kv), b = (int)(at / rows / a.kv), head = kvh * a.group + row - i * a.group;
     const float* ms = a.ws + per * a.splits * D;
     float m = -INFINITY;
-    for (int s = 0; s < a.splits; ++s) m = fmaxf(m, ms[2 * (s * per + at)]);
+    for (int s = lane; s < a.splits; s += LANES) m = fmaxf(m, ms[2 * (s * per + at)]);
+#pragma unroll
+    for (int n = LANES / 2; n; n >>= 1) m = fmaxf(m, __shfl_xor(m, n));
     f32x4 o = {0, 0, 0, 0};
     float sum = 0;
-#pragma unroll 4
-    for (int s = 0; s < a.splits; ++s) {
-        const float ps = ms[2 * (s * per + at)], f = ps == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ps - m);
-        sum = fmaf(ms[2 * (s * per + at) + 1], f, sum);
-        o += *(const f32x4*)(a.ws + (s * per + at) * D + d0) * f;
+    for (int s0 = 0; s0 < a.splits; s0 += LANES) {
+        float f = 0;
+        if (s0 + lane < a.splits) {
+            const long long p = 2 * ((s0 + lane) * per + at);
+            f = __builtin_amdgcn_exp2f(ms[p] - m);
+            sum = fmaf(ms[p + 1], f, sum);
+        }
+        const int n = min(LANES, a.splits - s0);
+#pragma unroll 8
+        for (int s = 0; s < n; ++s) o += *(const f32x4*)(a.ws + ((s0 + s) * per + at) * D + d0) * __shfl(f, s, LANES);
     }
+#pragma unroll
+    for (int n = LANES / 2; n; n >>= 1) sum += __shfl_xor(sum, n);
     const bool any = Lengths(a, b).seen(a, i) > 0;
     o = any ? o * (1.0f / sum) : f32x4{0, 0, 0, 0};
     store4((T*)a.out + b * a.os[0] + i * a.os[1] + head * a.os[2], d0, a.d, a.vec, o[0], o[1], o[2], o[3]);
@@ -188,7 +205,8 @@ int forward_splits(const ftp_attention_shape& s)
 template <typename T, int D>
 void run(const AttentionArgs& a, unsigned grid, hipStream_t st)
 {
-    k_attention<T, D><<<grid, 256, 0, st>>>(a);
+    if (a.vec) k_attention<T, D, true><<<grid, 256, 0, st>>>(a);
+    else k_attention<T, D, false><<<grid, 256, 0, st>>>(a);
     if (a.splits > 1) {
         const long long rows = (long long)a.batch * a.kv * a.q_len * a.group;
         k_attention_join<T, D><<<(unsigned)ceil_div(rows, 1024 / D), 256, 0, st>>>(a);
@@ -225,6 +243,7 @@ void attention_forward(const ftp_attention_shape& s, const void* q, const void* 
     const int el = s.dtype == FTP_BF16 ? 8 : 4;
     a.vec = s.head_dim % el == 0 && aligned(q, 16) && aligned(k, 16) && aligned(v, 16) && aligned(out, 16);
     for (int i = 0; i < 3; ++i) a.vec = a.vec && a.qs[i] % el == 0 && a.ks[i] % el == 0 && a.vs[i] % el == 0 && a.os[i] % el == 0;
+    a.vec = a.vec && near_rows(a.ks[1]) && near_rows(a.vs[1]);
     a.blocks = (int)ceil_div((long long)a.q_len * a.group, 32 * kWaves);
     a.splits = forward_splits(s);
     const unsigned grid = place_groups(a);

@@ -13,21 +13,22 @@
 namespace ftp {
 namespace {
 
-template <typename T> constexpr int kKeys = sizeof(T) == 4 ? 32 : 64;
+template <typename T, int D> constexpr int kKeys = sizeof(T) == 4 ? 32 : 64;       // keys of a tile
 
-template <typename T, int D>
-__global__ __launch_bounds__(256) void k_attention_dq(const AttentionArgs a)
+template <typename T, int D, bool VEC>
+__global__ __launch_bounds__(256, (D == 128 ? 1 : kPerCu<T, D>)) void k_attention_dq(const AttentionArgs a)
 {
     typedef Tile<T, D> L;
     typedef typename FragOf<T>::type Frag;
-    constexpr int BN = kKeys<T>, SUB = BN / 32, DT = D / 32, kTile = BN * L::kRow;
-    __shared__ __align__(16) char lds[2][2][kTile];
+    constexpr int BN = kKeys<T, D>, UNITS = BN / 32, KS = D / 16, DT = D / 32, kTile = BN * L::kRow;
+    struct Keys { char tile[2][kTile]; };           // a tile of keys and values
+    __shared__ __align__(16) Keys even, odd;        // (apart, so that reads of one need not wait for loads of the other)
     int block, split, b, kvh;
     if (!place_of(a, block, split, b, kvh)) return;
     if (a.causal) block = a.blocks - 1 - block;
     const Lengths len(a, b);
     const int rows = a.q_len * a.group;
-    const int wave = threadIdx.x >> 6, l = threadIdx.x & 63, h = l >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, h = l >> 5;
     const int first = block * 128, row = first + wave * 32 + (l & 31);
     const int i = query_of(a, row), head = kvh * a.group + row - i * a.group;
     const bool inside = row < rows;
@@ -35,17 +36,15 @@ __global__ __launch_bounds__(256) void k_attention_dq(const AttentionArgs a)
     const int last = query_of(a, min(first + 128, rows) - 1), i0 = query_of(a, first);
     const int end = i0 < len.q ? len.seen(a, min(last, len.q - 1)) : 0, common = len.seen(a, i0);
     const int tiles = (end + BN - 1) / BN, lo = (int)((long long)tiles * split / a.splits), hi = (int)((long long)tiles * (split + 1) / a.splits);
-    const bool busy = first + wave * 32 < rows;
-
     // this row's operands; delta from the same dout and the row of out
     Frag q[D / 16], g[D / 16];
     float delta = 0;
     {
-        row_operands<T, D>(g, seen ? (const T*)a.out + b * a.os[0] + i * a.os[1] + head * a.os[2] : nullptr, a.d, a.vec, false);
+        row_operands<T, D>(g, seen ? (const T*)a.out + b * a.os[0] + i * a.os[1] + head * a.os[2] : nullptr, a.d, VEC, false);
         Frag o[D / 16];
 #pragma unroll
         for (int s = 0; s < D / 16; ++s) o[s] = g[s];
-        row_operands<T, D>(g, seen ? (const T*)a.dout + b * a.gs[0] + i * a.gs[1] + head * a.gs[2] : nullptr, a.d, a.vec, false);
+        row_operands<T, D>(g, seen ? (const T*)a.dout + b * a.gs[0] + i * a.gs[1] + head * a.gs[2] : nullptr, a.d, VEC, false);
 #pragma unroll
         for (int s = 0; s < D / 16; ++s)
 #pragma unroll
@@ -54,58 +53,71 @@ __global__ __launch_bounds__(256) void k_attention_dq(const AttentionArgs a)
     }
     const long long at = (((long long)b * a.kv + kvh) * a.q_len) * a.group + row;
     if (split == 0 && inside && h == 0) a.delta[at] = delta;
-    row_operands<T, D>(q, seen ? (const T*)a.q + b * a.qs[0] + i * a.qs[1] + head * a.qs[2] : nullptr, a.d, a.vec, a.scale < 0);
+    row_operands<T, D>(q, seen ? (const T*)a.q + b * a.qs[0] + i * a.qs[1] + head * a.qs[2] : nullptr, a.d, VEC, a.scale < 0);
     const float lse = seen ? a.lse[((long long)b * a.heads + head) * a.q_len + i] * kLog2e : INFINITY;     // (a row that sees nothing: p = 0)
 
     const T* kp = (const T*)a.k + b * a.ks[0] + kvh * a.ks[2];
     const T* vp = (const T*)a.v + b * a.vs[0] + kvh * a.vs[2];
-    Staged<T, D, BN> sk, sv;
-    const auto fetch = [&](int t) {
-        sk.fetch([&](int r) { const int key = t * BN + r; return key < len.k ? kp + key * a.ks[1] : nullptr; }, a.d, a.vec);
-        sv.fetch([&](int r) { const int key = t * BN + r; return key < len.k ? vp + key * a.vs[1] : nullptr; }, a.d, a.vec);
+    Staged<T, D, BN, VEC> sk, sv;
+    typedef typename Staged<T, D, BN, VEC>::Bytes Bytes;
+    sk.init([&](int r) { return r * (Bytes)a.ks[1] * (Bytes)sizeof(T); }, a.d);
+    sv.init([&](int r) { return r * (Bytes)a.vs[1] * (Bytes)sizeof(T); }, a.d);
+    const auto fetch = [&](int t, Keys& to) __attribute__((always_inline)) {
+        sk.fetch(to.tile[0], kp + (long long)t * BN * a.ks[1], len.k - t * BN);
+        sv.fetch(to.tile[1], vp + (long long)t * BN * a.vs[1], len.k - t * BN);
+    };
+    const auto land = [&](Keys& to) __attribute__((always_inline)) {
+        sk.put(to.tile[0]);
+        sv.put(to.tile[1]);
+        wait_tiles();
+        __syncthreads();
     };
     f32x16 dq[DT] = {};
-    if (lo < hi) {
-        fetch(lo);
-        sk.put(lds[0][0]);
-        sv.put(lds[0][1]);
-        __syncthreads();
-    }
-    for (int t = lo; t < hi; ++t) {
-        const char* tk = lds[(t - lo) & 1][0];
-        const char* tv = lds[(t - lo) & 1][1];
-        if (t + 1 < hi) fetch(t + 1);
-        if (busy) {
+    const auto step = [&](int t, Keys& now, Keys& next) __attribute__((always_inline)) {
+        if (t + 1 < hi) fetch(t + 1, next);
+        f32x16 s[UNITS], p[UNITS];
 #pragma unroll
-            for (int u = 0; u < SUB; ++u) {
-                f32x16 s = {}, p = {};
+        for (int u = 0; u < UNITS; ++u) {
+            s[u] = f32x16{};
 #pragma unroll
-                for (int k = 0; k < D / 16; ++k) {
-                    s = mma(L::along(tk, 32 * u, k), q[k], s);
-                    p = mma(L::along(tv, 32 * u, k), g[k], p);
-                }
-                const bool mask = (t + 1) * BN > common;
+            for (int r = 0; r < 16; ++r) p[u][r] = -delta;
+        }
+        if ((t + 1) * BN > common) {
+            const int left = seen - t * BN - 4 * h; // keys of the tile that the row sees, counted from this lane's first
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const float e = __builtin_amdgcn_exp2f(fmaf(s[r], a.c, -lse)) * (p[r] - delta);
-                    s[r] = mask && t * BN + 32 * u + 8 * (r >> 2) + 4 * h + (r & 3) >= seen ? 0.0f : e;
-                }
+            for (int u = 0; u < UNITS; ++u)
 #pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const Frag ds = operand<T>(s, k);
+                for (int r = 0; r < 16; ++r) s[u][r] = 32 * u + 8 * (r >> 2) + (r & 3) >= left ? kHidden : 0.0f;
+        }
 #pragma unroll
-                    for (int d = 0; d < DT; ++d) dq[d] = mma(L::across(tk, 32 * u + 16 * k, 32 * d), ds, dq[d]);
-                }
+        for (int u = 0; u < UNITS; ++u) {
+#pragma unroll
+            for (int c = 0; c < KS; ++c) {
+                s[u] = mma(L::along(now.tile[0], 32 * u, c), q[c], s[u]);
+                p[u] = mma(L::along(now.tile[1], 32 * u, c), g[c], p[u]);
+            }
+#pragma unroll
+            for (int r = 0; r < 16; ++r) p[u][r] *= __builtin_amdgcn_exp2f(fmaf(s[u][r], a.c, -lse));
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                const Frag ds = operand<T>(p[u], c);
+#pragma unroll
+                for (int d = 0; d < DT; ++d) dq[d] = mma(L::across(now.tile[0], 32 * u + 16 * c, 32 * d), ds, dq[d]);
             }
         }
-        if (t + 1 < hi) {
-            sk.put(lds[(t + 1 - lo) & 1][0]);
-            sv.put(lds[(t + 1 - lo) & 1][1]);
-        }
-        __syncthreads();
+        if (t + 1 < hi) land(next);
+    };
+    if (lo < hi) {
+        fetch(lo, even);
+        land(even);
+    }
+    for (int t = lo; t < hi; t += 2) {
+        step(t, even, odd);
+        if (t + 1 < hi) step(t + 1, odd, even);
     }
     if (!inside) return;
     if (a.causal && __any(not_finite(dq))) {
+        const int row = again(first + wave * 32 + (l & 31)), i = query_of(a, row), head = kvh * a.group + row - i * a.group;      // (not worth registers before)
         const T* qr = (const T*)a.q + b * a.qs[0] + i * a.qs[1] + head * a.qs[2];
         const T* gr = (const T*)a.dout + b * a.gs[0] + i * a.gs[1] + head * a.gs[2];
         if (both_max(not_finite(dq) ? 1.0f : 0.0f) > 0) {
@@ -137,114 +149,169 @@ __global__ __launch_bounds__(256) void k_attention_dq(const AttentionArgs a)
         }
 }
 
-constexpr int kRows = 32;                           // rows of a tile of k_attention_dkv
+template <typename T, int D> constexpr int kRows = sizeof(T) == 4 ? 32 : 64;     // rows of a tile of k_attention_dkv
 
-template <typename T, int D>
-__global__ __launch_bounds__(256) void k_attention_dkv(const AttentionArgs a)
+// Rows that a tile of `most` takes: whole queries of all heads of the group, or for large groups a part of one query's that divides them.
+__host__ __device__ inline int rows_of_tile(int group, int most)
+{
+    if (group <= most) return most - most % group;
+    int n = most;
+    while (group % n) --n;
+    return n;
+}
+
+template <typename T, int D, bool VEC>
+__global__ __launch_bounds__(256, (D == 128 || sizeof(T) * D == 256 ? 1 : 2)) void k_attention_dkv(const AttentionArgs a)
 {
     typedef Tile<T, D> L;
     typedef typename FragOf<T>::type Frag;
-    constexpr int DT = D / 32, kTile = kRows * L::kRow;
-    __shared__ __align__(16) char lds[2][2][kTile];
-    __shared__ float stat[2][2][kRows];             // lse (in powers of 2) and delta of a tile's rows
-    __shared__ int seen_by[2][kRows];
+    constexpr int BM = kRows<T, D>, UNITS = BM / 32, KS = D / 16, DT = D / 32, kTile = BM * L::kRow;
+    // a tile of rows: queries, dout; and of its rows the log-sum in powers of 2, -delta, the number of keys seen
+    struct Rows { char tile[2][kTile]; float lse[BM], less[BM]; int seen[BM]; };
+    __shared__ __align__(16) Rows r0, r1, r2;       // three in turn (apart, so that reads of one need not wait for loads of another)
     int block, split, b, kvh;
     if (!place_of(a, block, split, b, kvh)) return;
     const Lengths len(a, b);
     const int rows = len.q * a.group;               // (rows past the lengths see nothing)
-    const int wave = threadIdx.x >> 6, l = threadIdx.x & 63, h = l >> 5;
-    const int key0 = block * 128, key = key0 + wave * 32 + (l & 31);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, h = l >> 5;
+    const int key0 = block * 128, mine = key0 + wave * 32, key = mine + (l & 31);
     const bool inside = key < len.k;
     // rows that see any of the keys: all from the first query that sees key0 on
-    const int from = key0 >= len.k ? rows : a.causal ? min((long long)rows, (long long)max(0, key0 - len.off) * a.group) : 0;
-    const int t0 = from / kRows, tiles = from < rows ? (rows + kRows - 1) / kRows - t0 : 0;
+    const int from = key0 >= len.k ? rows : a.causal ? (int)min((long long)rows, (long long)max(0, key0 - len.off) * a.group) : 0;
+    const int each = rows_of_tile(a.group, BM), t0 = from / each, tiles = from < rows ? (rows + each - 1) / each - t0 : 0;
     const int lo = t0 + (int)((long long)tiles * split / a.splits), hi = t0 + (int)((long long)tiles * (split + 1) / a.splits);
-    const bool busy = key0 + wave * 32 < len.k;
 
     Frag k[D / 16], v[D / 16];
-    row_operands<T, D>(k, inside ? (const T*)a.k + b * a.ks[0] + key * a.ks[1] + kvh * a.ks[2] : nullptr, a.d, a.vec, a.scale < 0);
-    row_operands<T, D>(v, inside ? (const T*)a.v + b * a.vs[0] + key * a.vs[1] + kvh * a.vs[2] : nullptr, a.d, a.vec, false);
+    row_operands<T, D>(k, inside ? (const T*)a.k + b * a.ks[0] + key * a.ks[1] + kvh * a.ks[2] : nullptr, a.d, VEC, a.scale < 0);
+    row_operands<T, D>(v, inside ? (const T*)a.v + b * a.vs[0] + key * a.vs[1] + kvh * a.vs[2] : nullptr, a.d, VEC, false);
     const T* qp = (const T*)a.q + b * a.qs[0] + kvh * a.group * a.qs[2];
     const T* gp = (const T*)a.dout + b * a.gs[0] + kvh * a.group * a.gs[2];
     const float* lsep = a.lse + ((long long)b * a.heads + kvh * a.group) * a.q_len;
     const float* deltap = a.delta + (((long long)b * a.kv + kvh) * a.q_len) * a.group;
-    Staged<T, D, kRows> sq, sg;
+    Staged<T, D, BM, VEC> sq, sg;
+    typedef typename Staged<T, D, BM, VEC>::Bytes Bytes;
     float sl = 0, sd = 0;
     int ss = 0;
-    const auto fetch = [&](int t) {
-        const auto address = [&](const T* p, const long long (&str)[3], int r) {
-            const int row = t * kRows + r, i = query_of(a, row);
-            return row < rows && len.seen(a, i) > 0 ? p + i * str[1] + (row - i * a.group) * str[2] : nullptr;
-        };
-        sq.fetch([&](int r) { return address(qp, a.qs, r); }, a.d, a.vec);
-        sg.fetch([&](int r) { return address(gp, a.gs, r); }, a.d, a.vec);
-        if (threadIdx.x < kRows) {
-            const int row = t * kRows + threadIdx.x, i = query_of(a, row);
-            ss = row < rows ? len.seen(a, i) : 0;
-            sl = ss ? lsep[(long long)(row - i * a.group) * a.q_len + i] * kLog2e : INFINITY;
-            sd = ss ? deltap[row] : 0.0f;
+    // row r of a tile is head j0 + r % group of query i0 + r / group (a tile is `each` rows: whole queries, or a part of one)
+    const int tr = threadIdx.x & (BM - 1), ti = a.group <= BM ? query_of(a, tr) : 0, tj = tr - ti * a.group;
+    const auto offset = [&](const long long (&str)[3], int r) {
+        const int i = a.group <= BM ? query_of(a, r) : 0;
+        return (i * (Bytes)str[1] + (r - i * a.group) * (Bytes)str[2]) * (Bytes)sizeof(T);
+    };
+    sq.init([&](int r) { return offset(a.qs, r); }, a.d);
+    sg.init([&](int r) { return offset(a.gs, r); }, a.d);
+    const int queries = a.group <= BM ? each / a.group : 0;
+    const auto first_query = [&](int t) { return queries ? t * queries : t * each / a.group; };
+    const auto fetch = [&](int t, Rows& to) __attribute__((always_inline)) {
+        const int i0 = first_query(t), j0 = t * each - i0 * a.group, there = min(rows - t * each, each);
+        sq.fetch(to.tile[0], qp + i0 * a.qs[1] + j0 * a.qs[2], there);
+        sg.fetch(to.tile[1], gp + i0 * a.gs[1] + j0 * a.gs[2], there);
+        if (threadIdx.x < BM) {
+            ss = tr < there ? len.seen(a, i0 + ti) : 0;
+            sl = ss ? lsep[(long long)(j0 + tj) * a.q_len + i0 + ti] * kLog2e : INFINITY;
+            sd = ss ? -deltap[t * each + tr] : 0.0f;
         }
     };
-    const auto put = [&](int buf) {
-        sq.put(lds[buf][0]);
-        sg.put(lds[buf][1]);
-        if (threadIdx.x < kRows) { stat[buf][0][threadIdx.x] = sl; stat[buf][1][threadIdx.x] = sd; seen_by[buf][threadIdx.x] = ss; }
+    const auto land = [&](Rows& to) __attribute__((always_inline)) {
+        sq.put(to.tile[0]);
+        sg.put(to.tile[1]);
+        if (threadIdx.x < BM) { to.lse[threadIdx.x] = sl; to.less[threadIdx.x] = sd; to.seen[threadIdx.x] = ss; }
+        wait_tiles();
+        __syncthreads();
     };
     f32x16 dk[DT] = {}, dv[DT] = {};
-    if (lo < hi) {
-        fetch(lo);
-        put(0);
-        __syncthreads();
-    }
-    for (int t = lo; t < hi; ++t) {
-        const int buf = (t - lo) & 1;
-        const char* tq = lds[buf][0];
-        const char* tg = lds[buf][1];
-        if (t + 1 < hi) fetch(t + 1);
-        if (busy) {
-            f32x16 s = {}, p = {};
+    // the sums that S and dP - delta of rows u .. u + 31 of a tile start from; hide: some row does not see all of the wavefront's keys
+    const auto start = [&](const Rows& at, int u, bool hide, f32x16& s, f32x16& p) __attribute__((always_inline)) {
 #pragma unroll
-            for (int c = 0; c < D / 16; ++c) {
-                s = mma(L::along(tq, 0, c), k[c], s);
-                p = mma(L::along(tg, 0, c), v[c], p);
-            }
-            // the tile's first row sees the fewest keys
-            const bool mask = a.causal && query_of(a, t * kRows) + len.off + 1 < key0 + 128;
-            f32x16 e;
+        for (int r = 0; r < 16; r += 4) {
+            const f32x4 less = *(const f32x4*)&at.less[u + 8 * (r >> 2) + 4 * h];
 #pragma unroll
-            for (int r = 0; r < 16; r += 4) {
-                const f32x4 lse = *(const f32x4*)&stat[buf][0][8 * (r >> 2) + 4 * h], delta = *(const f32x4*)&stat[buf][1][8 * (r >> 2) + 4 * h];
-                typedef int i32x4 __attribute__((ext_vector_type(4)));
-                const i32x4 seen = *(const i32x4*)&seen_by[buf][8 * (r >> 2) + 4 * h];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const float w = __builtin_amdgcn_exp2f(fmaf(s[r + j], a.c, -lse[j]));
-                    const bool hidden = mask && key >= seen[j];
-                    e[r + j] = hidden ? 0.0f : w * (p[r + j] - delta[j]);
-                    s[r + j] = hidden ? 0.0f : w;
-                }
-            }
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                const Frag fp = operand<T>(s, c), fe = operand<T>(e, c);
-#pragma unroll
-                for (int d = 0; d < DT; ++d) {
-                    dv[d] = mma(L::across(tg, 16 * c, 32 * d), fp, dv[d]);
-                    dk[d] = mma(L::across(tq, 16 * c, 32 * d), fe, dk[d]);
-                }
-            }
+            for (int j = 0; j < 4; ++j) { s[r + j] = 0; p[r + j] = less[j]; }
         }
-        if (t + 1 < hi) put(buf ^ 1);
-        __syncthreads();
+        if (hide) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[r] = key >= at.seen[u + 8 * (r >> 2) + 4 * h + (r & 3)] ? kHidden : 0.0f;
+        }
+    };
+    // this unit's probabilities and products (rows u .. of `now`), and the scores of the next one (rows w .. of `next`)
+    const auto unit = [&](const Rows& now, int u, const Rows& next, int w, bool hide, f32x16& s, f32x16& p, f32x16& s2, f32x16& p2) __attribute__((always_inline)) {
+        Frag fa[2 * KS], fc[2][2 * DT];
+        Words<T> ws, we;
+        f32x4 lse[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) lse[r] = *(const f32x4*)&now.lse[u + 8 * r + 4 * h];
+        start(next, w, hide, s2, p2);
+        overlap<2 * KS, 2 * DT>(
+            [&](int i) __attribute__((always_inline)) { fa[i] = L::along(next.tile[i & 1], w, i >> 1); },
+            [&](int i) __attribute__((always_inline)) {
+                if (i & 1) p2 = mma(fa[i], v[i >> 1], p2);
+                else s2 = mma(fa[i], k[i >> 1], s2);
+            },
+            [&](int g) __attribute__((always_inline)) {
+#pragma unroll
+                for (int r = 2 * g; r < 2 * g + 2; ++r) {
+                    s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], a.c, -lse[r >> 2][r & 3]));
+                    p[r] *= s[r];
+                }
+                ws.set(g, s[2 * g], s[2 * g + 1]);
+                we.set(g, p[2 * g], p[2 * g + 1]);
+            },
+            [&](int c, int i) __attribute__((always_inline)) { fc[c][i] = L::across(now.tile[1 - (i & 1)], u + 16 * c, 32 * (i >> 1)); },
+            [&](int c, int i) __attribute__((always_inline)) {
+                if (i & 1) dk[i >> 1] = mma(fc[c][i], we.f[c], dk[i >> 1]);
+                else dv[i >> 1] = mma(fc[c][i], ws.f[c], dv[i >> 1]);
+            });
+    };
+    f32x16 s0, p0, s1, p1;
+    const auto hides = [&](int t) { return a.causal && len.seen(a, first_query(t)) < mine + 32; };     // (a tile's first row sees the fewest keys)
+    const auto tile = [&](int t, Rows& now, Rows& next, Rows& after, auto odd) __attribute__((always_inline)) {
+#pragma unroll
+        for (int n = 0; n < UNITS; ++n) {
+            const bool end = n == UNITS - 1;
+            if (end) {                              // the next tile has landed, and nobody reads the one before this
+                if (t + 1 < hi) land(next);
+                if (t + 2 < hi) fetch(t + 2, after);
+            }
+            const Rows& then = end ? next : now;
+            const int w = end ? 0 : 32 * (n + 1);
+            const bool hide = hides(end ? t + 1 : t), flip = UNITS == 1 ? odd : n & 1;
+            if (flip) unit(now, 32 * n, then, w, hide, s1, p1, s0, p0);
+            else unit(now, 32 * n, then, w, hide, s0, p0, s1, p1);
+        }
+    };
+    if (lo < hi) {
+        fetch(lo, r0);
+        land(r0);
+        if (lo + 1 < hi) fetch(lo + 1, r1);
+        start(r0, 0, hides(lo), s0, p0);
+#pragma unroll
+        for (int c = 0; c < KS; ++c) {
+            s0 = mma(L::along(r0.tile[0], 0, c), k[c], s0);
+            p0 = mma(L::along(r0.tile[1], 0, c), v[c], p0);
+        }
+    }
+    const std::false_type even;
+    const std::true_type odd;
+    for (int t = lo; t < hi; t += 3) {
+        tile(t, r0, r1, r2, even);
+        if (t + 1 < hi) tile(t + 1, r1, r2, r0, odd);
+        if (t + 2 < hi) tile(t + 2, r2, r0, r1, even);
+        if constexpr (UNITS == 1) {                 // (the scores change places with every unit)
+            t += 3;
+            if (t < hi) tile(t, r0, r1, r2, odd);
+            if (t + 1 < hi) tile(t + 1, r1, r2, r0, even);
+            if (t + 2 < hi) tile(t + 2, r2, r0, r1, odd);
+        }
     }
     if (key >= a.kv_len) return;
     if (a.causal && __any(not_finite(dk) || not_finite(dv))) {
+        const int key = again(key0 + wave * 32 + (l & 31));         // (what follows is not worth registers before)
         if (both_max(not_finite(dk) || not_finite(dv) ? 1.0f : 0.0f) > 0 && inside) {
             const T* kr = (const T*)a.k + b * a.ks[0] + key * a.ks[1] + kvh * a.ks[2];
             const T* vr = (const T*)a.v + b * a.vs[0] + key * a.vs[1] + kvh * a.vs[2];
 #pragma unroll
             for (int d = 0; d < DT; ++d) dk[d] = dv[d] = f32x16{};
-            for (int row = lo * kRows; row < min(hi * kRows, rows); ++row) {
+            for (int row = lo * each; row < (int)min((long long)hi * each, (long long)rows); ++row) {
                 const int i = query_of(a, row), j = row - i * a.group;
                 if (len.seen(a, i) <= key) continue;
                 const T* qr = qp + i * a.qs[1] + j * a.qs[2];
@@ -282,30 +349,31 @@ __global__ __launch_bounds__(256) void k_attention_dkv(const AttentionArgs a)
         }
 }
 
-// Sums of the splits, first split first: rows of D floats `stride` floats apart from split to split, each to its place.  WHICH: 0 dq, 1 dk, 2 dv.
-template <typename T, int D, int WHICH>
-__global__ __launch_bounds__(256) void k_attention_add(const AttentionArgs a, const float* parts, long long stride, int splits)
+// Sums of the splits, first split first: rows of D floats, `stride` floats from split to split, each to its place.  KEYS: dk (blockIdx.y 0) and dv (1), else dq.
+template <typename T, int D, bool KEYS>
+__global__ __launch_bounds__(256) void k_attention_add(const AttentionArgs a, long long stride, int splits)
 {
     constexpr int LANES = D / 4;
-    const int rows = WHICH ? a.kv_len : a.q_len * a.group;
-    const long long at = (long long)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
-    if (at >= (long long)a.batch * a.kv * rows) return;
+    const int rows = KEYS ? a.kv_len : a.q_len * a.group;
+    const long long n = (long long)a.batch * a.kv * rows, at = (long long)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
+    if (at >= n) return;
     const int d0 = (threadIdx.x % LANES) * 4, row = (int)(at % rows), kvh = (int)(at / rows % a.kv), b = (int)(at / rows / a.kv);
+    const float* parts = a.ws + (blockIdx.y * n + at) * D + d0;
     f32x4 v = {0, 0, 0, 0};
-#pragma unroll 4
-    for (int s = 0; s < splits; ++s) v += *(const f32x4*)(parts + s * stride + at * D + d0);
+#pragma unroll 8
+    for (int s = 0; s < splits; ++s) v += *(const f32x4*)(parts + s * stride);
+    const Lengths len(a, b);
     T* p;
-    if constexpr (WHICH == 0) {
+    bool any;
+    if constexpr (KEYS) {
+        p = blockIdx.y ? (T*)a.dv + b * a.dvs[0] + row * a.dvs[1] + kvh * a.dvs[2] : (T*)a.dk + b * a.dks[0] + row * a.dks[1] + kvh * a.dks[2];
+        any = row < len.k;
+    } else {
         const int i = query_of(a, row);
         p = (T*)a.dq + b * a.dqs[0] + i * a.dqs[1] + (kvh * a.group + row - i * a.group) * a.dqs[2];
-        v = Lengths(a, b).seen(a, i) ? v * a.scale : f32x4{0, 0, 0, 0};
-    } else if constexpr (WHICH == 1) {
-        p = (T*)a.dk + b * a.dks[0] + row * a.dks[1] + kvh * a.dks[2];
-        v = row < Lengths(a, b).k ? v * a.scale : f32x4{0, 0, 0, 0};
-    } else {
-        p = (T*)a.dv + b * a.dvs[0] + row * a.dvs[1] + kvh * a.dvs[2];
-        v = row < Lengths(a, b).k ? v : f32x4{0, 0, 0, 0};
+        any = len.seen(a, i) > 0;
     }
+    v = any ? v * (blockIdx.y ? 1.0f : a.scale) : f32x4{0, 0, 0, 0};
     store4(p, d0, a.d, a.vec, v[0], v[1], v[2], v[3]);
 }
 
@@ -318,7 +386,7 @@ Splits backward_splits(const ftp_attention_shape& s)
     const auto pick = [](long long blocks, long long tiles) {
         return blocks >= 256 ? 1 : (int)std::max(1ll, std::min({512 / std::max(blocks, 1ll), tiles / 4, 64ll}));
     };
-    return {pick(nq, ceil_div(s.kv_len, s.dtype == FTP_BF16 ? 64 : 32)), pick(nk, ceil_div(rows, kRows))};
+    return {pick(nq, ceil_div(s.kv_len, s.dtype == FTP_BF16 ? 64 : 32)), pick(nk, ceil_div(rows, rows_of_tile(s.heads / s.kv_heads, s.dtype == FTP_BF16 ? 64 : 32)))};
 }
 
 int padded(const ftp_attention_shape& s) { return s.head_dim <= 32 ? 32 : s.head_dim <= 64 ? 64 : 128; }
@@ -331,19 +399,19 @@ void run(AttentionArgs a, const Splits& n, hipStream_t st)
         a.blocks = (int)ceil_div(rows, 128);
         a.splits = n.dq;
         const unsigned grid = place_groups(a);
-        k_attention_dq<T, D><<<grid, 256, 0, st>>>(a);
-        if (n.dq > 1) k_attention_add<T, D, 0><<<(unsigned)ceil_div(all * rows, 1024 / D), 256, 0, st>>>(a, a.ws, all * rows * D, n.dq);
+        if (a.vec) k_attention_dq<T, D, true><<<grid, 256, 0, st>>>(a);
+        else k_attention_dq<T, D, false><<<grid, 256, 0, st>>>(a);
+        if (n.dq > 1) k_attention_add<T, D, false><<<(unsigned)ceil_div(all * rows, 1024 / D), 256, 0, st>>>(a, all * rows * D, n.dq);
     }
     if (a.kv_len) {
         a.blocks = (int)ceil_div(a.kv_len, 128);
         a.splits = n.dkv;
         const unsigned grid = place_groups(a);
-        k_attention_dkv<T, D><<<grid, 256, 0, st>>>(a);
+        if (a.vec) k_attention_dkv<T, D, true><<<grid, 256, 0, st>>>(a);
+        else k_attention_dkv<T, D, false><<<grid, 256, 0, st>>>(a);
         if (n.dkv > 1) {
             const long long each = all * a.kv_len * D;
-            const unsigned adds = (unsigned)ceil_div(all * a.kv_len, 1024 / D);
-            k_attention_add<T, D, 1><<<adds, 256, 0, st>>>(a, a.ws, 2 * each, n.dkv);
-            k_attention_add<T, D, 2><<<adds, 256, 0, st>>>(a, a.ws + each, 2 * each, n.dkv);
+            k_attention_add<T, D, true><<<dim3((unsigned)ceil_div(all * a.kv_len, 1024 / D), 2), 256, 0, st>>>(a, 2 * each, n.dkv);
         }
     }
 }
@@ -372,6 +440,8 @@ void attention_backward(const ftp_attention_shape& s, const void* dout, const vo
     for (const void* p : {q, k, v, out, dout, (const void*)dq, (const void*)dk, (const void*)dv}) a.vec = a.vec && aligned(p, 16);
     for (const long long* t : {a.qs, a.ks, a.vs, a.os, a.gs, a.dqs, a.dks, a.dvs})
         for (int i = 0; i < 3; ++i) a.vec = a.vec && t[i] % el == 0;
+    for (const long long* t : {a.ks, a.vs, a.qs, a.gs}) a.vec = a.vec && near_rows(t[1]);
+    a.vec = a.vec && near_rows(a.qs[2] * a.group / 128) && near_rows(a.gs[2] * a.group / 128);
     const Splits n = backward_splits(s);
     if (s.dtype == FTP_BF16) {
         if (a.d <= 32) run<bf16_t, 32>(a, n, st);
