@@ -3,8 +3,8 @@
 // three bfloats whose sum it is (three products, about the fp32 instruction's accuracy at five times its rate).
 //
 // A workgroup is a 128 x 128 block of dW and a share of the rows: 4 wavefronts of 64 x 64.  The contraction runs down the slow axis of both operands, so both are staged in LDS as they
-// lie (dy after its split, codes after their conversion) and read through the transposing LDS load: 4 rows x 16 columns a 16 lanes.  A stage is 32 rows, two stages in LDS,
-// the next one's loads in flight during the products.  The shares' blocks are added up by a second kernel in a fixed order.
+// lie (dy after its split, codes after their conversion) and read through the transposing LDS load: 4 rows x 16 columns a 16 lanes.  A stage is 64 rows (32 of fp32), two stages in LDS
+// and two more on their way in registers: with one, a workgroup waited for HBM most of the time.  The shares' blocks are added up by a second kernel in a fixed order.
 #include "ftp_tokens.h"
 
 #include <algorithm>
@@ -19,10 +19,10 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 struct HeldWgradArgs {
     const void* dy; const int8_t* codes; const int8_t* exps; float* dw; float* partial;
     long long rows, dy_stride;
-    int N, K, nblocks, lgblock, shares, ntiles, ktiles, vec_dy, vec_codes;
+    int N, K, nblocks, lgblock, shares, ntiles, ktiles;
 };
 
-constexpr int kStage = 32;                          // rows of a stage
+template <typename T> constexpr int kStage = sizeof(T) == 4 ? 32 : 64;       // rows of a stage
 constexpr int kBlk = 128;                           // columns of either operand a workgroup takes
 
 // Byte offset of 8 columns (chunk) of a row of a [row][128] bfloat tile.  The chunk is exchanged so that 4 consecutive rows' equal chunks lie in different quarters of the
@@ -43,105 +43,118 @@ __device__ __forceinline__ b16x8 read_t(const char* tile, int row0, int col0)
     return __builtin_bit_cast(b16x8, __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
-template <typename T>
-__global__ __launch_bounds__(256) void k_held_wgrad(const HeldWgradArgs a)
+// VEC: addresses and sizes let 8 of dy and 16 codes go at once.
+template <typename T, bool VEC>
+__global__ __launch_bounds__(256, 2) void k_held_wgrad(const HeldWgradArgs a)
 {
     constexpr int P = sizeof(T) == 4 ? 3 : 1;       // bfloats of a dy
-    constexpr int kTile = kStage * 256;
+    constexpr int S = kStage<T>, kTile = S * 256, DR = S / 16, CR = S / 32;
     __shared__ __align__(16) char lds[2][(P + 1) * kTile];
     const int tid = threadIdx.x, wave = tid >> 6;
     const int tile = blockIdx.x % (a.ntiles * a.ktiles), share = blockIdx.x / (a.ntiles * a.ktiles);
     const int n0 = (tile % a.ntiles) * kBlk, k0 = (tile / a.ntiles) * kBlk;
     // a share is whole stages
-    const long long stages = (a.rows + kStage - 1) / kStage;
+    const long long stages = (a.rows + S - 1) / S;
     const long long lo = stages * share / a.shares, hi = stages * (share + 1) / a.shares;
     const int wn = (wave & 1) * 64, wk = (wave >> 1) * 64;
 
-    // this thread's part of a stage: of dy 8 columns of rows tid / 16 and tid / 16 + 16, of the codes 16 columns of row tid / 8
+    // this thread's part of a stage: of dy 8 columns of rows tid / 16 + 16 i, of the codes 16 columns of rows tid / 8 + 32 i.  Columns past the matrix' edge are
+    // read from inside it and not stored; rows past its end are read from its last row and cleared.
     const int drow = tid >> 4, dcol = (tid & 15) * 8, crow = tid >> 3, ccol = (tid & 7) * 16;
-    float d[2][8];
-    uint32_t c[4];
-    float unit = 0;
-    const auto fetch = [&](long long stage) {
+    const int dn = n0 + dcol < a.N ? n0 + dcol : 0, cn = k0 + ccol < a.K ? k0 + ccol : 0;
+    struct Part { Pack<T, VEC ? 8 : 1> d[DR][VEC ? 1 : 8]; uint32_t c[CR][4]; int e[CR]; };
+    const auto fetch = [&](Part& x, long long stage) __attribute__((always_inline)) {
+        const long long last = a.rows - 1;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const long long r = stage * kStage + drow + 16 * i;
-            const T* p = (const T*)a.dy + r * a.dy_stride + n0 + dcol;
-            const int n = r < a.rows ? a.N - n0 - dcol : 0;
-            if (a.vec_dy && n >= 8) {
-                Pack<T, 8> w;
-                w.load(p);
+        for (int i = 0; i < DR; ++i) {
+            const T* p = (const T*)a.dy + min(stage * S + drow + 16 * i, last) * a.dy_stride;
+            if constexpr (VEC) x.d[i][0].load(p + dn);
+            else {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) d[i][j] = w.get(j);
+                for (int j = 0; j < 8; ++j) x.d[i][j].load(p + min(dn + j, a.N - 1));
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < CR; ++i) {
+            const long long r = min(stage * S + crow + 32 * i, last);
+            const int8_t* p = a.codes + r * a.K;
+            if constexpr (VEC) {
+                const uint4 w = *(const uint4*)(p + cn);
+                x.c[i][0] = w.x; x.c[i][1] = w.y; x.c[i][2] = w.z; x.c[i][3] = w.w;
             } else {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) d[i][j] = j < n ? ld(p + j) : 0.0f;
+                for (int j = 0; j < 16; ++j) {
+                    const uint32_t v = (uint8_t)p[min(cn + j, a.K - 1)];
+                    x.c[i][j / 4] = (j & 3 ? x.c[i][j / 4] : 0) | v << (8 * (j & 3));
+                }
             }
+            x.e[i] = a.exps[r * a.nblocks + (cn >> a.lgblock)];
         }
-        const long long r = stage * kStage + crow;
-        const int n = r < a.rows ? a.K - k0 - ccol : 0;
-        const int8_t* p = a.codes + r * a.K + k0 + ccol;
-        if (a.vec_codes && n >= 16) {
-            const uint4 w = *(const uint4*)p;
-            c[0] = w.x; c[1] = w.y; c[2] = w.z; c[3] = w.w;
-        } else {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                c[j] = 0;
-#pragma unroll
-                for (int b = 0; b < 4; ++b) if (4 * j + b < n) c[j] |= (uint32_t)(uint8_t)p[4 * j + b] << (8 * b);
-            }
-        }
-        unit = n > 0 ? held_scale(a.exps[r * a.nblocks + ((k0 + ccol) >> a.lgblock)]) : 0.0f;
     };
-    const auto put = [&](char* t) {
+    const auto put = [&](const Part& x, char* t, long long stage) __attribute__((always_inline)) {
+        const int left = (int)min((long long)S, a.rows - stage * S);
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < DR; ++i) {
+            float d[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) d[j] = drow + 16 * i < left ? (VEC ? x.d[i][0].get(j) : x.d[i][VEC ? 0 : j].get(0)) : 0.0f;
             uint4 w[P];
             uint32_t* q = (uint32_t*)w;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                if constexpr (P == 1) q[j] = pack_bf16(d[i][2 * j], d[i][2 * j + 1]);
-                else split3(d[i][2 * j] * kSplitScale, d[i][2 * j + 1] * kSplitScale, q[j], q[4 + j], q[8 + j]);
+                if constexpr (P == 1) q[j] = pack_bf16(d[2 * j], d[2 * j + 1]);
+                else split3(d[2 * j] * kSplitScale, d[2 * j + 1] * kSplitScale, q[j], q[4 + j], q[8 + j]);
             }
 #pragma unroll
             for (int s = 0; s < P; ++s) *(uint4*)(t + s * kTile + tile_at(drow + 16 * i, dcol >> 3)) = w[s];
         }
-        uint4 w[2];
-        uint32_t* q = (uint32_t*)w;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int word = (int)c[j >> 1], sh = (j & 1) * 16;
-            q[j] = pack_bf16((float)(int8_t)(word >> sh) * unit, (float)(int8_t)(word >> (sh + 8)) * unit);
+        for (int i = 0; i < CR; ++i) {
+            const bool there = crow + 32 * i < left;
+            const float unit = there ? held_scale(x.e[i]) : 0.0f;
+            uint4 w[2];
+            uint32_t* q = (uint32_t*)w;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int word = (int)x.c[i][j >> 1], sh = (j & 1) * 16;
+                q[j] = pack_bf16((float)(int8_t)(word >> sh) * unit, (float)(int8_t)(word >> (sh + 8)) * unit);
+            }
+            *(uint4*)(t + P * kTile + tile_at(crow + 32 * i, ccol >> 3)) = w[0];
+            *(uint4*)(t + P * kTile + tile_at(crow + 32 * i, (ccol >> 3) + 1)) = w[1];
         }
-        *(uint4*)(t + P * kTile + tile_at(crow, ccol >> 3)) = w[0];
-        *(uint4*)(t + P * kTile + tile_at(crow, (ccol >> 3) + 1)) = w[1];
     };
 
     f32x16 acc[2][2] = {};
-    if (lo < hi) {
-        fetch(lo);
-        put(lds[0]);
+    // stage s is in LDS, `next` holds stage s + 1 and takes stage s + 3 once that is in LDS; stage s + 2 is on its way beside it
+    const auto step = [&](long long s, const char* now, char* then, Part& next) __attribute__((always_inline)) {
+#pragma unroll
+        for (int r0 = 0; r0 < S; r0 += 16) {
+            b16x8 b[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) b[j] = read_t(now + P * kTile, r0, wk + 32 * j);
+#pragma unroll
+            for (int p = P - 1; p >= 0; --p)         // smallest first
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const b16x8 x = read_t(now + p * kTile, r0, wn + 32 * i);
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, b[j], acc[i][j], 0, 0, 0);
+                }
+        }
+        if (s + 1 < hi) put(next, then, s + 1);
+        if (s + 3 < hi) fetch(next, s + 3);
         __syncthreads();
-        for (long long s = lo; s < hi; ++s) {
-            const char* t = lds[(s - lo) & 1];
-            if (s + 1 < hi) fetch(s + 1);
-#pragma unroll
-            for (int r0 = 0; r0 < kStage; r0 += 16) {
-                b16x8 b[2];
-#pragma unroll
-                for (int j = 0; j < 2; ++j) b[j] = read_t(t + P * kTile, r0, wk + 32 * j);
-#pragma unroll
-                for (int p = P - 1; p >= 0; --p)     // smallest first
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        const b16x8 x = read_t(t + p * kTile, r0, wn + 32 * i);
-#pragma unroll
-                        for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, b[j], acc[i][j], 0, 0, 0);
-                    }
-            }
-            if (s + 1 < hi) put(lds[(s + 1 - lo) & 1]);
-            __syncthreads();
+    };
+    if (lo < hi) {
+        Part x, y;
+        fetch(x, lo);
+        if (lo + 1 < hi) fetch(y, lo + 1);
+        put(x, lds[0], lo);
+        if (lo + 2 < hi) fetch(x, lo + 2);
+        __syncthreads();
+        for (long long s = lo; s < hi; s += 2) {
+            step(s, lds[0], lds[1], y);
+            if (s + 1 < hi) step(s + 1, lds[1], lds[0], x);
         }
     }
     // lane: column k = lane % 32 of a 32 x 32 block, rows n = 8 (r / 4) + 4 (lane / 32) + r % 4
@@ -160,28 +173,35 @@ __global__ __launch_bounds__(256) void k_held_wgrad(const HeldWgradArgs a)
         }
 }
 
+// The shares' sum: 64 elements x 4 groups of shares a workgroup.
 __global__ __launch_bounds__(256) void k_held_wgrad_sum(const float* partial, float* dw, long long n, int shares)
 {
-    const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
-    if (i >= n) return;
+    __shared__ float lds[4][64];
+    const int e = threadIdx.x & 63, grp = threadIdx.x >> 6;
+    const long long i = (long long)blockIdx.x * 64 + e;
     float s = 0;
+    if (i < n) {
 #pragma unroll 8
-    for (int k = 0; k < shares; ++k) s += partial[k * n + i];
-    dw[i] = s;
+        for (int k = grp; k < shares; k += 4) s += partial[k * n + i];
+    }
+    lds[grp][e] = s;
+    __syncthreads();
+    if (grp == 0 && i < n) dw[i] = (lds[0][e] + lds[1][e]) + (lds[2][e] + lds[3][e]);
 }
 
-// Shares of the rows: as many as give every CU a workgroup, of at least 8 stages.
-int wgrad_shares(long long rows, int n, int k)
+// Shares of the rows: two workgroups a CU, of at least two stages.
+int wgrad_shares(long long rows, int n, int k, int stage)
 {
     const long long tiles = ceil_div(n, kBlk) * ceil_div(k, kBlk);
-    return (int)std::max(1ll, std::min<long long>(ceil_div(256, tiles), rows / (8 * kStage)));
+    return (int)std::max(1ll, std::min<long long>(ceil_div(512, tiles), rows / (2 * stage)));
 }
+int stage_of(const ftp_checkpoint_shape& s) { return s.dtype == FTP_BF16 ? kStage<bf16_t> : kStage<float>; }
 
 }  // namespace
 
 size_t held_wgrad_workspace(const ftp_checkpoint_shape& s, int outputs)
 {
-    const int shares = wgrad_shares(s.rows, outputs, (int)s.cols);
+    const int shares = wgrad_shares(s.rows, outputs, (int)s.cols, stage_of(s));
     return shares > 1 ? (size_t)shares * outputs * s.cols * sizeof(float) : 0;
 }
 
@@ -193,15 +213,16 @@ void held_wgrad(const ftp_checkpoint_shape& s, const int8_t* codes, const int8_t
     a.rows = s.rows; a.dy_stride = dy_stride; a.N = outputs; a.K = (int)s.cols;
     a.nblocks = (int)ceil_div(s.cols, s.block);
     while ((1 << a.lgblock) < s.block) ++a.lgblock;
-    a.shares = wgrad_shares(s.rows, a.N, a.K);
+    a.shares = wgrad_shares(s.rows, a.N, a.K, stage_of(s));
     a.ntiles = (int)ceil_div(a.N, kBlk); a.ktiles = (int)ceil_div(a.K, kBlk);
     const bool bf = s.dtype == FTP_BF16;
-    a.vec_dy = aligned(dy, 16) && dy_stride % (bf ? 8 : 4) == 0;
-    a.vec_codes = aligned(codes, 16) && s.cols % 16 == 0;
+    const bool vec = aligned(dy, 16) && dy_stride % (bf ? 8 : 4) == 0 && a.N % 8 == 0 && aligned(codes, 16) && a.K % 16 == 0;
     const unsigned grid = (unsigned)(a.ntiles * a.ktiles * a.shares);
-    if (bf) k_held_wgrad<bf16_t><<<grid, 256, 0, st>>>(a);
-    else k_held_wgrad<float><<<grid, 256, 0, st>>>(a);
-    if (a.shares > 1) k_held_wgrad_sum<<<(unsigned)ceil_div((long long)a.N * a.K, 256), 256, 0, st>>>(partial, dw, (long long)a.N * a.K, a.shares);
+    if (bf && vec) k_held_wgrad<bf16_t, true><<<grid, 256, 0, st>>>(a);
+    else if (bf) k_held_wgrad<bf16_t, false><<<grid, 256, 0, st>>>(a);
+    else if (vec) k_held_wgrad<float, true><<<grid, 256, 0, st>>>(a);
+    else k_held_wgrad<float, false><<<grid, 256, 0, st>>>(a);
+    if (a.shares > 1) k_held_wgrad_sum<<<(unsigned)ceil_div((long long)a.N * a.K, 64), 256, 0, st>>>(partial, dw, (long long)a.N * a.K, a.shares);
 }
 
 }  // namespace ftp
