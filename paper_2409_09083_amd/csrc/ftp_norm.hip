@@ -32,11 +32,22 @@ __device__ __forceinline__ long long row_offset(long long row, long long inner, 
     return o * so + (row - o * inner) * si;
 }
 
-// Sum over the lanes of a row; every lane gets it.  WIDE: the row is the workgroup.
+// Sum over the `lanes` lanes of a row (a power of two); every lane gets it.  Neighbours are exchanged by the vector unit itself (data-parallel primitives, permlane swaps), not
+// through the LDS crossbar.  WIDE: the row is the workgroup.
+__device__ __forceinline__ float lane_sum(float v, int lanes)
+{
+    if (lanes > 1) v += quad_xor<1>(v);
+    if (lanes > 2) v += quad_xor<2>(v);
+    if (lanes > 4) v += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x141, 0xF, 0xF, true));      // row_half_mirror: the other quad of 8
+    if (lanes > 8) v += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x140, 0xF, 0xF, true));      // row_mirror: the other half of 16
+    if (lanes > 16) { const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false); v = __uint_as_float(r[0]) + __uint_as_float(r[1]); }
+    if (lanes > 32) { const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false); v = __uint_as_float(r[0]) + __uint_as_float(r[1]); }
+    return v;
+}
 template <bool WIDE>
 __device__ __forceinline__ float row_sum(float v, int lanes, float* lds)
 {
-    for (int m = (WIDE ? 64 : lanes) >> 1; m; m >>= 1) v += __shfl_xor(v, m);
+    v = lane_sum(v, WIDE ? 64 : lanes);
     if constexpr (WIDE) {
         if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
         __syncthreads();
@@ -97,15 +108,18 @@ __global__ __launch_bounds__(256) void k_norm_rows(const RowArgs a)
     }
 }
 
+constexpr int kBackThreads = 512;                   // (twice the wavefronts to a share of dgamma and dbeta than 256)
+
 // A workgroup walks over rows and keeps its part of dgamma and dbeta in registers; the next row's loads are in flight while this one is worked on.
 // HELD: x comes from its 8-bit checkpoint.
 template <typename T, int VEC, int NV, bool WIDE, bool HELD>
-__global__ __launch_bounds__(256) void k_norm_back_rows(const RowArgs a)
+__global__ __launch_bounds__(WIDE ? 256 : kBackThreads) void k_norm_back_rows(const RowArgs a)
 {
-    __shared__ float lds[WIDE ? 4 : 4 * 64 * VEC * NV];
+    constexpr int WAVES = kBackThreads / 64;
+    __shared__ float lds[WIDE ? 4 : WAVES * 64 * VEC * NV];
     typedef typename std::conditional<HELD, int8_t, T>::type X;
     const int lanes = WIDE ? 256 : a.lanes;
-    const int lane = threadIdx.x & (lanes - 1), per = 256 / lanes;
+    const int lane = threadIdx.x & (lanes - 1), per = WIDE ? 1 : kBackThreads / lanes;
     const long long step = (long long)gridDim.x * per;
     Pack<T, VEC> g[NV];
     float dg[NV][VEC], db[NV][VEC];
@@ -213,7 +227,12 @@ __global__ __launch_bounds__(256) void k_norm_back_rows(const RowArgs a)
                     if ((threadIdx.x & 63) < lanes) lds[(threadIdx.x >> 6) * width + (i * lanes + lane) * VEC + j] = v;
                 }
             __syncthreads();
-            for (int c = threadIdx.x; c < a.C; c += 256) out[c] = (lds[c] + lds[width + c]) + (lds[2 * width + c] + lds[3 * width + c]);
+            for (int c = threadIdx.x; c < a.C; c += kBackThreads) {
+                float v = 0;
+#pragma unroll
+                for (int w = 0; w < WAVES; ++w) v += lds[w * width + c];
+                out[c] = v;
+            }
         }
     }
 }
@@ -293,7 +312,7 @@ __global__ __launch_bounds__(1024) void k_norm_params(const float* partial, int 
     const int col = blockIdx.x * 32 + (threadIdx.x & 31), grp = threadIdx.x >> 5, width = 2 * C;
     float s = 0;
     if (col < width) {
-#pragma unroll 8
+#pragma unroll 16
         for (int i = grp; i < shares; i += 32) s += partial[(long long)i * width + col];
     }
     lds[grp][threadIdx.x & 31] = s;
@@ -355,14 +374,22 @@ __device__ __forceinline__ void tile_load(T* tile, const T* p, const long long (
     else tile_load_v<T, 16 / (int)sizeof(T)>(tile, p, s, C, px, shift, n, pitch);
 }
 
+// The parameters as fp32 in LDS (null: `none`).
+template <typename T>
+__device__ __forceinline__ void param_load(float* to, const void* p, float none, int C)
+{
+    for (int c = threadIdx.x; c < C; c += 256) to[c] = p ? ld((const T*)p + c) : none;
+}
+
 // p[token][channel] = f(channel, token); tokens below n.
 template <typename T, int V, class F>
 __device__ __forceinline__ void tile_store_v(T* p, const long long (&s)[3], int C, int px, int shift, int n, F f)
 {
     if (s[2] == 1) {
         const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-        for (int t = wave; t < n; t += 4)
-            for (int c = lane * V; c < C; c += 64 * V) {
+        for (int c = lane * V; c < C; c += 64 * V)
+#pragma unroll 4
+            for (int t = wave; t < n; t += 4) {
                 float v[V];
 #pragma unroll
                 for (int j = 0; j < V; ++j) v[j] = f(c + j, t);
@@ -416,7 +443,11 @@ __global__ __launch_bounds__(256) void k_norm_tiles(const TileArgs a)
     float* red = (float*)smem;
     float* mean = red + 256;
     float* rstd = mean + 64;
-    T* tile = (T*)(rstd + 64);
+    float* gamma = rstd + 64;
+    float* beta = gamma + a.C;
+    T* tile = (T*)(beta + a.C);
+    param_load<T>(gamma, a.gamma, 1.0f, a.C);
+    param_load<T>(beta, a.beta, 0.0f, a.C);
     const int o = blockIdx.x / a.tiles, pitch = tile_pitch<T>(a.px);
     const long long at = (long long)(blockIdx.x - o * a.tiles) << a.shift;
     const int n = (int)min((long long)a.px, a.inner - at);
@@ -436,7 +467,7 @@ __global__ __launch_bounds__(256) void k_norm_tiles(const TileArgs a)
     }
     __syncthreads();
     tile_store((T*)a.y + o * a.ys[0] + at * a.ys[1], a.ys, a.yvec, a.C, a.px, a.shift, n, [&](int c, int t) {
-        return fmaf((ld(tile + c * pitch + t) - mean[t]) * rstd[t], a.gamma ? ld((const T*)a.gamma + c) : 1.0f, a.beta ? ld((const T*)a.beta + c) : 0.0f);
+        return fmaf((ld(tile + c * pitch + t) - mean[t]) * rstd[t], gamma[c], beta[c]);
     });
 }
 
@@ -451,7 +482,9 @@ __global__ __launch_bounds__(256) void k_norm_back_tiles(const TileArgs a)
     float* s2 = s1 + 64;
     float* acc = s2 + 64;                           // [2][C], a thread its own channels
     const int pitch = tile_pitch<T>(a.px);
-    T* tx = (T*)(acc + 2 * a.C);
+    float* gamma = acc + 2 * a.C;
+    T* tx = (T*)(gamma + a.C);
+    param_load<T>(gamma, a.gamma, 1.0f, a.C);
     T* ty = tx + (long long)a.C * pitch;
     for (int c = threadIdx.x; c < a.C; c += 256) acc[c] = acc[a.C + c] = 0;
     const float inv = 1.0f / (float)a.C;
@@ -467,12 +500,11 @@ __global__ __launch_bounds__(256) void k_norm_back_tiles(const TileArgs a)
         tile_load(tx, (const T*)a.x + o * a.xs[0] + at * a.xs[1], a.xs, a.xvec, a.C, a.px, a.shift, n, pitch);
         tile_load(ty, (const T*)a.dy + o * a.gs[0] + at * a.gs[1], a.gs, a.gvec, a.C, a.px, a.shift, n, pitch);
         __syncthreads();
-        const auto gamma = [&](int c) { return a.gamma ? ld((const T*)a.gamma + c) : 1.0f; };
         const auto h = [&](int c, int t) { return (ld(tx + c * pitch + t) - mean[t]) * rstd[t]; };
-        token_sums(s1, red, a.C, a.px, a.shift, [&](int c, int t) { return ld(ty + c * pitch + t) * gamma(c); });
-        token_sums(s2, red, a.C, a.px, a.shift, [&](int c, int t) { return ld(ty + c * pitch + t) * gamma(c) * h(c, t); });
+        token_sums(s1, red, a.C, a.px, a.shift, [&](int c, int t) { return ld(ty + c * pitch + t) * gamma[c]; });
+        token_sums(s2, red, a.C, a.px, a.shift, [&](int c, int t) { return ld(ty + c * pitch + t) * gamma[c] * h(c, t); });
         tile_store((T*)a.dx + o * a.ys[0] + at * a.ys[1], a.ys, a.yvec, a.C, a.px, a.shift, n, [&](int c, int t) {
-            return rstd[t] * (fmaf(ld(ty + c * pitch + t), gamma(c), -s1[t] * inv) - h(c, t) * (s2[t] * inv));
+            return rstd[t] * (fmaf(ld(ty + c * pitch + t), gamma[c], -s1[t] * inv) - h(c, t) * (s2[t] * inv));
         });
         if (a.partial)
             for (int c = threadIdx.x; c < a.C; c += 256) {
@@ -490,7 +522,7 @@ __global__ __launch_bounds__(256) void k_norm_back_tiles(const TileArgs a)
 
 // ---- which kernel --------------------------------------------------------------------------------------------------------------------------------------
 
-constexpr int kShares = 1024;                       // workgroups of a backward pass at most: each leaves 2 C sums
+constexpr int kShares = 512;                        // workgroups of a backward pass at most: each leaves 2 C sums
 
 // The strides that a pass uses: x, y and no third, or x (not from a checkpoint), dx and dy.
 struct Strides { const int64_t* x; const int64_t* y; const int64_t* g; };
@@ -544,10 +576,10 @@ void run_rows(const RowArgs& a, const RowForm& f, bool back, unsigned grid, hipS
             else k_norm_rows<T, VEC, NV, false><<<grid, 256, 0, st>>>(a);
         } else if (a.codes) {
             if (f.wide) k_norm_back_rows<T, VEC, NV, true, true><<<grid, 256, 0, st>>>(a);
-            else k_norm_back_rows<T, VEC, NV, false, true><<<grid, 256, 0, st>>>(a);
+            else k_norm_back_rows<T, VEC, NV, false, true><<<grid, kBackThreads, 0, st>>>(a);
         } else {
             if (f.wide) k_norm_back_rows<T, VEC, NV, true, false><<<grid, 256, 0, st>>>(a);
-            else k_norm_back_rows<T, VEC, NV, false, false><<<grid, 256, 0, st>>>(a);
+            else k_norm_back_rows<T, VEC, NV, false, false><<<grid, kBackThreads, 0, st>>>(a);
         }
     }
 }
@@ -574,15 +606,17 @@ void run_rows_t(const RowArgs& a, int vec, const RowForm& f, bool back, unsigned
     }
 }
 
-// Tokens a tile: as many as leave a CU two tiles at least (64 KB), up to 64.
 size_t tile_bytes(const ftp_norm_shape& s, int px, bool back)
 {
     const size_t es = s.dtype == FTP_BF16 ? 2 : 4;
-    return (256 + (back ? 256 : 128)) * 4 + (back ? 2 * (size_t)s.channels * 4 : 0) + (back ? 2 : 1) * (size_t)s.channels * (px + 4 / es) * es;
+    return (256 + (back ? 256 : 128)) * 4 + (back ? 3 : 2) * (size_t)s.channels * 4 + (back ? 2 : 1) * (size_t)s.channels * (px + 4 / es) * es;
 }
+// Tokens a tile: 128 bytes of a map's row; fewer, down to 64 bytes, where a CU would hold less than four workgroups, and as few as it takes to stay within 64 KB.
 int tile_tokens(const ftp_norm_shape& s, bool back)
 {
-    int px = 64;
+    const int es = s.dtype == FTP_BF16 ? 2 : 4;
+    int px = 128 / es;
+    while (px * es > 64 && tile_bytes(s, px, back) > 40960) px >>= 1;
     while (px > 1 && tile_bytes(s, px, back) > 65536) px >>= 1;
     while (px > 4 && px / 2 >= s.inner) px >>= 1;
     return px;
@@ -675,7 +709,7 @@ void norm_backward(const ftp_norm_shape& s, const void* dy, const void* x, const
             if (bf) k_norm_back_long<bf16_t><<<(unsigned)a.rows, 256, 0, st>>>(a);
             else k_norm_back_long<float><<<(unsigned)a.rows, 256, 0, st>>>(a);
         } else {
-            shares = (int)std::min<long long>(kShares, ceil_div(a.rows, 256 / f.lanes));
+            shares = (int)std::min<long long>(kShares, ceil_div(a.rows, f.wide ? 1 : kBackThreads / f.lanes));
             if (bf) run_rows_t<bf16_t>(a, vec, f, true, shares, st);
             else run_rows_t<float>(a, vec, f, true, shares, st);
         }

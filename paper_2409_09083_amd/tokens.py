@@ -63,7 +63,14 @@ def _scratch(nbytes, device):
 
 class _Operator:
     def _stream(self):
-        return torch.cuda.current_stream(self.device).cuda_stream
+        # (the handle of torch.cuda.current_stream(), without making a Stream object: a third of a small call's host time)
+        return torch._C._cuda_getCurrentRawStream(self.device.index)
+
+    def _set_strides(self, name, strides):
+        """Strides of a tensor into the description, where they differ from what it holds."""
+        if self._strides.get(name) != strides:
+            getattr(self.desc, name)[:] = strides
+            self._strides[name] = strides
 
 
 class Norm(_Operator):
@@ -79,13 +86,14 @@ class Norm(_Operator):
         self.device = _device(device)
         self.shape = torch.Size((outer, inner, channels))
         self.desc = B.ftp_norm_shape(outer=outer, inner=inner, channels=channels, dtype=code, eps=eps)
-        for stride in (self.desc.x_stride, self.desc.y_stride, self.desc.dy_stride, self.desc.dx_stride):
-            stride[:] = (inner * channels, channels, 1)
+        self._strides = {}
         self._ws_bytes = B.ftp_norm_workspace(self.desc)
         self._layouts = {"x": x_layout, "y": y_layout}
         self.y_buffer, self.y = self._buffer("y")
         self.mean = torch.empty((outer, inner), dtype=torch.float32, device=self.device)
         self.rstd = torch.empty_like(self.mean)
+        self._outputs = self.y.data_ptr(), self.mean.data_ptr(), self.rstd.data_ptr()
+        self._set_strides("y_stride", self.y.stride())
         self.dx = self.dx_buffer = self.dgamma = self.dbeta = self._ws = None
 
     def _buffer(self, of):
@@ -101,11 +109,8 @@ class Norm(_Operator):
 
     def forward(self, x, gamma=None, beta=None):
         px = _need("x", x, self.shape, self.tdtype, self.device)
-        d = self.desc
-        d.x_stride[:] = x.stride()
-        d.y_stride[:] = self.y.stride()
-        B.ftp_norm_forward(d, px, self._param("gamma", gamma), self._param("beta", beta), self.y.data_ptr(), self.mean.data_ptr(),
-                           self.rstd.data_ptr(), self._stream())
+        self._set_strides("x_stride", x.stride())
+        B.ftp_norm_forward(self.desc, px, self._param("gamma", gamma), self._param("beta", beta), *self._outputs, self._stream())
         return self.y
 
     def backward(self, dy, x, gamma=None, mean=None, rstd=None):
@@ -116,7 +121,6 @@ class Norm(_Operator):
             self.dgamma = torch.empty(self.shape[2], dtype=torch.float32, device=self.device)
             self.dbeta = torch.empty_like(self.dgamma)
             self._ws = _scratch(self._ws_bytes, self.device)
-        d = self.desc
         pdy = _need("dy", dy, self.shape, self.tdtype, self.device)
         px = pc = pe = block = 0
         if isinstance(x, Checkpoint):
@@ -125,12 +129,12 @@ class Norm(_Operator):
             pc, pe, block = x.codes.data_ptr(), x.exponents.data_ptr(), x.block
         else:
             px = _need("x", x, self.shape, self.tdtype, self.device)
-            d.x_stride[:] = x.stride()
-        d.dy_stride[:] = dy.stride()
-        d.dx_stride[:] = self.dx.stride()
+            self._set_strides("x_stride", x.stride())
+        self._set_strides("dy_stride", dy.stride())
+        self._set_strides("dx_stride", self.dx.stride())
         stat = [_dense(n, t, self.mean.shape, torch.float32, self.device)
                 for n, t in (("mean", self.mean if mean is None else mean), ("rstd", self.rstd if rstd is None else rstd))]
-        B.ftp_norm_backward(d, pdy, px, pc, pe, block, self._param("gamma", gamma), stat[0], stat[1], self.dx.data_ptr(),
+        B.ftp_norm_backward(self.desc, pdy, px, pc, pe, block, self._param("gamma", gamma), stat[0], stat[1], self.dx.data_ptr(),
                             self.dgamma.data_ptr(), self.dbeta.data_ptr(), self._ws.data_ptr(), self._stream())
         return self.dx, self.dgamma, self.dbeta
 
@@ -223,6 +227,7 @@ class Attention(_Operator):
         scale = (head_dim ** -0.5 if head_dim > 0 else 1.0) if scale is None else scale
         self.desc = B.ftp_attention_shape(batch=batch, heads=heads, kv_heads=kv_heads, q_len=q_len, kv_len=kv_len,
                                           head_dim=head_dim, dtype=code, causal=1 if causal else 0, scale=scale)
+        self._strides = {}
         forward, backward = B.ftp_attention_workspace(self.desc)
         self.q_shape = torch.Size((batch, q_len, heads, head_dim))
         self.k_shape = torch.Size((batch, kv_len, kv_heads, head_dim))
@@ -236,17 +241,15 @@ class Attention(_Operator):
         self.desc.out_stride[:] = self.out.stride()[:3]
         self._ws = _scratch(max(forward, backward if training else 0), self.device)
 
-    def _tensor(self, name, t, shape, stride):
+    def _tensor(self, name, t, shape):
         p = _need(name, t, shape, self.tdtype, self.device)
         if t.stride(3) != 1 and shape[3] > 1:
             raise ValueError("%s has channel stride %d" % (name, t.stride(3)))
-        stride[:] = t.stride()[:3]
+        self._set_strides(name + "_stride", t.stride()[:3])
         return p
 
     def _inputs(self, q, k, v, q_lens, kv_lens):
-        d = self.desc
-        return (self._tensor("q", q, self.q_shape, d.q_stride), self._tensor("k", k, self.k_shape, d.k_stride),
-                self._tensor("v", v, self.k_shape, d.v_stride), _dense("q_lens", q_lens, (self.batch,), torch.int32, self.device),
+        return (self._tensor("q", q, self.q_shape), self._tensor("k", k, self.k_shape), self._tensor("v", v, self.k_shape), _dense("q_lens", q_lens, (self.batch,), torch.int32, self.device),
                 _dense("kv_lens", kv_lens, (self.batch,), torch.int32, self.device))
 
     def forward(self, q, k, v, q_lens=None, kv_lens=None):
@@ -259,7 +262,7 @@ class Attention(_Operator):
         if not self.training:
             raise ValueError("made without `training`")
         inputs = self._inputs(q, k, v, q_lens, kv_lens)
-        pd = self._tensor("dout", dout, self.q_shape, self.desc.dout_stride)
+        pd = self._tensor("dout", dout, self.q_shape)
         B.ftp_attention_backward(self.desc, pd, *inputs, self.out.data_ptr(), self.lse.data_ptr(), self.dq.data_ptr(), self.dk.data_ptr(),
                                  self.dv.data_ptr(), self._ws.data_ptr(), self._stream())
         return self.dq, self.dk, self.dv
