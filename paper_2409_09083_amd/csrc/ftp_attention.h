@@ -3,7 +3,8 @@
 // The queries of the heads that share a key head are rows of one list: row r is query r / group of head r % group of those.  A tile of keys is
 // then read once for the whole group, gradients of shared keys need no sum over heads, and one query of a long cache still fills rows.
 //
-// All products run on 32x32 blocks: bfloats 16 deep (v_mfma_f32_32x32x16_bf16), fp32 numbers 2 deep (v_mfma_f32_32x32x2_f32, eight of them in the bfloat one's place).  A lane holds of
+// All products run on 32x32 blocks, 16 deep, on the bfloat matrix cores (v_mfma_f32_32x32x16_bf16).  An fp32 number goes in as three bfloats whose sum it is (ftp_split.h), a product as the
+// six of theirs that are above 2^-24 of it: 192 cycles where the fp32 instruction takes 512.  Tiles are split once, on their way into LDS.  A lane holds of
 // an operand the 8 values (index lane % 32; contraction 8 h + j, h = lane / 32, j < 8), and of a result column lane % 32 and rows 8 (i / 4) + 4 h + i % 4, i < 16.
 // The contraction may run over any order that both operands share.  So a result is the next product's operand as it lies: its registers 8 s .. 8 s + 7 are the operand
 // (index lane % 32; contraction 16 s + 8 (j / 4) + 4 h + j % 4), and the other operand is loaded in that order.  No probability passes through LDS.
@@ -20,87 +21,120 @@ typedef __bf16 b16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef float f32x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
+struct Split { b16x8 h, m, l; };                    // 8 fp32 numbers
 template <typename T> struct FragOf { typedef b16x8 type; };
-template <> struct FragOf<float> { typedef f32x8 type; };
+template <> struct FragOf<float> { typedef Split type; };
 
 __device__ __forceinline__ f32x16 mma(b16x8 a, b16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
-__device__ __forceinline__ f32x16 mma(f32x8 a, f32x8 b, f32x16 c)
+__device__ __forceinline__ f32x16 mma(const Split& a, const Split& b, f32x16 c)
 {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b[j], c, 0, 0, 0);
-    return c;
+    c = mma(a.l, b.h, c);                           // smallest first
+    c = mma(a.h, b.l, c);
+    c = mma(a.m, b.m, c);
+    c = mma(a.m, b.h, c);
+    c = mma(a.h, b.m, c);
+    return mma(a.h, b.h, c);
 }
+
+// Operands of pairs of neighbouring registers of a result, as they become known.
+__device__ __forceinline__ void set_word(b16x8& f, int j, uint32_t v)
+{
+    u32x4 w = __builtin_bit_cast(u32x4, f);
+    w[j] = v;
+    f = __builtin_bit_cast(b16x8, w);
+}
+template <typename T>
+struct Words {
+    typename FragOf<T>::type f[2];
+    __device__ __forceinline__ void set(int pair, float a, float b)
+    {
+        if constexpr (sizeof(T) == 4) {
+            uint32_t h, m, l;
+            split3(a, b, h, m, l);
+            Split& x = f[pair >> 2];
+            set_word(x.h, pair & 3, h); set_word(x.m, pair & 3, m); set_word(x.l, pair & 3, l);
+        } else set_word(f[pair >> 2], pair & 3, pack_bf16(a, b));
+    }
+};
 
 // Registers 8 s .. 8 s + 7 of a result as an operand: rounded to bfloats where the operands are bfloats (the probabilities and their gradients lose
 // what the inputs have lost already; sums stay fp32).
 template <typename T>
 __device__ __forceinline__ typename FragOf<T>::type operand(const f32x16& v, int s)
 {
-    if constexpr (sizeof(T) == 4) {
-        f32x8 r;
+    Words<T> w;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) r[j] = v[8 * s + j];
-        return r;
-    } else {
-        u32x4 r;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) r[j] = pack_bf16(v[8 * s + 2 * j], v[8 * s + 2 * j + 1]);
-        return __builtin_bit_cast(b16x8, r);
-    }
+    for (int j = 0; j < 4; ++j) w.set(j, v[8 * s + 2 * j], v[8 * s + 2 * j + 1]);
+    return w.f[0];
 }
 
-// A tile of rows of D channels in LDS, in chunks of 16 bytes.  Chunks are exchanged within a row by the row's low bits, so that neither 16 rows of one chunk (operand along the channels) nor the
-// transposing load's 4 rows x 64 bytes meet on the 64 banks.
-template <typename T, int D>
+// A tile of ROWS rows of D channels in LDS, in chunks of 8 bfloats (16 bytes); of fp32 numbers three planes of them.  Chunks are exchanged within a row by the row's low bits, so that neither
+// 16 rows of one chunk (operand along the channels) nor the transposing load's 4 rows x 64 bytes meet on the 64 banks.
+template <typename T, int D, int ROWS>
 struct Tile {
-    static constexpr int kEl = 16 / (int)sizeof(T), kChunks = D / kEl, kRow = D * (int)sizeof(T);
+    static constexpr int kChunks = D / 8, kRow = D * 2, kPlane = ROWS * kRow, kBytes = kPlane * (sizeof(T) == 4 ? 3 : 1);
     static __device__ __forceinline__ int mix(int row)
     {
-        if constexpr (sizeof(T) == 4) return D == 32 ? (row >> 1) & 7 : row & 15;
-        else return D == 32 ? (row >> 2) & 3 : D == 64 ? ((row & 2) << 1) | ((row >> 2) & 3) : ((row & 3) << 2) | ((row >> 2) & 3);
+        return D == 32 ? (row >> 2) & 3 : D == 64 ? ((row & 2) << 1) | ((row >> 2) & 3) : ((row & 3) << 2) | ((row >> 2) & 3);
     }
     static __device__ __forceinline__ int at(int row, int chunk) { return row * kRow + ((chunk ^ mix(row)) << 4); }
 
+    template <class F>
+    static __device__ __forceinline__ typename FragOf<T>::type planes(F f)
+    {
+        if constexpr (sizeof(T) == 4) return Split{f(0), f(kPlane), f(2 * kPlane)};
+        else return f(0);
+    }
     // (mix() goes by a row's low four bits: row0, a multiple of 16, only moves the address)
     // operand (index: row row0 + lane % 32; contraction: channels 16 s + 8 h + j)
     static __device__ __forceinline__ typename FragOf<T>::type along(const char* t, int row0, int s)
     {
-        const int l = threadIdx.x & 63, row = l & 31, h = l >> 5;
-        t += row0 * kRow;
-        if constexpr (sizeof(T) == 4) {
-            const f32x4 a = *(const f32x4*)(t + at(row, 4 * s + 2 * h)), b = *(const f32x4*)(t + at(row, 4 * s + 2 * h + 1));
-            return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
-        } else {
-            return *(const b16x8*)(t + at(row, 2 * s + h));
-        }
+        const int l = threadIdx.x & 63;
+        const char* p = t + row0 * kRow + at(l & 31, 2 * s + (l >> 5));
+        return planes([&](int plane) __attribute__((always_inline)) { return *(const b16x8*)(p + plane); });
     }
     // operand (index: channel d0 + lane % 32; contraction: rows row0 + 8 (j / 4) + 4 h + j % 4)
     static __device__ __forceinline__ typename FragOf<T>::type across(const char* t, int row0, int d0)
     {
-        const int l = threadIdx.x & 63, h = l >> 5;
-        t += row0 * kRow;
-        if constexpr (sizeof(T) == 4) {
-            const int d = d0 + (l & 31);
-            f32x8 r;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) r[j] = *(const float*)(t + at(8 * (j >> 2) + 4 * h + (j & 3), d >> 2) + (d & 3) * 4);
-            return r;
-        } else {
-            // each 16 lanes: 4 rows x 16 channels, lane i brings 8 bytes of row i / 4 and takes channel i of the four rows
-            const int i = l & 15, col = d0 + (l & 16) + (i & 3) * 4;
+        // each 16 lanes: 4 rows x 16 channels, lane i brings 8 bytes of row i / 4 and takes channel i of the four rows
+        const int l = threadIdx.x & 63, h = l >> 5, i = l & 15, col = d0 + (l & 16) + (i & 3) * 4;
+        return planes([&](int plane) __attribute__((always_inline)) {
             s16x4 v[2];
 #pragma unroll
             for (int j = 0; j < 2; ++j)
                 v[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                    (s16x4 __attribute__((address_space(3)))*)(t + at(8 * j + 4 * h + (i >> 2), col >> 3) + (col & 7) * 2));
+                    (s16x4 __attribute__((address_space(3)))*)(t + plane + row0 * kRow + at(8 * j + 4 * h + (i >> 2), col >> 3) + (col & 7) * 2));
             return __builtin_bit_cast(b16x8, __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7));
-        }
+        });
     }
 };
+
+// 8 fp32 numbers as an operand
+__device__ __forceinline__ Split split8(u32x4 a, u32x4 b)
+{
+    u32x4 h, m, l;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        uint32_t x, y, z;
+        const u32x4& from = j < 2 ? a : b;
+        split3(__uint_as_float(from[2 * (j & 1)]), __uint_as_float(from[2 * (j & 1) + 1]), x, y, z);
+        h[j] = x; m[j] = y; l[j] = z;
+    }
+    return Split{__builtin_bit_cast(b16x8, h), __builtin_bit_cast(b16x8, m), __builtin_bit_cast(b16x8, l)};
+}
+
+// v of the other half's lane with the same lane % 32, combined with f: both halves get the result.
+template <class F>
+__device__ __forceinline__ float across_halves(float v, F f)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return f(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float both_sum(float v) { return across_halves(v, [](float a, float b) { return a + b; }); }
+__device__ __forceinline__ float both_max(float v) { return across_halves(v, [](float a, float b) { return fmaxf(a, b); }); }
 
 // The 16 bytes of channels [d0, d0 + 16 / sizeof(T)) of a row; zero past channel d.  vec: addresses allow one load (and d is whole chunks).
 template <typename T>
@@ -121,18 +155,19 @@ __device__ __forceinline__ u32x4 chunk_of(const T* row, int d0, int d, bool vec)
     return r;
 }
 
-// Rows of a tile on their way from memory to LDS, for the workgroup's 256 threads.  VEC: straight into LDS (buffer loads whose lanes fill 16 bytes each, one
-// after the other; what is out of the resource's range arrives as zeros), landed once wait_tiles() returns.  Else, where addresses or the head size do not allow
+// Rows of a tile on their way from memory to LDS, for the workgroup's 256 threads.  Bfloats where VEC: straight into LDS (buffer loads whose lanes fill 16 bytes each, one
+// after the other; what is out of the resource's range arrives as zeros), landed once wait_tiles() returns.  fp32 numbers, and bfloats whose addresses or head size do not allow
 // 16 bytes at once: through registers, written by put().  Where a row lies in its tile is the same for all tiles and is worked out once: offset(r), bytes from
 // the tile's base (wavefront-uniform).
 template <typename T, int D, int ROWS, bool VEC>
 struct Staged {
-    typedef Tile<T, D> L;
+    typedef Tile<T, D, ROWS> L;
     typedef typename std::conditional<VEC, int, long long>::type Bytes;
-    static constexpr int kAll = ROWS * L::kChunks, kEach = (kAll + 255) / 256, kNone = -1;
+    static constexpr bool kDirect = VEC && sizeof(T) == 2;
+    static constexpr int kAll = ROWS * L::kChunks, kEach = (kAll + 255) / 256, kNone = -1, kWords = kDirect ? 1 : (int)sizeof(T) / 2;
     static_assert(kAll % 256 == 0 || kEach == 1, "whole chunks a thread");
     Bytes at[kEach];
-    u32x4 r[VEC ? 1 : kEach];
+    u32x4 r[kDirect ? 1 : kEach][kWords];
     int d;
     template <class Offset>
     __device__ __forceinline__ void init(Offset offset, int d_)
@@ -140,14 +175,14 @@ struct Staged {
         d = d_;
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
-            const int u = threadIdx.x + 256 * i, row = u / L::kChunks, chunk = (u % L::kChunks) ^ (VEC ? L::mix(row) : 0);       // (the chunk that lies here)
-            at[i] = (kAll < 256 && u >= kAll) || chunk * L::kEl >= d ? (Bytes)kNone : offset(row) + chunk * 16;
+            const int u = threadIdx.x + 256 * i, row = u / L::kChunks, chunk = (u % L::kChunks) ^ (kDirect ? L::mix(row) : 0);       // (the chunk that lies here)
+            at[i] = (kAll < 256 && u >= kAll) || chunk * 8 >= d ? (Bytes)kNone : offset(row) + chunk * 8 * (int)sizeof(T);
         }
     }
     // `rows`: how many rows there are, the others are zeros
     __device__ __forceinline__ void fetch(char* tile, const T* base, int rows)
     {
-        if constexpr (VEC) {
+        if constexpr (kDirect) {
             const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)base, (short)0, (int)0x80000000u, 0x00020000);
             if (rows >= ROWS) {
 #pragma unroll
@@ -159,20 +194,31 @@ struct Staged {
         } else {
 #pragma unroll
             for (int i = 0; i < kEach; ++i) {
-                const int u = threadIdx.x + 256 * i, chunk = u % L::kChunks;
-                r[i] = u32x4{0, 0, 0, 0};
-                if (u / L::kChunks < rows && at[i] >= 0) r[i] = chunk_of((const T*)((const char*)base + (at[i] - chunk * 16)), chunk * L::kEl, d, false);
+                const int u = threadIdx.x + 256 * i, d0 = (u % L::kChunks) * 8;
+                const bool there = u / L::kChunks < rows && at[i] >= 0;
+                const T* row = (const T*)((const char*)base + (there ? at[i] : 0)) - (there ? d0 : 0);
+#pragma unroll
+                for (int k = 0; k < kWords; ++k) {
+                    r[i][k] = u32x4{0, 0, 0, 0};
+                    if (there) r[i][k] = chunk_of(row, d0 + k * (16 / (int)sizeof(T)), d, VEC);
+                }
             }
         }
     }
     __device__ __forceinline__ void put(char* tile) const
     {
-        if constexpr (!VEC) {
+        if constexpr (!kDirect) {
 #pragma unroll
             for (int i = 0; i < kEach; ++i) {
                 const int u = threadIdx.x + 256 * i;
                 if (kAll < 256 && u >= kAll) continue;
-                *(u32x4*)(tile + L::at(u / L::kChunks, u % L::kChunks)) = r[i];
+                char* p = tile + L::at(u / L::kChunks, u % L::kChunks);
+                if constexpr (sizeof(T) == 4) {
+                    const Split x = split8(r[i][0], r[i][1]);
+                    *(b16x8*)p = x.h;
+                    *(b16x8*)(p + L::kPlane) = x.m;
+                    *(b16x8*)(p + 2 * L::kPlane) = x.l;
+                } else *(u32x4*)p = r[i][0];
             }
         }
     }
@@ -220,51 +266,60 @@ __device__ __forceinline__ void overlap(LoadA load_a, MmaA mma_a, Valu valu, Loa
 // Scores of hidden pairs start from this instead of 0: their exponential is 0, whatever is added.
 constexpr float kHidden = -3e38f;
 
-// Operand words of two neighbouring registers of a result as they become known (see operand()).
-template <typename T>
-struct Words {
-    typename FragOf<T>::type f[2];
-    __device__ __forceinline__ void set(int pair, float a, float b)
-    {
-        if constexpr (sizeof(T) == 4) { f[pair >> 2][2 * (pair & 3)] = a; f[pair >> 2][2 * (pair & 3) + 1] = b; }
-        else {
-            u32x4 w = __builtin_bit_cast(u32x4, f[pair >> 2]);
-            w[pair & 3] = pack_bf16(a, b);
-            f[pair >> 2] = __builtin_bit_cast(b16x8, w);
-        }
-    }
-};
-
 // Workgroups a CU that the register budget is set for: two (all sums and operands in 256 registers) where they fit.
 template <typename T, int D> constexpr int kPerCu = sizeof(T) == 4 && D == 128 ? 1 : 2;
 
-// Operands (index: this lane's row; contraction: channels 16 s + 8 h + j) straight from memory; row null: zeros.
+// Channels 16 s + 8 h .. + 7 of this lane's row, s < D / 16, as they lie in memory; row null: zeros.
+template <typename T, int D>
+struct RowWords {
+    u32x4 w[D / 16][sizeof(T) / 2];
+    __device__ __forceinline__ void load(const T* row, int d, bool vec)
+    {
+        const int h = (threadIdx.x >> 5) & 1;
+#pragma unroll
+        for (int s = 0; s < D / 16; ++s)
+#pragma unroll
+            for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
+                w[s][i] = u32x4{0, 0, 0, 0};
+                if (row) w[s][i] = chunk_of(row, 16 * s + 8 * h + 4 * i, d, vec);
+            }
+    }
+    __device__ __forceinline__ float dot(const RowWords& o) const          // of the two lanes of a row
+    {
+        float v = 0;
+#pragma unroll
+        for (int s = 0; s < D / 16; ++s)
+#pragma unroll
+            for (int i = 0; i < (int)sizeof(T) / 2; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const uint32_t x = w[s][i][j], y = o.w[s][i][j];
+                    if constexpr (sizeof(T) == 4) v = fmaf(__uint_as_float(x), __uint_as_float(y), v);
+                    else {
+                        v = fmaf(__uint_as_float(x << 16), __uint_as_float(y << 16), v);
+                        v = fmaf(__uint_as_float(x & 0xFFFF0000u), __uint_as_float(y & 0xFFFF0000u), v);
+                    }
+                }
+        return both_sum(v);
+    }
+    // operands (index: this lane's row; contraction: channels 16 s + 8 h + j)
+    __device__ __forceinline__ void operands(typename FragOf<T>::type (&f)[D / 16], bool negate) const
+    {
+        const uint32_t sign = !negate ? 0u : sizeof(T) == 4 ? 0x80000000u : 0x80008000u;
+#pragma unroll
+        for (int s = 0; s < D / 16; ++s) {
+            if constexpr (sizeof(T) == 4) f[s] = split8(w[s][0] ^ sign, w[s][1] ^ sign);
+            else f[s] = __builtin_bit_cast(b16x8, w[s][0] ^ sign);
+        }
+    }
+};
 template <typename T, int D>
 __device__ __forceinline__ void row_operands(typename FragOf<T>::type (&f)[D / 16], const T* row, int d, bool vec, bool negate)
 {
-    const int h = (threadIdx.x >> 5) & 1;
-#pragma unroll
-    for (int s = 0; s < D / 16; ++s) {
-        u32x4 w[sizeof(T) / 2];
-#pragma unroll
-        for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
-            w[i] = u32x4{0, 0, 0, 0};
-            if (row) w[i] = chunk_of(row, 16 * s + 8 * h + 4 * i, d, vec);
-            if (negate) w[i] ^= sizeof(T) == 4 ? 0x80000000u : 0x80008000u;
-        }
-        __builtin_memcpy(&f[s], w, sizeof(f[s]));
-    }
+    RowWords<T, D> w;
+    w.load(row, d, vec);
+    w.operands(f, negate);
 }
-
-// v of the other half's lane with the same lane % 32, combined with f: both halves get the result.
-template <class F>
-__device__ __forceinline__ float across_halves(float v, F f)
-{
-    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    return f(__uint_as_float(r[0]), __uint_as_float(r[1]));
-}
-__device__ __forceinline__ float both_sum(float v) { return across_halves(v, [](float a, float b) { return a + b; }); }
-__device__ __forceinline__ float both_max(float v) { return across_halves(v, [](float a, float b) { return fmaxf(a, b); }); }
 
 // Four neighbouring channels d0 .. d0 + 3 of a row, those below d.
 template <typename T>

@@ -17,9 +17,10 @@ template <typename T, int D> constexpr int kKeys = sizeof(T) == 4 ? 32 : 64;    
 template <typename T, int D, bool VEC>
 __global__ __launch_bounds__(256, (kPerCu<T, D>)) void k_attention(const AttentionArgs a)
 {
-    typedef Tile<T, D> L;
     typedef typename FragOf<T>::type Frag;
-    constexpr int BN = kKeys<T, D>, UNITS = BN / 32, KS = D / 16, DT = D / 32, kTile = BN * L::kRow;
+    constexpr int BN = kKeys<T, D>, UNITS = BN / 32, KS = D / 16, DT = D / 32;
+    typedef Tile<T, D, BN> L;
+    constexpr int kTile = L::kBytes;
     struct Keys { char tile[2][kTile]; };           // a tile of keys and values
     __shared__ __align__(16) Keys even, odd;        // (apart, so that reads of one need not wait for loads of the other)
     int block, split, b, kvh;
@@ -156,17 +157,17 @@ __global__ __launch_bounds__(256, (kPerCu<T, D>)) void k_attention(const Attenti
     if (h == 0 && a.lse) a.lse[((long long)b * a.heads + head) * a.q_len + i] = seen ? fmaf(m, kLn2, logf(sum)) : -INFINITY;
 }
 
-// Joins the splits of a row: D / 4 lanes a row, four channels each; the lanes work out the splits' weights side by side.
+// Joins the splits of a row: a workgroup a row, D / 4 lanes with four channels each x groups of splits, so that all loads are on their way at once.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void k_attention_join(const AttentionArgs a)
 {
-    constexpr int LANES = D / 4;
-    const int rows = a.q_len * a.group;
-    const long long per = (long long)a.batch * a.kv * rows, at = (long long)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
-    if (at >= per) return;
-    const int lane = threadIdx.x % LANES, d0 = lane * 4;
-    const int row = (int)(at % rows), i = query_of(a, row);
-    const int kvh = (int)(at / rows % a.kv), b = (int)(at / rows / a.kv), head = kvh * a.group + row - i * a.group;
+    constexpr int LANES = D / 4, GROUPS = 256 / LANES;
+    __shared__ f32x4 part[GROUPS][LANES];
+    __shared__ float part_sum[GROUPS];
+    const int rows = a.q_len * a.group, at = blockIdx.x;               // (few rows: there are splits)
+    const long long per = (long long)a.batch * a.kv * rows;
+    const int lane = threadIdx.x % LANES, grp = threadIdx.x / LANES, d0 = lane * 4;
+    const int bk = at / rows, row = at - bk * rows, b = bk / a.kv, kvh = bk - b * a.kv, i = query_of(a, row), head = kvh * a.group + row - i * a.group;
     const float* ms = a.ws + per * a.splits * D;
     float m = -INFINITY;
     for (int s = lane; s < a.splits; s += LANES) m = fmaxf(m, ms[2 * (s * per + at)]);
@@ -174,19 +175,19 @@ __global__ __launch_bounds__(256) void k_attention_join(const AttentionArgs a)
     for (int n = LANES / 2; n; n >>= 1) m = fmaxf(m, __shfl_xor(m, n));
     f32x4 o = {0, 0, 0, 0};
     float sum = 0;
-    for (int s0 = 0; s0 < a.splits; s0 += LANES) {
-        float f = 0;
-        if (s0 + lane < a.splits) {
-            const long long p = 2 * ((s0 + lane) * per + at);
-            f = __builtin_amdgcn_exp2f(ms[p] - m);
-            sum = fmaf(ms[p + 1], f, sum);
-        }
-        const int n = min(LANES, a.splits - s0);
-#pragma unroll 8
-        for (int s = 0; s < n; ++s) o += *(const f32x4*)(a.ws + ((s0 + s) * per + at) * D + d0) * __shfl(f, s, LANES);
+#pragma unroll 4
+    for (int s = grp; s < a.splits; s += GROUPS) {
+        const long long p = s * per + at;
+        const float f = __builtin_amdgcn_exp2f(ms[2 * p] - m);
+        o += *(const f32x4*)(a.ws + p * D + d0) * f;
+        sum = fmaf(ms[2 * p + 1], f, sum);
     }
+    part[grp][lane] = o;
+    if (lane == 0) part_sum[grp] = sum;
+    __syncthreads();
+    if (grp) return;
 #pragma unroll
-    for (int n = LANES / 2; n; n >>= 1) sum += __shfl_xor(sum, n);
+    for (int n = 1; n < GROUPS; ++n) { o += part[n][lane]; sum += part_sum[n]; }
     const bool any = Lengths(a, b).seen(a, i) > 0;
     o = any ? o * (1.0f / sum) : f32x4{0, 0, 0, 0};
     store4((T*)a.out + b * a.os[0] + i * a.os[1] + head * a.os[2], d0, a.d, a.vec, o[0], o[1], o[2], o[3]);
@@ -209,7 +210,7 @@ void run(const AttentionArgs& a, unsigned grid, hipStream_t st)
     else k_attention<T, D, false><<<grid, 256, 0, st>>>(a);
     if (a.splits > 1) {
         const long long rows = (long long)a.batch * a.kv * a.q_len * a.group;
-        k_attention_join<T, D><<<(unsigned)ceil_div(rows, 1024 / D), 256, 0, st>>>(a);
+        k_attention_join<T, D><<<(unsigned)rows, 256, 0, st>>>(a);
     }
 }
 

@@ -18,9 +18,10 @@ template <typename T, int D> constexpr int kKeys = sizeof(T) == 4 ? 32 : 64;    
 template <typename T, int D, bool VEC>
 __global__ __launch_bounds__(256, (D == 128 ? 1 : kPerCu<T, D>)) void k_attention_dq(const AttentionArgs a)
 {
-    typedef Tile<T, D> L;
     typedef typename FragOf<T>::type Frag;
-    constexpr int BN = kKeys<T, D>, UNITS = BN / 32, KS = D / 16, DT = D / 32, kTile = BN * L::kRow;
+    constexpr int BN = kKeys<T, D>, UNITS = BN / 32, KS = D / 16, DT = D / 32;
+    typedef Tile<T, D, BN> L;
+    constexpr int kTile = L::kBytes;
     struct Keys { char tile[2][kTile]; };           // a tile of keys and values
     __shared__ __align__(16) Keys even, odd;        // (apart, so that reads of one need not wait for loads of the other)
     int block, split, b, kvh;
@@ -38,18 +39,13 @@ __global__ __launch_bounds__(256, (D == 128 ? 1 : kPerCu<T, D>)) void k_attentio
     const int tiles = (end + BN - 1) / BN, lo = (int)((long long)tiles * split / a.splits), hi = (int)((long long)tiles * (split + 1) / a.splits);
     // this row's operands; delta from the same dout and the row of out
     Frag q[D / 16], g[D / 16];
-    float delta = 0;
+    float delta;
     {
-        row_operands<T, D>(g, seen ? (const T*)a.out + b * a.os[0] + i * a.os[1] + head * a.os[2] : nullptr, a.d, VEC, false);
-        Frag o[D / 16];
-#pragma unroll
-        for (int s = 0; s < D / 16; ++s) o[s] = g[s];
-        row_operands<T, D>(g, seen ? (const T*)a.dout + b * a.gs[0] + i * a.gs[1] + head * a.gs[2] : nullptr, a.d, VEC, false);
-#pragma unroll
-        for (int s = 0; s < D / 16; ++s)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) delta = fmaf((float)o[s][j], (float)g[s][j], delta);
-        delta = both_sum(delta);
+        RowWords<T, D> o, w;
+        o.load(seen ? (const T*)a.out + b * a.os[0] + i * a.os[1] + head * a.os[2] : nullptr, a.d, VEC);
+        w.load(seen ? (const T*)a.dout + b * a.gs[0] + i * a.gs[1] + head * a.gs[2] : nullptr, a.d, VEC);
+        delta = w.dot(o);
+        w.operands(g, false);
     }
     const long long at = (((long long)b * a.kv + kvh) * a.q_len) * a.group + row;
     if (split == 0 && inside && h == 0) a.delta[at] = delta;
@@ -161,11 +157,12 @@ __host__ __device__ inline int rows_of_tile(int group, int most)
 }
 
 template <typename T, int D, bool VEC>
-__global__ __launch_bounds__(256, (D == 128 || sizeof(T) * D == 256 ? 1 : 2)) void k_attention_dkv(const AttentionArgs a)
+__global__ __launch_bounds__(256, (D == 128 || sizeof(T) == 4 ? 1 : 2)) void k_attention_dkv(const AttentionArgs a)
 {
-    typedef Tile<T, D> L;
     typedef typename FragOf<T>::type Frag;
-    constexpr int BM = kRows<T, D>, UNITS = BM / 32, KS = D / 16, DT = D / 32, kTile = BM * L::kRow;
+    constexpr int BM = kRows<T, D>, UNITS = BM / 32, KS = D / 16, DT = D / 32;
+    typedef Tile<T, D, BM> L;
+    constexpr int kTile = L::kBytes;
     // a tile of rows: queries, dout; and of its rows the log-sum in powers of 2, -delta, the number of keys seen
     struct Rows { char tile[2][kTile]; float lse[BM], less[BM]; int seen[BM]; };
     __shared__ __align__(16) Rows r0, r1, r2;       // three in turn (apart, so that reads of one need not wait for loads of another)
