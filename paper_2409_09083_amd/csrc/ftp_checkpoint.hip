@@ -71,36 +71,39 @@ __device__ __forceinline__ Place place(const HeldArgs& a, uint32_t u)
     return p;
 }
 
-// VECTOR: rows, strides and addresses let 8 neighbours go at once.
+// 8 neighbours, n of which are there.  VECTOR: sizes and addresses are whole vectors of 16 (codes 8) bytes, all 8 are there or none.  Otherwise 8 go at once where they are there,
+// at any address, and the last ones of a row one by one (4000 rows of 5001: 38 us there and back; element by element everywhere 101; 189 million in aligned rows: unpacking 167 us
+// with VECTOR, 232 without).
 template <typename T, bool VECTOR>
 __device__ __forceinline__ void load8(float (&v)[8], const T* p, int n)
 {
-    if constexpr (VECTOR) {
-        if (n > 0) {
-            Pack<T, 8> w;
-            w.load(p);
+    Pack<T, 8> w;
+    w.zero();
+    if constexpr (VECTOR) { if (n > 0) w.load(p); }
+    else if (n == 8) w.load_any(p);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = w.get(i);
-            return;
-        }
-    }
+    for (int i = 0; i < 8; ++i) v[i] = w.get(i);
+    if (VECTOR || n == 8) return;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        Pack<T, 1> w;
-        w.zero();
-        if (!VECTOR && i < n) w.load(p + i);
-        v[i] = w.get(0);
+        Pack<T, 1> e;
+        e.zero();
+        if (i < n) e.load(p + i);
+        v[i] = e.get(0);
     }
 }
 template <typename T, bool VECTOR>
 __device__ __forceinline__ void store8(const float (&v)[8], T* p, int n)
 {
-    if constexpr (VECTOR) {
-        if (n > 0) { Pack<T, 8> w; w.put(v); w.store(p); }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) if (i < n) st(p + i, v[i]);
+    if (VECTOR || n == 8) {
+        Pack<T, 8> w;
+        w.put(v);
+        if constexpr (VECTOR) w.store(p);
+        else w.store_any(p);
+        return;
     }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) if (i < n) st(p + i, v[i]);
 }
 
 template <typename T, bool VECTOR>
@@ -127,10 +130,11 @@ __global__ __launch_bounds__(256) void k_held_pack(const HeldArgs a)
     }
     if (n <= 0) return;
     int8_t* c = a.codes + p.row * a.cols + p.col;
-    if constexpr (VECTOR) {
+    if (VECTOR || n == 8) {
         Pack<int8_t, 8> o;
         o.w[0] = {w[0], w[1]};
-        o.store(c);
+        if constexpr (VECTOR) o.store(c);
+        else o.store_any(c);
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) if (i < n) c[i] = (int8_t)(w[i / 4] >> (8 * (i & 3)));
@@ -148,8 +152,9 @@ __global__ __launch_bounds__(256) void k_held_act(const HeldArgs a)
     const Place p = place(a, u);
     if (p.n <= 0) return;
     float v[8], y[8];
-    load8<int8_t, VECTOR>(v, a.codes + p.row * a.cols + p.col, p.n);
-    const float unit = held_scale(a.exps[p.row * a.nblocks + (p.col >> (a.lg + 3))]);
+    const int e = a.exps[p.row * a.nblocks + (p.col >> (a.lg + 3))];
+    load8<int8_t, VECTOR>(v, (const int8_t*)a.codes + p.row * a.cols + p.col, p.n);
+    const float unit = held_scale(e);
     const long long at = p.row * a.stride + p.col;
     if constexpr (BACK) load8<T, VECTOR>(y, (const T*)a.dy + at, p.n);
 #pragma unroll
@@ -193,8 +198,9 @@ void by_launches(HeldArgs a, int es, F launch)
 }
 
 template <typename T, bool BACK, int ACT>
-void run_act(const HeldArgs& a, bool vec, hipStream_t st)
+void run_act(const HeldArgs& a, hipStream_t st)
 {
+    const bool vec = by_vectors(a, BACK ? a.dy : a.out, a.out);
     by_launches(a, sizeof(T), [&](const HeldArgs& b, unsigned grid) {
         if (vec) k_held_act<T, true, ACT, BACK><<<grid, 256, 0, st>>>(b);
         else k_held_act<T, false, ACT, BACK><<<grid, 256, 0, st>>>(b);
@@ -202,13 +208,13 @@ void run_act(const HeldArgs& a, bool vec, hipStream_t st)
 }
 
 template <typename T, bool BACK>
-void run_acts(const HeldArgs& a, int act, bool vec, hipStream_t st)
+void run_acts(const HeldArgs& a, int act, hipStream_t st)
 {
     switch (act) {
-        case FTP_ACT_LEAKY: run_act<T, BACK, FTP_ACT_LEAKY>(a, vec, st); break;
-        case FTP_ACT_GELU: run_act<T, BACK, FTP_ACT_GELU>(a, vec, st); break;
-        case FTP_ACT_SILU: run_act<T, BACK, FTP_ACT_SILU>(a, vec, st); break;
-        default: run_act<T, BACK, FTP_ACT_NONE>(a, vec, st); break;
+        case FTP_ACT_LEAKY: run_act<T, BACK, FTP_ACT_LEAKY>(a, st); break;
+        case FTP_ACT_GELU: run_act<T, BACK, FTP_ACT_GELU>(a, st); break;
+        case FTP_ACT_SILU: run_act<T, BACK, FTP_ACT_SILU>(a, st); break;
+        default: run_act<T, BACK, FTP_ACT_NONE>(a, st); break;
     }
 }
 
@@ -231,18 +237,16 @@ void held_unpack(const ftp_checkpoint_shape& s, const int8_t* codes, const int8_
 {
     HeldArgs a = held_args(s, codes, exponents);
     a.out = out; a.slope = slope;
-    const bool vec = by_vectors(a, out, out);
-    if (s.dtype == FTP_BF16) run_acts<bf16_t, false>(a, act, vec, st);
-    else run_acts<float, false>(a, act, vec, st);
+    if (s.dtype == FTP_BF16) run_acts<bf16_t, false>(a, act, st);
+    else run_acts<float, false>(a, act, st);
 }
 
 void held_act_backward(const ftp_checkpoint_shape& s, const int8_t* codes, const int8_t* exponents, int act, float slope, const void* dy, void* dx, hipStream_t st)
 {
     HeldArgs a = held_args(s, codes, exponents);
     a.dy = dy; a.out = dx; a.slope = slope;
-    const bool vec = by_vectors(a, dy, dx);
-    if (s.dtype == FTP_BF16) run_acts<bf16_t, true>(a, act, vec, st);
-    else run_acts<float, true>(a, act, vec, st);
+    if (s.dtype == FTP_BF16) run_acts<bf16_t, true>(a, act, st);
+    else run_acts<float, true>(a, act, st);
 }
 
 }  // namespace ftp

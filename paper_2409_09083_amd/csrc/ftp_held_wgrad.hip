@@ -19,7 +19,7 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 struct HeldWgradArgs {
     const void* dy; const int8_t* codes; const int8_t* exps; float* dw; float* partial;
     long long rows, dy_stride;
-    int N, K, nblocks, lgblock, shares, ntiles, ktiles;
+    int N, K, nblocks, lgblock, shares, ntiles, ktiles, wide;
 };
 
 template <typename T> constexpr int kStage = sizeof(T) == 4 ? 32 : 64;       // rows of a stage
@@ -43,8 +43,7 @@ __device__ __forceinline__ b16x8 read_t(const char* tile, int row0, int col0)
     return __builtin_bit_cast(b16x8, __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
-// VEC: addresses and sizes let 8 of dy and 16 codes go at once.
-template <typename T, bool VEC>
+template <typename T>
 __global__ __launch_bounds__(256, 2) void k_held_wgrad(const HeldWgradArgs a)
 {
     constexpr int P = sizeof(T) == 4 ? 3 : 1;       // bfloats of a dy
@@ -62,34 +61,39 @@ __global__ __launch_bounds__(256, 2) void k_held_wgrad(const HeldWgradArgs a)
     // read from inside it and not stored; rows past its end are read from its last row and cleared.
     const int drow = tid >> 4, dcol = (tid & 15) * 8, crow = tid >> 3, ccol = (tid & 7) * 16;
     const int dn = n0 + dcol < a.N ? n0 + dcol : 0, cn = k0 + ccol < a.K ? k0 + ccol : 0;
-    struct Part { Pack<T, VEC ? 8 : 1> d[DR][VEC ? 1 : 8]; uint32_t c[CR][4]; int e[CR]; };
+    struct Part { Pack<T, 8> d[DR]; uint4 c[CR]; int e[CR]; };
+    const long long last = a.rows - 1;
+    const auto fetch_exps = [&](Part& x, long long stage) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < CR; ++i) x.e[i] = a.exps[min(stage * S + crow + 32 * i, last) * a.nblocks + (cn >> a.lgblock)];
+    };
+    // 8 of dy and 16 codes at once, at any address; past a row's end they come from the next row
     const auto fetch = [&](Part& x, long long stage) __attribute__((always_inline)) {
-        const long long last = a.rows - 1;
+#pragma unroll
+        for (int i = 0; i < DR; ++i) x.d[i].load_any((const T*)a.dy + (stage * S + drow + 16 * i) * a.dy_stride + dn);
+#pragma unroll
+        for (int i = 0; i < CR; ++i) __builtin_memcpy(&x.c[i], a.codes + (stage * S + crow + 32 * i) * a.K + cn, 16);
+        fetch_exps(x, stage);
+    };
+    // ... one by one, for the last stage, whose last row has no next one, and for rows that are too short
+    const auto fetch_each = [&](Part& x, long long stage) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < DR; ++i) {
             const T* p = (const T*)a.dy + min(stage * S + drow + 16 * i, last) * a.dy_stride;
-            if constexpr (VEC) x.d[i][0].load(p + dn);
-            else {
+            T v[8];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) x.d[i][j].load(p + min(dn + j, a.N - 1));
-            }
+            for (int j = 0; j < 8; ++j) v[j] = p[min(dn + j, a.N - 1)];
+            __builtin_memcpy(x.d[i].w, v, sizeof(v));
         }
 #pragma unroll
         for (int i = 0; i < CR; ++i) {
-            const long long r = min(stage * S + crow + 32 * i, last);
-            const int8_t* p = a.codes + r * a.K;
-            if constexpr (VEC) {
-                const uint4 w = *(const uint4*)(p + cn);
-                x.c[i][0] = w.x; x.c[i][1] = w.y; x.c[i][2] = w.z; x.c[i][3] = w.w;
-            } else {
+            const int8_t* p = a.codes + min(stage * S + crow + 32 * i, last) * a.K;
+            int8_t v[16];
 #pragma unroll
-                for (int j = 0; j < 16; ++j) {
-                    const uint32_t v = (uint8_t)p[min(cn + j, a.K - 1)];
-                    x.c[i][j / 4] = (j & 3 ? x.c[i][j / 4] : 0) | v << (8 * (j & 3));
-                }
-            }
-            x.e[i] = a.exps[r * a.nblocks + (cn >> a.lgblock)];
+            for (int j = 0; j < 16; ++j) v[j] = p[min(cn + j, a.K - 1)];
+            __builtin_memcpy(&x.c[i], v, 16);
         }
+        fetch_exps(x, stage);
     };
     const auto put = [&](const Part& x, char* t, long long stage) __attribute__((always_inline)) {
         const int left = (int)min((long long)S, a.rows - stage * S);
@@ -97,7 +101,7 @@ __global__ __launch_bounds__(256, 2) void k_held_wgrad(const HeldWgradArgs a)
         for (int i = 0; i < DR; ++i) {
             float d[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) d[j] = drow + 16 * i < left ? (VEC ? x.d[i][0].get(j) : x.d[i][VEC ? 0 : j].get(0)) : 0.0f;
+            for (int j = 0; j < 8; ++j) d[j] = drow + 16 * i < left ? x.d[i].get(j) : 0.0f;
             uint4 w[P];
             uint32_t* q = (uint32_t*)w;
 #pragma unroll
@@ -116,7 +120,7 @@ __global__ __launch_bounds__(256, 2) void k_held_wgrad(const HeldWgradArgs a)
             uint32_t* q = (uint32_t*)w;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const int word = (int)x.c[i][j >> 1], sh = (j & 1) * 16;
+                const int word = (int)(j < 2 ? x.c[i].x : j < 4 ? x.c[i].y : j < 6 ? x.c[i].z : x.c[i].w), sh = (j & 1) * 16;
                 q[j] = pack_bf16((float)(int8_t)(word >> sh) * unit, (float)(int8_t)(word >> (sh + 8)) * unit);
             }
             *(uint4*)(t + P * kTile + tile_at(crow + 32 * i, ccol >> 3)) = w[0];
@@ -125,8 +129,7 @@ __global__ __launch_bounds__(256, 2) void k_held_wgrad(const HeldWgradArgs a)
     };
 
     f32x16 acc[2][2] = {};
-    // stage s is in LDS, `next` holds stage s + 1 and takes stage s + 3 once that is in LDS; stage s + 2 is on its way beside it
-    const auto step = [&](long long s, const char* now, char* then, Part& next) __attribute__((always_inline)) {
+    const auto products = [&](const char* now) __attribute__((always_inline)) {
 #pragma unroll
         for (int r0 = 0; r0 < S; r0 += 16) {
             b16x8 b[2];
@@ -141,21 +144,34 @@ __global__ __launch_bounds__(256, 2) void k_held_wgrad(const HeldWgradArgs a)
                     for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, b[j], acc[i][j], 0, 0, 0);
                 }
         }
-        if (s + 1 < hi) put(next, then, s + 1);
-        if (s + 3 < hi) fetch(next, s + 3);
+    };
+    const long long full = a.wide ? min(hi, stages - 1) : lo;          // stages below this one go the fast way
+    // stage s is in LDS, `next` holds stage s + 1 and takes stage s + 3 once that is in LDS; stage s + 2 is on its way beside it
+    const auto step = [&](long long s, const char* now, char* then, Part& next) __attribute__((always_inline)) {
+        products(now);
+        if (s + 1 < full) put(next, then, s + 1);
+        if (s + 3 < full) fetch(next, s + 3);
         __syncthreads();
     };
-    if (lo < hi) {
+    if (lo < full) {
         Part x, y;
         fetch(x, lo);
-        if (lo + 1 < hi) fetch(y, lo + 1);
+        if (lo + 1 < full) fetch(y, lo + 1);
         put(x, lds[0], lo);
-        if (lo + 2 < hi) fetch(x, lo + 2);
+        if (lo + 2 < full) fetch(x, lo + 2);
         __syncthreads();
-        for (long long s = lo; s < hi; s += 2) {
+        for (long long s = lo; s < full; s += 2) {
             step(s, lds[0], lds[1], y);
-            if (s + 1 < hi) step(s + 1, lds[1], lds[0], x);
+            if (s + 1 < full) step(s + 1, lds[1], lds[0], x);
         }
+    }
+    for (long long s = max(lo, full); s < hi; ++s) {
+        Part x;
+        fetch_each(x, s);
+        put(x, lds[0], s);
+        __syncthreads();
+        products(lds[0]);
+        __syncthreads();
     }
     // lane: column k = lane % 32 of a 32 x 32 block, rows n = 8 (r / 4) + 4 (lane / 32) + r % 4
     const int l = tid & 63;
@@ -216,12 +232,10 @@ void held_wgrad(const ftp_checkpoint_shape& s, const int8_t* codes, const int8_t
     a.shares = wgrad_shares(s.rows, a.N, a.K, stage_of(s));
     a.ntiles = (int)ceil_div(a.N, kBlk); a.ktiles = (int)ceil_div(a.K, kBlk);
     const bool bf = s.dtype == FTP_BF16;
-    const bool vec = aligned(dy, 16) && dy_stride % (bf ? 8 : 4) == 0 && a.N % 8 == 0 && aligned(codes, 16) && a.K % 16 == 0;
+    a.wide = dy_stride >= 8 && a.K >= 16;
     const unsigned grid = (unsigned)(a.ntiles * a.ktiles * a.shares);
-    if (bf && vec) k_held_wgrad<bf16_t, true><<<grid, 256, 0, st>>>(a);
-    else if (bf) k_held_wgrad<bf16_t, false><<<grid, 256, 0, st>>>(a);
-    else if (vec) k_held_wgrad<float, true><<<grid, 256, 0, st>>>(a);
-    else k_held_wgrad<float, false><<<grid, 256, 0, st>>>(a);
+    if (bf) k_held_wgrad<bf16_t><<<grid, 256, 0, st>>>(a);
+    else k_held_wgrad<float><<<grid, 256, 0, st>>>(a);
     if (a.shares > 1) k_held_wgrad_sum<<<(unsigned)ceil_div((long long)a.N * a.K, 64), 256, 0, st>>>(partial, dw, (long long)a.N * a.K, a.shares);
 }
 

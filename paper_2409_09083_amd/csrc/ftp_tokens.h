@@ -57,6 +57,9 @@ struct Pack {
 #pragma unroll
         for (int i = 0; i < kWords; ++i) ((Raw*)p)[i] = w[i];
     }
+    // ... from and to any address: the hardware takes unaligned vectors from global memory
+    __device__ __forceinline__ void load_any(const T* p) { __builtin_memcpy(w, p, sizeof(w)); }
+    __device__ __forceinline__ void store_any(T* p) const { __builtin_memcpy(p, w, sizeof(w)); }
     __device__ __forceinline__ void zero()
     {
 #pragma unroll
