@@ -6,8 +6,10 @@
 // lie (dy after its split, codes after their conversion) and read through the transposing LDS load: 4 rows x 16 columns a 16 lanes.  A stage is 64 rows (32 of fp32), two stages in LDS
 // and two more on their way in registers: with one, a workgroup waited for HBM most of the time.  The shares' blocks are added up by a second kernel in a fixed order.
 #include "ftp_tokens.h"
+#include "ftp_order.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace ftp {
 namespace {
@@ -50,7 +52,12 @@ __global__ __launch_bounds__(256, 2) void k_held_wgrad(const HeldWgradArgs a)
     constexpr int S = kStage<T>, kTile = S * 256, DR = S / 16, CR = S / 32;
     __shared__ __align__(16) char lds[2][(P + 1) * kTile];
     const int tid = threadIdx.x, wave = tid >> 6;
-    const int tile = blockIdx.x % (a.ntiles * a.ktiles), share = blockIdx.x / (a.ntiles * a.ktiles);
+    // all blocks of a share on one XCD where there are shares for all eight: its L2 serves the rows that they have in common
+    int tile, share;
+    if (a.shares < 8) {
+        share = blockIdx.x / (a.ntiles * a.ktiles);
+        tile = blockIdx.x - share * a.ntiles * a.ktiles;
+    } else if (!xcd_order((int)blockIdx.x, a.shares, a.ntiles * a.ktiles, share, tile)) return;
     const int n0 = (tile % a.ntiles) * kBlk, k0 = (tile / a.ntiles) * kBlk;
     // a share is whole stages
     const long long stages = (a.rows + S - 1) / S;
@@ -95,33 +102,35 @@ __global__ __launch_bounds__(256, 2) void k_held_wgrad(const HeldWgradArgs a)
         }
         fetch_exps(x, stage);
     };
-    const auto put = [&](const Part& x, char* t, long long stage) __attribute__((always_inline)) {
-        const int left = (int)min((long long)S, a.rows - stage * S);
+    // left: rows of the stage that are there
+    const auto put = [&](const Part& x, char* t, auto all, int left) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < DR; ++i) {
-            float d[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) d[j] = drow + 16 * i < left ? x.d[i].get(j) : 0.0f;
+            const bool there = all || drow + 16 * i < left;
             uint4 w[P];
             uint32_t* q = (uint32_t*)w;
+            if constexpr (P == 1) {
+                __builtin_memcpy(w, x.d[i].w, 16);
+                if (!there) w[0] = uint4{0, 0, 0, 0};
+            } else {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if constexpr (P == 1) q[j] = pack_bf16(d[2 * j], d[2 * j + 1]);
-                else split3(d[2 * j] * kSplitScale, d[2 * j + 1] * kSplitScale, q[j], q[4 + j], q[8 + j]);
+                for (int j = 0; j < 4; ++j)
+                    split3(there ? x.d[i].get(2 * j) * kSplitScale : 0.0f, there ? x.d[i].get(2 * j + 1) * kSplitScale : 0.0f, q[j], q[4 + j], q[8 + j]);
             }
 #pragma unroll
             for (int s = 0; s < P; ++s) *(uint4*)(t + s * kTile + tile_at(drow + 16 * i, dcol >> 3)) = w[s];
         }
 #pragma unroll
         for (int i = 0; i < CR; ++i) {
-            const bool there = crow + 32 * i < left;
-            const float unit = there ? held_scale(x.e[i]) : 0.0f;
+            // q * 2^e = (q + 128) * 2^e - 128 * 2^e, exact; q + 128 as an unsigned byte takes one conversion from where it lies
+            const float unit = all || crow + 32 * i < left ? held_scale(x.e[i]) : 0.0f, less = -128.0f * unit;
             uint4 w[2];
             uint32_t* q = (uint32_t*)w;
+            const uint32_t c[4] = {x.c[i].x ^ 0x80808080u, x.c[i].y ^ 0x80808080u, x.c[i].z ^ 0x80808080u, x.c[i].w ^ 0x80808080u};
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const int word = (int)(j < 2 ? x.c[i].x : j < 4 ? x.c[i].y : j < 6 ? x.c[i].z : x.c[i].w), sh = (j & 1) * 16;
-                q[j] = pack_bf16((float)(int8_t)(word >> sh) * unit, (float)(int8_t)(word >> (sh + 8)) * unit);
+                const uint32_t v = c[j >> 1] >> (16 * (j & 1));
+                q[j] = pack_bf16(fmaf((float)(v & 0xFFu), unit, less), fmaf((float)((v >> 8) & 0xFFu), unit, less));
             }
             *(uint4*)(t + P * kTile + tile_at(crow + 32 * i, ccol >> 3)) = w[0];
             *(uint4*)(t + P * kTile + tile_at(crow + 32 * i, (ccol >> 3) + 1)) = w[1];
@@ -149,7 +158,7 @@ __global__ __launch_bounds__(256, 2) void k_held_wgrad(const HeldWgradArgs a)
     // stage s is in LDS, `next` holds stage s + 1 and takes stage s + 3 once that is in LDS; stage s + 2 is on its way beside it
     const auto step = [&](long long s, const char* now, char* then, Part& next) __attribute__((always_inline)) {
         products(now);
-        if (s + 1 < full) put(next, then, s + 1);
+        if (s + 1 < full) put(next, then, std::true_type{}, S);
         if (s + 3 < full) fetch(next, s + 3);
         __syncthreads();
     };
@@ -157,7 +166,7 @@ __global__ __launch_bounds__(256, 2) void k_held_wgrad(const HeldWgradArgs a)
         Part x, y;
         fetch(x, lo);
         if (lo + 1 < full) fetch(y, lo + 1);
-        put(x, lds[0], lo);
+        put(x, lds[0], std::true_type{}, S);
         if (lo + 2 < full) fetch(x, lo + 2);
         __syncthreads();
         for (long long s = lo; s < full; s += 2) {
@@ -168,7 +177,7 @@ __global__ __launch_bounds__(256, 2) void k_held_wgrad(const HeldWgradArgs a)
     for (long long s = max(lo, full); s < hi; ++s) {
         Part x;
         fetch_each(x, s);
-        put(x, lds[0], s);
+        put(x, lds[0], std::false_type{}, (int)min((long long)S, a.rows - s * S));
         __syncthreads();
         products(lds[0]);
         __syncthreads();
@@ -233,7 +242,7 @@ void held_wgrad(const ftp_checkpoint_shape& s, const int8_t* codes, const int8_t
     a.ntiles = (int)ceil_div(a.N, kBlk); a.ktiles = (int)ceil_div(a.K, kBlk);
     const bool bf = s.dtype == FTP_BF16;
     a.wide = dy_stride >= 8 && a.K >= 16;
-    const unsigned grid = (unsigned)(a.ntiles * a.ktiles * a.shares);
+    const unsigned grid = a.shares < 8 ? (unsigned)(a.ntiles * a.ktiles * a.shares) : xcd_grid(a.shares, a.ntiles * a.ktiles);
     if (bf) k_held_wgrad<bf16_t><<<grid, 256, 0, st>>>(a);
     else k_held_wgrad<float><<<grid, 256, 0, st>>>(a);
     if (a.shares > 1) k_held_wgrad_sum<<<(unsigned)ceil_div((long long)a.N * a.K, 64), 256, 0, st>>>(partial, dw, (long long)a.N * a.K, a.shares);
