@@ -363,7 +363,9 @@ struct Lengths {
 __device__ __forceinline__ int query_of(const AttentionArgs& a, int row) { return a.group == 1 ? row : (int)((uint32_t)row / (uint32_t)a.group); }
 
 // Which block, split, image and key head a workgroup has; false: none.  Blocks of one (image, key head) read the same keys (queries) and run on one XCD where
-// the groups are many enough to load all eight.
+// the groups are many enough, and alike enough, to load all eight evenly.  Otherwise the groups' first blocks (of causal calls the longest) come first, a group's blocks on XCDs in turn:
+// a few images of their own lengths loaded the XCDs unevenly (prompts, 4 images x 2 key heads, 1550 to 2704 tokens: 69 -> 62 us; 2 x 3 key heads of 4000, causal: 78 -> 63; but
+// 6 x 4 key heads of 750 to 1500 113 us by XCDs, 120 in turn).
 __device__ __forceinline__ bool place_of(const AttentionArgs& a, int& block, int& split, int& b, int& kvh)
 {
     int g;
@@ -371,8 +373,8 @@ __device__ __forceinline__ bool place_of(const AttentionArgs& a, int& block, int
     if (a.by_xcd) {
         if (!xcd_order(index, a.groups, a.blocks, g, block)) return false;
     } else {
-        g = index / a.blocks;
-        block = index - g * a.blocks;
+        block = index / a.groups;
+        g = (index - block * a.groups + block) % a.groups;
     }
     split = g % a.splits;
     g /= a.splits;
@@ -383,7 +385,7 @@ __device__ __forceinline__ bool place_of(const AttentionArgs& a, int& block, int
 inline unsigned place_groups(AttentionArgs& a)
 {
     a.groups = a.batch * a.kv * a.splits;
-    a.by_xcd = a.groups % 8 == 0 || a.groups >= 48;
+    a.by_xcd = (a.groups % 8 == 0 && a.groups >= (a.q_lens || a.kv_lens ? 24 : 8)) || a.groups >= 48;
     return a.by_xcd ? xcd_grid(a.groups, a.blocks) : (unsigned)(a.groups * a.blocks);
 }
 

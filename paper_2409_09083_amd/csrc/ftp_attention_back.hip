@@ -16,7 +16,7 @@ namespace {
 template <typename T, int D> constexpr int kKeys = sizeof(T) == 4 ? 32 : 64;       // keys of a tile
 
 template <typename T, int D, bool VEC>
-__global__ __launch_bounds__(256, (D == 128 ? 1 : kPerCu<T, D>)) void k_attention_dq(const AttentionArgs a)
+__global__ __launch_bounds__(256, (kPerCu<T, D>)) void k_attention_dq(const AttentionArgs a)
 {
     typedef typename FragOf<T>::type Frag;
     constexpr int BN = kKeys<T, D>, UNITS = BN / 32, KS = D / 16, DT = D / 32;
@@ -72,36 +72,30 @@ __global__ __launch_bounds__(256, (D == 128 ? 1 : kPerCu<T, D>)) void k_attentio
     // few: only the row's delta, of p and dP themselves
     const auto step = [&](int t, Keys& now, Keys& next, auto few) __attribute__((always_inline)) {
         if (t + 1 < hi) fetch(t + 1, next);
-        f32x16 s[UNITS], p[UNITS];
 #pragma unroll
         for (int u = 0; u < UNITS; ++u) {
-            s[u] = f32x16{};
+            f32x16 s = {}, p;
 #pragma unroll
-            for (int r = 0; r < 16; ++r) p[u][r] = few ? 0.0f : -delta;
-        }
-        if ((t + 1) * BN > common) {
-            const int left = seen - t * BN - 4 * h; // keys of the tile that the row sees, counted from this lane's first
+            for (int r = 0; r < 16; ++r) p[r] = few ? 0.0f : -delta;
+            if (t * BN + 32 * u + 32 > common) {
+                const int left = seen - t * BN - 32 * u - 4 * h;       // keys of the unit that the row sees, counted from this lane's first
 #pragma unroll
-            for (int u = 0; u < UNITS; ++u)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) s[u][r] = 32 * u + 8 * (r >> 2) + (r & 3) >= left ? kHidden : 0.0f;
-        }
-#pragma unroll
-        for (int u = 0; u < UNITS; ++u) {
-#pragma unroll
-            for (int c = 0; c < KS; ++c) {
-                s[u] = mma(L::along(now.tile[0], 32 * u, c), q[c], s[u]);
-                p[u] = mma(L::along(now.tile[1], 32 * u, c), g[c], p[u]);
+                for (int r = 0; r < 16; ++r) s[r] = 8 * (r >> 2) + (r & 3) >= left ? kHidden : 0.0f;
             }
 #pragma unroll
-            for (int r = 0; r < 16; ++r) p[u][r] *= __builtin_amdgcn_exp2f(fmaf(s[u][r], a.c, -lse));
+            for (int c = 0; c < KS; ++c) {
+                s = mma(L::along(now.tile[0], 32 * u, c), q[c], s);
+                p = mma(L::along(now.tile[1], 32 * u, c), g[c], p);
+            }
+#pragma unroll
+            for (int r = 0; r < 16; ++r) p[r] *= __builtin_amdgcn_exp2f(fmaf(s[r], a.c, -lse));
             if constexpr (few) {
 #pragma unroll
-                for (int r = 0; r < 16; ++r) exact += p[u][r];
+                for (int r = 0; r < 16; ++r) exact += p[r];
             } else {
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
-                    const Frag ds = operand<T>(p[u], c);
+                    const Frag ds = operand<T>(p, c);
 #pragma unroll
                     for (int d = 0; d < DT; ++d) dq[d] = mma(L::across(now.tile[0], 32 * u + 16 * c, 32 * d), ds, dq[d]);
                 }
@@ -398,10 +392,13 @@ Splits backward_splits(const ftp_attention_shape& s)
 {
     const long long rows = (long long)s.q_len * (s.heads / s.kv_heads), all = (long long)s.batch * s.kv_heads;
     const long long nq = ceil_div(rows, 128) * all, nk = ceil_div(s.kv_len, 128) * all;
-    const auto pick = [](long long blocks, long long tiles) {
-        return blocks >= 256 ? 1 : (int)std::max(1ll, std::min({512 / std::max(blocks, 1ll), tiles / 4, 64ll}));
+    const bool bf = s.dtype == FTP_BF16, wide = s.head_dim > 64;
+    // The pipelined kernel (dk, dv) computes one unit too many a split, and with fp32 or wide heads has a CU by itself: its splits are longer (577 x 701 tokens of 40, fp32, 3 x 2 key
+    // heads, 3 heads each: 77 us the pass with 4 tiles, 72 with 8).
+    const auto pick = [](long long blocks, long long tiles, int least) {
+        return blocks == 0 || blocks >= 256 ? 1 : (int)std::max(1ll, std::min({512 / blocks, tiles / least, 64ll}));
     };
-    return {pick(nq, ceil_div(s.kv_len, s.dtype == FTP_BF16 ? 64 : 32)), pick(nk, ceil_div(rows, rows_of_tile(s.heads / s.kv_heads, s.dtype == FTP_BF16 ? 64 : 32)))};
+    return {pick(nq, ceil_div(s.kv_len, bf ? 64 : 32), 4), pick(nk, ceil_div(rows, rows_of_tile(s.heads / s.kv_heads, bf ? 64 : 32)), wide || !bf ? 8 : 4)};
 }
 
 int padded(const ftp_attention_shape& s) { return s.head_dim <= 32 ? 32 : s.head_dim <= 64 ? 64 : 128; }
