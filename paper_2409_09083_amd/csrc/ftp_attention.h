@@ -179,23 +179,24 @@ struct Staged {
             at[i] = (kAll < 256 && u >= kAll) || chunk * 8 >= d ? (Bytes)kNone : offset(row) + chunk * 8 * (int)sizeof(T);
         }
     }
-    // `rows`: how many rows there are, the others are zeros
-    __device__ __forceinline__ void fetch(char* tile, const T* base, int rows)
+    // `rows`: how many rows there are, the others are zeros, and so are those from `zero0` to `zero1` - 1
+    __device__ __forceinline__ void fetch(char* tile, const T* base, int rows, int zero0 = 0, int zero1 = 0)
     {
+        const auto is_there = [&](int row) { return row < rows && (row < zero0 || row >= zero1); };
         if constexpr (kDirect) {
             const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)base, (short)0, (int)0x80000000u, 0x00020000);
-            if (rows >= ROWS) {
+            if (rows >= ROWS && zero1 <= zero0) {
 #pragma unroll
                 for (int i = 0; i < kEach; ++i) load(tile, rsrc, i, at[i]);
             } else {
 #pragma unroll
-                for (int i = 0; i < kEach; ++i) load(tile, rsrc, i, (int)(threadIdx.x + 256 * i) / L::kChunks < rows ? at[i] : kNone);
+                for (int i = 0; i < kEach; ++i) load(tile, rsrc, i, is_there((int)(threadIdx.x + 256 * i) / L::kChunks) ? at[i] : kNone);
             }
         } else {
 #pragma unroll
             for (int i = 0; i < kEach; ++i) {
                 const int u = threadIdx.x + 256 * i, d0 = (u % L::kChunks) * 8;
-                const bool there = u / L::kChunks < rows && at[i] >= 0;
+                const bool there = is_there(u / L::kChunks) && at[i] >= 0;
                 const T* row = (const T*)((const char*)base + (there ? at[i] : 0)) - (there ? d0 : 0);
 #pragma unroll
                 for (int k = 0; k < kWords; ++k) {

@@ -152,7 +152,7 @@ __global__ __launch_bounds__(256, (kPerCu<T, D>)) void k_attention_dq(const Atte
     for (int d = 0; d < DT; ++d)
 #pragma unroll
         for (int r = 0; r < 16; r += 4) {
-            const f32x4 v = seen ? f32x4{dq[d][r], dq[d][r + 1], dq[d][r + 2], dq[d][r + 3]} * a.scale : f32x4{0, 0, 0, 0};
+            const f32x4 v = seen > 1 ? f32x4{dq[d][r], dq[d][r + 1], dq[d][r + 2], dq[d][r + 3]} * a.scale : f32x4{0, 0, 0, 0};      // (one key: probability 1, no gradient)
             store4(p, 32 * d + 8 * (r >> 2) + 4 * h, a.d, a.vec, v[0], v[1], v[2], v[3]);
         }
 }
@@ -209,15 +209,18 @@ __global__ __launch_bounds__(256, (D == 128 || sizeof(T) == 4 ? 1 : 2)) void k_a
     };
     sq.init([&](int r) { return offset(a.qs, r); }, a.d);
     sg.init([&](int r) { return offset(a.gs, r); }, a.d);
+    // Rows one0 .. one1 - 1 see one key, the first: their probability is 1 and their ds 0, exactly.  They come in with q = 0 and a log-sum of 0.
+    const int first_seeing = a.causal ? min(max(0, -len.off), len.q) : 0;
+    const int one0 = first_seeing * a.group, one1 = len.k == 1 ? rows : a.causal && len.off <= 0 ? min(one0 + a.group, rows) : one0;
     const int queries = a.group <= BM ? each / a.group : 0;
     const auto first_query = [&](int t) { return queries ? t * queries : t * each / a.group; };
     const auto fetch = [&](int t, Rows& to) __attribute__((always_inline)) {
         const int i0 = first_query(t), j0 = t * each - i0 * a.group, there = min(rows - t * each, each);
-        sq.fetch(to.tile[0], qp + i0 * a.qs[1] + j0 * a.qs[2], there);
+        sq.fetch(to.tile[0], qp + i0 * a.qs[1] + j0 * a.qs[2], there, max(one0 - t * each, 0), one1 - t * each);
         sg.fetch(to.tile[1], gp + i0 * a.gs[1] + j0 * a.gs[2], there);
         if (threadIdx.x < BM) {
             ss = tr < there ? len.seen(a, i0 + ti) : 0;
-            sl = ss ? lsep[(long long)(j0 + tj) * a.q_len + i0 + ti] * kLog2e : INFINITY;
+            sl = ss > 1 ? lsep[(long long)(j0 + tj) * a.q_len + i0 + ti] * kLog2e : ss ? 0.0f : INFINITY;
             sd = ss ? -deltap[t * each + tr] : 0.0f;
         }
     };
@@ -325,6 +328,7 @@ __global__ __launch_bounds__(256, (D == 128 || sizeof(T) == 4 ? 1 : 2)) void k_a
                 if (len.seen(a, i) <= key) continue;
                 const T* qr = qp + i * a.qs[1] + j * a.qs[2];
                 const T* gr = gp + i * a.gs[1] + j * a.gs[2];
+                if (len.seen(a, i) == 1) { add_row<T, DT>(dv, 1.0f, gr, a.d); continue; }
                 const float s = dot_of(qr, kr, a.d), p = __builtin_amdgcn_exp2f(fmaf(a.scale < 0 ? -s : s, a.c, -lsep[(long long)j * a.q_len + i] * kLog2e));
                 add_row<T, DT>(dv, p, gr, a.d);
                 add_row<T, DT>(dk, p * (dot_of(gr, vr, a.d) - deltap[row]), qr, a.d);
@@ -380,7 +384,7 @@ __global__ __launch_bounds__(256) void k_attention_add(const AttentionArgs a, lo
     } else {
         const int i = query_of(a, row);
         p = (T*)a.dq + b * a.dqs[0] + i * a.dqs[1] + (kvh * a.group + row - i * a.group) * a.dqs[2];
-        any = len.seen(a, i) > 0;
+        any = len.seen(a, i) > 1;
     }
     v = any ? v * (blockIdx.y ? 1.0f : a.scale) : f32x4{0, 0, 0, 0};
     store4(p, d0, a.d, a.vec, v[0], v[1], v[2], v[3]);

@@ -209,6 +209,23 @@ def test_large_scores(dtype):
     assert (a.dv[0, 50, 0].double() - want).abs().le(2.0 ** -8 * want.abs() + 1e-5).all()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape,causal,lens", [((2, 4, 2, 1, 1, 64), True, None), ((1, 2, 1, 70, 1, 40), False, None), ((2, 6, 2, 90, 90, 64), True, None),
+                                               ((2, 2, 2, 60, 50, 128), True, None), ((3, 4, 1, 33, 500, 32), False, [1, 500, 1]),
+                                               ((1, 80, 1, 3, 3, 16), True, None), ((1, 2, 2, 1500, 1, 64), True, None)])
+def test_rows_that_see_one_key(shape, causal, lens, dtype):
+    """Probability 1 whatever the score: dq exactly 0, nothing of them in dk, their dout in dv."""
+    a, (q, k, v, do) = _both(shape, dtype, causal, kv_lens=lens)
+    b, h, kv, ql, kl, d = shape
+    for n in range(b):
+        kn = kl if lens is None else lens[n]
+        seen = [min(max(i + kn - ql + 1, 0), kn) if causal else kn for i in range(ql)]
+        one = [i for i in range(ql) if seen[i] == 1]
+        assert a.dq[n, one].abs().sum() == 0
+        if kn == 1:
+            assert a.dk[n].abs().sum() == 0
+
+
 def test_gradient_by_differences():
     """Against central differences in 64 bits, with shared heads."""
     q, k, v, do = _make(1, 4, 2, 9, 12, 16, "f32")
