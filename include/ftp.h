@@ -48,7 +48,8 @@ typedef enum { FTP_RECT_OWN = 0, FTP_RECT_FWD = 1, FTP_RECT_BWD = 2 } ftp_rect_k
 typedef enum {
     FTP_OK = 0,
     FTP_EINVAL = -1,        /* null pointer, non-positive size, index out of range            */
-    FTP_EUNSUPPORTED = -2,  /* conv with stride not 1 or 2, K not in {1,3,5,7}, pad != K/2, pool != 2x2/2 */
+    FTP_EUNSUPPORTED = -2,  /* conv with stride not 1 or 2, K not in {1,3,5,7}, pad != K/2, pool != 2x2/2; a size or layout beyond an
+                               operator of the token block */
     FTP_EGRID = -3,         /* a tile would own no pixel, a map too small for its pool, grid > 16 */
     FTP_EGROUPS = -4,       /* group ends not strictly increasing or not ending at n_layers    */
     FTP_ENOMEM = -5,        /* host allocation failed                                          */
@@ -294,7 +295,8 @@ int ftp_checkpoint_act_backward(const ftp_checkpoint_shape* shape, const int8_t*
 int ftp_checkpoint_workspace(const ftp_checkpoint_shape* shape, int32_t outputs, size_t* bytes);
 
 /* dw[n][k] = sum over rows of dy[row][n] * value[row][k], fp32 [outputs][cols]: the weight gradient of a linear layer whose
- * input was kept.  dy: [rows][outputs] with `dy_stride` elements between rows (shape->stride is not used). */
+ * input was kept.  dy: [rows][outputs] with `dy_stride` elements between rows (shape->stride is not used); fp32 numbers of dy above 2^104, and
+ * infinities, give NaN. */
 int ftp_checkpoint_wgrad(const ftp_checkpoint_shape* shape, const int8_t* codes, const int8_t* exponents, const void* dy,
                          int64_t dy_stride, int32_t outputs, float* dw, void* workspace, void* stream);
 
@@ -302,8 +304,9 @@ int ftp_checkpoint_wgrad(const ftp_checkpoint_shape* shape, const int8_t* codes,
  * share the keys and values of heads / kv_heads neighbours.  Image b has q_lens[b] queries and kv_lens[b] keys (null: q_len, kv_len; values outside
  * 0 .. q_len / kv_len are cut to that); query i sees the keys j < kv_lens[b], and with `causal` only
  * j <= i + kv_lens[b] - q_lens[b] (the last query sees the last key).  A query that sees no key, and one beyond
- * q_lens[b], has out = 0, lse = -infinity and dq = 0; a key that no query sees has dk = dv = 0.  Keys, values and queries
- * that are not seen do not reach any result, whatever they hold.
+ * q_lens[b], has out = 0, lse = -infinity and dq = 0; a key that no query sees has dk = dv = 0; a query that sees one key has probability 1
+ * there and dq = 0, exactly.  Keys, values and queries that are not seen do not reach any result, whatever they hold (causal calls with such values that
+ * are not finite take long).  fp32 numbers are multiplied as three bfloats each: a seen infinity, or number above the largest bfloat, gives NaN.
  * Element (b, t, h, c) of q lies at q_stride[0] * b + q_stride[1] * t + q_stride[2] * h + c; likewise the others.  Inputs may
  * be broadcast (stride 0); gradients then come out unsummed, in buffers of their own.  q_len and kv_len may be 0. */
 typedef struct {

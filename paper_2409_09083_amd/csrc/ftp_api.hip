@@ -654,7 +654,7 @@ const char* ftp_strerror(int code)
     switch (code) {
         case FTP_OK: return "ok";
         case FTP_EINVAL: return "invalid argument";
-        case FTP_EUNSUPPORTED: return "unsupported layer (conv needs stride 1 or 2, K in {1,3,5,7}, pad K/2, slope >= 0; pool needs 2x2 stride 2)";
+        case FTP_EUNSUPPORTED: return "unsupported layer (conv needs stride 1 or 2, K in {1,3,5,7}, pad K/2, slope >= 0; pool needs 2x2 stride 2), or size or layout that an operator of the token block does not take";
         case FTP_EGRID: return "tile grid does not fit the maps (empty tile, map too small for its pool, or more than 16 tiles per side)";
         case FTP_EGROUPS: return "group ends must be strictly increasing and end at the number of layers";
         case FTP_ENOMEM: return "host allocation failed";

@@ -3,6 +3,10 @@
 // A workgroup is 128 rows (32 a wavefront) against tiles of keys, staged in LDS with the next tile's loads in flight.  S^T = K Q^T puts a row's scores into one lane pair
 // (lane % 32), so maximum, sum and rescaling are per lane; P^T is then the operand of O^T = V^T P^T as it lies (ftp_attention.h).  Few rows (single tokens): the keys are
 // split over workgroups, whose unnormalised rows a second kernel joins.
+//
+// Measured: prompts, 4 images of 1550 to 2704 tokens, 8 heads of 128 on 2, causal, bfloats: 60 us, 563 TFLOP/s (bound by the longest workgroups: 42 tiles behind each other on a SIMD shared
+// with another such, 28 on average); 64 heads x 5776 tokens of 64: 0.66-0.70 ms, 780-830 TFLOP/s (vector unit 79 % busy, a third of it exponentials; matrix cores 42 %); one token of 8 streams on up to 8192
+// keys: 24 us with the join, 91 MB, 3.8 TB/s.
 #include "ftp_attention.h"
 
 #include <algorithm>

@@ -2,7 +2,8 @@
 // q = round(x / 2^e) and stands for q * 2^e.  A scale that is a power of two costs up to one bit of a code against max|x| / 127, and gives: a scale of one byte; codes and values without
 // any other rounding (the quotient is exact, and so is q * 2^e as a bfloat), so that a matrix product can take the values as bfloat operands.
 // Bound by memory: packing reads a value and writes a byte, the others read a byte (and dy) and write a value.  A lane takes 8 neighbours, 2^k lanes a
-// block; no LDS.
+// block; no LDS.  Measured at 189 million fp32 values, blocks of 128: packing 187 us (946 MB, 5.1 TB/s), unpacking 170 us (5.6 TB/s; a large copy: 4.8); GELU's derivative of 46208 x 1024 bfloats 45 us
+// (237 MB, 5.2 TB/s): its 20 vector instructions and two transcendental ones a value stay below the memory's time.
 #include "ftp_tokens.h"
 
 #include <algorithm>
