@@ -1,12 +1,12 @@
 // Softmax attention, forward: out = softmax(scale q k^T) v over the keys a query sees, one pass over the keys with the running maximum and sum of each row.
 //
-// A workgroup is 128 rows (32 a wavefront) against tiles of keys, staged in LDS with the next tile's loads in flight.  S^T = K Q^T puts a row's scores into one lane pair
+// A workgroup is 128 rows (32 a wavefront; or 64, two wavefronts to 32) against tiles of keys, staged in LDS with the next tile's loads in flight.  S^T = K Q^T puts a row's scores into one lane pair
 // (lane % 32), so maximum, sum and rescaling are per lane; P^T is then the operand of O^T = V^T P^T as it lies (ftp_attention.h).  Few rows (single tokens): the keys are
 // split over workgroups, whose unnormalised rows a second kernel joins.
 //
 // Measured: prompts, 4 images of 1550 to 2704 tokens, 8 heads of 128 on 2, causal, bfloats: 60 us, 563 TFLOP/s (bound by the longest workgroups: 42 tiles behind each other on a SIMD shared
 // with another such, 28 on average); 64 heads x 5776 tokens of 64: 0.66-0.70 ms, 780-830 TFLOP/s (vector unit 79 % busy, a third of it exponentials; matrix cores 42 %); one token of 8 streams on up to 8192
-// keys: 24 us with the join, 91 MB, 3.8 TB/s.
+// keys: 23 us with the join, 91 MB, 4.0 TB/s.
 #include "ftp_attention.h"
 
 #include <algorithm>
@@ -15,30 +15,33 @@
 namespace ftp {
 namespace {
 
-constexpr int kWaves = 4;
 template <typename T, int D> constexpr int kKeys = sizeof(T) == 4 ? 32 : 64;       // keys of a tile
 
-template <typename T, int D, bool VEC>
+// HALVES 1: 128 rows a workgroup, 32 a wavefront.  2: 64 rows, each by two wavefronts that take the tile's 32-key units in turn and join their rows through LDS at the end: half as long
+// chains, twice the staging (see halves()).
+template <typename T, int D, bool VEC, int HALVES>
 __global__ __launch_bounds__(256, (kPerCu<T, D>)) void k_attention(const AttentionArgs a)
 {
     typedef typename FragOf<T>::type Frag;
-    constexpr int BN = kKeys<T, D>, UNITS = BN / 32, KS = D / 16, DT = D / 32;
+    constexpr int BN = kKeys<T, D>, UNITS = BN / 32 / HALVES, KS = D / 16, DT = D / 32, ROWS = 128 / HALVES;
     typedef Tile<T, D, BN> L;
     constexpr int kTile = L::kBytes;
     struct Keys { char tile[2][kTile]; };           // a tile of keys and values
     __shared__ __align__(16) Keys even, odd;        // (apart, so that reads of one need not wait for loads of the other)
+    static_assert(UNITS > 0 && (HALVES == 1 || (int)sizeof(Keys) >= 2 * DT * 4096), "a unit a wavefront; two wavefronts' rows in a tile's place");
     int block, split, b, kvh;
     if (!place_of(a, block, split, b, kvh)) return;
     if (a.causal) block = a.blocks - 1 - block;     // the longest ones first
     const Lengths len(a, b);
     const int rows = a.q_len * a.group;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, h = l >> 5;
-    const int first = block * 32 * kWaves, row = first + wave * 32 + (l & 31);
+    const int half = HALVES == 2 ? wave >> 1 : 0, at0 = (HALVES == 2 ? wave & 1 : wave) * 32, mine0 = 32 * half;         // this wavefront's rows, and its unit's first key of a tile
+    const int first = block * ROWS, row = first + at0 + (l & 31);
     const int i = query_of(a, row), head = kvh * a.group + row - i * a.group;
     const bool inside = row < rows;
     const int seen = inside ? len.seen(a, i) : 0;
     // keys that some row of the workgroup sees, and those that all its rows inside the lengths see
-    const int last = query_of(a, min(first + 32 * kWaves, rows) - 1), i0 = query_of(a, first);
+    const int last = query_of(a, min(first + ROWS, rows) - 1), i0 = query_of(a, first);
     const int end = i0 < len.q ? len.seen(a, min(last, len.q - 1)) : 0, common = len.seen(a, i0);
     const int tiles = (end + BN - 1) / BN, lo = (int)((long long)tiles * split / a.splits), hi = (int)((long long)tiles * (split + 1) / a.splits);
 
@@ -68,7 +71,7 @@ __global__ __launch_bounds__(256, (kPerCu<T, D>)) void k_attention(const Attenti
         if (t + 1 < hi) fetch(t + 1, next);
         f32x16 s[UNITS] = {};
         if ((t + 1) * BN > common) {
-            const int left = seen - t * BN - 4 * h; // keys of the tile that the row sees, counted from this lane's first
+            const int left = seen - t * BN - mine0 - 4 * h;            // keys of the tile that the row sees, counted from this lane's first
 #pragma unroll
             for (int u = 0; u < UNITS; ++u)
 #pragma unroll
@@ -78,7 +81,7 @@ __global__ __launch_bounds__(256, (kPerCu<T, D>)) void k_attention(const Attenti
 #pragma unroll
         for (int u = 0; u < UNITS; ++u) {
 #pragma unroll
-            for (int c = 0; c < KS; ++c) s[u] = mma(L::along(now.tile[0], 32 * u, c), q[c], s[u]);
+            for (int c = 0; c < KS; ++c) s[u] = mma(L::along(now.tile[0], mine0 + 32 * u, c), q[c], s[u]);
 #pragma unroll
             for (int r = 0; r < 16; ++r) top = fmaxf(top, s[u][r]);
         }
@@ -105,7 +108,7 @@ __global__ __launch_bounds__(256, (kPerCu<T, D>)) void k_attention(const Attenti
             for (int c = 0; c < 2; ++c) {
                 const Frag p = operand<T>(s[u], c);
 #pragma unroll
-                for (int d = 0; d < DT; ++d) o[d] = mma(L::across(now.tile[1], 32 * u + 16 * c, 32 * d), p, o[d]);
+                for (int d = 0; d < DT; ++d) o[d] = mma(L::across(now.tile[1], mine0 + 32 * u + 16 * c, 32 * d), p, o[d]);
             }
         }
         if (t + 1 < hi) land(next);
@@ -118,18 +121,19 @@ __global__ __launch_bounds__(256, (kPerCu<T, D>)) void k_attention(const Attenti
         step(t, even, odd);
         if (t + 1 < hi) step(t + 1, odd, even);
     }
-    if (!inside) return;
     if (a.causal && __any(not_finite(o) || !(sum < INFINITY))) {
-        const int row = again(first + wave * 32 + (l & 31)), i = query_of(a, row), head = kvh * a.group + row - i * a.group;      // (not worth registers before)
+        const int row = again(first + at0 + (l & 31)), i = query_of(a, row), head = kvh * a.group + row - i * a.group;      // (not worth registers before)
         const T* qr = (const T*)a.q + b * a.qs[0] + i * a.qs[1] + head * a.qs[2];
+        const auto other = [&](int key) { return HALVES == 2 && ((key >> 5) & 1) != half; };
         if (both_max(not_finite(o) || !(sum < INFINITY) ? 1.0f : 0.0f) > 0) {
             const auto score = [&](int key) { const float s = dot_of(qr, kp + key * a.ks[1], a.d); return (a.scale < 0 ? -s : s) * a.c; };
 #pragma unroll
             for (int d = 0; d < DT; ++d) o[d] = f32x16{};
             m = nothing;
             sum = 0;
-            for (int key = lo * BN; key < min(hi * BN, seen); ++key) m = fmaxf(m, score(key));
+            for (int key = lo * BN; key < min(hi * BN, seen); ++key) if (!other(key)) m = fmaxf(m, score(key));
             for (int key = lo * BN; key < min(hi * BN, seen); ++key) {
+                if (other(key)) continue;
                 const float p = __builtin_amdgcn_exp2f(score(key) - m);
                 add_row<T, DT>(o, p, vp + key * a.vs[1], a.d);
                 sum += h ? 0.0f : p;
@@ -137,6 +141,34 @@ __global__ __launch_bounds__(256, (kPerCu<T, D>)) void k_attention(const Attenti
         }
     }
     sum = both_sum(sum);
+    if constexpr (HALVES == 2) {
+        // (the tiles' last readers are behind a barrier: a wavefront leaves the loop's last tile by itself, so one more)
+        f32x4* part = (f32x4*)&even + (at0 / 32) * DT * 4 * 64;
+        float* stats = (float*)&odd + (at0 / 32) * 128;
+        __syncthreads();
+        if (half) {
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) part[(d * 4 + r) * 64 + l] = f32x4{o[d][4 * r], o[d][4 * r + 1], o[d][4 * r + 2], o[d][4 * r + 3]};
+            stats[l] = m;
+            stats[64 + l] = sum;
+        }
+        __syncthreads();
+        if (half) return;
+        const float m2 = stats[l], top = fmaxf(m, m2), f = __builtin_amdgcn_exp2f(m - top), f2 = __builtin_amdgcn_exp2f(m2 - top);
+        sum = sum * f + stats[64 + l] * f2;
+        m = top;
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const f32x4 v = part[(d * 4 + r) * 64 + l];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) o[d][4 * r + j] = o[d][4 * r + j] * f + v[j] * f2;
+            }
+    }
+    if (!inside) return;
     if (a.splits > 1) {
         // [split][image][key head][row][D], and the rows' maxima and sums behind
         const long long at = (((long long)split * a.batch + b) * a.kv + kvh) * rows + row, n = (long long)a.splits * a.batch * a.kv * rows;
@@ -203,20 +235,36 @@ __global__ __launch_bounds__(256) void k_attention_join(const AttentionArgs a)
     if (d0 == 0 && a.lse) a.lse[((long long)b * a.heads + head) * a.q_len + i] = any ? fmaf(m, kLn2, logf(sum)) : -INFINITY;
 }
 
+// Wavefronts to a row.  Two (bfloats: an fp32 tile is one unit) where a workgroup has at most 64 rows anyway (256 streams of one token on 200 keys 26.4 -> 21.3 us), and where 128 rows each
+// leave the chip few chains of tiles, or uneven ones that causal calls end on (4 x 12 heads x 577 tokens 23.3 -> 13.8 us, 2 x 8 x 2600 55 -> 48, causal 4 x 8 x 2600 66 -> 51); heads of 128 pay
+// more for staging twice (causal 2 x 8 x 2600 56 -> 51, all pairs 78 -> 87).  With enough of them 128 rows are better: 8 x 8 x 5776 tokens 671 us, halves 720.
+int halves(const ftp_attention_shape& s)
+{
+    const long long rows = (long long)s.q_len * (s.heads / s.kv_heads), groups = ceil_div(rows, 128) * s.batch * s.kv_heads;
+    const bool narrow = s.head_dim <= 64;
+    if (s.dtype != FTP_BF16) return 1;
+    return rows <= 64 || groups < (narrow && s.causal ? 768 : narrow || s.causal ? 384 : 256) ? 2 : 1;
+}
+
 // Splits of the keys: none where the blocks of rows give every CU a workgroup; else as many as do, of at least 4 tiles.
 int forward_splits(const ftp_attention_shape& s)
 {
-    const long long blocks = ceil_div((long long)s.q_len * (s.heads / s.kv_heads), 32 * kWaves) * s.batch * s.kv_heads;
+    const long long blocks = ceil_div((long long)s.q_len * (s.heads / s.kv_heads), 128 / halves(s)) * s.batch * s.kv_heads;
     const long long tiles = ceil_div(s.kv_len, s.dtype == FTP_BF16 ? 64 : 32);
     if (blocks == 0 || blocks >= 256) return 1;
     return (int)std::max(1ll, std::min({512 / blocks, tiles / 4, 128ll}));
 }
 
 template <typename T, int D>
-void run(const AttentionArgs& a, unsigned grid, hipStream_t st)
+void run(const AttentionArgs& a, bool two, unsigned grid, hipStream_t st)
 {
-    if (a.vec) k_attention<T, D, true><<<grid, 256, 0, st>>>(a);
-    else k_attention<T, D, false><<<grid, 256, 0, st>>>(a);
+    if (sizeof(T) == 2 && two) {
+        if (a.vec) k_attention<T, D, true, sizeof(T) == 2 ? 2 : 1><<<grid, 256, 0, st>>>(a);
+        else k_attention<T, D, false, sizeof(T) == 2 ? 2 : 1><<<grid, 256, 0, st>>>(a);
+    } else {
+        if (a.vec) k_attention<T, D, true, 1><<<grid, 256, 0, st>>>(a);
+        else k_attention<T, D, false, 1><<<grid, 256, 0, st>>>(a);
+    }
     if (a.splits > 1) {
         const long long rows = (long long)a.batch * a.kv * a.q_len * a.group;
         if (rows <= 2048) k_attention_join<T, D, 1024 / D><<<(unsigned)rows, 256, 0, st>>>(a);
@@ -255,17 +303,18 @@ void attention_forward(const ftp_attention_shape& s, const void* q, const void* 
     a.vec = s.head_dim % el == 0 && aligned(q, 16) && aligned(k, 16) && aligned(v, 16) && aligned(out, 16);
     for (int i = 0; i < 3; ++i) a.vec = a.vec && a.qs[i] % el == 0 && a.ks[i] % el == 0 && a.vs[i] % el == 0 && a.os[i] % el == 0;
     a.vec = a.vec && near_rows(a.ks[1]) && near_rows(a.vs[1]);
-    a.blocks = (int)ceil_div((long long)a.q_len * a.group, 32 * kWaves);
+    const bool two = halves(s) == 2;
+    a.blocks = (int)ceil_div((long long)a.q_len * a.group, two ? 64 : 128);
     a.splits = forward_splits(s);
     const unsigned grid = place_groups(a);
     if (s.dtype == FTP_BF16) {
-        if (a.d <= 32) run<bf16_t, 32>(a, grid, st);
-        else if (a.d <= 64) run<bf16_t, 64>(a, grid, st);
-        else run<bf16_t, 128>(a, grid, st);
+        if (a.d <= 32) run<bf16_t, 32>(a, two, grid, st);
+        else if (a.d <= 64) run<bf16_t, 64>(a, two, grid, st);
+        else run<bf16_t, 128>(a, two, grid, st);
     } else {
-        if (a.d <= 32) run<float, 32>(a, grid, st);
-        else if (a.d <= 64) run<float, 64>(a, grid, st);
-        else run<float, 128>(a, grid, st);
+        if (a.d <= 32) run<float, 32>(a, two, grid, st);
+        else if (a.d <= 64) run<float, 64>(a, two, grid, st);
+        else run<float, 128>(a, two, grid, st);
     }
 }
 

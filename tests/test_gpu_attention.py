@@ -132,6 +132,30 @@ def test_few_keys_of_many_queries(dtype):
     _both((1, 2, 2, 1500, 100, 64), dtype)
 
 
+# enough of them that a workgroup takes 128 rows, a wavefront each: bfloats with heads of up to 64 and of up to 128
+@pytest.mark.parametrize("shape,causal", [((40, 20, 20, 70, 130, 64), True), ((40, 20, 20, 129, 33, 40), True), ((20, 20, 20, 100, 65, 31), False),
+                                          ((20, 20, 20, 70, 100, 128), False), ((20, 40, 20, 65, 97, 100), True)])
+def test_many_images_and_heads(shape, causal):
+    b, ql, kl = shape[0], shape[3], shape[4]
+    _both(shape, "bf16", causal, q_lens=[(17 * n) % (ql + 1) for n in range(b)], kv_lens=[kl - (13 * n) % (kl + 1) for n in range(b)])
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+@pytest.mark.parametrize("images", [1, 800])
+def test_hidden_values_in_either_half_of_a_tile(images, bad):
+    """Key and value 40 or 70 (the second 32 of their tile of 64, the first of the next): the queries before them are as without."""
+    q, k, v, do = _make(images, 1, 1, 80, 80, 64, "bf16")
+    want = _run(q, k, v, do, "bf16", True)
+    for at in (40, 70):
+        k2, v2 = k.clone(), v.clone()
+        k2[0, at, 0], v2[0, at, 0, 1] = bad, bad
+        got = _run(q, k2, v2, do, "bf16", True)
+        for x, y in ((got.out, want.out), (got.dq, want.dq)):
+            assert (x[0, :at] - y[0, :at]).abs().max() <= 3e-2 * y[0, :at].abs().max()
+            assert torch.equal(x[1:], y[1:])
+        assert not got.out[0, at:].isfinite().all()
+
+
 @pytest.mark.parametrize("scale", [-0.2, 0.0, 1.0])
 def test_other_scales(scale):
     _both((1, 2, 2, 70, 70, 32), "f32", True, scale=scale)
