@@ -174,32 +174,37 @@ __host__ __device__ inline int rows_of_tile(int group, int most)
 }
 
 // A workgroup is 128 keys against tiles of 64 rows (fp32: 32), three tiles in LDS in turn with one barrier a tile.  The scores of the next 32 rows are computed beside this unit's exponentials
-// (overlap()): 1.28-1.37 -> 1.19 ms against one unit after the other.  fp32 and heads of more than 64 channels need the registers of a whole CU; fp32 heads of 128 spill some of them all the same.
-template <typename T, int D, bool VEC>
+// (overlap()): 1.28-1.37 -> 1.19 ms against one unit after the other.  fp32 and heads of more than 64 channels need the registers of a whole CU.
+//
+// HALVES 2, fp32 heads of 128, whose sums and operands one wavefront's registers do not hold (332 spilled): 64 keys, 32 to two wavefronts that take half of the channels each.  Their parts of the
+// scores are exchanged through LDS, then each has the gradients of its own channels (4 x 8 heads x 2000, causal: pass 1990 -> 1120 us; 11 x 64 heads on 8 x 15 of 104 70 -> 39; heads of 64 lose,
+// 635 -> 1025).
+template <typename T, int D, bool VEC, int HALVES>
 __global__ __launch_bounds__(256, (D == 128 || sizeof(T) == 4 ? 1 : 2)) void k_attention_dkv(const AttentionArgs a)
 {
     typedef typename FragOf<T>::type Frag;
-    constexpr int BM = kRows<T, D>, UNITS = BM / 32, KS = D / 16, DT = D / 32;
+    constexpr int BM = kRows<T, D>, UNITS = BM / 32, MY = D / HALVES, KS = MY / 16, DT = MY / 32, KEYS = 128 / HALVES;
     typedef Tile<T, D, BM> L;
     constexpr int kTile = L::kBytes;
     // a tile of rows: queries, dout; and of its rows the log-sum in powers of 2, -delta, the number of keys seen
     struct Rows { char tile[2][kTile]; float lse[BM], less[BM]; int seen[BM]; };
-    __shared__ __align__(16) Rows r0, r1, r2;       // three in turn (apart, so that reads of one need not wait for loads of another)
+    __shared__ __align__(16) Rows r0, r1;           // (apart, so that reads of one need not wait for loads of another)
     int block, split, b, kvh;
     if (!place_of(a, block, split, b, kvh)) return;
     const Lengths len(a, b);
     const int rows = len.q * a.group;               // (rows past the lengths see nothing)
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, h = l >> 5;
-    const int key0 = block * 128, mine = key0 + wave * 32, key = mine + (l & 31);
+    const int half = HALVES == 2 ? wave >> 1 : 0, c0 = half * MY, my = a.d - c0;      // this wavefront's channels: c0 .. c0 + MY - 1, `my` or fewer of them there
+    const int key0 = block * KEYS, mine = key0 + (HALVES == 2 ? wave & 1 : wave) * 32, key = mine + (l & 31);
     const bool inside = key < len.k;
     // rows that see any of the keys: all from the first query that sees key0 on
     const int from = key0 >= len.k ? rows : a.causal ? (int)min((long long)rows, (long long)max(0, key0 - len.off) * a.group) : 0;
     const int each = rows_of_tile(a.group, BM), t0 = from / each, tiles = from < rows ? (rows + each - 1) / each - t0 : 0;
     const int lo = t0 + (int)((long long)tiles * split / a.splits), hi = t0 + (int)((long long)tiles * (split + 1) / a.splits);
 
-    Frag k[D / 16], v[D / 16];
-    row_operands<T, D>(k, inside ? (const T*)a.k + b * a.ks[0] + key * a.ks[1] + kvh * a.ks[2] : nullptr, a.d, VEC, a.scale < 0);
-    row_operands<T, D>(v, inside ? (const T*)a.v + b * a.vs[0] + key * a.vs[1] + kvh * a.vs[2] : nullptr, a.d, VEC, false);
+    Frag k[KS], v[KS];
+    row_operands<T, MY>(k, inside ? (const T*)a.k + b * a.ks[0] + key * a.ks[1] + kvh * a.ks[2] + c0 : nullptr, my, VEC, a.scale < 0);
+    row_operands<T, MY>(v, inside ? (const T*)a.v + b * a.vs[0] + key * a.vs[1] + kvh * a.vs[2] + c0 : nullptr, my, VEC, false);
     const T* qp = (const T*)a.q + b * a.qs[0] + kvh * a.group * a.qs[2];
     const T* gp = (const T*)a.dout + b * a.gs[0] + kvh * a.group * a.gs[2];
     const float* lsep = a.lse + ((long long)b * a.heads + kvh * a.group) * a.q_len;
@@ -252,79 +257,133 @@ __global__ __launch_bounds__(256, (D == 128 || sizeof(T) == 4 ? 1 : 2)) void k_a
             for (int r = 0; r < 16; ++r) s[r] = key >= at.seen[u + 8 * (r >> 2) + 4 * h + (r & 3)] ? kHidden : 0.0f;
         }
     };
-    // this unit's probabilities and products (rows u .. of `now`), and the scores of the next one (rows w .. of `next`)
-    const auto unit = [&](const Rows& now, int u, const Rows& next, int w, bool hide, f32x16& s, f32x16& p, f32x16& s2, f32x16& p2) __attribute__((always_inline)) {
-        Frag fa[2 * KS], fc[2][2 * DT];
-        Words<T> ws, we;
-        f32x4 lse[4];
-#pragma unroll
-        for (int r = 0; r < 4; ++r) lse[r] = *(const f32x4*)&now.lse[u + 8 * r + 4 * h];
-        start(next, w, hide, s2, p2);
-        overlap<2 * KS, 2 * DT>(
-            [&](int i) __attribute__((always_inline)) { fa[i] = L::along(next.tile[i & 1], w, i >> 1); },
-            [&](int i) __attribute__((always_inline)) {
-                if (i & 1) p2 = mma(fa[i], v[i >> 1], p2);
-                else s2 = mma(fa[i], k[i >> 1], s2);
-            },
-            [&](int g) __attribute__((always_inline)) {
-#pragma unroll
-                for (int r = 2 * g; r < 2 * g + 2; ++r) {
-                    s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], a.c, -lse[r >> 2][r & 3]));
-                    p[r] *= s[r];
-                }
-                ws.set(g, s[2 * g], s[2 * g + 1]);
-                we.set(g, p[2 * g], p[2 * g + 1]);
-            },
-            [&](int c, int i) __attribute__((always_inline)) { fc[c][i] = L::across(now.tile[1 - (i & 1)], u + 16 * c, 32 * (i >> 1)); },
-            [&](int c, int i) __attribute__((always_inline)) {
-                if (i & 1) dk[i >> 1] = mma(fc[c][i], we.f[c], dk[i >> 1]);
-                else dv[i >> 1] = mma(fc[c][i], ws.f[c], dv[i >> 1]);
-            });
-    };
-    f32x16 s0, p0, s1, p1;
     const auto hides = [&](int t) { return a.causal && len.seen(a, first_query(t)) < mine + 32; };     // (a tile's first row sees the fewest keys)
-    const auto tile = [&](int t, Rows& now, Rows& next, Rows& after, auto odd) __attribute__((always_inline)) {
+    if constexpr (HALVES == 2) {
+        static_assert(UNITS == 1, "a tile is a unit");
+        __shared__ __align__(16) f32x4 parts[4][8][64];         // of S and dP - delta, by wavefront
+        const bool any = mine < len.k;
+        const auto tile = [&](int t, Rows& now, Rows& next) __attribute__((always_inline)) {
+            if (t + 1 < hi) fetch(t + 1, next);
+            f32x16 s = {}, p = {};
+            if (any) {
+                if (half == 0) start(now, 0, hides(t), s, p);
 #pragma unroll
-        for (int n = 0; n < UNITS; ++n) {
-            const bool end = n == UNITS - 1;
-            if (end) {                              // the next tile has landed, and nobody reads the one before this
-                if (t + 1 < hi) land(next);
-                if (t + 2 < hi) fetch(t + 2, after);
+                for (int c = 0; c < KS; ++c) {
+                    s = mma(L::along(now.tile[0], 0, half * KS + c), k[c], s);
+                    p = mma(L::along(now.tile[1], 0, half * KS + c), v[c], p);
+                }
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    parts[wave][r][l] = f32x4{s[4 * r], s[4 * r + 1], s[4 * r + 2], s[4 * r + 3]};
+                    parts[wave][4 + r][l] = f32x4{p[4 * r], p[4 * r + 1], p[4 * r + 2], p[4 * r + 3]};
+                }
             }
-            const Rows& then = end ? next : now;
-            const int w = end ? 0 : 32 * (n + 1);
-            const bool hide = hides(end ? t + 1 : t), flip = UNITS == 1 ? odd : n & 1;
-            if (flip) unit(now, 32 * n, then, w, hide, s1, p1, s0, p0);
-            else unit(now, 32 * n, then, w, hide, s0, p0, s1, p1);
-        }
-    };
-    if (lo < hi) {
-        fetch(lo, r0);
-        land(r0);
-        if (lo + 1 < hi) fetch(lo + 1, r1);
-        start(r0, 0, hides(lo), s0, p0);
+            __syncthreads();                        // (and nobody reads the tile before this any more)
+            if (any) {
 #pragma unroll
-        for (int c = 0; c < KS; ++c) {
-            s0 = mma(L::along(r0.tile[0], 0, c), k[c], s0);
-            p0 = mma(L::along(r0.tile[1], 0, c), v[c], p0);
+                for (int r = 0; r < 4; ++r) {
+                    const f32x4 s2 = parts[wave ^ 2][r][l], p2 = parts[wave ^ 2][4 + r][l], lse = *(const f32x4*)&now.lse[8 * r + 4 * h];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        s[4 * r + j] = __builtin_amdgcn_exp2f(fmaf(s[4 * r + j] + s2[j], a.c, -lse[j]));
+                        p[4 * r + j] = (p[4 * r + j] + p2[j]) * s[4 * r + j];
+                    }
+                }
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    const Frag ps = operand<T>(s, c), ds = operand<T>(p, c);
+#pragma unroll
+                    for (int d = 0; d < DT; ++d) {
+                        dv[d] = mma(L::across(now.tile[1], 16 * c, c0 + 32 * d), ps, dv[d]);
+                        dk[d] = mma(L::across(now.tile[0], 16 * c, c0 + 32 * d), ds, dk[d]);
+                    }
+                }
+            }
+            if (t + 1 < hi) land(next);
+        };
+        if (lo < hi) {
+            fetch(lo, r0);
+            land(r0);
         }
-    }
-    const std::false_type even;
-    const std::true_type odd;
-    for (int t = lo; t < hi; t += 3) {
-        tile(t, r0, r1, r2, even);
-        if (t + 1 < hi) tile(t + 1, r1, r2, r0, odd);
-        if (t + 2 < hi) tile(t + 2, r2, r0, r1, even);
-        if constexpr (UNITS == 1) {                 // (the scores change places with every unit)
-            t += 3;
-            if (t < hi) tile(t, r0, r1, r2, odd);
-            if (t + 1 < hi) tile(t + 1, r1, r2, r0, even);
-            if (t + 2 < hi) tile(t + 2, r2, r0, r1, odd);
+        for (int t = lo; t < hi; t += 2) {
+            tile(t, r0, r1);
+            if (t + 1 < hi) tile(t + 1, r1, r0);
+        }
+    } else {
+        __shared__ __align__(16) Rows r2;               // (a third)
+        // this unit's probabilities and products (rows u .. of `now`), and the scores of the next one (rows w .. of `next`)
+        const auto unit = [&](const Rows& now, int u, const Rows& next, int w, bool hide, f32x16& s, f32x16& p, f32x16& s2, f32x16& p2) __attribute__((always_inline)) {
+            Frag fa[2 * KS], fc[2][2 * DT];
+            Words<T> ws, we;
+            f32x4 lse[4];
+    #pragma unroll
+            for (int r = 0; r < 4; ++r) lse[r] = *(const f32x4*)&now.lse[u + 8 * r + 4 * h];
+            start(next, w, hide, s2, p2);
+            overlap<2 * KS, 2 * DT>(
+                [&](int i) __attribute__((always_inline)) { fa[i] = L::along(next.tile[i & 1], w, i >> 1); },
+                [&](int i) __attribute__((always_inline)) {
+                    if (i & 1) p2 = mma(fa[i], v[i >> 1], p2);
+                    else s2 = mma(fa[i], k[i >> 1], s2);
+                },
+                [&](int g) __attribute__((always_inline)) {
+    #pragma unroll
+                    for (int r = 2 * g; r < 2 * g + 2; ++r) {
+                        s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], a.c, -lse[r >> 2][r & 3]));
+                        p[r] *= s[r];
+                    }
+                    ws.set(g, s[2 * g], s[2 * g + 1]);
+                    we.set(g, p[2 * g], p[2 * g + 1]);
+                },
+                [&](int c, int i) __attribute__((always_inline)) { fc[c][i] = L::across(now.tile[1 - (i & 1)], u + 16 * c, 32 * (i >> 1)); },
+                [&](int c, int i) __attribute__((always_inline)) {
+                    if (i & 1) dk[i >> 1] = mma(fc[c][i], we.f[c], dk[i >> 1]);
+                    else dv[i >> 1] = mma(fc[c][i], ws.f[c], dv[i >> 1]);
+                });
+        };
+        f32x16 s0, p0, s1, p1;
+        const auto tile = [&](int t, Rows& now, Rows& next, Rows& after, auto odd) __attribute__((always_inline)) {
+    #pragma unroll
+            for (int n = 0; n < UNITS; ++n) {
+                const bool end = n == UNITS - 1;
+                if (end) {                              // the next tile has landed, and nobody reads the one before this
+                    if (t + 1 < hi) land(next);
+                    if (t + 2 < hi) fetch(t + 2, after);
+                }
+                const Rows& then = end ? next : now;
+                const int w = end ? 0 : 32 * (n + 1);
+                const bool hide = hides(end ? t + 1 : t), flip = UNITS == 1 ? odd : n & 1;
+                if (flip) unit(now, 32 * n, then, w, hide, s1, p1, s0, p0);
+                else unit(now, 32 * n, then, w, hide, s0, p0, s1, p1);
+            }
+        };
+        if (lo < hi) {
+            fetch(lo, r0);
+            land(r0);
+            if (lo + 1 < hi) fetch(lo + 1, r1);
+            start(r0, 0, hides(lo), s0, p0);
+    #pragma unroll
+            for (int c = 0; c < KS; ++c) {
+                s0 = mma(L::along(r0.tile[0], 0, c), k[c], s0);
+                p0 = mma(L::along(r0.tile[1], 0, c), v[c], p0);
+            }
+        }
+        const std::false_type even;
+        const std::true_type odd;
+        for (int t = lo; t < hi; t += 3) {
+            tile(t, r0, r1, r2, even);
+            if (t + 1 < hi) tile(t + 1, r1, r2, r0, odd);
+            if (t + 2 < hi) tile(t + 2, r2, r0, r1, even);
+            if constexpr (UNITS == 1) {                 // (the scores change places with every unit)
+                t += 3;
+                if (t < hi) tile(t, r0, r1, r2, odd);
+                if (t + 1 < hi) tile(t + 1, r1, r2, r0, even);
+                if (t + 2 < hi) tile(t + 2, r2, r0, r1, odd);
+            }
         }
     }
     if (key >= a.kv_len) return;
     if (a.causal && __any(not_finite(dk) || not_finite(dv))) {
-        const int key = again(key0 + wave * 32 + (l & 31));         // (what follows is not worth registers before)
+        const int key = again(mine + (l & 31));         // (what follows is not worth registers before)
         if (both_max(not_finite(dk) || not_finite(dv) ? 1.0f : 0.0f) > 0 && inside) {
             const T* kr = (const T*)a.k + b * a.ks[0] + key * a.ks[1] + kvh * a.ks[2];
             const T* vr = (const T*)a.v + b * a.vs[0] + key * a.vs[1] + kvh * a.vs[2];
@@ -335,17 +394,17 @@ __global__ __launch_bounds__(256, (D == 128 || sizeof(T) == 4 ? 1 : 2)) void k_a
                 if (len.seen(a, i) <= key) continue;
                 const T* qr = qp + i * a.qs[1] + j * a.qs[2];
                 const T* gr = gp + i * a.gs[1] + j * a.gs[2];
-                if (len.seen(a, i) == 1) { add_row<T, DT>(dv, 1.0f, gr, a.d); continue; }
+                if (len.seen(a, i) == 1) { add_row<T, DT>(dv, 1.0f, gr + c0, my); continue; }
                 const float s = dot_of(qr, kr, a.d), p = __builtin_amdgcn_exp2f(fmaf(a.scale < 0 ? -s : s, a.c, -lsep[(long long)j * a.q_len + i] * kLog2e));
-                add_row<T, DT>(dv, p, gr, a.d);
-                add_row<T, DT>(dk, p * (dot_of(gr, vr, a.d) - deltap[row]), qr, a.d);
+                add_row<T, DT>(dv, p, gr + c0, my);
+                add_row<T, DT>(dk, p * (dot_of(gr, vr, a.d) - deltap[row]), qr + c0, my);
             }
         }
     }
     if (a.splits > 1) {
         const long long n = (long long)a.batch * a.kv * a.kv_len;
         const long long at = ((long long)b * a.kv + kvh) * a.kv_len + key;
-        float* pk = a.ws + ((2 * split) * n + at) * D;
+        float* pk = a.ws + ((2 * split) * n + at) * D + c0;
         float* pv = pk + n * D;
 #pragma unroll
         for (int d = 0; d < DT; ++d)
@@ -356,16 +415,16 @@ __global__ __launch_bounds__(256, (D == 128 || sizeof(T) == 4 ? 1 : 2)) void k_a
             }
         return;
     }
-    T* pk = (T*)a.dk + b * a.dks[0] + key * a.dks[1] + kvh * a.dks[2];
-    T* pv = (T*)a.dv + b * a.dvs[0] + key * a.dvs[1] + kvh * a.dvs[2];
+    T* pk = (T*)a.dk + b * a.dks[0] + key * a.dks[1] + kvh * a.dks[2] + c0;
+    T* pv = (T*)a.dv + b * a.dvs[0] + key * a.dvs[1] + kvh * a.dvs[2] + c0;
 #pragma unroll
     for (int d = 0; d < DT; ++d)
 #pragma unroll
         for (int r = 0; r < 16; r += 4) {
             const f32x4 x = inside ? f32x4{dk[d][r], dk[d][r + 1], dk[d][r + 2], dk[d][r + 3]} * a.scale : f32x4{0, 0, 0, 0};
             const f32x4 y = inside ? f32x4{dv[d][r], dv[d][r + 1], dv[d][r + 2], dv[d][r + 3]} : f32x4{0, 0, 0, 0};
-            store4(pk, 32 * d + 8 * (r >> 2) + 4 * h, a.d, a.vec, x[0], x[1], x[2], x[3]);
-            store4(pv, 32 * d + 8 * (r >> 2) + 4 * h, a.d, a.vec, y[0], y[1], y[2], y[3]);
+            store4(pk, 32 * d + 8 * (r >> 2) + 4 * h, my, a.vec, x[0], x[1], x[2], x[3]);
+            store4(pv, 32 * d + 8 * (r >> 2) + 4 * h, my, a.vec, y[0], y[1], y[2], y[3]);
         }
 }
 
@@ -397,25 +456,37 @@ __global__ __launch_bounds__(256) void k_attention_add(const AttentionArgs a, lo
     store4(p, d0, a.d, a.vec, v[0], v[1], v[2], v[3]);
 }
 
+// Wavefronts to a key in k_attention_dkv (see there).
+int key_halves(const ftp_attention_shape& s) { return s.dtype != FTP_BF16 && s.head_dim > 64 ? 2 : 1; }
+
 // Splits of the keys (dq) and of the rows (dk, dv): see forward_splits.
 struct Splits { int dq, dkv; };
 Splits backward_splits(const ftp_attention_shape& s)
 {
     const long long rows = (long long)s.q_len * (s.heads / s.kv_heads), all = (long long)s.batch * s.kv_heads;
-    const long long nq = ceil_div(rows, 128) * all, nk = ceil_div(s.kv_len, 128) * all;
+    const long long nq = ceil_div(rows, 128) * all, nk = ceil_div(s.kv_len, 128 / key_halves(s)) * all;
     const bool bf = s.dtype == FTP_BF16, wide = s.head_dim > 64;
-    // The pipelined kernel (dk, dv) computes one unit too many a split, and with fp32 or wide heads has a CU by itself: its splits are longer (577 x 701 tokens of 40, fp32, 3 x 2 key
-    // heads, 3 heads each: 77 us the pass with 4 tiles, 72 with 8).
-    const auto pick = [](long long blocks, long long tiles, int least) {
-        return blocks == 0 || blocks >= 256 ? 1 : (int)std::max(1ll, std::min({512 / blocks, tiles / least, 64ll}));
+    // Workgroups that have a CU by themselves (alone) come in rounds of 256: a split costs its tiles and about as long as 6 for its start, a unit too many and its part of the sum
+    // (fp32, 13 x 8 heads on 1, 7 x 1172 tokens of 120: 53 us the pass with splits of at least 8 tiles, 47; 4 heads x 300 of 64 59 -> 41; 8 heads x 1000 of 128 171 -> 144).  More than a round
+    // of blocks is split for the last one's sake where a tile is long and the blocks are alike (fp32, 16 heads x 1144 of 128: 473 -> 394; causal bfloats of 128 95 -> 123).
+    const bool rounds = !bf && wide && !s.causal;
+    const auto pick = [rounds](long long blocks, long long tiles, bool alone) {
+        if (blocks == 0) return 1;
+        if (blocks >= 256 && !rounds) return 1;
+        if (!alone) return (int)std::max(1ll, std::min({512 / blocks, tiles / 4, 64ll}));
+        const auto cost = [&](long long n) { return ceil_div(blocks * n, 256) * (ceil_div(tiles, n) + 6); };
+        long long best = 1;
+        for (long long n = 2; n <= std::min(64ll, tiles / 2) && blocks * n < 2048; ++n)
+            if (cost(n) < cost(best)) best = n;
+        return (int)best;
     };
-    return {pick(nq, ceil_div(s.kv_len, bf ? 64 : 32), 4), pick(nk, ceil_div(rows, rows_of_tile(s.heads / s.kv_heads, bf ? 64 : 32)), wide || !bf ? 8 : 4)};
+    return {pick(nq, ceil_div(s.kv_len, bf ? 64 : 32), wide && !bf), pick(nk, ceil_div(rows, rows_of_tile(s.heads / s.kv_heads, bf ? 64 : 32)), wide || !bf)};
 }
 
 int padded(const ftp_attention_shape& s) { return s.head_dim <= 32 ? 32 : s.head_dim <= 64 ? 64 : 128; }
 
 template <typename T, int D>
-void run(AttentionArgs a, const Splits& n, hipStream_t st)
+void run(AttentionArgs a, const Splits& n, int halves, hipStream_t st)
 {
     const long long rows = (long long)a.q_len * a.group, all = (long long)a.batch * a.kv;
     if (rows) {
@@ -427,11 +498,17 @@ void run(AttentionArgs a, const Splits& n, hipStream_t st)
         if (n.dq > 1) k_attention_add<T, D, false><<<(unsigned)ceil_div(all * rows, 1024 / D), 256, 0, st>>>(a, all * rows * D, n.dq);
     }
     if (a.kv_len) {
-        a.blocks = (int)ceil_div(a.kv_len, 128);
+        a.blocks = (int)ceil_div(a.kv_len, 128 / halves);
         a.splits = n.dkv;
         const unsigned grid = place_groups(a);
-        if (a.vec) k_attention_dkv<T, D, true><<<grid, 256, 0, st>>>(a);
-        else k_attention_dkv<T, D, false><<<grid, 256, 0, st>>>(a);
+        constexpr int TWO = sizeof(T) == 4 && D > 32 ? 2 : 1;
+        if (halves == TWO) {
+            if (a.vec) k_attention_dkv<T, D, true, TWO><<<grid, 256, 0, st>>>(a);
+            else k_attention_dkv<T, D, false, TWO><<<grid, 256, 0, st>>>(a);
+        } else {
+            if (a.vec) k_attention_dkv<T, D, true, 1><<<grid, 256, 0, st>>>(a);
+            else k_attention_dkv<T, D, false, 1><<<grid, 256, 0, st>>>(a);
+        }
         if (n.dkv > 1) {
             const long long each = all * a.kv_len * D;
             k_attention_add<T, D, true><<<dim3((unsigned)ceil_div(all * a.kv_len, 1024 / D), 2), 256, 0, st>>>(a, 2 * each, n.dkv);
@@ -467,13 +544,13 @@ void attention_backward(const ftp_attention_shape& s, const void* dout, const vo
     a.vec = a.vec && near_rows(a.qs[2] * a.group / 128) && near_rows(a.gs[2] * a.group / 128);
     const Splits n = backward_splits(s);
     if (s.dtype == FTP_BF16) {
-        if (a.d <= 32) run<bf16_t, 32>(a, n, st);
-        else if (a.d <= 64) run<bf16_t, 64>(a, n, st);
-        else run<bf16_t, 128>(a, n, st);
+        if (a.d <= 32) run<bf16_t, 32>(a, n, key_halves(s), st);
+        else if (a.d <= 64) run<bf16_t, 64>(a, n, key_halves(s), st);
+        else run<bf16_t, 128>(a, n, key_halves(s), st);
     } else {
-        if (a.d <= 32) run<float, 32>(a, n, st);
-        else if (a.d <= 64) run<float, 64>(a, n, st);
-        else run<float, 128>(a, n, st);
+        if (a.d <= 32) run<float, 32>(a, n, key_halves(s), st);
+        else if (a.d <= 64) run<float, 64>(a, n, key_halves(s), st);
+        else run<float, 128>(a, n, key_halves(s), st);
     }
 }
 

@@ -156,6 +156,27 @@ def test_hidden_values_in_either_half_of_a_tile(images, bad):
         assert not got.out[0, at:].isfinite().all()
 
 
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+def test_hidden_values_of_wide_heads(bad):
+    """fp32 heads of 128: the gradients of a key's first and last 64 channels are two wavefronts' work."""
+    q, k, v, do = _make(1, 2, 1, 90, 90, 100, "f32")
+    want = _run(q, k, v, do, "f32", True)
+    for c in (3, 97):
+        do2 = do.clone()
+        do2[0, 40, 1, c] = bad                                  # seen by the keys up to 40
+        got = _run(q, k, v, do2, "f32", True)
+        for t in ("dk", "dv"):
+            x, y = getattr(got, t)[0, 41:], getattr(want, t)[0, 41:]
+            assert (x - y).abs().max() <= 1e-5 * y.abs().max(), t
+        assert not got.dv[0, :41, :, c].isfinite().any()
+        k2, v2 = k.clone(), v.clone()
+        k2[0, 70, 0, c], v2[0, 70, 0, c] = bad, bad             # only the queries from 70 on see them
+        got = _run(q, k2, v2, do, "f32", True)
+        for t in ("out", "dq"):
+            x, y = getattr(got, t)[0, :70], getattr(want, t)[0, :70]
+            assert (x - y).abs().max() <= 1e-5 * y.abs().max(), t
+
+
 @pytest.mark.parametrize("scale", [-0.2, 0.0, 1.0])
 def test_other_scales(scale):
     _both((1, 2, 2, 70, 70, 32), "f32", True, scale=scale)
