@@ -428,6 +428,8 @@ __device__ __forceinline__ void add_row(f32x16 (&v)[DT], float f, const T* row, 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 AttentionArgs attention_args(const ftp_attention_shape& s);
+// Wavefronts to a row of 32 in the kernels that walk over the keys: 1 or 2.
+int attention_halves(const ftp_attention_shape& s);
 
 // Offsets within a tile (at most 64 such strides) stay below 2^30 bytes.
 inline bool near_rows(long long stride) { return stride < (1ll << 21); }

@@ -18,7 +18,7 @@ namespace {
 template <typename T, int D> constexpr int kKeys = sizeof(T) == 4 ? 32 : 64;       // keys of a tile
 
 // HALVES 1: 128 rows a workgroup, 32 a wavefront.  2: 64 rows, each by two wavefronts that take the tile's 32-key units in turn and join their rows through LDS at the end: half as long
-// chains, twice the staging (see halves()).
+// chains, twice the staging (see attention_halves()).
 template <typename T, int D, bool VEC, int HALVES>
 __global__ __launch_bounds__(256, (kPerCu<T, D>)) void k_attention(const AttentionArgs a)
 {
@@ -235,21 +235,10 @@ __global__ __launch_bounds__(256) void k_attention_join(const AttentionArgs a)
     if (d0 == 0 && a.lse) a.lse[((long long)b * a.heads + head) * a.q_len + i] = any ? fmaf(m, kLn2, logf(sum)) : -INFINITY;
 }
 
-// Wavefronts to a row.  Two (bfloats: an fp32 tile is one unit) where a workgroup has at most 64 rows anyway (256 streams of one token on 200 keys 26.4 -> 21.3 us), and where 128 rows each
-// leave the chip few chains of tiles, or uneven ones that causal calls end on (4 x 12 heads x 577 tokens 23.3 -> 13.8 us, 2 x 8 x 2600 55 -> 48, causal 4 x 8 x 2600 66 -> 51); heads of 128 pay
-// more for staging twice (causal 2 x 8 x 2600 56 -> 51, all pairs 78 -> 87).  With enough of them 128 rows are better: 8 x 8 x 5776 tokens 671 us, halves 720.
-int halves(const ftp_attention_shape& s)
-{
-    const long long rows = (long long)s.q_len * (s.heads / s.kv_heads), groups = ceil_div(rows, 128) * s.batch * s.kv_heads;
-    const bool narrow = s.head_dim <= 64;
-    if (s.dtype != FTP_BF16) return 1;
-    return rows <= 64 || groups < (narrow && s.causal ? 768 : narrow || s.causal ? 384 : 256) ? 2 : 1;
-}
-
 // Splits of the keys: none where the blocks of rows give every CU a workgroup; else as many as do, of at least 4 tiles.
 int forward_splits(const ftp_attention_shape& s)
 {
-    const long long blocks = ceil_div((long long)s.q_len * (s.heads / s.kv_heads), 128 / halves(s)) * s.batch * s.kv_heads;
+    const long long blocks = ceil_div((long long)s.q_len * (s.heads / s.kv_heads), 128 / attention_halves(s)) * s.batch * s.kv_heads;
     const long long tiles = ceil_div(s.kv_len, s.dtype == FTP_BF16 ? 64 : 32);
     if (blocks == 0 || blocks >= 256) return 1;
     return (int)std::max(1ll, std::min({512 / blocks, tiles / 4, 128ll}));
@@ -273,6 +262,17 @@ void run(const AttentionArgs& a, bool two, unsigned grid, hipStream_t st)
 }
 
 }  // namespace
+
+// Wavefronts to a row.  Two (bfloats: an fp32 tile is one unit) where a workgroup has at most 64 rows anyway (256 streams of one token on 200 keys 26.4 -> 21.3 us), and where 128 rows each
+// leave the chip few chains of tiles, or uneven ones that causal calls end on (4 x 12 heads x 577 tokens 23.3 -> 13.8 us, 2 x 8 x 2600 55 -> 48, causal 4 x 8 x 2600 66 -> 51); heads of 128 pay
+// more for staging twice (causal 2 x 8 x 2600 56 -> 51, all pairs 78 -> 87).  With enough of them 128 rows are better: 8 x 8 x 5776 tokens 671 us, halves 720.
+int attention_halves(const ftp_attention_shape& s)
+{
+    const long long rows = (long long)s.q_len * (s.heads / s.kv_heads), groups = ceil_div(rows, 128) * s.batch * s.kv_heads;
+    const bool narrow = s.head_dim <= 64;
+    if (s.dtype != FTP_BF16) return 1;
+    return rows <= 64 || groups < (narrow && s.causal ? 768 : narrow || s.causal ? 384 : 256) ? 2 : 1;
+}
 
 AttentionArgs attention_args(const ftp_attention_shape& s)
 {
@@ -303,7 +303,7 @@ void attention_forward(const ftp_attention_shape& s, const void* q, const void* 
     a.vec = s.head_dim % el == 0 && aligned(q, 16) && aligned(k, 16) && aligned(v, 16) && aligned(out, 16);
     for (int i = 0; i < 3; ++i) a.vec = a.vec && a.qs[i] % el == 0 && a.ks[i] % el == 0 && a.vs[i] % el == 0 && a.os[i] % el == 0;
     a.vec = a.vec && near_rows(a.ks[1]) && near_rows(a.vs[1]);
-    const bool two = halves(s) == 2;
+    const bool two = attention_halves(s) == 2;
     a.blocks = (int)ceil_div((long long)a.q_len * a.group, two ? 64 : 128);
     a.splits = forward_splits(s);
     const unsigned grid = place_groups(a);

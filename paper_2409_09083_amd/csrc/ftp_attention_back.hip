@@ -20,11 +20,14 @@ namespace {
 template <typename T, int D> constexpr int kKeys = sizeof(T) == 4 ? 32 : 64;       // keys of a tile
 
 // A workgroup is 128 rows against tiles of 64 keys (fp32: 32), two tiles in LDS.  The compiler's order of a tile's instructions is kept: by hand as in k_attention_dkv it was slower here (0.80 -> 0.93 ms).
-template <typename T, int D, bool VEC>
+//
+// HALVES 2, bfloats: 64 rows, each by two wavefronts that take a unit of every tile and add up their rows through LDS at the end (attention_halves(): 4 x 12 heads x 577 tokens 53.9 -> 45.7 us the pass,
+// causal 4 x 8 x 2600 164 -> 151).  fp32 tiles of two units for it would cost the second workgroup of a CU: 16 heads x 1144 of 64 161 -> 207.
+template <typename T, int D, bool VEC, int HALVES>
 __global__ __launch_bounds__(256, (kPerCu<T, D>)) void k_attention_dq(const AttentionArgs a)
 {
     typedef typename FragOf<T>::type Frag;
-    constexpr int BN = kKeys<T, D>, UNITS = BN / 32, KS = D / 16, DT = D / 32;
+    constexpr int BN = kKeys<T, D>, UNITS = BN / 32 / HALVES, KS = D / 16, DT = D / 32, ROWS = 128 / HALVES;
     typedef Tile<T, D, BN> L;
     constexpr int kTile = L::kBytes;
     struct Keys { char tile[2][kTile]; };           // a tile of keys and values
@@ -35,11 +38,12 @@ __global__ __launch_bounds__(256, (kPerCu<T, D>)) void k_attention_dq(const Atte
     const Lengths len(a, b);
     const int rows = a.q_len * a.group;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, h = l >> 5;
-    const int first = block * 128, row = first + wave * 32 + (l & 31);
+    const int half = HALVES == 2 ? wave >> 1 : 0, at0 = (HALVES == 2 ? wave & 1 : wave) * 32, mine0 = 32 * half;         // this wavefront's rows, and its unit's first key of a tile
+    const int first = block * ROWS, row = first + at0 + (l & 31);
     const int i = query_of(a, row), head = kvh * a.group + row - i * a.group;
     const bool inside = row < rows;
     const int seen = inside ? len.seen(a, i) : 0;
-    const int last = query_of(a, min(first + 128, rows) - 1), i0 = query_of(a, first);
+    const int last = query_of(a, min(first + ROWS, rows) - 1), i0 = query_of(a, first);
     const int end = i0 < len.q ? len.seen(a, min(last, len.q - 1)) : 0, common = len.seen(a, i0);
     const int tiles = (end + BN - 1) / BN, lo = (int)((long long)tiles * split / a.splits), hi = (int)((long long)tiles * (split + 1) / a.splits);
     // this row's operands; delta from the same dout and the row of out
@@ -82,15 +86,15 @@ __global__ __launch_bounds__(256, (kPerCu<T, D>)) void k_attention_dq(const Atte
             f32x16 s = {}, p;
 #pragma unroll
             for (int r = 0; r < 16; ++r) p[r] = few ? 0.0f : -delta;
-            if (t * BN + 32 * u + 32 > common) {
-                const int left = seen - t * BN - 32 * u - 4 * h;       // keys of the unit that the row sees, counted from this lane's first
+            if (t * BN + mine0 + 32 * u + 32 > common) {
+                const int left = seen - t * BN - mine0 - 32 * u - 4 * h;       // keys of the unit that the row sees, counted from this lane's first
 #pragma unroll
                 for (int r = 0; r < 16; ++r) s[r] = 8 * (r >> 2) + (r & 3) >= left ? kHidden : 0.0f;
             }
 #pragma unroll
             for (int c = 0; c < KS; ++c) {
-                s = mma(L::along(now.tile[0], 32 * u, c), q[c], s);
-                p = mma(L::along(now.tile[1], 32 * u, c), g[c], p);
+                s = mma(L::along(now.tile[0], mine0 + 32 * u, c), q[c], s);
+                p = mma(L::along(now.tile[1], mine0 + 32 * u, c), g[c], p);
             }
 #pragma unroll
             for (int r = 0; r < 16; ++r) p[r] *= __builtin_amdgcn_exp2f(fmaf(s[r], a.c, -lse));
@@ -102,7 +106,7 @@ __global__ __launch_bounds__(256, (kPerCu<T, D>)) void k_attention_dq(const Atte
                 for (int c = 0; c < 2; ++c) {
                     const Frag ds = operand<T>(p, c);
 #pragma unroll
-                    for (int d = 0; d < DT; ++d) dq[d] = mma(L::across(now.tile[0], 32 * u + 16 * c, 32 * d), ds, dq[d]);
+                    for (int d = 0; d < DT; ++d) dq[d] = mma(L::across(now.tile[0], mine0 + 32 * u + 16 * c, 32 * d), ds, dq[d]);
                 }
             }
         }
@@ -124,25 +128,53 @@ __global__ __launch_bounds__(256, (kPerCu<T, D>)) void k_attention_dq(const Atte
     if (sizeof(T) == 2 && a.splits == 1 && tiles * BN <= 256) {
         walk(std::true_type{});
         exact = both_sum(exact);
+        if constexpr (HALVES == 2) {
+            float* parts = (float*)&odd;            // (odd: the second walk starts with even)
+            parts[(wave >> 1) * 128 + at0 * 2 + l] = exact;
+            __syncthreads();
+            exact = parts[at0 * 2 + l] + parts[128 + at0 * 2 + l];
+        }
         if (fabsf(exact) < INFINITY) delta = exact;            // (not where hidden values made it NaN)
     }
-    if (split == 0 && inside && h == 0) a.delta[at] = delta;
+    if (split == 0 && half == 0 && inside && h == 0) a.delta[at] = delta;
     walk(std::false_type{});
-    if (!inside) return;
     if (a.causal && __any(not_finite(dq))) {
-        const int row = again(first + wave * 32 + (l & 31)), i = query_of(a, row), head = kvh * a.group + row - i * a.group;      // (not worth registers before)
+        const int row = again(first + at0 + (l & 31)), i = query_of(a, row), head = kvh * a.group + row - i * a.group;      // (not worth registers before)
         const T* qr = (const T*)a.q + b * a.qs[0] + i * a.qs[1] + head * a.qs[2];
         const T* gr = (const T*)a.dout + b * a.gs[0] + i * a.gs[1] + head * a.gs[2];
         if (both_max(not_finite(dq) ? 1.0f : 0.0f) > 0) {
 #pragma unroll
             for (int d = 0; d < DT; ++d) dq[d] = f32x16{};
             for (int key = lo * BN; key < min(hi * BN, seen); ++key) {
+                if (HALVES == 2 && ((key >> 5) & 1) != half) continue;
                 const T* kr = kp + key * a.ks[1];
                 const float s = dot_of(qr, kr, a.d), p = __builtin_amdgcn_exp2f(fmaf(a.scale < 0 ? -s : s, a.c, -lse));
                 add_row<T, DT>(dq, p * (dot_of(gr, vp + key * a.vs[1], a.d) - delta), kr, a.d);
             }
         }
     }
+    if constexpr (HALVES == 2) {
+        static_assert((int)sizeof(Keys) >= 2 * DT * 4096, "two wavefronts' rows in a tile's place");
+        f32x4* parts = (f32x4*)&even + (at0 / 32) * DT * 4 * 64;
+        __syncthreads();                            // (nobody reads tiles any more)
+        if (half) {
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) parts[(d * 4 + r) * 64 + l] = f32x4{dq[d][4 * r], dq[d][4 * r + 1], dq[d][4 * r + 2], dq[d][4 * r + 3]};
+        }
+        __syncthreads();
+        if (half) return;
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const f32x4 v = parts[(d * 4 + r) * 64 + l];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) dq[d][4 * r + j] += v[j];
+            }
+    }
+    if (!inside) return;
     if (a.splits > 1) {
         float* p = a.ws + (((long long)split * a.batch * a.kv * rows) + at) * D;
 #pragma unroll
@@ -464,7 +496,7 @@ struct Splits { int dq, dkv; };
 Splits backward_splits(const ftp_attention_shape& s)
 {
     const long long rows = (long long)s.q_len * (s.heads / s.kv_heads), all = (long long)s.batch * s.kv_heads;
-    const long long nq = ceil_div(rows, 128) * all, nk = ceil_div(s.kv_len, 128 / key_halves(s)) * all;
+    const long long nq = ceil_div(rows, 128 / attention_halves(s)) * all, nk = ceil_div(s.kv_len, 128 / key_halves(s)) * all;
     const bool bf = s.dtype == FTP_BF16, wide = s.head_dim > 64;
     // Workgroups that have a CU by themselves (alone) come in rounds of 256: a split costs its tiles and about as long as 6 for its start, a unit too many and its part of the sum
     // (fp32, 13 x 8 heads on 1, 7 x 1172 tokens of 120: 53 us the pass with splits of at least 8 tiles, 47; 4 heads x 300 of 64 59 -> 41; 8 heads x 1000 of 128 171 -> 144).  More than a round
@@ -486,23 +518,29 @@ Splits backward_splits(const ftp_attention_shape& s)
 int padded(const ftp_attention_shape& s) { return s.head_dim <= 32 ? 32 : s.head_dim <= 64 ? 64 : 128; }
 
 template <typename T, int D>
-void run(AttentionArgs a, const Splits& n, int halves, hipStream_t st)
+void run(AttentionArgs a, const Splits& n, int row_halves, int key_halves, hipStream_t st)
 {
     const long long rows = (long long)a.q_len * a.group, all = (long long)a.batch * a.kv;
     if (rows) {
-        a.blocks = (int)ceil_div(rows, 128);
+        a.blocks = (int)ceil_div(rows, 128 / row_halves);
         a.splits = n.dq;
         const unsigned grid = place_groups(a);
-        if (a.vec) k_attention_dq<T, D, true><<<grid, 256, 0, st>>>(a);
-        else k_attention_dq<T, D, false><<<grid, 256, 0, st>>>(a);
+        constexpr int TWO = sizeof(T) == 4 ? 1 : 2;
+        if (row_halves == TWO) {
+            if (a.vec) k_attention_dq<T, D, true, TWO><<<grid, 256, 0, st>>>(a);
+            else k_attention_dq<T, D, false, TWO><<<grid, 256, 0, st>>>(a);
+        } else {
+            if (a.vec) k_attention_dq<T, D, true, 1><<<grid, 256, 0, st>>>(a);
+            else k_attention_dq<T, D, false, 1><<<grid, 256, 0, st>>>(a);
+        }
         if (n.dq > 1) k_attention_add<T, D, false><<<(unsigned)ceil_div(all * rows, 1024 / D), 256, 0, st>>>(a, all * rows * D, n.dq);
     }
     if (a.kv_len) {
-        a.blocks = (int)ceil_div(a.kv_len, 128 / halves);
+        a.blocks = (int)ceil_div(a.kv_len, 128 / key_halves);
         a.splits = n.dkv;
         const unsigned grid = place_groups(a);
         constexpr int TWO = sizeof(T) == 4 && D > 32 ? 2 : 1;
-        if (halves == TWO) {
+        if (key_halves == TWO) {
             if (a.vec) k_attention_dkv<T, D, true, TWO><<<grid, 256, 0, st>>>(a);
             else k_attention_dkv<T, D, false, TWO><<<grid, 256, 0, st>>>(a);
         } else {
@@ -544,13 +582,13 @@ void attention_backward(const ftp_attention_shape& s, const void* dout, const vo
     a.vec = a.vec && near_rows(a.qs[2] * a.group / 128) && near_rows(a.gs[2] * a.group / 128);
     const Splits n = backward_splits(s);
     if (s.dtype == FTP_BF16) {
-        if (a.d <= 32) run<bf16_t, 32>(a, n, key_halves(s), st);
-        else if (a.d <= 64) run<bf16_t, 64>(a, n, key_halves(s), st);
-        else run<bf16_t, 128>(a, n, key_halves(s), st);
+        if (a.d <= 32) run<bf16_t, 32>(a, n, attention_halves(s), key_halves(s), st);
+        else if (a.d <= 64) run<bf16_t, 64>(a, n, attention_halves(s), key_halves(s), st);
+        else run<bf16_t, 128>(a, n, attention_halves(s), key_halves(s), st);
     } else {
-        if (a.d <= 32) run<float, 32>(a, n, key_halves(s), st);
-        else if (a.d <= 64) run<float, 64>(a, n, key_halves(s), st);
-        else run<float, 128>(a, n, key_halves(s), st);
+        if (a.d <= 32) run<float, 32>(a, n, attention_halves(s), key_halves(s), st);
+        else if (a.d <= 64) run<float, 64>(a, n, attention_halves(s), key_halves(s), st);
+        else run<float, 128>(a, n, attention_halves(s), key_halves(s), st);
     }
 }
 
