@@ -194,6 +194,7 @@ __global__ __launch_bounds__(256, (kPerCu<T, D>)) void k_attention_dq(const Atte
         }
 }
 
+template <typename T, int D> constexpr int kKeyHalves = sizeof(T) == 4 && D == 128 ? 2 : 1;        // wavefronts to a key (HALVES below)
 template <typename T, int D> constexpr int kRows = sizeof(T) == 4 ? 32 : 64;     // rows of a tile of k_attention_dkv
 
 // Rows that a tile of `most` takes: whole queries of all heads of the group, or for large groups a part of one query's that divides them.
@@ -488,19 +489,16 @@ __global__ __launch_bounds__(256) void k_attention_add(const AttentionArgs a, lo
     store4(p, d0, a.d, a.vec, v[0], v[1], v[2], v[3]);
 }
 
-// Wavefronts to a key in k_attention_dkv (see there).
-int key_halves(const ftp_attention_shape& s) { return s.dtype != FTP_BF16 && s.head_dim > 64 ? 2 : 1; }
-
 // Splits of the keys (dq) and of the rows (dk, dv): see forward_splits.
 struct Splits { int dq, dkv; };
 Splits backward_splits(const ftp_attention_shape& s)
 {
-    const long long rows = (long long)s.q_len * (s.heads / s.kv_heads), all = (long long)s.batch * s.kv_heads;
-    const long long nq = ceil_div(rows, 128 / attention_halves(s)) * all, nk = ceil_div(s.kv_len, 128 / key_halves(s)) * all;
     const bool bf = s.dtype == FTP_BF16, wide = s.head_dim > 64;
+    const long long rows = (long long)s.q_len * (s.heads / s.kv_heads), all = (long long)s.batch * s.kv_heads;
+    const long long nq = ceil_div(rows, 128 / attention_halves(s)) * all, nk = ceil_div(s.kv_len, bf || !wide ? 128 : 64) * all;
     // Workgroups that have a CU by themselves (alone) come in rounds of 256: a split costs its tiles and about as long as 6 for its start, a unit too many and its part of the sum
     // (fp32, 13 x 8 heads on 1, 7 x 1172 tokens of 120: 53 us the pass with splits of at least 8 tiles, 47; 4 heads x 300 of 64 59 -> 41; 8 heads x 1000 of 128 171 -> 144).  More than a round
-    // of blocks is split for the last one's sake where a tile is long and the blocks are alike (fp32, 16 heads x 1144 of 128: 473 -> 394; causal bfloats of 128 95 -> 123).
+    // of blocks is split for the last one's sake where a tile is long and the blocks are alike (fp32, 16 heads x 1144 of 128: 473 -> 394; split so, causal bfloats of 128 go 95 -> 123).
     const bool rounds = !bf && wide && !s.causal;
     const auto pick = [rounds](long long blocks, long long tiles, bool alone) {
         if (blocks == 0) return 1;
@@ -518,15 +516,15 @@ Splits backward_splits(const ftp_attention_shape& s)
 int padded(const ftp_attention_shape& s) { return s.head_dim <= 32 ? 32 : s.head_dim <= 64 ? 64 : 128; }
 
 template <typename T, int D>
-void run(AttentionArgs a, const Splits& n, int row_halves, int key_halves, hipStream_t st)
+void run(AttentionArgs a, const Splits& n, int halves, hipStream_t st)
 {
     const long long rows = (long long)a.q_len * a.group, all = (long long)a.batch * a.kv;
     if (rows) {
-        a.blocks = (int)ceil_div(rows, 128 / row_halves);
+        a.blocks = (int)ceil_div(rows, 128 / halves);
         a.splits = n.dq;
         const unsigned grid = place_groups(a);
         constexpr int TWO = sizeof(T) == 4 ? 1 : 2;
-        if (row_halves == TWO) {
+        if (halves == TWO) {
             if (a.vec) k_attention_dq<T, D, true, TWO><<<grid, 256, 0, st>>>(a);
             else k_attention_dq<T, D, false, TWO><<<grid, 256, 0, st>>>(a);
         } else {
@@ -536,17 +534,11 @@ void run(AttentionArgs a, const Splits& n, int row_halves, int key_halves, hipSt
         if (n.dq > 1) k_attention_add<T, D, false><<<(unsigned)ceil_div(all * rows, 1024 / D), 256, 0, st>>>(a, all * rows * D, n.dq);
     }
     if (a.kv_len) {
-        a.blocks = (int)ceil_div(a.kv_len, 128 / key_halves);
+        a.blocks = (int)ceil_div(a.kv_len, 128 / kKeyHalves<T, D>);
         a.splits = n.dkv;
         const unsigned grid = place_groups(a);
-        constexpr int TWO = sizeof(T) == 4 && D > 32 ? 2 : 1;
-        if (key_halves == TWO) {
-            if (a.vec) k_attention_dkv<T, D, true, TWO><<<grid, 256, 0, st>>>(a);
-            else k_attention_dkv<T, D, false, TWO><<<grid, 256, 0, st>>>(a);
-        } else {
-            if (a.vec) k_attention_dkv<T, D, true, 1><<<grid, 256, 0, st>>>(a);
-            else k_attention_dkv<T, D, false, 1><<<grid, 256, 0, st>>>(a);
-        }
+        if (a.vec) k_attention_dkv<T, D, true, kKeyHalves<T, D>><<<grid, 256, 0, st>>>(a);
+        else k_attention_dkv<T, D, false, kKeyHalves<T, D>><<<grid, 256, 0, st>>>(a);
         if (n.dkv > 1) {
             const long long each = all * a.kv_len * D;
             k_attention_add<T, D, true><<<dim3((unsigned)ceil_div(all * a.kv_len, 1024 / D), 2), 256, 0, st>>>(a, 2 * each, n.dkv);
@@ -582,13 +574,13 @@ void attention_backward(const ftp_attention_shape& s, const void* dout, const vo
     a.vec = a.vec && near_rows(a.qs[2] * a.group / 128) && near_rows(a.gs[2] * a.group / 128);
     const Splits n = backward_splits(s);
     if (s.dtype == FTP_BF16) {
-        if (a.d <= 32) run<bf16_t, 32>(a, n, attention_halves(s), key_halves(s), st);
-        else if (a.d <= 64) run<bf16_t, 64>(a, n, attention_halves(s), key_halves(s), st);
-        else run<bf16_t, 128>(a, n, attention_halves(s), key_halves(s), st);
+        if (a.d <= 32) run<bf16_t, 32>(a, n, attention_halves(s), st);
+        else if (a.d <= 64) run<bf16_t, 64>(a, n, attention_halves(s), st);
+        else run<bf16_t, 128>(a, n, attention_halves(s), st);
     } else {
-        if (a.d <= 32) run<float, 32>(a, n, attention_halves(s), key_halves(s), st);
-        else if (a.d <= 64) run<float, 64>(a, n, attention_halves(s), key_halves(s), st);
-        else run<float, 128>(a, n, attention_halves(s), key_halves(s), st);
+        if (a.d <= 32) run<float, 32>(a, n, attention_halves(s), st);
+        else if (a.d <= 64) run<float, 64>(a, n, attention_halves(s), st);
+        else run<float, 128>(a, n, attention_halves(s), st);
     }
 }
 
