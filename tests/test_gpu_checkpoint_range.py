@@ -1,0 +1,52 @@
+"""Weight gradients from 8-bit checkpoints whose values lie at the ends of the range, against 64 bits.
+
+Bounds as for moderate numbers: products are exact, sums of n terms one after the other: (n + 8) 2^-24 sum|terms|."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+def _check(kept, dy, rows):
+    held = kept.unpack().double()
+    got = kept.wgrad(dy).double()
+    d = dy.double().t().contiguous()
+    want, terms = d @ held, d.abs() @ held.abs()
+    assert want.abs().max() < 2.0 ** 127
+    assert (got - want).abs().le((rows + 8) * 2.0 ** -24 * terms).all()
+    return got
+
+
+# 3 rows go one by one, 700 as whole stages; the columns are a tile's, and end inside a vector
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows", [3, 700])
+@pytest.mark.parametrize("cols,n", [(160, 24), (157, 9)])
+def test_blocks_of_the_largest_numbers(rows, cols, n, dtype):
+    """Exponents 120, 121 and 122, whose 128 * 2^e is no finite number: zeros, small codes and the largest, rows of dy that are zero."""
+    from paper_2409_09083_amd import tokens
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.randn((rows, cols), generator=g, device="cuda")
+    top = float(torch.finfo(TYPES[dtype]).max)
+    for b, largest in enumerate((top, 2.0 ** 127, 2.0 ** 126, 2.0 ** 125)):
+        part = x[:, 32 * b:32 * b + 32]
+        part *= largest / 8
+        part.clamp_(-largest, largest)
+        part[:, 0], part[:, 1], part[::2, 2] = largest, -largest, 0.0
+    dy = torch.randn((rows, n), generator=g, device="cuda") * 2.0 ** -40
+    dy[::3] = 0
+    kept = tokens.Checkpoint(rows, cols, dtype, 32, outputs=n).pack(x.to(TYPES[dtype]))
+    assert {120, 121, 122} <= set(kept.exponents.unique().tolist())
+    _check(kept, dy.to(TYPES[dtype]), rows)
+
+
+@pytest.mark.parametrize("dtype,power", [("f32", -110), ("bf16", -110), ("bf16", -122)])
+@pytest.mark.parametrize("rows", [3, 700])
+def test_blocks_of_the_smallest_numbers(rows, dtype, power):
+    """Exponents down to -126, small codes among them."""
+    from paper_2409_09083_amd import tokens
+    g = torch.Generator(device="cuda").manual_seed(2)
+    x = torch.randn((rows, 96), generator=g, device="cuda") * 2.0 ** power
+    dy = torch.randn((rows, 24), generator=g, device="cuda") * 2.0 ** 60
+    kept = tokens.Checkpoint(rows, 96, dtype, 32, outputs=24).pack(x.to(TYPES[dtype]))
+    _check(kept, dy.to(TYPES[dtype]), rows)
