@@ -295,8 +295,8 @@ int ftp_checkpoint_act_backward(const ftp_checkpoint_shape* shape, const int8_t*
 int ftp_checkpoint_workspace(const ftp_checkpoint_shape* shape, int32_t outputs, size_t* bytes);
 
 /* dw[n][k] = sum over rows of dy[row][n] * value[row][k], fp32 [outputs][cols]: the weight gradient of a linear layer whose
- * input was kept.  dy: [rows][outputs] with `dy_stride` elements between rows (shape->stride is not used); fp32 numbers of dy above 2^104, and
- * infinities, give NaN. */
+ * input was kept.  dy: [rows][outputs] with `dy_stride` elements between rows (shape->stride is not used); fp32 numbers of dy above 2^116, and
+ * infinities, give NaN.  fp32: dy below 2^-122 and held values below 2^-114 lose low bits. */
 int ftp_checkpoint_wgrad(const ftp_checkpoint_shape* shape, const int8_t* codes, const int8_t* exponents, const void* dy,
                          int64_t dy_stride, int32_t outputs, float* dw, void* workspace, void* stream);
 

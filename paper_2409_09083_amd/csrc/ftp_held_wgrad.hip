@@ -30,9 +30,12 @@ struct HeldWgradArgs {
 
 template <typename T> constexpr int kStage = sizeof(T) == 4 ? 32 : 64;       // rows of a stage
 constexpr int kBlk = 128;                           // columns of either operand a workgroup takes
-// Held values go into the products at a quarter of their size: 128 * 2^e, which their conversion subtracts, is no finite number at the largest exponents 121 and 122.  (Subtracting
-// 128 before the scale needs one instruction a value more: 80 -> 83 us for 46208 rows, 512 -> 1024, bfloats.)
-constexpr float kHeldPart = 0.25f;
+// Held values go into the products at a part of their size: 128 * 2^e, which their conversion subtracts, is no finite number at the largest exponents 121 and 122.  (Subtracting
+// 128 before the scale needs one instruction a value more: 80 -> 83 us for 46208 rows, 512 -> 1024, bfloats.)  With bfloats a quarter, made good at the end.  fp32 dy is split at
+// as many times its size, so that sums are neither larger nor smaller than the result; 2^12 leaves the low bits of numbers down to 2^-122 in their lowest plane (ftp_split.h), and those of held
+// values down to 2^-114 (at 2^24, as other kernels split, results above 2^104 would be infinite, or small held values lose as much more).
+template <typename T> constexpr float kHeldPart = sizeof(T) == 4 ? 1.0f / 4096.0f : 0.25f;
+template <typename T> constexpr float kDyTimes = sizeof(T) == 4 ? 4096.0f : 1.0f;
 
 // Byte offset of 8 columns (chunk) of a row of a [row][128] bfloat tile.  The chunk is exchanged so that 4 consecutive rows' equal chunks lie in different quarters of the
 // 64 banks (a transposing load reads 4 rows x 64 bytes a half wavefront).
@@ -122,15 +125,15 @@ __global__ __launch_bounds__(256, 2) void k_held_wgrad(const HeldWgradArgs a)
             } else {
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
-                    split3(there ? x.d[i].get(2 * j) * kSplitScale : 0.0f, there ? x.d[i].get(2 * j + 1) * kSplitScale : 0.0f, q[j], q[4 + j], q[8 + j]);
+                    split3(there ? x.d[i].get(2 * j) * kDyTimes<T> : 0.0f, there ? x.d[i].get(2 * j + 1) * kDyTimes<T> : 0.0f, q[j], q[4 + j], q[8 + j]);
             }
 #pragma unroll
             for (int s = 0; s < P; ++s) *(uint4*)(t + s * kTile + tile_at(drow + 16 * i, dcol >> 3)) = w[s];
         }
 #pragma unroll
         for (int i = 0; i < CR; ++i) {
-            // q * 2^e / 4 = (q + 128) * 2^(e - 2) - 128 * 2^(e - 2), exact; q + 128 as an unsigned byte takes one conversion from where it lies
-            const float unit = all || crow + 32 * i < left ? held_scale(x.e[i]) * kHeldPart : 0.0f, less = -128.0f * unit;
+            // a part of q * 2^e = (q + 128) * unit - 128 * unit, exact; q + 128 as an unsigned byte takes one conversion from where it lies
+            const float unit = all || crow + 32 * i < left ? held_scale(x.e[i]) * kHeldPart<T> : 0.0f, less = -128.0f * unit;
             uint4 w[2];
             uint32_t* q = (uint32_t*)w;
             const uint32_t c[4] = {x.c[i].x ^ 0x80808080u, x.c[i].y ^ 0x80808080u, x.c[i].z ^ 0x80808080u, x.c[i].w ^ 0x80808080u};
@@ -200,7 +203,7 @@ __global__ __launch_bounds__(256, 2) void k_held_wgrad(const HeldWgradArgs a)
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 const int n = n0 + wn + 32 * i + 8 * (r >> 2) + 4 * (l >> 5) + (r & 3);
-                if (n < a.N && k < a.K) out[(long long)n * a.K + k] = acc[i][j][r] * (P == 3 ? 1.0f / (kSplitScale * kHeldPart) : 1.0f / kHeldPart);
+                if (n < a.N && k < a.K) out[(long long)n * a.K + k] = acc[i][j][r] * (1.0f / (kDyTimes<T> * kHeldPart<T>));
             }
         }
 }

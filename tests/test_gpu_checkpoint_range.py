@@ -50,3 +50,27 @@ def test_blocks_of_the_smallest_numbers(rows, dtype, power):
     dy = torch.randn((rows, 24), generator=g, device="cuda") * 2.0 ** 60
     kept = tokens.Checkpoint(rows, 96, dtype, 32, outputs=24).pack(x.to(TYPES[dtype]))
     _check(kept, dy.to(TYPES[dtype]), rows)
+
+
+@pytest.mark.parametrize("rows", [3, 300])
+def test_large_sums_of_fp32(rows):
+    """Results up to the largest fp32 number, of moderate dy and of moderate values."""
+    from paper_2409_09083_amd import tokens
+    for value, d in ((1e35 / rows, 1.0), (1.0, 1e30), (3e5, 1e29), (2.0 ** 126 / rows, 1.0)):
+        x = torch.linspace(-1, 1, 64, device="cuda").repeat(rows, 1) * value
+        x[:, 5] = value
+        dy = torch.full((rows, 16), d, device="cuda")
+        dy[:, 3] *= -0.5
+        kept = tokens.Checkpoint(rows, 64, "f32", 32, outputs=16).pack(x)
+        got = _check(kept, dy, rows)
+        assert got.isfinite().all()
+
+
+@pytest.mark.parametrize("power", [-100, -60, 0, 60])
+def test_low_bits_of_fp32_at_any_size(power):
+    """1 + 2^-23 against whole codes comes out exact, whatever the codes' exponent."""
+    from paper_2409_09083_amd import tokens
+    kept = tokens.Checkpoint(64, 32, "f32", 32, outputs=32).pack(torch.eye(64, 32, device="cuda") * 64 * 2.0 ** power)
+    for size in (1.0, 2.0 ** -20):
+        dy = (1 + torch.arange(64 * 32, device="cuda").view(64, 32).float() * 2.0 ** -23) * size
+        assert torch.equal(kept.wgrad(dy), dy[:32].t() * 64 * 2.0 ** power)
