@@ -264,8 +264,8 @@ __device__ __forceinline__ void overlap(LoadA load_a, MmaA mma_a, Valu valu, Loa
     });
 }
 
-// Scores of hidden pairs start from this instead of 0: their exponential is 0, whatever is added.
-constexpr float kHidden = -3e38f;
+// The score that replaces a hidden pair's, whatever that came out as: its exponential is 0.
+constexpr float kHidden = -INFINITY;
 
 // Workgroups a CU that the register budget is set for: two (all sums and operands in 256 registers) where they fit.
 template <typename T, int D> constexpr int kPerCu = sizeof(T) == 4 && D == 128 ? 1 : 2;

@@ -70,25 +70,27 @@ __global__ __launch_bounds__(256, (kPerCu<T, D>)) void k_attention(const Attenti
     const auto step = [&](int t, Keys& now, Keys& next) __attribute__((always_inline)) {
         if (t + 1 < hi) fetch(t + 1, next);
         f32x16 s[UNITS] = {};
+#pragma unroll
+        for (int u = 0; u < UNITS; ++u)
+#pragma unroll
+            for (int c = 0; c < KS; ++c) s[u] = mma(L::along(now.tile[0], mine0 + 32 * u, c), q[c], s[u]);
         if ((t + 1) * BN > common) {
             const int left = seen - t * BN - mine0 - 4 * h;            // keys of the tile that the row sees, counted from this lane's first
 #pragma unroll
             for (int u = 0; u < UNITS; ++u)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) s[u][r] = 32 * u + 8 * (r >> 2) + (r & 3) >= left ? kHidden : 0.0f;
+                for (int r = 0; r < 16; ++r) s[u][r] = 32 * u + 8 * (r >> 2) + (r & 3) >= left ? kHidden : s[u][r];
         }
         float top = kHidden;
 #pragma unroll
-        for (int u = 0; u < UNITS; ++u) {
-#pragma unroll
-            for (int c = 0; c < KS; ++c) s[u] = mma(L::along(now.tile[0], mine0 + 32 * u, c), q[c], s[u]);
+        for (int u = 0; u < UNITS; ++u)
 #pragma unroll
             for (int r = 0; r < 16; ++r) top = fmaxf(top, s[u][r]);
-        }
         top = both_max(top) * a.c;
-        // the reference only has to keep the powers in range: it follows the maximum once that is 2^8 ahead (exact all the same: sums and rows share it)
+        // the reference only has to keep the powers in range: it follows the maximum once that is 2^8 ahead (exact all the same: sums and rows share it), and only then, so
+        // that a row's bits do not go by its neighbours'
         if (__any(top > m + 8.0f)) {
-            top = fmaxf(m, top);
+            top = top > m + 8.0f ? top : m;
             const float f = __builtin_amdgcn_exp2f(m - top);
             sum *= f;
 #pragma unroll

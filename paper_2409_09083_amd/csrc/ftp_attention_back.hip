@@ -86,15 +86,19 @@ __global__ __launch_bounds__(256, (kPerCu<T, D>)) void k_attention_dq(const Atte
             f32x16 s = {}, p;
 #pragma unroll
             for (int r = 0; r < 16; ++r) p[r] = few ? 0.0f : -delta;
-            if (t * BN + mine0 + 32 * u + 32 > common) {
-                const int left = seen - t * BN - mine0 - 32 * u - 4 * h;       // keys of the unit that the row sees, counted from this lane's first
-#pragma unroll
-                for (int r = 0; r < 16; ++r) s[r] = 8 * (r >> 2) + (r & 3) >= left ? kHidden : 0.0f;
-            }
 #pragma unroll
             for (int c = 0; c < KS; ++c) {
                 s = mma(L::along(now.tile[0], mine0 + 32 * u, c), q[c], s);
                 p = mma(L::along(now.tile[1], mine0 + 32 * u, c), g[c], p);
+            }
+            if (t * BN + mine0 + 32 * u + 32 > common) {
+                const int left = seen - t * BN - mine0 - 32 * u - 4 * h;       // keys of the unit that the row sees, counted from this lane's first
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const bool hidden = 8 * (r >> 2) + (r & 3) >= left;
+                    s[r] = hidden ? kHidden : s[r];
+                    p[r] = hidden ? 0.0f : p[r];
+                }
             }
 #pragma unroll
             for (int r = 0; r < 16; ++r) p[r] *= __builtin_amdgcn_exp2f(fmaf(s[r], a.c, -lse));
@@ -277,19 +281,26 @@ __global__ __launch_bounds__(256, (D == 128 || sizeof(T) == 4 ? 1 : 2)) void k_a
         __syncthreads();
     };
     f32x16 dk[DT] = {}, dv[DT] = {};
-    // the sums that S and dP - delta of rows u .. u + 31 of a tile start from; hide: some row does not see all of the wavefront's keys
-    const auto start = [&](const Rows& at, int u, bool hide, f32x16& s, f32x16& p) __attribute__((always_inline)) {
+    // the sums that S and dP - delta of rows u .. u + 31 of a tile start from
+    const auto start = [&](const Rows& at, int u, f32x16& s, f32x16& p) __attribute__((always_inline)) {
 #pragma unroll
         for (int r = 0; r < 16; r += 4) {
             const f32x4 less = *(const f32x4*)&at.less[u + 8 * (r >> 2) + 4 * h];
 #pragma unroll
             for (int j = 0; j < 4; ++j) { s[r + j] = 0; p[r + j] = less[j]; }
         }
-        if (hide) {
+    };
+    // pairs of those rows with keys that they do not see: probability and gradient 0, whatever the row's log-sum and delta are
+    const auto hide = [&](const Rows& at, int u, f32x16& s, f32x16& p, f32x4 (&lse)[4]) __attribute__((always_inline)) {
 #pragma unroll
-            for (int r = 0; r < 16; ++r) s[r] = key >= at.seen[u + 8 * (r >> 2) + 4 * h + (r & 3)] ? kHidden : 0.0f;
+        for (int r = 0; r < 16; ++r) {
+            const bool hidden = key >= at.seen[u + 8 * (r >> 2) + 4 * h + (r & 3)];
+            s[r] = hidden ? kHidden : s[r];
+            p[r] = hidden ? 0.0f : p[r];
+            lse[r >> 2][r & 3] = hidden ? 0.0f : lse[r >> 2][r & 3];
         }
     };
+    // whether some row of the tile does not see all of the wavefront's keys
     const auto hides = [&](int t) { return a.causal && len.seen(a, first_query(t)) < mine + 32; };     // (a tile's first row sees the fewest keys)
     if constexpr (HALVES == 2) {
         static_assert(UNITS == 1, "a tile is a unit");
@@ -299,7 +310,7 @@ __global__ __launch_bounds__(256, (D == 128 || sizeof(T) == 4 ? 1 : 2)) void k_a
             if (t + 1 < hi) fetch(t + 1, next);
             f32x16 s = {}, p = {};
             if (any) {
-                if (half == 0) start(now, 0, hides(t), s, p);
+                if (half == 0) start(now, 0, s, p);
 #pragma unroll
                 for (int c = 0; c < KS; ++c) {
                     s = mma(L::along(now.tile[0], 0, half * KS + c), k[c], s);
@@ -313,14 +324,19 @@ __global__ __launch_bounds__(256, (D == 128 || sizeof(T) == 4 ? 1 : 2)) void k_a
             }
             __syncthreads();                        // (and nobody reads the tile before this any more)
             if (any) {
+                f32x4 lse[4];
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const f32x4 s2 = parts[wave ^ 2][r][l], p2 = parts[wave ^ 2][4 + r][l], lse = *(const f32x4*)&now.lse[8 * r + 4 * h];
+                    const f32x4 s2 = parts[wave ^ 2][r][l], p2 = parts[wave ^ 2][4 + r][l];
+                    lse[r] = *(const f32x4*)&now.lse[8 * r + 4 * h];
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        s[4 * r + j] = __builtin_amdgcn_exp2f(fmaf(s[4 * r + j] + s2[j], a.c, -lse[j]));
-                        p[4 * r + j] = (p[4 * r + j] + p2[j]) * s[4 * r + j];
-                    }
+                    for (int j = 0; j < 4; ++j) { s[4 * r + j] += s2[j]; p[4 * r + j] += p2[j]; }
+                }
+                if (hides(t)) hide(now, 0, s, p, lse);
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], a.c, -lse[r >> 2][r & 3]));
+                    p[r] *= s[r];
                 }
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
@@ -345,13 +361,14 @@ __global__ __launch_bounds__(256, (D == 128 || sizeof(T) == 4 ? 1 : 2)) void k_a
     } else {
         __shared__ __align__(16) Rows r2;               // (a third)
         // this unit's probabilities and products (rows u .. of `now`), and the scores of the next one (rows w .. of `next`)
-        const auto unit = [&](const Rows& now, int u, const Rows& next, int w, bool hide, f32x16& s, f32x16& p, f32x16& s2, f32x16& p2) __attribute__((always_inline)) {
+        const auto unit = [&](const Rows& now, int u, const Rows& next, int w, bool some_hidden, f32x16& s, f32x16& p, f32x16& s2, f32x16& p2) __attribute__((always_inline)) {
             Frag fa[2 * KS], fc[2][2 * DT];
             Words<T> ws, we;
             f32x4 lse[4];
     #pragma unroll
             for (int r = 0; r < 4; ++r) lse[r] = *(const f32x4*)&now.lse[u + 8 * r + 4 * h];
-            start(next, w, hide, s2, p2);
+            if (some_hidden) hide(now, u, s, p, lse);
+            start(next, w, s2, p2);
             overlap<2 * KS, 2 * DT>(
                 [&](int i) __attribute__((always_inline)) { fa[i] = L::along(next.tile[i & 1], w, i >> 1); },
                 [&](int i) __attribute__((always_inline)) {
@@ -384,16 +401,16 @@ __global__ __launch_bounds__(256, (D == 128 || sizeof(T) == 4 ? 1 : 2)) void k_a
                 }
                 const Rows& then = end ? next : now;
                 const int w = end ? 0 : 32 * (n + 1);
-                const bool hide = hides(end ? t + 1 : t), flip = UNITS == 1 ? odd : n & 1;
-                if (flip) unit(now, 32 * n, then, w, hide, s1, p1, s0, p0);
-                else unit(now, 32 * n, then, w, hide, s0, p0, s1, p1);
+                const bool some_hidden = hides(t), flip = UNITS == 1 ? odd : n & 1;
+                if (flip) unit(now, 32 * n, then, w, some_hidden, s1, p1, s0, p0);
+                else unit(now, 32 * n, then, w, some_hidden, s0, p0, s1, p1);
             }
         };
         if (lo < hi) {
             fetch(lo, r0);
             land(r0);
             if (lo + 1 < hi) fetch(lo + 1, r1);
-            start(r0, 0, hides(lo), s0, p0);
+            start(r0, 0, s0, p0);
     #pragma unroll
             for (int c = 0; c < KS; ++c) {
                 s0 = mma(L::along(r0.tile[0], 0, c), k[c], s0);
