@@ -65,7 +65,7 @@ __global__ __launch_bounds__(256, (kPerCu<T, D>)) void k_attention(const Attenti
     };
 
     f32x16 o[DT] = {};
-    const float nothing = -1e30f * a.c;             // the reference of a row that has seen no key
+    constexpr float nothing = -3e38f;               // the reference of a row that has seen no key: below all scores, and a number
     float m = nothing, sum = 0;
     const auto step = [&](int t, Keys& now, Keys& next) __attribute__((always_inline)) {
         if (t + 1 < hi) fetch(t + 1, next);
@@ -286,7 +286,7 @@ AttentionArgs attention_args(const ftp_attention_shape& s)
     a.batch = s.batch; a.heads = s.heads; a.kv = s.kv_heads; a.group = s.heads / s.kv_heads;
     a.q_len = s.q_len; a.kv_len = s.kv_len; a.d = s.head_dim; a.causal = s.causal;
     a.scale = s.scale;
-    a.c = std::max(std::fabs(s.scale) * kLog2e, 1e-30f);             // (0 would make NaN of a hidden score, -infinity)
+    a.c = std::max(std::fabs(s.scale) * kLog2e, 1e-45f);             // (0 would make NaN of a hidden score, -infinity; this leaves 5e-7 of the largest one)
     return a;
 }
 
