@@ -306,7 +306,7 @@ int ftp_checkpoint_wgrad(const ftp_checkpoint_shape* shape, const int8_t* codes,
  * j <= i + kv_lens[b] - q_lens[b] (the last query sees the last key).  A query that sees no key, and one beyond
  * q_lens[b], has out = 0, lse = -infinity and dq = 0; a key that no query sees has dk = dv = 0; a query that sees one key has probability 1
  * there and dq = 0, exactly.  Keys, values and queries that are not seen do not reach any result, whatever they hold (causal calls with such values that
- * are not finite take long).  fp32 numbers are multiplied as three bfloats each: a seen infinity, or number above the largest bfloat, gives NaN.
+ * are not finite may take a second walk over the keys).  fp32 numbers are multiplied as three bfloats each: a seen infinity, or number above the largest bfloat, gives NaN.
  * Element (b, t, h, c) of q lies at q_stride[0] * b + q_stride[1] * t + q_stride[2] * h + c; likewise the others.  Inputs may
  * be broadcast (stride 0); gradients then come out unsummed, in buffers of their own.  q_len and kv_len may be 0. */
 typedef struct {

@@ -67,8 +67,8 @@ __global__ __launch_bounds__(256, (kPerCu<T, D>)) void k_attention(const Attenti
     f32x16 o[DT] = {};
     constexpr float nothing = -3e38f;               // the reference of a row that has seen no key: below all scores, and a number
     float m = nothing, sum = 0;
-    const auto step = [&](int t, Keys& now, Keys& next) __attribute__((always_inline)) {
-        if (t + 1 < hi) fetch(t + 1, next);
+    const auto step = [&](int t, int to, int seen, Keys& now, Keys& next) __attribute__((always_inline)) {
+        if (t + 1 < to) fetch(t + 1, next);
         f32x16 s[UNITS] = {};
 #pragma unroll
         for (int u = 0; u < UNITS; ++u)
@@ -113,86 +113,104 @@ __global__ __launch_bounds__(256, (kPerCu<T, D>)) void k_attention(const Attenti
                 for (int d = 0; d < DT; ++d) o[d] = mma(L::across(now.tile[1], mine0 + 32 * u + 16 * c, 32 * d), p, o[d]);
             }
         }
-        if (t + 1 < hi) land(next);
+        if (t + 1 < to) land(next);
     };
-    if (lo < hi) {
-        fetch(lo, even);
-        land(even);
-    }
-    for (int t = lo; t < hi; t += 2) {
-        step(t, even, odd);
-        if (t + 1 < hi) step(t + 1, odd, even);
-    }
-    if (a.causal && __any(not_finite(o) || !(sum < INFINITY))) {
-        const int row = again(first + at0 + (l & 31)), i = query_of(a, row), head = kvh * a.group + row - i * a.group;      // (not worth registers before)
-        const T* qr = (const T*)a.q + b * a.qs[0] + i * a.qs[1] + head * a.qs[2];
-        const auto other = [&](int key) { return HALVES == 2 && ((key >> 5) & 1) != half; };
-        if (both_max(not_finite(o) || !(sum < INFINITY) ? 1.0f : 0.0f) > 0) {
-            const auto score = [&](int key) { const float s = dot_of(qr, kp + key * a.ks[1], a.d); return (a.scale < 0 ? -s : s) * a.c; };
-#pragma unroll
-            for (int d = 0; d < DT; ++d) o[d] = f32x16{};
-            m = nothing;
-            sum = 0;
-            for (int key = lo * BN; key < min(hi * BN, seen); ++key) if (!other(key)) m = fmaxf(m, score(key));
-            for (int key = lo * BN; key < min(hi * BN, seen); ++key) {
-                if (other(key)) continue;
-                const float p = __builtin_amdgcn_exp2f(score(key) - m);
-                add_row<T, DT>(o, p, vp + key * a.vs[1], a.d);
-                sum += h ? 0.0f : p;
-            }
+    const auto walk = [&](int to, int seen) __attribute__((always_inline)) {
+        if (lo < to) {
+            fetch(lo, even);
+            land(even);
         }
-    }
-    sum = both_sum(sum);
-    if constexpr (HALVES == 2) {
-        // (the tiles' last readers are behind a barrier: a wavefront leaves the loop's last tile by itself, so one more)
-        f32x4* part = (f32x4*)&even + (at0 / 32) * DT * 4 * 64;
-        float* stats = (float*)&odd + (at0 / 32) * 128;
-        __syncthreads();
-        if (half) {
+        for (int t = lo; t < to; t += 2) {
+            step(t, to, seen, even, odd);
+            if (t + 1 < to) step(t + 1, to, seen, odd, even);
+        }
+    };
+    // two wavefronts' rows and sums become the first one's
+    const auto join = [&]() __attribute__((always_inline)) {
+        if constexpr (HALVES == 2) {
+            // (the tiles' last readers are behind a barrier: a wavefront leaves the loop's last tile by itself, so one more)
+            f32x4* part = (f32x4*)&even + (at0 / 32) * DT * 4 * 64;
+            float* stats = (float*)&odd + (at0 / 32) * 128;
+            __syncthreads();
+            if (half) {
+#pragma unroll
+                for (int d = 0; d < DT; ++d)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) part[(d * 4 + r) * 64 + l] = f32x4{o[d][4 * r], o[d][4 * r + 1], o[d][4 * r + 2], o[d][4 * r + 3]};
+                stats[l] = m;
+                stats[64 + l] = sum;
+            }
+            __syncthreads();
+            if (half) return;
+            const float m2 = stats[l], top = fmaxf(m, m2), f = __builtin_amdgcn_exp2f(m - top), f2 = __builtin_amdgcn_exp2f(m2 - top);
+            sum = sum * f + stats[64 + l] * f2;
+            m = top;
 #pragma unroll
             for (int d = 0; d < DT; ++d)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) part[(d * 4 + r) * 64 + l] = f32x4{o[d][4 * r], o[d][4 * r + 1], o[d][4 * r + 2], o[d][4 * r + 3]};
-            stats[l] = m;
-            stats[64 + l] = sum;
+                for (int r = 0; r < 4; ++r) {
+                    const f32x4 v = part[(d * 4 + r) * 64 + l];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) o[d][4 * r + j] = o[d][4 * r + j] * f + v[j] * f2;
+                }
         }
-        __syncthreads();
-        if (half) return;
-        const float m2 = stats[l], top = fmaxf(m, m2), f = __builtin_amdgcn_exp2f(m - top), f2 = __builtin_amdgcn_exp2f(m2 - top);
-        sum = sum * f + stats[64 + l] * f2;
-        m = top;
+    };
+    const auto store = [&](int row, int seen, float sum, bool stats) __attribute__((always_inline)) {
+        const int i = query_of(a, row), head = kvh * a.group + row - i * a.group;
+        if (a.splits > 1) {
+            // [split][image][key head][row][D], and the rows' maxima and sums behind
+            const long long at = (((long long)split * a.batch + b) * a.kv + kvh) * rows + row, n = (long long)a.splits * a.batch * a.kv * rows;
+            float* p = a.ws + at * D;
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int r = 0; r < 16; r += 4)
+                    *(f32x4*)(p + 32 * d + 8 * (r >> 2) + 4 * h) = f32x4{o[d][r], o[d][r + 1], o[d][r + 2], o[d][r + 3]};
+            if (h == 0 && stats) { a.ws[n * D + 2 * at] = m; a.ws[n * D + 2 * at + 1] = sum; }
+            return;
+        }
+        const float inv = seen ? 1.0f / sum : 0.0f;
+        T* p = (T*)a.out + b * a.os[0] + i * a.os[1] + head * a.os[2];
 #pragma unroll
         for (int d = 0; d < DT; ++d)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const f32x4 v = part[(d * 4 + r) * 64 + l];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) o[d][4 * r + j] = o[d][4 * r + j] * f + v[j] * f2;
+            for (int r = 0; r < 16; r += 4) {
+                const f32x4 v = seen ? f32x4{o[d][r] * inv, o[d][r + 1] * inv, o[d][r + 2] * inv, o[d][r + 3] * inv} : f32x4{0, 0, 0, 0};
+                store4(p, 32 * d + 8 * (r >> 2) + 4 * h, a.d, a.vec, v[0], v[1], v[2], v[3]);
             }
-    }
-    if (!inside) return;
-    if (a.splits > 1) {
-        // [split][image][key head][row][D], and the rows' maxima and sums behind
-        const long long at = (((long long)split * a.batch + b) * a.kv + kvh) * rows + row, n = (long long)a.splits * a.batch * a.kv * rows;
-        float* p = a.ws + at * D;
+        if (h == 0 && a.lse && stats) a.lse[((long long)b * a.heads + head) * a.q_len + i] = seen ? fmaf(m, kLn2, logf(sum)) : -INFINITY;
+    };
+    walk(hi, seen);
+    sum = both_sum(sum);
+    join();
+    if (!half && inside) store(row, seen, sum, true);
+    if (!a.causal) return;
+    // A second look at rows whose values, but not their scores, spoiled them: the maxima and sums stand.
+    {
+        const unsigned long long spoiled = bad_channels(o);
+        bool go = !half && inside && sum < INFINITY && both_max(spoiled ? 1.0f : 0.0f) > 0;
+        if (!__syncthreads_or(go)) return;
+        const int to = min(hi, common / BN), key0 = max(lo, to) * BN, key1 = min(hi * BN, end);
+        if (!__syncthreads_or(find_bad<T>(min(hi * BN, len.k) - key0, a.d, [&](int r) { return vp + (key0 + r) * a.vs[1]; }))) return;       // (of whole tiles)
+        const int row = again(first + at0 + (l & 31)), i = query_of(a, row), head = kvh * a.group + row - i * a.group;      // (not worth registers before)
+        const int seen = row < rows ? len.seen(a, i) : 0;
+        const T* qr = (const T*)a.q + b * a.qs[0] + i * a.qs[1] + head * a.qs[2];
 #pragma unroll
-        for (int d = 0; d < DT; ++d)
-#pragma unroll
-            for (int r = 0; r < 16; r += 4)
-                *(f32x4*)(p + 32 * d + 8 * (r >> 2) + 4 * h) = f32x4{o[d][r], o[d][r + 1], o[d][r + 2], o[d][r + 3]};
-        if (h == 0) { a.ws[n * D + 2 * at] = m; a.ws[n * D + 2 * at + 1] = sum; }
-        return;
-    }
-    const float inv = seen ? 1.0f / sum : 0.0f;
-    T* p = (T*)a.out + b * a.os[0] + i * a.os[1] + head * a.os[2];
-#pragma unroll
-    for (int d = 0; d < DT; ++d)
-#pragma unroll
-        for (int r = 0; r < 16; r += 4) {
-            const f32x4 v = seen ? f32x4{o[d][r] * inv, o[d][r + 1] * inv, o[d][r + 2] * inv, o[d][r + 3] * inv} : f32x4{0, 0, 0, 0};
-            store4(p, 32 * d + 8 * (r >> 2) + 4 * h, a.d, a.vec, v[0], v[1], v[2], v[3]);
+        for (int d = 0; d < DT; ++d) o[d] = f32x16{};
+        for (int key = key0; key < key1 && __any(go); ++key) {
+            if (go && key < seen) {
+                const float s = dot_of(qr, kp + key * a.ks[1], a.d);
+                add_row<T, DT>(o, __builtin_amdgcn_exp2f(fmaf(a.scale < 0 ? -s : s, a.c, -m)), vp + key * a.vs[1], a.d);
+            }
+            go = go && both_max(spoiled & ~bad_channels(o) ? 1.0f : 0.0f) > 0;
         }
-    if (h == 0 && a.lse) a.lse[((long long)b * a.heads + head) * a.q_len + i] = seen ? fmaf(m, kLn2, logf(sum)) : -INFINITY;
+        if (!__syncthreads_or(go)) return;
+        const float total = sum;
+        row_operands<T, D>(q, seen ? qr : nullptr, a.d, VEC, a.scale < 0);
+        walk(to, seen);
+        join();
+        if (go) store(row, seen, total, false);
+    }
 }
 
 // Joins the splits of a row: D / 4 lanes with four channels each, GROUPS of them with every GROUPS-th split.  Few rows have a workgroup each, so that all loads are on their way at
@@ -284,7 +302,7 @@ AttentionArgs attention_args(const ftp_attention_shape& s)
         a.gs[i] = s.dout_stride[i]; a.dqs[i] = s.dq_stride[i]; a.dks[i] = s.dk_stride[i]; a.dvs[i] = s.dv_stride[i];
     }
     a.batch = s.batch; a.heads = s.heads; a.kv = s.kv_heads; a.group = s.heads / s.kv_heads;
-    a.q_len = s.q_len; a.kv_len = s.kv_len; a.d = s.head_dim; a.causal = s.causal;
+    a.q_len = s.q_len; a.kv_len = s.kv_len; a.d = s.head_dim; a.causal = s.causal && s.q_len > 1;             // (one query sees all keys)
     a.scale = s.scale;
     a.c = std::max(std::fabs(s.scale) * kLog2e, 1e-45f);             // (0 would make NaN of a hidden score, -infinity; this leaves 5e-7 of the largest one)
     return a;

@@ -79,8 +79,8 @@ __global__ __launch_bounds__(256, (kPerCu<T, D>)) void k_attention_dq(const Atte
     f32x16 dq[DT] = {};
     float exact = 0;
     // few: only the row's delta, of p and dP themselves
-    const auto step = [&](int t, Keys& now, Keys& next, auto few) __attribute__((always_inline)) {
-        if (t + 1 < hi) fetch(t + 1, next);
+    const auto step = [&](int t, int to, int seen, Keys& now, Keys& next, auto few) __attribute__((always_inline)) {
+        if (t + 1 < to) fetch(t + 1, next);
 #pragma unroll
         for (int u = 0; u < UNITS; ++u) {
             f32x16 s = {}, p;
@@ -114,23 +114,23 @@ __global__ __launch_bounds__(256, (kPerCu<T, D>)) void k_attention_dq(const Atte
                 }
             }
         }
-        if (t + 1 < hi) land(next);
+        if (t + 1 < to) land(next);
         else if constexpr (few) __syncthreads();    // (the second walk starts with the same tiles)
     };
-    const auto walk = [&](auto few) __attribute__((always_inline)) {
-        if (lo < hi) {
+    const auto walk = [&](int to, int seen, auto few) __attribute__((always_inline)) {
+        if (lo < to) {
             fetch(lo, even);
             land(even);
         }
-        for (int t = lo; t < hi; t += 2) {
-            step(t, even, odd, few);
-            if (t + 1 < hi) step(t + 1, odd, even, few);
+        for (int t = lo; t < to; t += 2) {
+            step(t, to, seen, even, odd, few);
+            if (t + 1 < to) step(t + 1, to, seen, odd, even, few);
         }
     };
     // Where rows see few keys the rounding of out shows in delta (the products' rounding averages out with the keys, this does not): bfloat rows of up to 256 keys
     // take delta from p and dP, in a walk before (40 tokens: dk and dq 0.0027 -> 0.0024 of their size away, 0.0017 of it the rounding of the results).
     if (sizeof(T) == 2 && a.splits == 1 && tiles * BN <= 256) {
-        walk(std::true_type{});
+        walk(hi, seen, std::true_type{});
         exact = both_sum(exact);
         if constexpr (HALVES == 2) {
             float* parts = (float*)&odd;            // (odd: the second walk starts with even)
@@ -138,64 +138,85 @@ __global__ __launch_bounds__(256, (kPerCu<T, D>)) void k_attention_dq(const Atte
             __syncthreads();
             exact = parts[at0 * 2 + l] + parts[128 + at0 * 2 + l];
         }
-        if (fabsf(exact) < INFINITY) delta = exact;            // (not where hidden values made it NaN)
+        delta = exact;
     }
     if (split == 0 && half == 0 && inside && h == 0) a.delta[at] = delta;
-    walk(std::false_type{});
-    if (a.causal && __any(not_finite(dq))) {
+    // two wavefronts' rows become the first one's
+    const auto join = [&]() __attribute__((always_inline)) {
+        if constexpr (HALVES == 2) {
+            static_assert((int)sizeof(Keys) >= 2 * DT * 4096, "two wavefronts' rows in a tile's place");
+            f32x4* parts = (f32x4*)&even + (at0 / 32) * DT * 4 * 64;
+            __syncthreads();                        // (nobody reads tiles any more)
+            if (half) {
+#pragma unroll
+                for (int d = 0; d < DT; ++d)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) parts[(d * 4 + r) * 64 + l] = f32x4{dq[d][4 * r], dq[d][4 * r + 1], dq[d][4 * r + 2], dq[d][4 * r + 3]};
+            }
+            __syncthreads();
+            if (half) return;
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const f32x4 v = parts[(d * 4 + r) * 64 + l];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) dq[d][4 * r + j] += v[j];
+                }
+        }
+    };
+    const auto store = [&](int row, int seen) __attribute__((always_inline)) {
+        if (a.splits > 1) {
+            float* p = a.ws + (((long long)split * a.batch * a.kv * rows) + (((long long)b * a.kv + kvh) * a.q_len) * a.group + row) * D;
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int r = 0; r < 16; r += 4)
+                    *(f32x4*)(p + 32 * d + 8 * (r >> 2) + 4 * h) = f32x4{dq[d][r], dq[d][r + 1], dq[d][r + 2], dq[d][r + 3]};
+            return;
+        }
+        const int i = query_of(a, row), head = kvh * a.group + row - i * a.group;
+        T* p = (T*)a.dq + b * a.dqs[0] + i * a.dqs[1] + head * a.dqs[2];
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4) {
+                const f32x4 v = seen > 1 ? f32x4{dq[d][r], dq[d][r + 1], dq[d][r + 2], dq[d][r + 3]} * a.scale : f32x4{0, 0, 0, 0};      // (one key: probability 1, no gradient)
+                store4(p, 32 * d + 8 * (r >> 2) + 4 * h, a.d, a.vec, v[0], v[1], v[2], v[3]);
+            }
+    };
+    walk(hi, seen, std::false_type{});
+    join();
+    if (!half && inside) store(row, seen);
+    if (!a.causal) return;
+    // A second look at rows that are not spoiled by their own log-sum or delta.
+    {
+        const unsigned long long spoiled = bad_channels(dq);
+        bool go = !half && inside && fabsf(lse) < INFINITY && fabsf(delta) < INFINITY && both_max(spoiled ? 1.0f : 0.0f) > 0;
+        if (!__syncthreads_or(go)) return;
+        const int to = min(hi, common / BN), key0 = max(lo, to) * BN, key1 = min(hi * BN, end);
+        if (!__syncthreads_or(find_bad<T>(min(hi * BN, len.k) - key0, a.d, [&](int r) { return kp + (key0 + r) * a.ks[1]; }))) return;       // (of whole tiles)
         const int row = again(first + at0 + (l & 31)), i = query_of(a, row), head = kvh * a.group + row - i * a.group;      // (not worth registers before)
+        const int seen = row < rows ? len.seen(a, i) : 0;
         const T* qr = (const T*)a.q + b * a.qs[0] + i * a.qs[1] + head * a.qs[2];
         const T* gr = (const T*)a.dout + b * a.gs[0] + i * a.gs[1] + head * a.gs[2];
-        if (both_max(not_finite(dq) ? 1.0f : 0.0f) > 0) {
 #pragma unroll
-            for (int d = 0; d < DT; ++d) dq[d] = f32x16{};
-            for (int key = lo * BN; key < min(hi * BN, seen); ++key) {
-                if (HALVES == 2 && ((key >> 5) & 1) != half) continue;
+        for (int d = 0; d < DT; ++d) dq[d] = f32x16{};
+        for (int key = key0; key < key1 && __any(go); ++key) {
+            if (go && key < seen) {
                 const T* kr = kp + key * a.ks[1];
                 const float s = dot_of(qr, kr, a.d), p = __builtin_amdgcn_exp2f(fmaf(a.scale < 0 ? -s : s, a.c, -lse));
                 add_row<T, DT>(dq, p * (dot_of(gr, vp + key * a.vs[1], a.d) - delta), kr, a.d);
             }
+            go = go && both_max(spoiled & ~bad_channels(dq) ? 1.0f : 0.0f) > 0;
         }
+        if (!__syncthreads_or(go)) return;
+        row_operands<T, D>(q, seen ? qr : nullptr, a.d, VEC, a.scale < 0);
+        row_operands<T, D>(g, seen ? gr : nullptr, a.d, VEC, false);
+        walk(to, seen, std::false_type{});
+        join();
+        if (go) store(row, seen);
     }
-    if constexpr (HALVES == 2) {
-        static_assert((int)sizeof(Keys) >= 2 * DT * 4096, "two wavefronts' rows in a tile's place");
-        f32x4* parts = (f32x4*)&even + (at0 / 32) * DT * 4 * 64;
-        __syncthreads();                            // (nobody reads tiles any more)
-        if (half) {
-#pragma unroll
-            for (int d = 0; d < DT; ++d)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) parts[(d * 4 + r) * 64 + l] = f32x4{dq[d][4 * r], dq[d][4 * r + 1], dq[d][4 * r + 2], dq[d][4 * r + 3]};
-        }
-        __syncthreads();
-        if (half) return;
-#pragma unroll
-        for (int d = 0; d < DT; ++d)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const f32x4 v = parts[(d * 4 + r) * 64 + l];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) dq[d][4 * r + j] += v[j];
-            }
-    }
-    if (!inside) return;
-    if (a.splits > 1) {
-        float* p = a.ws + (((long long)split * a.batch * a.kv * rows) + at) * D;
-#pragma unroll
-        for (int d = 0; d < DT; ++d)
-#pragma unroll
-            for (int r = 0; r < 16; r += 4)
-                *(f32x4*)(p + 32 * d + 8 * (r >> 2) + 4 * h) = f32x4{dq[d][r], dq[d][r + 1], dq[d][r + 2], dq[d][r + 3]};
-        return;
-    }
-    T* p = (T*)a.dq + b * a.dqs[0] + i * a.dqs[1] + head * a.dqs[2];
-#pragma unroll
-    for (int d = 0; d < DT; ++d)
-#pragma unroll
-        for (int r = 0; r < 16; r += 4) {
-            const f32x4 v = seen > 1 ? f32x4{dq[d][r], dq[d][r + 1], dq[d][r + 2], dq[d][r + 3]} * a.scale : f32x4{0, 0, 0, 0};      // (one key: probability 1, no gradient)
-            store4(p, 32 * d + 8 * (r >> 2) + 4 * h, a.d, a.vec, v[0], v[1], v[2], v[3]);
-        }
 }
 
 template <typename T, int D> constexpr int kKeyHalves = sizeof(T) == 4 && D == 128 ? 2 : 1;        // wavefronts to a key (HALVES below)
@@ -302,180 +323,203 @@ __global__ __launch_bounds__(256, (D == 128 || sizeof(T) == 4 ? 1 : 2)) void k_a
     };
     // whether some row of the tile does not see all of the wavefront's keys
     const auto hides = [&](int t) { return a.causal && len.seen(a, first_query(t)) < mine + 32; };     // (a tile's first row sees the fewest keys)
-    if constexpr (HALVES == 2) {
-        static_assert(UNITS == 1, "a tile is a unit");
-        __shared__ __align__(16) f32x4 parts[4][8][64];         // of S and dP - delta, by wavefront
-        const bool any = mine < len.k;
-        const auto tile = [&](int t, Rows& now, Rows& next) __attribute__((always_inline)) {
-            if (t + 1 < hi) fetch(t + 1, next);
-            f32x16 s = {}, p = {};
-            if (any) {
-                if (half == 0) start(now, 0, s, p);
+    const auto walk = [&](int begin) __attribute__((always_inline)) {
+        if constexpr (HALVES == 2) {
+            static_assert(UNITS == 1, "a tile is a unit");
+            __shared__ __align__(16) f32x4 parts[4][8][64];         // of S and dP - delta, by wavefront
+            const bool any = mine < len.k;
+            const auto tile = [&](int t, Rows& now, Rows& next) __attribute__((always_inline)) {
+                if (t + 1 < hi) fetch(t + 1, next);
+                f32x16 s = {}, p = {};
+                if (any) {
+                    if (half == 0) start(now, 0, s, p);
 #pragma unroll
-                for (int c = 0; c < KS; ++c) {
-                    s = mma(L::along(now.tile[0], 0, half * KS + c), k[c], s);
-                    p = mma(L::along(now.tile[1], 0, half * KS + c), v[c], p);
-                }
+                    for (int c = 0; c < KS; ++c) {
+                        s = mma(L::along(now.tile[0], 0, half * KS + c), k[c], s);
+                        p = mma(L::along(now.tile[1], 0, half * KS + c), v[c], p);
+                    }
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    parts[wave][r][l] = f32x4{s[4 * r], s[4 * r + 1], s[4 * r + 2], s[4 * r + 3]};
-                    parts[wave][4 + r][l] = f32x4{p[4 * r], p[4 * r + 1], p[4 * r + 2], p[4 * r + 3]};
-                }
-            }
-            __syncthreads();                        // (and nobody reads the tile before this any more)
-            if (any) {
-                f32x4 lse[4];
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const f32x4 s2 = parts[wave ^ 2][r][l], p2 = parts[wave ^ 2][4 + r][l];
-                    lse[r] = *(const f32x4*)&now.lse[8 * r + 4 * h];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) { s[4 * r + j] += s2[j]; p[4 * r + j] += p2[j]; }
-                }
-                if (hides(t)) hide(now, 0, s, p, lse);
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], a.c, -lse[r >> 2][r & 3]));
-                    p[r] *= s[r];
-                }
-#pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    const Frag ps = operand<T>(s, c), ds = operand<T>(p, c);
-#pragma unroll
-                    for (int d = 0; d < DT; ++d) {
-                        dv[d] = mma(L::across(now.tile[1], 16 * c, c0 + 32 * d), ps, dv[d]);
-                        dk[d] = mma(L::across(now.tile[0], 16 * c, c0 + 32 * d), ds, dk[d]);
+                    for (int r = 0; r < 4; ++r) {
+                        parts[wave][r][l] = f32x4{s[4 * r], s[4 * r + 1], s[4 * r + 2], s[4 * r + 3]};
+                        parts[wave][4 + r][l] = f32x4{p[4 * r], p[4 * r + 1], p[4 * r + 2], p[4 * r + 3]};
                     }
                 }
-            }
-            if (t + 1 < hi) land(next);
-        };
-        if (lo < hi) {
-            fetch(lo, r0);
-            land(r0);
-        }
-        for (int t = lo; t < hi; t += 2) {
-            tile(t, r0, r1);
-            if (t + 1 < hi) tile(t + 1, r1, r0);
-        }
-    } else {
-        __shared__ __align__(16) Rows r2;               // (a third)
-        // this unit's probabilities and products (rows u .. of `now`), and the scores of the next one (rows w .. of `next`)
-        const auto unit = [&](const Rows& now, int u, const Rows& next, int w, bool some_hidden, f32x16& s, f32x16& p, f32x16& s2, f32x16& p2) __attribute__((always_inline)) {
-            Frag fa[2 * KS], fc[2][2 * DT];
-            Words<T> ws, we;
-            f32x4 lse[4];
-    #pragma unroll
-            for (int r = 0; r < 4; ++r) lse[r] = *(const f32x4*)&now.lse[u + 8 * r + 4 * h];
-            if (some_hidden) hide(now, u, s, p, lse);
-            start(next, w, s2, p2);
-            overlap<2 * KS, 2 * DT>(
-                [&](int i) __attribute__((always_inline)) { fa[i] = L::along(next.tile[i & 1], w, i >> 1); },
-                [&](int i) __attribute__((always_inline)) {
-                    if (i & 1) p2 = mma(fa[i], v[i >> 1], p2);
-                    else s2 = mma(fa[i], k[i >> 1], s2);
-                },
-                [&](int g) __attribute__((always_inline)) {
-    #pragma unroll
-                    for (int r = 2 * g; r < 2 * g + 2; ++r) {
+                __syncthreads();                        // (and nobody reads the tile before this any more)
+                if (any) {
+                    f32x4 lse[4];
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const f32x4 s2 = parts[wave ^ 2][r][l], p2 = parts[wave ^ 2][4 + r][l];
+                        lse[r] = *(const f32x4*)&now.lse[8 * r + 4 * h];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) { s[4 * r + j] += s2[j]; p[4 * r + j] += p2[j]; }
+                    }
+                    if (hides(t)) hide(now, 0, s, p, lse);
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
                         s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], a.c, -lse[r >> 2][r & 3]));
                         p[r] *= s[r];
                     }
-                    ws.set(g, s[2 * g], s[2 * g + 1]);
-                    we.set(g, p[2 * g], p[2 * g + 1]);
-                },
-                [&](int c, int i) __attribute__((always_inline)) { fc[c][i] = L::across(now.tile[1 - (i & 1)], u + 16 * c, 32 * (i >> 1)); },
-                [&](int c, int i) __attribute__((always_inline)) {
-                    if (i & 1) dk[i >> 1] = mma(fc[c][i], we.f[c], dk[i >> 1]);
-                    else dv[i >> 1] = mma(fc[c][i], ws.f[c], dv[i >> 1]);
-                });
-        };
-        f32x16 s0, p0, s1, p1;
-        const auto tile = [&](int t, Rows& now, Rows& next, Rows& after, auto odd) __attribute__((always_inline)) {
-    #pragma unroll
-            for (int n = 0; n < UNITS; ++n) {
-                const bool end = n == UNITS - 1;
-                if (end) {                              // the next tile has landed, and nobody reads the one before this
-                    if (t + 1 < hi) land(next);
-                    if (t + 2 < hi) fetch(t + 2, after);
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        const Frag ps = operand<T>(s, c), ds = operand<T>(p, c);
+#pragma unroll
+                        for (int d = 0; d < DT; ++d) {
+                            dv[d] = mma(L::across(now.tile[1], 16 * c, c0 + 32 * d), ps, dv[d]);
+                            dk[d] = mma(L::across(now.tile[0], 16 * c, c0 + 32 * d), ds, dk[d]);
+                        }
+                    }
                 }
-                const Rows& then = end ? next : now;
-                const int w = end ? 0 : 32 * (n + 1);
-                const bool some_hidden = hides(t), flip = UNITS == 1 ? odd : n & 1;
-                if (flip) unit(now, 32 * n, then, w, some_hidden, s1, p1, s0, p0);
-                else unit(now, 32 * n, then, w, some_hidden, s0, p0, s1, p1);
+                if (t + 1 < hi) land(next);
+            };
+            if (begin < hi) {
+                fetch(begin, r0);
+                land(r0);
             }
-        };
-        if (lo < hi) {
-            fetch(lo, r0);
-            land(r0);
-            if (lo + 1 < hi) fetch(lo + 1, r1);
-            start(r0, 0, s0, p0);
-    #pragma unroll
-            for (int c = 0; c < KS; ++c) {
-                s0 = mma(L::along(r0.tile[0], 0, c), k[c], s0);
-                p0 = mma(L::along(r0.tile[1], 0, c), v[c], p0);
+            for (int t = begin; t < hi; t += 2) {
+                tile(t, r0, r1);
+                if (t + 1 < hi) tile(t + 1, r1, r0);
+            }
+        } else {
+            __shared__ __align__(16) Rows r2;               // (a third)
+            // this unit's probabilities and products (rows u .. of `now`), and the scores of the next one (rows w .. of `next`)
+            const auto unit = [&](const Rows& now, int u, const Rows& next, int w, bool some_hidden, f32x16& s, f32x16& p, f32x16& s2, f32x16& p2) __attribute__((always_inline)) {
+                Frag fa[2 * KS], fc[2][2 * DT];
+                Words<T> ws, we;
+                f32x4 lse[4];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) lse[r] = *(const f32x4*)&now.lse[u + 8 * r + 4 * h];
+                if (some_hidden) hide(now, u, s, p, lse);
+                start(next, w, s2, p2);
+                overlap<2 * KS, 2 * DT>(
+                    [&](int i) __attribute__((always_inline)) { fa[i] = L::along(next.tile[i & 1], w, i >> 1); },
+                    [&](int i) __attribute__((always_inline)) {
+                        if (i & 1) p2 = mma(fa[i], v[i >> 1], p2);
+                        else s2 = mma(fa[i], k[i >> 1], s2);
+                    },
+                    [&](int g) __attribute__((always_inline)) {
+#pragma unroll
+                        for (int r = 2 * g; r < 2 * g + 2; ++r) {
+                            s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], a.c, -lse[r >> 2][r & 3]));
+                            p[r] *= s[r];
+                        }
+                        ws.set(g, s[2 * g], s[2 * g + 1]);
+                        we.set(g, p[2 * g], p[2 * g + 1]);
+                    },
+                    [&](int c, int i) __attribute__((always_inline)) { fc[c][i] = L::across(now.tile[1 - (i & 1)], u + 16 * c, 32 * (i >> 1)); },
+                    [&](int c, int i) __attribute__((always_inline)) {
+                        if (i & 1) dk[i >> 1] = mma(fc[c][i], we.f[c], dk[i >> 1]);
+                        else dv[i >> 1] = mma(fc[c][i], ws.f[c], dv[i >> 1]);
+                    });
+            };
+            f32x16 s0, p0, s1, p1;
+            const auto tile = [&](int t, Rows& now, Rows& next, Rows& after, auto odd) __attribute__((always_inline)) {
+#pragma unroll
+                for (int n = 0; n < UNITS; ++n) {
+                    const bool end = n == UNITS - 1;
+                    if (end) {                              // the next tile has landed, and nobody reads the one before this
+                        if (t + 1 < hi) land(next);
+                        if (t + 2 < hi) fetch(t + 2, after);
+                    }
+                    const Rows& then = end ? next : now;
+                    const int w = end ? 0 : 32 * (n + 1);
+                    const bool some_hidden = hides(t), flip = UNITS == 1 ? odd : n & 1;
+                    if (flip) unit(now, 32 * n, then, w, some_hidden, s1, p1, s0, p0);
+                    else unit(now, 32 * n, then, w, some_hidden, s0, p0, s1, p1);
+                }
+            };
+            if (begin < hi) {
+                fetch(begin, r0);
+                land(r0);
+                if (begin + 1 < hi) fetch(begin + 1, r1);
+                start(r0, 0, s0, p0);
+#pragma unroll
+                for (int c = 0; c < KS; ++c) {
+                    s0 = mma(L::along(r0.tile[0], 0, c), k[c], s0);
+                    p0 = mma(L::along(r0.tile[1], 0, c), v[c], p0);
+                }
+            }
+            const std::false_type even;
+            const std::true_type odd;
+            for (int t = begin; t < hi; t += 3) {
+                tile(t, r0, r1, r2, even);
+                if (t + 1 < hi) tile(t + 1, r1, r2, r0, odd);
+                if (t + 2 < hi) tile(t + 2, r2, r0, r1, even);
+                if constexpr (UNITS == 1) {                 // (the scores change places with every unit)
+                    t += 3;
+                    if (t < hi) tile(t, r0, r1, r2, odd);
+                    if (t + 1 < hi) tile(t + 1, r1, r2, r0, even);
+                    if (t + 2 < hi) tile(t + 2, r2, r0, r1, odd);
+                }
             }
         }
-        const std::false_type even;
-        const std::true_type odd;
-        for (int t = lo; t < hi; t += 3) {
-            tile(t, r0, r1, r2, even);
-            if (t + 1 < hi) tile(t + 1, r1, r2, r0, odd);
-            if (t + 2 < hi) tile(t + 2, r2, r0, r1, even);
-            if constexpr (UNITS == 1) {                 // (the scores change places with every unit)
-                t += 3;
-                if (t < hi) tile(t, r0, r1, r2, odd);
-                if (t + 1 < hi) tile(t + 1, r1, r2, r0, even);
-                if (t + 2 < hi) tile(t + 2, r2, r0, r1, odd);
-            }
+    };
+    const auto store = [&](int key) __attribute__((always_inline)) {
+        if (a.splits > 1) {
+            const long long n = (long long)a.batch * a.kv * a.kv_len;
+            const long long at = ((long long)b * a.kv + kvh) * a.kv_len + key;
+            float* pk = a.ws + ((2 * split) * n + at) * D + c0;
+            float* pv = pk + n * D;
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int r = 0; r < 16; r += 4) {
+                    *(f32x4*)(pk + 32 * d + 8 * (r >> 2) + 4 * h) = f32x4{dk[d][r], dk[d][r + 1], dk[d][r + 2], dk[d][r + 3]};
+                    *(f32x4*)(pv + 32 * d + 8 * (r >> 2) + 4 * h) = f32x4{dv[d][r], dv[d][r + 1], dv[d][r + 2], dv[d][r + 3]};
+                }
+        } else {
+            T* pk = (T*)a.dk + b * a.dks[0] + key * a.dks[1] + kvh * a.dks[2] + c0;
+            T* pv = (T*)a.dv + b * a.dvs[0] + key * a.dvs[1] + kvh * a.dvs[2] + c0;
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int r = 0; r < 16; r += 4) {
+                    const f32x4 x = inside ? f32x4{dk[d][r], dk[d][r + 1], dk[d][r + 2], dk[d][r + 3]} * a.scale : f32x4{0, 0, 0, 0};
+                    const f32x4 y = inside ? f32x4{dv[d][r], dv[d][r + 1], dv[d][r + 2], dv[d][r + 3]} : f32x4{0, 0, 0, 0};
+                    store4(pk, 32 * d + 8 * (r >> 2) + 4 * h, my, a.vec, x[0], x[1], x[2], x[3]);
+                    store4(pv, 32 * d + 8 * (r >> 2) + 4 * h, my, a.vec, y[0], y[1], y[2], y[3]);
+                }
         }
+    };
+    walk(lo);
+    if (key < a.kv_len) store(key);
+    if (!a.causal) return;
+    // A second look: the tiles with hidden pairs are the first ones.
+    {
+        const unsigned long long spoiled_k = bad_channels(dk), spoiled_v = bad_channels(dv);
+        bool go = inside && both_max(spoiled_k | spoiled_v ? 1.0f : 0.0f) > 0;
+        if (!__syncthreads_or(go)) return;
+        int begin = lo;
+        while (begin < hi && len.seen(a, first_query(begin)) < min(key0 + KEYS, len.k)) ++begin;
+        const int row0 = lo * each, row1 = (int)min((long long)begin * each, (long long)rows);
+        const auto row_of = [&](const T* p, const long long (&str)[3], int row) { const int i = query_of(a, row); return p + i * str[1] + (row - i * a.group) * str[2]; };
+        if (!__syncthreads_or(find_bad<T>(row1 - row0, a.d, [&](int r) { return row_of(qp, a.qs, row0 + r); }) ||
+                              find_bad<T>(row1 - row0, a.d, [&](int r) { return row_of(gp, a.gs, row0 + r); }))) return;
+        const int key = again(mine + (l & 31));         // (not worth registers before)
+        const T* kr = (const T*)a.k + b * a.ks[0] + key * a.ks[1] + kvh * a.ks[2];
+        const T* vr = (const T*)a.v + b * a.vs[0] + key * a.vs[1] + kvh * a.vs[2];
+#pragma unroll
+        for (int d = 0; d < DT; ++d) dk[d] = dv[d] = f32x16{};
+        for (int row = row0; row < row1 && __any(go); ++row) {
+            const int i = query_of(a, row), sees = len.seen(a, i);
+            if (go && sees > key) {
+                const T* qr = row_of(qp, a.qs, row);
+                const T* gr = row_of(gp, a.gs, row);
+                if (sees == 1) add_row<T, DT>(dv, 1.0f, gr + c0, my);
+                else {
+                    const float s = dot_of(qr, kr, a.d), p = __builtin_amdgcn_exp2f(fmaf(a.scale < 0 ? -s : s, a.c, -lsep[(long long)(row - i * a.group) * a.q_len + i] * kLog2e));
+                    add_row<T, DT>(dv, p, gr + c0, my);
+                    add_row<T, DT>(dk, p * (dot_of(gr, vr, a.d) - deltap[row]), qr + c0, my);
+                }
+            }
+            go = go && both_max((spoiled_k & ~bad_channels(dk)) | (spoiled_v & ~bad_channels(dv)) ? 1.0f : 0.0f) > 0;
+        }
+        if (!__syncthreads_or(go)) return;
+        row_operands<T, MY>(k, go ? kr + c0 : nullptr, my, VEC, a.scale < 0);
+        row_operands<T, MY>(v, go ? vr + c0 : nullptr, my, VEC, false);
+        walk(begin);
+        if (go) store(key);
     }
-    if (key >= a.kv_len) return;
-    if (a.causal && __any(not_finite(dk) || not_finite(dv))) {
-        const int key = again(mine + (l & 31));         // (what follows is not worth registers before)
-        if (both_max(not_finite(dk) || not_finite(dv) ? 1.0f : 0.0f) > 0 && inside) {
-            const T* kr = (const T*)a.k + b * a.ks[0] + key * a.ks[1] + kvh * a.ks[2];
-            const T* vr = (const T*)a.v + b * a.vs[0] + key * a.vs[1] + kvh * a.vs[2];
-#pragma unroll
-            for (int d = 0; d < DT; ++d) dk[d] = dv[d] = f32x16{};
-            for (int row = lo * each; row < (int)min((long long)hi * each, (long long)rows); ++row) {
-                const int i = query_of(a, row), j = row - i * a.group;
-                if (len.seen(a, i) <= key) continue;
-                const T* qr = qp + i * a.qs[1] + j * a.qs[2];
-                const T* gr = gp + i * a.gs[1] + j * a.gs[2];
-                if (len.seen(a, i) == 1) { add_row<T, DT>(dv, 1.0f, gr + c0, my); continue; }
-                const float s = dot_of(qr, kr, a.d), p = __builtin_amdgcn_exp2f(fmaf(a.scale < 0 ? -s : s, a.c, -lsep[(long long)j * a.q_len + i] * kLog2e));
-                add_row<T, DT>(dv, p, gr + c0, my);
-                add_row<T, DT>(dk, p * (dot_of(gr, vr, a.d) - deltap[row]), qr + c0, my);
-            }
-        }
-    }
-    if (a.splits > 1) {
-        const long long n = (long long)a.batch * a.kv * a.kv_len;
-        const long long at = ((long long)b * a.kv + kvh) * a.kv_len + key;
-        float* pk = a.ws + ((2 * split) * n + at) * D + c0;
-        float* pv = pk + n * D;
-#pragma unroll
-        for (int d = 0; d < DT; ++d)
-#pragma unroll
-            for (int r = 0; r < 16; r += 4) {
-                *(f32x4*)(pk + 32 * d + 8 * (r >> 2) + 4 * h) = f32x4{dk[d][r], dk[d][r + 1], dk[d][r + 2], dk[d][r + 3]};
-                *(f32x4*)(pv + 32 * d + 8 * (r >> 2) + 4 * h) = f32x4{dv[d][r], dv[d][r + 1], dv[d][r + 2], dv[d][r + 3]};
-            }
-        return;
-    }
-    T* pk = (T*)a.dk + b * a.dks[0] + key * a.dks[1] + kvh * a.dks[2] + c0;
-    T* pv = (T*)a.dv + b * a.dvs[0] + key * a.dvs[1] + kvh * a.dvs[2] + c0;
-#pragma unroll
-    for (int d = 0; d < DT; ++d)
-#pragma unroll
-        for (int r = 0; r < 16; r += 4) {
-            const f32x4 x = inside ? f32x4{dk[d][r], dk[d][r + 1], dk[d][r + 2], dk[d][r + 3]} * a.scale : f32x4{0, 0, 0, 0};
-            const f32x4 y = inside ? f32x4{dv[d][r], dv[d][r + 1], dv[d][r + 2], dv[d][r + 3]} : f32x4{0, 0, 0, 0};
-            store4(pk, 32 * d + 8 * (r >> 2) + 4 * h, my, a.vec, x[0], x[1], x[2], x[3]);
-            store4(pv, 32 * d + 8 * (r >> 2) + 4 * h, my, a.vec, y[0], y[1], y[2], y[3]);
-        }
 }
 
 // Sums of the splits, first split first: rows of D floats, `stride` floats from split to split, each to its place.  KEYS: dk (blockIdx.y 0) and dv (1), else dq.

@@ -1,4 +1,6 @@
-"""Causal attention where what a query does not see holds the type's largest numbers."""
+"""Causal attention where what a query does not see holds the type's largest numbers, infinities or NaN."""
+import math
+
 import pytest
 import torch
 
@@ -44,3 +46,76 @@ def test_hidden_queries_of_the_largest_numbers(shape, dtype):
     got = A._run(q2, k, v, do2, dtype, True)
     assert torch.equal(got.dk[:, 6:], want.dk[:, 6:])
     assert torch.equal(got.dv[:, 6:], want.dv[:, 6:])
+
+
+def _times(call, n):
+    call()
+    torch.cuda.synchronize()
+    a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    a.record()
+    for _ in range(n):
+        call()
+    b.record()
+    b.synchronize()
+    return a.elapsed_time(b) / n
+
+
+@pytest.mark.parametrize("what", ["all", "keys and values", "one channel of the values", "query 500's dout"])
+def test_time_where_numbers_are_not_finite(what):
+    """A call on NaN takes a bounded multiple of one on numbers: one more walk over the tiles at most, and up to 192 keys (queries) of a row (key) that some of its neighbours do not see, one by
+    one: 5 products of 64 channels each, about 50 cycles a channel, 3 million cycles or 1.5 ms; 1024 workgroups are two to a CU, in two rounds: 3 ms a kernel.  One kernel
+    forward, two backward; and 2.5 times the finite call."""
+    from paper_2409_09083_amd import tokens
+    q, k, v, do = A._make(4, 4, 4, 4096, 4096, 64, "bf16")
+    a = tokens.Attention(4, 4, 4, 4096, 4096, 64, "bf16", causal=True)
+    forward, backward = _times(lambda: a.forward(q, k, v), 5), _times(lambda: a.backward(do, q, k, v), 5)
+    if what == "query 500's dout":
+        do[:, 500] = math.nan
+    else:
+        for t in (q, k, v, do)[slice(0, 4) if what == "all" else slice(1, 3) if what == "keys and values" else slice(2, 3)]:
+            if what == "one channel of the values":
+                t[..., 7] = math.nan
+            else:
+                t.fill_(math.nan)
+    f2, b2 = _times(lambda: a.forward(q, k, v), 1), _times(lambda: a.backward(do, q, k, v), 1)
+    print(what, forward, f2, backward, b2)
+    assert f2 <= 2.5 * forward + 3 and b2 <= 2.5 * backward + 6
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+@pytest.mark.parametrize("shape", [(1, 2, 2, 400, 400, 64), (2, 6, 2, 333, 333, 128), (300, 2, 1, 150, 150, 32), (1, 1, 1, 300, 700, 40), (1, 2, 1, 500, 300, 64)])
+def test_one_bad_token_in_the_middle(shape, bad, dtype):
+    """Queries before it and keys behind it are as without it; queries behind it have its value's channel spoiled and the others right."""
+    b, h, kv, ql, kl, d = shape
+    q, k, v, do = A._make(*shape, dtype)
+    want = A._run(q, k, v, do, dtype, True)
+    at = kl // 2
+    first = max(0, at - (kl - ql))                              # the first query that sees key `at`
+    tol = 2e-5 if dtype == "f32" else 3e-2
+
+    def near(x, y):
+        return x.numel() == 0 or (x.isfinite().all() and (x - y).abs().max() <= tol * y.abs().max())
+    v2 = v.clone()
+    v2[:, at, :, 3] = bad
+    got = A._run(q, k, v2, do, dtype, True)
+    others = [c for c in range(d) if c != 3]
+    assert near(got.out[:, :first], want.out[:, :first])
+    assert near(got.out[:, first:][..., others], want.out[:, first:][..., others])
+    assert not got.out[:, first:, :, 3].isfinite().any()
+    assert torch.equal(got.lse, want.lse)
+    assert near(got.dq[:, :first], want.dq[:, :first])
+    assert not got.dq[:, first + 1:].isfinite().any()
+    k2 = k.clone()
+    k2[:, at, :, 3] = math.nan
+    got = A._run(q, k2, v, do, dtype, True)
+    assert near(got.out[:, :first], want.out[:, :first]) and not got.out[:, first:].isfinite().any()
+    do2, q2 = do.clone(), q.clone()
+    do2[:, first + 9] = bad
+    q2[:, first + 9] = math.nan
+    last = first + 9 + kl - ql                                  # the last key that this query sees
+    for got in (A._run(q, k, v, do2, dtype, True), A._run(q2, k, v, do, dtype, True)):
+        for t in ("dk", "dv"):
+            assert near(getattr(got, t)[:, last + 1:], getattr(want, t)[:, last + 1:]), t
+        assert not got.dv[:, :last + 1].isfinite().any()
+        assert torch.equal(got.dq[:, :first + 9], want.dq[:, :first + 9]) and torch.equal(got.dq[:, first + 10:], want.dq[:, first + 10:])
