@@ -42,6 +42,18 @@ int check(const ftp_attention_shape* s)
     return FTP_OK;
 }
 
+bool negative(const int64_t (&stride)[3]) { return stride[0] < 0 || stride[1] < 0 || stride[2] < 0; }
+
+// ... and the strides that a pass uses (rows of a tile are fetched at offsets from its first one, where a negative one means no row).
+int check(const ftp_attention_shape* s, bool back)
+{
+    const int rc = check(s);
+    if (rc != FTP_OK) return rc;
+    if (negative(s->q_stride) || negative(s->k_stride) || negative(s->v_stride) || negative(s->out_stride)) return FTP_EINVAL;
+    if (back && (negative(s->dout_stride) || negative(s->dq_stride) || negative(s->dk_stride) || negative(s->dv_stride))) return FTP_EINVAL;
+    return FTP_OK;
+}
+
 bool is_act(int32_t act) { return act >= FTP_ACT_NONE && act <= FTP_ACT_SILU; }
 
 }  // namespace
@@ -147,7 +159,7 @@ int ftp_attention_workspace(const ftp_attention_shape* shape, size_t* forward_by
 int ftp_attention_forward(const ftp_attention_shape* shape, const void* q, const void* k, const void* v, const int32_t* q_lens, const int32_t* kv_lens,
                           void* out, float* lse, void* workspace, void* stream)
 {
-    const int rc = check(shape);
+    const int rc = check(shape, false);
     if (rc != FTP_OK || shape->batch == 0 || shape->q_len == 0) return rc;
     if (!q || !out || (shape->kv_len && (!k || !v)) || (!workspace && attention_forward_workspace(*shape))) return FTP_EINVAL;
     attention_forward(*shape, q, k, v, q_lens, kv_lens, out, lse, (float*)workspace, (hipStream_t)stream);
@@ -157,7 +169,7 @@ int ftp_attention_forward(const ftp_attention_shape* shape, const void* q, const
 int ftp_attention_backward(const ftp_attention_shape* shape, const void* dout, const void* q, const void* k, const void* v, const int32_t* q_lens,
                            const int32_t* kv_lens, const void* out, const float* lse, void* dq, void* dk, void* dv, void* workspace, void* stream)
 {
-    const int rc = check(shape);
+    const int rc = check(shape, true);
     if (rc != FTP_OK || shape->batch == 0) return rc;
     if (shape->q_len && (!dout || !q || !out || !lse || !dq || !workspace)) return FTP_EINVAL;
     if (shape->kv_len && (!k || !v || !dk || !dv)) return FTP_EINVAL;
