@@ -308,7 +308,8 @@ int ftp_checkpoint_wgrad(const ftp_checkpoint_shape* shape, const int8_t* codes,
  * there and dq = 0, exactly.  Keys, values and queries that are not seen do not reach any result, whatever they hold (causal calls with such values that
  * are not finite may take a second walk over the keys).  fp32 numbers are multiplied as three bfloats each: a seen infinity, or number above the largest bfloat, gives NaN.
  * Element (b, t, h, c) of q lies at q_stride[0] * b + q_stride[1] * t + q_stride[2] * h + c; likewise the others; no stride is
- * negative.  Inputs may be broadcast (stride 0); gradients then come out unsummed, in buffers of their own.  q_len and kv_len may be 0. */
+ * negative.  Inputs may be broadcast (stride 0); gradients then come out unsummed, in buffers of their own.  q_len and kv_len may be 0.
+ * A launch's workgroups of 128 (64) queries or keys of an image's key head are fewer than 2^24, counted over all of them. */
 typedef struct {
     int32_t batch, heads, kv_heads;     /* kv_heads divides heads */
     int32_t q_len, kv_len;

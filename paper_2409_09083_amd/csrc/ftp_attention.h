@@ -383,11 +383,15 @@ __device__ __forceinline__ bool place_of(const AttentionArgs& a, int& block, int
     kvh = g - b * a.kv;
     return true;
 }
+// Workgroups of `blocks` blocks each of (image, key head, split) groups.
+inline bool by_xcd(long long groups, bool ragged) { return (groups % 8 == 0 && groups >= (ragged ? 24 : 8)) || groups >= 48; }
+inline long long place_count(long long groups, long long blocks, bool ragged) { return by_xcd(groups, ragged) ? ceil_div(groups, 8) * 8 * blocks : groups * blocks; }
 inline unsigned place_groups(AttentionArgs& a)
 {
+    const bool ragged = a.q_lens || a.kv_lens;
     a.groups = a.batch * a.kv * a.splits;
-    a.by_xcd = (a.groups % 8 == 0 && a.groups >= (a.q_lens || a.kv_lens ? 24 : 8)) || a.groups >= 48;
-    return a.by_xcd ? xcd_grid(a.groups, a.blocks) : (unsigned)(a.groups * a.blocks);
+    a.by_xcd = by_xcd(a.groups, ragged);
+    return (unsigned)place_count(a.groups, a.blocks, ragged);
 }
 
 // Hidden keys and rows are multiplied by 0 inside a block, which makes NaN of what is not finite there (only causal calls have hidden values in a block: rows past the lengths are
@@ -448,6 +452,8 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 AttentionArgs attention_args(const ftp_attention_shape& s);
 // Wavefronts to a row of 32 in the kernels that walk over the keys: 1 or 2.
 int attention_halves(const ftp_attention_shape& s);
+// Keys of a workgroup of the key gradients.
+inline int attention_key_block(bool wide_fp32) { return wide_fp32 ? 64 : 128; }
 
 // Offsets within a tile (at most 64 such strides) stay below 2^30 bytes.
 inline bool near_rows(long long stride) { return stride < (1ll << 21); }

@@ -294,6 +294,14 @@ int attention_halves(const ftp_attention_shape& s)
     return rows <= 64 || groups < (narrow && s.causal ? 768 : narrow || s.causal ? 384 : 256) ? 2 : 1;
 }
 
+bool attention_fits(const ftp_attention_shape& s)
+{
+    const long long rows = (long long)s.q_len * (s.heads / s.kv_heads), groups = (long long)s.batch * s.kv_heads;
+    const long long blocks = std::max(ceil_div(rows, 128 / attention_halves(s)), ceil_div(s.kv_len, attention_key_block(s.dtype == FTP_F32 && s.head_dim > 64)));
+    // (splits come only where there are few; what rounds groups up to eights may come or not, by the lengths)
+    return groups <= kMostGroups && blocks <= kMostGroups && std::max(place_count(groups, blocks, true), place_count(groups, blocks, false)) <= kMostGroups;
+}
+
 AttentionArgs attention_args(const ftp_attention_shape& s)
 {
     AttentionArgs a = {};

@@ -556,7 +556,7 @@ Splits backward_splits(const ftp_attention_shape& s)
 {
     const bool bf = s.dtype == FTP_BF16, wide = s.head_dim > 64;
     const long long rows = (long long)s.q_len * (s.heads / s.kv_heads), all = (long long)s.batch * s.kv_heads;
-    const long long nq = ceil_div(rows, 128 / attention_halves(s)) * all, nk = ceil_div(s.kv_len, bf || !wide ? 128 : 64) * all;
+    const long long nq = ceil_div(rows, 128 / attention_halves(s)) * all, nk = ceil_div(s.kv_len, attention_key_block(!bf && wide)) * all;
     // Workgroups that have a CU by themselves (alone) come in rounds of 256: a split costs its tiles and about as long as 6 for its start, a unit too many and its part of the sum
     // (fp32, 13 x 8 heads on 1, 7 x 1172 tokens of 120: 53 us the pass with splits of at least 8 tiles, 47; 4 heads x 300 of 64 59 -> 41; 8 heads x 1000 of 128 171 -> 144).  More than a round
     // of blocks is split for the last one's sake where a tile is long and the blocks are alike (fp32, 16 heads x 1144 of 128: 473 -> 394; split so, causal bfloats of 128 go 95 -> 123).

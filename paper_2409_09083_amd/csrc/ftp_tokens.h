@@ -24,6 +24,9 @@ size_t held_wgrad_workspace(const ftp_checkpoint_shape& s, int outputs);
 void held_wgrad(const ftp_checkpoint_shape& s, const int8_t* codes, const int8_t* exponents, const void* dy, long long dy_stride, int outputs, float* dw,
                 float* partial, hipStream_t st);
 
+// A launch has less than 2^32 threads.
+constexpr long long kMostGroups = (1ll << 24) - 1;  // ... in workgroups of 256
+bool attention_fits(const ftp_attention_shape& s);  // (of shapes whose rows, keys and heads are 32-bit numbers)
 size_t attention_forward_workspace(const ftp_attention_shape& s);
 size_t attention_backward_workspace(const ftp_attention_shape& s);
 void attention_forward(const ftp_attention_shape& s, const void* q, const void* k, const void* v, const int* q_lens, const int* kv_lens, void* out, float* lse,

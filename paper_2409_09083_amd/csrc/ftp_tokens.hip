@@ -36,9 +36,8 @@ int check(const ftp_attention_shape* s)
     if (!s || !is_type(s->dtype) || s->batch < 0 || s->heads < 1 || s->kv_heads < 1 || s->heads % s->kv_heads || s->q_len < 0 || s->kv_len < 0 ||
         s->head_dim < 1 || !std::isfinite(s->scale)) return FTP_EINVAL;
     if (s->head_dim > 128) return FTP_EUNSUPPORTED;
-    // rows and keys, with a block's overhang, are 32-bit numbers, and so is the number of workgroups
-    const double rows = (double)s->q_len * (s->heads / s->kv_heads), heads = (double)s->batch * s->kv_heads;
-    if (rows > 2e9 || s->kv_len > 2000000000 || heads * (rows / 128 + s->kv_len / 128.0 + 2) > 1e9) return FTP_EUNSUPPORTED;
+    // rows and keys, with a block's overhang, are 32-bit numbers
+    if ((double)s->q_len * (s->heads / s->kv_heads) > 2e9 || s->kv_len > 2000000000 || (double)s->batch * s->kv_heads > 2e9 || !attention_fits(*s)) return FTP_EUNSUPPORTED;
     return FTP_OK;
 }
 
@@ -141,7 +140,7 @@ int ftp_checkpoint_wgrad(const ftp_checkpoint_shape* shape, const int8_t* codes,
     const int rc = check(shape);
     if (rc != FTP_OK) return rc;
     if (outputs < 1 || dy_stride < outputs || !dw || (shape->rows && (!codes || !exponents || !dy))) return FTP_EINVAL;
-    if ((double)((outputs + 127) / 128) * (double)((shape->cols + 127) / 128) > 1e9) return FTP_EUNSUPPORTED;
+    if (ceil_div(outputs, 128) * ceil_div(shape->cols, 128) > kMostGroups) return FTP_EUNSUPPORTED;
     if (!workspace && held_wgrad_workspace(*shape, outputs)) return FTP_EINVAL;
     held_wgrad(*shape, codes, exponents, dy, dy_stride, outputs, dw, (float*)workspace, (hipStream_t)stream);
     return launched();
