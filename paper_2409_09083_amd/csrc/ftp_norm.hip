@@ -23,6 +23,7 @@ struct RowArgs {
     long long rows, inner;                          // inner: tokens to an outer step (rows: one step)
     long long xo, xi, yo, yi, go, gi;               // strides: x, y (forward) or dx (backward), dy
     int C, lanes, block, nblocks;
+    uint32_t first;                                 // workgroups in earlier launches of the pass
     float eps;
 };
 
@@ -67,7 +68,7 @@ __global__ __launch_bounds__(256) void k_norm_rows(const RowArgs a)
     __shared__ float lds[4];
     const int lanes = WIDE ? 256 : a.lanes;
     const int lane = threadIdx.x & (lanes - 1);
-    const long long row = (long long)blockIdx.x * (256 / lanes) + (WIDE ? 0 : threadIdx.x / lanes);
+    const long long row = (long long)(a.first + blockIdx.x) * (256 / lanes) + (WIDE ? 0 : threadIdx.x / lanes);
     const bool live = row < a.rows;
     Pack<T, VEC> x[NV];
     const T* px = (const T*)a.x + (live ? row_offset(row, a.inner, a.rows, a.xo, a.xi) : 0);
@@ -246,7 +247,7 @@ template <typename T>
 __global__ __launch_bounds__(256) void k_norm_long(const RowArgs a)
 {
     __shared__ float lds[4];
-    const long long row = blockIdx.x;
+    const long long row = a.first + blockIdx.x;
     const T* px = (const T*)a.x + row_offset(row, a.inner, a.rows, a.xo, a.xi);
     T* py = (T*)a.y + row_offset(row, a.inner, a.rows, a.yo, a.yi);
     float s = 0;
@@ -274,7 +275,7 @@ template <typename T>
 __global__ __launch_bounds__(256) void k_norm_back_long(const RowArgs a)
 {
     __shared__ float lds[4];
-    const long long row = blockIdx.x, off = row_offset(row, a.inner, a.rows, a.xo, a.xi);
+    const long long row = a.first + blockIdx.x, off = row_offset(row, a.inner, a.rows, a.xo, a.xi);
     const T* py = (const T*)a.dy + row_offset(row, a.inner, a.rows, a.go, a.gi);
     T* pd = (T*)a.dx + row_offset(row, a.inner, a.rows, a.yo, a.yi);
     const float mean = a.mean[row], rstd = a.rstd[row];
@@ -337,6 +338,7 @@ struct TileArgs {
     long long outer, inner;
     long long xs[3], ys[3], gs[3];                  // strides: x, y (forward) or dx (backward), dy
     int C, px, shift, tiles;                        // px = 2^shift tokens a tile, `tiles` tiles to an outer step
+    uint32_t first;                                 // workgroups in earlier launches of the pass
     int xvec, yvec, gvec;                           // elements of x, y or dx, dy that go together along the tile's contiguous axis (1, or 16 bytes)
     float eps;
 };
@@ -454,8 +456,9 @@ __global__ __launch_bounds__(256) void k_norm_tiles(const TileArgs a)
     T* tile = (T*)(beta + a.C);
     param_load<T>(gamma, a.gamma, 1.0f, a.C);
     param_load<T>(beta, a.beta, 0.0f, a.C);
-    const int o = blockIdx.x / a.tiles, pitch = tile_pitch<T>(a.px);
-    const long long at = (long long)(blockIdx.x - o * a.tiles) << a.shift;
+    const uint32_t block = a.first + blockIdx.x;
+    const int o = block / (uint32_t)a.tiles, pitch = tile_pitch<T>(a.px);
+    const long long at = (long long)(block - (uint32_t)o * a.tiles) << a.shift;
     const int n = (int)min((long long)a.px, a.inner - at);
     tile_load(tile, (const T*)a.x + o * a.xs[0] + at * a.xs[1], a.xs, a.xvec, a.C, a.px, a.shift, n, pitch);
     __syncthreads();
@@ -628,6 +631,15 @@ int tile_tokens(const ftp_norm_shape& s, bool back)
     while (px > 4 && px / 2 >= s.inner) px >>= 1;
     return px;
 }
+// A pass of `groups` workgroups of 256 in as many launches as it takes.
+template <class Args, class F>
+void by_launches(Args a, long long groups, F launch)
+{
+    for (long long at = 0; at < groups; at += kMostGroups) {
+        a.first = (uint32_t)at;
+        launch(a, (unsigned)std::min(kMostGroups, groups - at));
+    }
+}
 // Elements that go together along the contiguous axis of one tensor: 16 bytes or one.
 int tile_vec(const ftp_norm_shape& s, const int64_t* str, int px, const void* p)
 {
@@ -660,9 +672,10 @@ void norm_forward(const ftp_norm_shape& s, const void* x, const void* gamma, con
         TileArgs a = tile_args(s, t, false);
         a.x = x; a.gamma = gamma; a.beta = beta; a.y = y; a.mean = mean; a.rstd = rstd;
         a.xvec = tile_vec(s, t.x, a.px, x); a.yvec = tile_vec(s, t.y, a.px, y);
-        const unsigned grid = (unsigned)(s.outer * a.tiles);
-        if (bf) k_norm_tiles<bf16_t><<<grid, 256, tile_bytes(s, a.px, false), st>>>(a);
-        else k_norm_tiles<float><<<grid, 256, tile_bytes(s, a.px, false), st>>>(a);
+        by_launches(a, s.outer * a.tiles, [&](const TileArgs& a, unsigned grid) {
+            if (bf) k_norm_tiles<bf16_t><<<grid, 256, tile_bytes(s, a.px, false), st>>>(a);
+            else k_norm_tiles<float><<<grid, 256, tile_bytes(s, a.px, false), st>>>(a);
+        });
         return;
     }
     RowArgs a = row_args(s, t);
@@ -671,14 +684,13 @@ void norm_forward(const ftp_norm_shape& s, const void* x, const void* gamma, con
     const int vec = row_vec(a, bf ? 2 : 4, ptrs, 4, nullptr);
     const RowForm f = row_form(a.C, vec);
     a.lanes = f.lanes;
-    if (f.nv == 0) {
-        if (bf) k_norm_long<bf16_t><<<(unsigned)a.rows, 256, 0, st>>>(a);
-        else k_norm_long<float><<<(unsigned)a.rows, 256, 0, st>>>(a);
-        return;
-    }
-    const unsigned grid = (unsigned)ceil_div(a.rows, 256 / f.lanes);
-    if (bf) run_rows_t<bf16_t>(a, vec, f, false, grid, st);
-    else run_rows_t<float>(a, vec, f, false, grid, st);
+    by_launches(a, ceil_div(a.rows, 256 / f.lanes), [&](const RowArgs& a, unsigned grid) {
+        if (f.nv == 0) {
+            if (bf) k_norm_long<bf16_t><<<grid, 256, 0, st>>>(a);
+            else k_norm_long<float><<<grid, 256, 0, st>>>(a);
+        } else if (bf) run_rows_t<bf16_t>(a, vec, f, false, grid, st);
+        else run_rows_t<float>(a, vec, f, false, grid, st);
+    });
 }
 
 void norm_backward(const ftp_norm_shape& s, const void* dy, const void* x, const int8_t* codes, const int8_t* exponents, int block, const void* gamma,
@@ -713,8 +725,10 @@ void norm_backward(const ftp_norm_shape& s, const void* dy, const void* x, const
                 if (bf) k_norm_long_params<bf16_t><<<grid, 256, 0, st>>>(a, shares);
                 else k_norm_long_params<float><<<grid, 256, 0, st>>>(a, shares);
             }
-            if (bf) k_norm_back_long<bf16_t><<<(unsigned)a.rows, 256, 0, st>>>(a);
-            else k_norm_back_long<float><<<(unsigned)a.rows, 256, 0, st>>>(a);
+            by_launches(a, a.rows, [&](const RowArgs& a, unsigned grid) {
+                if (bf) k_norm_back_long<bf16_t><<<grid, 256, 0, st>>>(a);
+                else k_norm_back_long<float><<<grid, 256, 0, st>>>(a);
+            });
         } else {
             shares = (int)std::min<long long>(kShares, ceil_div(a.rows, f.wide ? 1 : kBackThreads / f.lanes));
             if (bf) run_rows_t<bf16_t>(a, vec, f, true, shares, st);
