@@ -9,18 +9,20 @@ namespace {
 
 bool is_type(int32_t dtype) { return dtype == FTP_F32 || dtype == FTP_BF16; }
 
-// FTP_OK if there is something to do; *nothing: an empty call, which is no error.
-int check(const ftp_norm_shape* s, bool back, bool* nothing)
+// FTP_OK if there is something to do; *nothing: an empty call, which is no error.  Strides are those that the pass uses: x and y, or x (not from a checkpoint: held), dy and dx.
+int check(const ftp_norm_shape* s, bool back, bool held, bool* nothing)
 {
     *nothing = false;
     if (!s || !is_type(s->dtype) || s->outer < 0 || s->inner < 0 || s->channels < 1 || !(s->eps >= 0)) return FTP_EINVAL;
-    for (int i = 0; i < 3; ++i)
-        if (s->x_stride[i] < 0 || (back ? s->dy_stride[i] < 0 || s->dx_stride[i] < 0 : s->y_stride[i] < 0)) return FTP_EINVAL;
+    const int64_t* used[] = {held ? s->dy_stride : s->x_stride, back ? s->dy_stride : s->y_stride, back ? s->dx_stride : s->y_stride};
+    bool rows = true;
+    for (const int64_t* t : used) {
+        if (t[0] < 0 || t[1] < 0 || t[2] < 0) return FTP_EINVAL;
+        rows = rows && t[2] == 1;
+    }
     if (s->outer == 0 || s->inner == 0) { *nothing = true; return FTP_OK; }
     if (s->outer > 0x7FFFFFFFll || s->inner > 0x7FFFFFFFll || s->outer * s->inner > 0x7FFFFFFFll) return FTP_EUNSUPPORTED;
-    if ((s->x_stride[2] != 1 || (back ? s->dy_stride[2] != 1 || s->dx_stride[2] != 1 : s->y_stride[2] != 1)) && s->channels > kNormMapChannels)
-        return FTP_EUNSUPPORTED;
-    return FTP_OK;
+    return rows || s->channels <= kNormMapChannels ? FTP_OK : FTP_EUNSUPPORTED;
 }
 
 int check(const ftp_checkpoint_shape* s)
@@ -62,7 +64,7 @@ extern "C" {
 int ftp_norm_forward(const ftp_norm_shape* shape, const void* x, const void* gamma, const void* beta, void* y, float* mean, float* rstd, void* stream)
 {
     bool nothing;
-    const int rc = check(shape, false, &nothing);
+    const int rc = check(shape, false, false, &nothing);
     if (rc != FTP_OK || nothing) return rc;
     if (!x || !y) return FTP_EINVAL;
     norm_forward(*shape, x, gamma, beta, y, mean, rstd, (hipStream_t)stream);
@@ -80,7 +82,7 @@ int ftp_norm_backward(const ftp_norm_shape* shape, const void* dy, const void* x
                       const void* gamma, const float* mean, const float* rstd, void* dx, float* dgamma, float* dbeta, void* workspace, void* stream)
 {
     bool nothing;
-    const int rc = check(shape, true, &nothing);
+    const int rc = check(shape, true, codes != nullptr, &nothing);
     if (rc != FTP_OK) return rc;
     if (!dgamma != !dbeta || !codes != !exponents || (x && codes)) return FTP_EINVAL;
     if (codes) {
