@@ -538,7 +538,7 @@ constexpr int kShares = 512;                        // workgroups of a backward 
 struct Strides { const int64_t* x; const int64_t* y; const int64_t* g; };
 Strides strides_of(const ftp_norm_shape& s, bool back, bool held) { return back ? Strides{held ? s.dy_stride : s.x_stride, s.dx_stride, s.dy_stride} : Strides{s.x_stride, s.y_stride, s.y_stride}; }
 
-bool by_rows(const Strides& t) { return t.x[2] == 1 && t.y[2] == 1 && t.g[2] == 1; }
+bool by_rows(const Strides& t, int channels) { return channels == 1 || (t.x[2] == 1 && t.y[2] == 1 && t.g[2] == 1); }
 
 RowArgs row_args(const ftp_norm_shape& s, const Strides& t)
 {
@@ -668,7 +668,7 @@ void norm_forward(const ftp_norm_shape& s, const void* x, const void* gamma, con
 {
     const bool bf = s.dtype == FTP_BF16;
     const Strides t = strides_of(s, false, false);
-    if (!by_rows(t)) {
+    if (!by_rows(t, s.channels)) {
         TileArgs a = tile_args(s, t, false);
         a.x = x; a.gamma = gamma; a.beta = beta; a.y = y; a.mean = mean; a.rstd = rstd;
         a.xvec = tile_vec(s, t.x, a.px, x); a.yvec = tile_vec(s, t.y, a.px, y);
@@ -700,7 +700,7 @@ void norm_backward(const ftp_norm_shape& s, const void* dy, const void* x, const
     const Strides t = strides_of(s, true, codes != nullptr);
     int shares = 0;
     if (s.outer == 0 || s.inner == 0) {             // (sums of nothing)
-    } else if (!by_rows(t)) {
+    } else if (!by_rows(t, s.channels)) {
         TileArgs a = tile_args(s, t, true);
         a.x = x; a.gamma = gamma; a.dy = dy; a.dx = dx; a.mean = (float*)mean; a.rstd = (float*)rstd;
         a.partial = dgamma ? partial : nullptr;

@@ -18,7 +18,7 @@ int check(const ftp_norm_shape* s, bool back, bool held, bool* nothing)
     bool rows = true;
     for (const int64_t* t : used) {
         if (t[0] < 0 || t[1] < 0 || t[2] < 0) return FTP_EINVAL;
-        rows = rows && t[2] == 1;
+        rows = rows && (t[2] == 1 || s->channels == 1);
     }
     if (s->outer == 0 || s->inner == 0) { *nothing = true; return FTP_OK; }
     if (s->outer > 0x7FFFFFFFll || s->inner > 0x7FFFFFFFll || s->outer * s->inner > 0x7FFFFFFFll) return FTP_EUNSUPPORTED;
@@ -87,7 +87,7 @@ int ftp_norm_backward(const ftp_norm_shape* shape, const void* dy, const void* x
     if (!dgamma != !dbeta || !codes != !exponents || (x && codes)) return FTP_EINVAL;
     if (codes) {
         if (block != 32 && block != 64 && block != 128 && block != 256) return FTP_EUNSUPPORTED;
-        if (shape->dx_stride[2] != 1 || shape->dy_stride[2] != 1) return FTP_EUNSUPPORTED;
+        if (shape->channels > 1 && (shape->dx_stride[2] != 1 || shape->dy_stride[2] != 1)) return FTP_EUNSUPPORTED;
     }
     if (dgamma && !workspace) return FTP_EINVAL;
     if (!nothing && (!dy || (!x && !codes) || !mean || !rstd || !dx)) return FTP_EINVAL;
