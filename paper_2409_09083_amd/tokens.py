@@ -25,6 +25,9 @@ _TYPES = {"f32": (torch.float32, B.FTP_F32), "bf16": (torch.bfloat16, B.FTP_BF16
 _ACTS = {"none": B.FTP_ACT_NONE, "leaky": B.FTP_ACT_LEAKY, "gelu": B.FTP_ACT_GELU, "silu": B.FTP_ACT_SILU}
 _LAYOUTS = ("rows", "map")
 
+# torch.cuda.current_device() and the handle of torch.cuda.current_stream(), without a check of the start-up and a Stream object: a third of a small call's host time
+_current_device, _current_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+
 
 def _types(dtype):
     if dtype not in _TYPES:
@@ -62,9 +65,13 @@ def _scratch(nbytes, device):
 
 
 class _Operator:
-    def _stream(self):
-        # (the handle of torch.cuda.current_stream(), without making a Stream object: a third of a small call's host time)
-        return torch._C._cuda_getCurrentRawStream(self.device.index)
+    def _call(self, f, *args):
+        """f(*args, stream) on the current stream of this object's device, with that device the current one: kernels start there."""
+        index = self.device.index
+        if _current_device() != index:
+            with torch.cuda.device(index):
+                return self._call(f, *args)
+        return f(*args, _current_stream(index))
 
     def _set_strides(self, name, strides):
         """Strides of a tensor into the description, where they differ from what it holds."""
@@ -110,7 +117,7 @@ class Norm(_Operator):
     def forward(self, x, gamma=None, beta=None):
         px = _need("x", x, self.shape, self.tdtype, self.device)
         self._set_strides("x_stride", x.stride())
-        B.ftp_norm_forward(self.desc, px, self._param("gamma", gamma), self._param("beta", beta), *self._outputs, self._stream())
+        self._call(B.ftp_norm_forward, self.desc, px, self._param("gamma", gamma), self._param("beta", beta), *self._outputs)
         return self.y
 
     def backward(self, dy, x, gamma=None, mean=None, rstd=None):
@@ -134,8 +141,8 @@ class Norm(_Operator):
         self._set_strides("dx_stride", self.dx.stride())
         stat = [_dense(n, t, self.mean.shape, torch.float32, self.device)
                 for n, t in (("mean", self.mean if mean is None else mean), ("rstd", self.rstd if rstd is None else rstd))]
-        B.ftp_norm_backward(self.desc, pdy, px, pc, pe, block, self._param("gamma", gamma), stat[0], stat[1], self.dx.data_ptr(),
-                            self.dgamma.data_ptr(), self.dbeta.data_ptr(), self._ws.data_ptr(), self._stream())
+        self._call(B.ftp_norm_backward, self.desc, pdy, px, pc, pe, block, self._param("gamma", gamma), stat[0], stat[1], self.dx.data_ptr(),
+                   self.dgamma.data_ptr(), self.dbeta.data_ptr(), self._ws.data_ptr())
         return self.dx, self.dgamma, self.dbeta
 
 
@@ -179,7 +186,7 @@ class Checkpoint(_Operator):
 
     def pack(self, x):
         p, self.desc.stride = self._rows("x", x, self.cols)
-        B.ftp_checkpoint_pack(self.desc, p, self.codes.data_ptr(), self.exponents.data_ptr(), self._stream())
+        self._call(B.ftp_checkpoint_pack, self.desc, p, self.codes.data_ptr(), self.exponents.data_ptr())
         return self
 
     def unpack(self, act="none", slope=0.1, out=None):
@@ -187,7 +194,7 @@ class Checkpoint(_Operator):
         act = self._act(act)
         out = self._output(out)
         p, self.desc.stride = self._rows("out", out, self.cols)
-        B.ftp_checkpoint_unpack(self.desc, self.codes.data_ptr(), self.exponents.data_ptr(), act, slope, p, self._stream())
+        self._call(B.ftp_checkpoint_unpack, self.desc, self.codes.data_ptr(), self.exponents.data_ptr(), act, slope, p)
         return out
 
     def act_backward(self, dy, act, slope=0.1, out=None):
@@ -198,7 +205,7 @@ class Checkpoint(_Operator):
         q, self.desc.stride = self._rows("out", out, self.cols)
         if stride != self.desc.stride:
             raise ValueError("dy has row stride %d, the output %d" % (stride, self.desc.stride))
-        B.ftp_checkpoint_act_backward(self.desc, self.codes.data_ptr(), self.exponents.data_ptr(), act, slope, p, q, self._stream())
+        self._call(B.ftp_checkpoint_act_backward, self.desc, self.codes.data_ptr(), self.exponents.data_ptr(), act, slope, p, q)
         return out
 
     def wgrad(self, dy):
@@ -206,8 +213,8 @@ class Checkpoint(_Operator):
         if self.dw is None:
             raise ValueError("made without `outputs`")
         p, stride = self._rows("dy", dy, self.outputs)
-        B.ftp_checkpoint_wgrad(self.desc, self.codes.data_ptr(), self.exponents.data_ptr(), p, stride, self.outputs, self.dw.data_ptr(),
-                               self._ws.data_ptr(), self._stream())
+        self._call(B.ftp_checkpoint_wgrad, self.desc, self.codes.data_ptr(), self.exponents.data_ptr(), p, stride, self.outputs, self.dw.data_ptr(),
+                   self._ws.data_ptr())
         return self.dw
 
 
@@ -253,8 +260,8 @@ class Attention(_Operator):
                 _dense("kv_lens", kv_lens, (self.batch,), torch.int32, self.device))
 
     def forward(self, q, k, v, q_lens=None, kv_lens=None):
-        B.ftp_attention_forward(self.desc, *self._inputs(q, k, v, q_lens, kv_lens), self.out.data_ptr(), self.lse.data_ptr(),
-                                self._ws.data_ptr(), self._stream())
+        self._call(B.ftp_attention_forward, self.desc, *self._inputs(q, k, v, q_lens, kv_lens), self.out.data_ptr(), self.lse.data_ptr(),
+                   self._ws.data_ptr())
         return self.out
 
     def backward(self, dout, q, k, v, q_lens=None, kv_lens=None):
@@ -263,6 +270,6 @@ class Attention(_Operator):
             raise ValueError("made without `training`")
         inputs = self._inputs(q, k, v, q_lens, kv_lens)
         pd = self._tensor("dout", dout, self.q_shape)
-        B.ftp_attention_backward(self.desc, pd, *inputs, self.out.data_ptr(), self.lse.data_ptr(), self.dq.data_ptr(), self.dk.data_ptr(),
-                                 self.dv.data_ptr(), self._ws.data_ptr(), self._stream())
+        self._call(B.ftp_attention_backward, self.desc, pd, *inputs, self.out.data_ptr(), self.lse.data_ptr(), self.dq.data_ptr(), self.dk.data_ptr(),
+                   self.dv.data_ptr(), self._ws.data_ptr())
         return self.dq, self.dk, self.dv
