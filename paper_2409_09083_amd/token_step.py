@@ -5,7 +5,8 @@
 The early layers run through `harness.Session`; their output map is normalised and turned into token rows, goes through attention and a
 two-layer perceptron (both residual), and the loss' gradient comes back the same way into the map's delta and the filters.  What the
 block's backward pass needs of its linear layers' inputs, of its second norm's input and of the perceptron's hidden layer is held as
-8-bit checkpoints; attention's probabilities are computed again.  Plain matrix products are torch's.
+8-bit checkpoints, and the tensors themselves are let go; attention keeps q, k, v and its output, and computes its probabilities again.
+Plain matrix products are torch's.
 """
 import argparse
 
@@ -29,9 +30,10 @@ class TokenBlock:
         self.norm1 = Norm(batch, pixels, channels, dtype, x_layout="map", device=device)
         self.norm2 = Norm(batch, pixels, channels, dtype, device=device)
         self.attention = Attention(batch, heads, kv_heads, pixels, pixels, self.hd, dtype, device=device)
-        kept = lambda cols, outputs=0: Checkpoint(self.rows, cols, dtype, block, outputs, device)       # noqa: E731
-        self.kept_n1, self.kept_out, self.kept_x2 = kept(channels, width), kept(channels, channels), kept(channels)
+        kept = lambda cols, outputs=0: Checkpoint(self.rows, cols, dtype, block, outputs, device)        # noqa: E731
+        self.kept_n1, self.kept_x2 = kept(channels, width), kept(channels)
         self.kept_n2, self.kept_h, self.kept_a = kept(channels, hidden), kept(hidden), kept(hidden, channels)
+        self.out8 = kept(channels, channels)                        # (only in the backward pass, for the weight gradient: attention keeps its output itself)
         g = torch.Generator(device=device).manual_seed(seed)
         t = self.norm1.tdtype
 
@@ -48,18 +50,20 @@ class TokenBlock:
         b, n, c = self.shape
         p = self.params
         self.x = y.view(b, c, n).transpose(1, 2)                    # the map seen as tokens
-        n1 = self.norm1.forward(self.x, p["g1"], p["b1"]).view(-1, c)
+        new = lambda cols: torch.empty((self.rows, cols), dtype=y.dtype, device=y.device)      # noqa: E731
+        n1 = new(c)                                                 # (gone when this pass ends, as n2 and a)
+        self.norm1.forward(self.x, p["g1"], p["b1"], out=n1.view(self.shape))
         self.kept_n1.pack(n1)
         qkv = (n1 @ p["wqkv"].t()).view(b, n, -1, self.hd)
         self.qkv = qkv.split((self.heads, self.kv_heads, self.kv_heads), 2)
         out = self.attention.forward(*self.qkv).view(-1, c)
-        self.kept_out.pack(out)
         x2 = torch.addmm(self.x.reshape(-1, c), out, p["wo"].t())
         self.kept_x2.pack(x2)
-        n2 = self.norm2.forward(x2.view(self.shape), p["g2"], p["b2"]).view(-1, c)
+        n2 = new(c)
+        self.norm2.forward(x2.view(self.shape), p["g2"], p["b2"], out=n2.view(self.shape))
         self.kept_n2.pack(n2)
         self.kept_h.pack(n2 @ p["w1"].t())
-        a = self.kept_h.unpack(act="gelu")
+        a = self.kept_h.unpack(act="gelu", out=new(self.kept_h.cols))
         self.kept_a.pack(a)
         return torch.addmm(x2, a, p["w2"].t())
 
@@ -67,11 +71,12 @@ class TokenBlock:
         """dz: rows; returns the gradient of y as a map [batch][channels][pixels].  Parameter gradients: self.grads (32 bits)."""
         p, g = self.params, self.grads
         g["w2"] = self.kept_a.wgrad(dz)
-        dh = self.kept_h.act_backward(dz @ p["w2"], act="gelu")
+        dh = dz @ p["w2"]
+        self.kept_h.act_backward(dh, act="gelu", out=dh)
         g["w1"] = self.kept_n2.wgrad(dh)
         dx2, g["g2"], g["b2"] = self.norm2.backward((dh @ p["w1"]).view(self.shape), self.kept_x2, p["g2"])
         dx2 = dx2.view(-1, self.c) + dz
-        g["wo"] = self.kept_out.wgrad(dx2)
+        g["wo"] = self.out8.pack(self.attention.out.view(-1, self.c)).wgrad(dx2)
         dout = (dx2 @ p["wo"]).view(self.shape[0], self.shape[1], self.heads, self.hd)
         dqkv = torch.cat(self.attention.backward(dout, *self.qkv), 2).view(self.rows, -1)
         g["wqkv"] = self.kept_n1.wgrad(dqkv)
@@ -82,11 +87,21 @@ class TokenBlock:
         for name, w in self.params.items():
             w.add_(self.grads[name].to(w.dtype), alpha=-lr)
 
+    def _kept(self):
+        return self.kept_n1, self.kept_x2, self.kept_n2, self.kept_h, self.kept_a
+
     def kept_bytes(self):
         """Bytes of the 8-bit checkpoints, and of the same values in the block's own type."""
-        kept = (self.kept_n1, self.kept_out, self.kept_x2, self.kept_n2, self.kept_h, self.kept_a)
-        return (sum(k.codes.numel() + k.exponents.numel() for k in kept),
-                sum(k.codes.numel() for k in kept) * self.params["wo"].element_size())
+        return (sum(k.codes.nbytes + k.exponents.nbytes for k in self._kept()),
+                sum(k.codes.numel() for k in self._kept()) * self.params["wo"].element_size())
+
+    def other_bytes(self):
+        """Bytes of what else stays between the passes: q, k, v, attention's output and the statistics; the buffers of gradients and scratch, which every step writes again."""
+        n1, n2, a = self.norm1, self.norm2, self.attention
+        tensors = [a.out, a.lse, n1.mean, n1.rstd, n2.mean, n2.rstd]
+        buffers = [a.dq, a.dk, a.dv, a._ws] + [t for n in (n1, n2) for t in (n.dx_buffer, n.dgamma, n.dbeta, n._ws)] + [t for k in self._kept() for t in (k.dw, k._ws)]
+        buffers += [self.out8.codes, self.out8.exponents, self.out8.dw, self.out8._ws]
+        return (sum(t.nbytes for t in tensors) + self.qkv[0].untyped_storage().nbytes(), sum(t.nbytes for t in buffers if t is not None))
 
 
 class TokenStep:
@@ -135,7 +150,9 @@ def main(argv=None):
         end.synchronize()
         print("step %d: loss %.5f, %.2f ms" % (i, float(loss), start.elapsed_time(end)))
     held, plain = s.block.kept_bytes()
-    print("kept between the passes: %.1f MB in 8 bits, %.1f MB otherwise" % (held / 1e6, plain / 1e6))
+    tensors, buffers = s.block.other_bytes()
+    print("kept between the passes: %.1f MB in 8 bits for %.1f MB, and %.1f MB of q, k, v, attention's output and statistics" % (held / 1e6, plain / 1e6, tensors / 1e6))
+    print("buffers of gradients and scratch: %.1f MB" % (buffers / 1e6))
 
 
 if __name__ == "__main__":

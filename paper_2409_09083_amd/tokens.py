@@ -84,7 +84,8 @@ class Norm(_Operator):
     """Layer norm over the channels of outer x inner tokens (outer: images or sequences, inner: pixels or tokens).
 
     y_layout, x_layout: how the buffers of y (forward) and dx (backward) lie: "rows" [outer][inner][channels] or "map"
-    [outer][channels][inner].  y, dx: those buffers seen as [outer][inner][channels]; y_buffer, dx_buffer: as they lie."""
+    [outer][channels][inner].  y, dx: those buffers seen as [outer][inner][channels]; y_buffer, dx_buffer: as they lie.  A buffer is made by the
+    first call that needs it."""
 
     def __init__(self, outer, inner, channels, dtype="f32", eps=1e-5, x_layout="rows", y_layout="rows", device="cuda"):
         self.tdtype, code = _types(dtype)
@@ -96,11 +97,10 @@ class Norm(_Operator):
         self._strides = {}
         self._ws_bytes = B.ftp_norm_workspace(self.desc)
         self._layouts = {"x": x_layout, "y": y_layout}
-        self.y_buffer, self.y = self._buffer("y")
+        self._y = self._y_buffer = None
         self.mean = torch.empty((outer, inner), dtype=torch.float32, device=self.device)
         self.rstd = torch.empty_like(self.mean)
-        self._outputs = self.y.data_ptr(), self.mean.data_ptr(), self.rstd.data_ptr()
-        self._set_strides("y_stride", self.y.stride())
+        self._stats = self.mean.data_ptr(), self.rstd.data_ptr()
         self.dx = self.dx_buffer = self.dgamma = self.dbeta = self._ws = None
 
     def _buffer(self, of):
@@ -111,14 +111,42 @@ class Norm(_Operator):
         t = torch.empty((o, c, i), dtype=self.tdtype, device=self.device)
         return t, t.transpose(1, 2)
 
+    def _own_y(self):
+        """The buffer of y, made when it is first asked for."""
+        if self._y is None:
+            self._y_buffer, self._y = self._buffer("y")
+            self._outputs = (self._y.data_ptr(),) + self._stats
+            self._set_strides("y_stride", self._y.stride())
+        return self._y
+
+    @property
+    def y(self):
+        return self._own_y()
+
+    @property
+    def y_buffer(self):
+        self._own_y()
+        return self._y_buffer
+
     def _param(self, name, t):
         return _dense(name, t, (self.shape[2],), self.tdtype, self.device)
 
-    def forward(self, x, gamma=None, beta=None):
+    def forward(self, x, gamma=None, beta=None, out=None):
+        """y, in `out` ([outer][inner][channels], any strides, apart from x) or the object's buffer."""
         px = _need("x", x, self.shape, self.tdtype, self.device)
         self._set_strides("x_stride", x.stride())
-        self._call(B.ftp_norm_forward, self.desc, px, self._param("gamma", gamma), self._param("beta", beta), *self._outputs)
-        return self.y
+        if out is None:
+            if self._y is None:
+                self._own_y()
+            self._call(B.ftp_norm_forward, self.desc, px, self._param("gamma", gamma), self._param("beta", beta), *self._outputs)
+            return self._y
+        py, own = _need("out", out, self.shape, self.tdtype, self.device), self.desc.y_stride[:]
+        self.desc.y_stride[:] = out.stride()
+        try:
+            self._call(B.ftp_norm_forward, self.desc, px, self._param("gamma", gamma), self._param("beta", beta), py, *self._stats)
+        finally:
+            self.desc.y_stride[:] = own
+        return out
 
     def backward(self, dy, x, gamma=None, mean=None, rstd=None):
         """x: the forward pass' input, or a Checkpoint of it (outer * inner rows of the channels).  mean, rstd: default: as the last
