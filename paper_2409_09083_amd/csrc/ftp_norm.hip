@@ -9,6 +9,7 @@
 //
 // Measured: k_norm_rows 4 tokens of 256 2.3 us (one round trip to memory and the launch); k_norm_back_rows 92416 x 512 bfloats 46.6 us, 285 MB, 6.1 TB/s (a large copy: 4.8, but the
 // last-level cache keeps part), 17797 x 250 fp32 from a checkpoint 13.5 us, 40 MB; k_norm_params behind it 4.2 us; k_norm_tiles 16 images of 76 x 76, 128 channels fp32 to rows 27 us, 95 MB, 3.5 TB/s.
+#include "ftp_norm_rows.h"
 #include "ftp_tokens.h"
 
 #include <algorithm>
@@ -30,9 +31,7 @@ struct RowArgs {
 __device__ __forceinline__ long long row_offset(long long row, long long inner, long long rows, long long so, long long si)
 {
     if (inner == rows) return row * si;
-    long long o;
-    if (rows <= 0x7FFFFFFFll) o = (uint32_t)row / (uint32_t)inner;
-    else o = row / inner;
+    const long long o = (uint32_t)row / (uint32_t)inner;            // (rows are fewer than 2^31)
     return o * so + (row - o * inner) * si;
 }
 
@@ -564,33 +563,22 @@ int row_vec(const RowArgs& a, int es, const void* const* ptrs, int n, const int8
     return 1;
 }
 
-// Lanes of a row and vectors of a lane: a row in one wavefront where its vectors fit (at most 8, and 32 values), else a workgroup.  NV 0: too long for registers.
-struct RowForm { int lanes, nv; bool wide; };
-RowForm row_form(int C, int vec)
-{
-    const int vecs = (C + vec - 1) / vec, most = std::min(8, 32 / vec);
-    if (vecs <= 64 * most) {
-        const int lanes = std::min(64, ceil_pow2(vecs));
-        return {lanes, ceil_pow2((vecs + lanes - 1) / lanes), false};
-    }
-    if (vecs <= 256 * most) return {256, ceil_pow2((vecs + 255) / 256), true};
-    return {256, 0, true};
-}
-
 template <typename T, int VEC, int NV>
 void run_rows(const RowArgs& a, const RowForm& f, bool back, unsigned grid, hipStream_t st)
 {
-    if constexpr (VEC * NV <= 32) {
-        if (!back) {
-            if (f.wide) k_norm_rows<T, VEC, NV, true><<<grid, 256, 0, st>>>(a);
-            else k_norm_rows<T, VEC, NV, false><<<grid, 256, 0, st>>>(a);
-        } else if (a.codes) {
-            if (f.wide) k_norm_back_rows<T, VEC, NV, true, true><<<grid, 256, 0, st>>>(a);
-            else k_norm_back_rows<T, VEC, NV, false, true><<<grid, kBackThreads, 0, st>>>(a);
-        } else {
-            if (f.wide) k_norm_back_rows<T, VEC, NV, true, false><<<grid, 256, 0, st>>>(a);
-            else k_norm_back_rows<T, VEC, NV, false, false><<<grid, kBackThreads, 0, st>>>(a);
+    // (f.wide and NV are what row_form() gives)
+    if constexpr (row_built(VEC, NV, true)) {
+        if (f.wide) {
+            if (!back) k_norm_rows<T, VEC, NV, true><<<grid, 256, 0, st>>>(a);
+            else if (a.codes) k_norm_back_rows<T, VEC, NV, true, true><<<grid, 256, 0, st>>>(a);
+            else k_norm_back_rows<T, VEC, NV, true, false><<<grid, 256, 0, st>>>(a);
+            return;
         }
+    }
+    if constexpr (row_built(VEC, NV, false)) {
+        if (!back) k_norm_rows<T, VEC, NV, false><<<grid, 256, 0, st>>>(a);
+        else if (a.codes) k_norm_back_rows<T, VEC, NV, false, true><<<grid, kBackThreads, 0, st>>>(a);
+        else k_norm_back_rows<T, VEC, NV, false, false><<<grid, kBackThreads, 0, st>>>(a);
     }
 }
 

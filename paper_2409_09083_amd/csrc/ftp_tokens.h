@@ -35,7 +35,6 @@ void attention_backward(const ftp_attention_shape& s, const void* dout, const vo
                         const void* out, const float* lse, void* dq, void* dk, void* dv, float* ws, hipStream_t st);
 
 inline bool aligned(const void* p, size_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
-inline int ceil_pow2(int v) { int p = 1; while (p < v) p <<= 1; return p; }
 inline long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
 
 // VEC neighbouring elements as they lie in memory, loaded and stored at once.
