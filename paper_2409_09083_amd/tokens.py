@@ -92,7 +92,7 @@ class Norm(_Operator):
         if x_layout not in _LAYOUTS or y_layout not in _LAYOUTS:
             raise ValueError("a layout is one of %s" % ", ".join(_LAYOUTS))
         self.device = _device(device)
-        self.shape = torch.Size((outer, inner, channels))
+        self.shape, self._channels = torch.Size((outer, inner, channels)), torch.Size((channels,))
         self.desc = B.ftp_norm_shape(outer=outer, inner=inner, channels=channels, dtype=code, eps=eps)
         self._strides = {}
         self._ws_bytes = B.ftp_norm_workspace(self.desc)
@@ -129,7 +129,7 @@ class Norm(_Operator):
         return self._y_buffer
 
     def _param(self, name, t):
-        return _dense(name, t, (self.shape[2],), self.tdtype, self.device)
+        return _dense(name, t, self._channels, self.tdtype, self.device)
 
     def forward(self, x, gamma=None, beta=None, out=None):
         """y, in `out` ([outer][inner][channels], any strides, apart from x) or the object's buffer."""
