@@ -242,7 +242,7 @@ int ftp_profile_read(ftp_plan_t* plan, ftp_kernel_time* out, int32_t capacity, i
  * outer * inner is at most 2^31 - 1. */
 typedef struct {
     int64_t outer, inner;
-    int32_t channels;              /* >= 1; at most 4096 unless all tensors of a pass have channel stride 1 */
+    int32_t channels;              /* >= 1; at most 4096 unless all tensors that a pass uses have channel stride 1 */
     int32_t dtype;                 /* ftp_dtype of x, y, gamma, beta, dy, dx */
     float eps;
     int32_t reserved;
@@ -305,8 +305,10 @@ int ftp_checkpoint_wgrad(const ftp_checkpoint_shape* shape, const int8_t* codes,
  * 0 .. q_len / kv_len are cut to that); query i sees the keys j < kv_lens[b], and with `causal` only
  * j <= i + kv_lens[b] - q_lens[b] (the last query sees the last key).  A query that sees no key, and one beyond
  * q_lens[b], has out = 0, lse = -infinity and dq = 0; a key that no query sees has dk = dv = 0; a query that sees one key has probability 1
- * there and dq = 0, exactly.  Keys, values and queries that are not seen do not reach any result, whatever they hold (causal calls with such values that
- * are not finite may take a second walk over the keys).  fp32 numbers are multiplied as three bfloats each: a seen infinity, or number above the largest bfloat, gives NaN.
+ * there and dq = 0, exactly.  Keys, values and queries that are not seen do not reach any result, whatever they hold (causal calls where they are not
+ * finite may take a second walk over the keys, whose results are rounded a little differently).  fp32 numbers are multiplied as three bfloats each: a seen infinity, or number above the largest bfloat, gives NaN, and numbers
+ * below 2^-110 lose low bits.  Where the tensors are bfloats, probabilities and their gradients are rounded to bfloats as
+ * operands of the products behind them, and dout . out takes the rounded out for queries among more than 256 keys.
  * Element (b, t, h, c) of q lies at q_stride[0] * b + q_stride[1] * t + q_stride[2] * h + c; likewise the others; no stride is
  * negative.  Inputs may be broadcast (stride 0); gradients then come out unsummed, in buffers of their own.  q_len and kv_len may be 0.
  * A launch's workgroups of 128 (64) queries or keys of an image's key head are fewer than 2^24, counted over all of them. */

@@ -4,9 +4,10 @@
 // (lane % 32), so maximum, sum and rescaling are per lane; P^T is then the operand of O^T = V^T P^T as it lies (ftp_attention.h).  Few rows (single tokens): the keys are
 // split over workgroups, whose unnormalised rows a second kernel joins.
 //
-// Measured: prompts, 4 images of 1550 to 2704 tokens, 8 heads of 128 on 2, causal, bfloats: 60 us, 563 TFLOP/s (bound by the longest workgroups: 42 tiles behind each other on a SIMD shared
-// with another such, 28 on average); 64 heads x 5776 tokens of 64: 0.66-0.70 ms, 780-830 TFLOP/s (vector unit 79 % busy, a third of it exponentials; matrix cores 42 %); one token of 8 streams on up to 8192
-// keys: 23 us with the join, 91 MB, 4.0 TB/s.
+// Measured: prompts, 4 images of 1550 to 2704 tokens, 8 heads of 128 on 2, causal, bfloats: 61.5 us, 552 TFLOP/s (bound by the longest workgroups: 42 tiles behind each other on a SIMD shared
+// with another such, 28 on average); 64 heads x 5776 tokens of 64: 0.59-0.64 ms, 850-920 TFLOP/s (vector unit 81 % busy, a third of it exponentials; matrix cores 46 %); one token of 8 streams on up to 8192
+// keys: 26 us among other calls, 23 with what the call before left in the last-level cache (91 MB, 4.0 TB/s), 4 of them the join.  fp32: prompts 323 us (105 TFLOP/s), one token 106 (1.7 TB/s:
+// a CU holds one workgroup).
 #include "ftp_attention.h"
 
 #include <algorithm>
@@ -283,9 +284,9 @@ void run(const AttentionArgs& a, bool two, unsigned grid, hipStream_t st)
 
 }  // namespace
 
-// Wavefronts to a row.  Two (bfloats: an fp32 tile is one unit) where a workgroup has at most 64 rows anyway (256 streams of one token on 200 keys 26.4 -> 21.3 us), and where 128 rows each
-// leave the chip few chains of tiles, or uneven ones that causal calls end on (4 x 12 heads x 577 tokens 23.3 -> 13.8 us, 2 x 8 x 2600 55 -> 48, causal 4 x 8 x 2600 66 -> 51); heads of 128 pay
-// more for staging twice (causal 2 x 8 x 2600 56 -> 51, all pairs 78 -> 87).  With enough of them 128 rows are better: 8 x 8 x 5776 tokens 671 us, halves 720.
+// Wavefronts to a row.  Two (bfloats: an fp32 tile is one unit) where a workgroup has at most 64 rows anyway (256 streams x 8 heads of one token on 200 keys 25.8 -> 23.7 us), and where 128 rows each
+// leave the chip few chains of tiles, or uneven ones that causal calls end on (4 x 12 heads x 577 tokens 22.6 -> 13.1 us, 2 x 8 x 2600 52 -> 46, causal 4 x 8 x 2600 62 -> 49); heads of 128 pay
+// more for staging twice (causal 2 x 8 x 2600 56 -> 50, all pairs 77 -> 88).  With enough of them 128 rows are better: 8 x 8 x 5776 tokens 597 us, halves 656.
 int attention_halves(const ftp_attention_shape& s)
 {
     const long long rows = (long long)s.q_len * (s.heads / s.kv_heads), groups = ceil_div(rows, 128) * s.batch * s.kv_heads;

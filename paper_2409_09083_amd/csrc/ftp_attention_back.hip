@@ -6,8 +6,8 @@
 // atomics, in an order that changes.  In dq S^T and dP^T have a row per lane, in dkv S and dP a key per lane, so that P and dS again are operands as they lie
 // (ftp_attention.h).  Where 128-row (key) blocks are too few for the CUs, the other axis is split and the parts are added up by a third kernel.
 //
-// Measured, 64 heads x 5776 tokens of 64, bfloats (1.91 TFLOP in seven products, 1.37 in five): dq 0.81-0.87 ms (940-1010 TFLOP/s of its three products), dk and dv 1.20-1.28 ms (850-910 of their four); a large
-// library product reaches 1265 on the same card.  Matrix cores busy 56 and 44-49 % of the cycles, at a clock that the load lowers to 1.9-2.05 GHz; LDS 30-37 %, without bank conflicts; without any load from
+// Measured, 64 heads x 5776 tokens of 64, bfloats (1.91 TFLOP in seven products, 1.37 in five): dq 0.80-0.87 ms (940-1020 TFLOP/s of its three products), dk and dv 1.20-1.30 ms (840-910 of their four); a large
+// library product reaches 1265 on the same card.  Matrix cores busy 58 and 43-49 % of the cycles, at a clock that the load lowers to 1.9-2.05 GHz; LDS 30-37 %, without bank conflicts; without any load from
 // memory the two took 0.78 and 0.99 ms.  577 x 701 tokens of 40, fp32, 3 x 2 key heads: dq 25 us, dk and dv 39, sums of the splits 5 + 5: a workgroup's chain of 4 to 8 tiles.
 #include "ftp_attention.h"
 
@@ -21,8 +21,8 @@ template <typename T, int D> constexpr int kKeys = sizeof(T) == 4 ? 32 : 64;    
 
 // A workgroup is 128 rows against tiles of 64 keys (fp32: 32), two tiles in LDS.  The compiler's order of a tile's instructions is kept: by hand as in k_attention_dkv it was slower here (0.80 -> 0.93 ms).
 //
-// HALVES 2, bfloats: 64 rows, each by two wavefronts that take a unit of every tile and add up their rows through LDS at the end (attention_halves(): 4 x 12 heads x 577 tokens 53.9 -> 45.7 us the pass,
-// causal 4 x 8 x 2600 164 -> 151).  fp32 tiles of two units for it would cost the second workgroup of a CU: 16 heads x 1144 of 64 161 -> 207.
+// HALVES 2, bfloats: 64 rows, each by two wavefronts that take a unit of every tile and add up their rows through LDS at the end (attention_halves(): 4 x 12 heads x 577 tokens 52.6 -> 45.3 us the pass,
+// causal 4 x 8 x 2600 155 -> 144).  fp32 tiles of two units for it would cost the second workgroup of a CU: 16 heads x 1144 of 64 161 -> 207.
 template <typename T, int D, bool VEC, int HALVES>
 __global__ __launch_bounds__(256, (kPerCu<T, D>)) void k_attention_dq(const AttentionArgs a)
 {

@@ -6,8 +6,8 @@
 // lie (dy after its split, codes after their conversion) and read through the transposing LDS load: 4 rows x 16 columns a 16 lanes.  A stage is 64 rows (32 of fp32), two stages in LDS
 // and two more on their way in registers: with one, a workgroup waited for HBM most of the time (331 us).  The shares' blocks are added up by a second kernel in a fixed order.
 //
-// Measured: 46208 rows, 512 -> 1024, bfloats: 80 us with the sum (48.5 GFLOP, 600 TFLOP/s; a large library product of bfloats reaches 1265): matrix cores busy 31 % of the cycles, the codes'
-// conversion and the stores into LDS take the issue slots between them, and 512 workgroups end in one uneven round.  4995 rows, 202 -> 133, fp32: 16.5 us, of which 14 are a workgroup's chain of
+// Measured: 46208 rows, 512 -> 1024, bfloats: a pass 86 us among others (48.5 GFLOP, 564 TFLOP/s; a large library product of bfloats reaches 1265), 80 on inputs of the call before; in a trace
+// the product 81 and the sum 6.5; fp32 dy 160: matrix cores busy 31 % of the cycles, the codes' conversion and the stores into LDS take the issue slots between them, and 512 workgroups end in one uneven round.  4995 rows, 202 -> 133, fp32: 16.5 us, of which 14 are a workgroup's chain of
 // two stages, loads, split, products, store, and the rest the sum of 78 shares.
 #include "ftp_tokens.h"
 #include "ftp_order.h"

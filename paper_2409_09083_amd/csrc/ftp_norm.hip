@@ -7,8 +7,8 @@
 // Tokens whose channels lie side by side (rows) stay in registers: 2^k lanes a row, 16 bytes a load where alignment lets it.  Anything else (NCHW
 // maps, map to rows) goes through LDS in tiles of up to 64 tokens x all channels, read along whichever axis is contiguous.
 //
-// Measured: k_norm_rows 4 tokens of 256 2.3 us (one round trip to memory and the launch); k_norm_back_rows 92416 x 512 bfloats 46.6 us, 285 MB, 6.1 TB/s (a large copy: 4.8, but the
-// last-level cache keeps part), 17797 x 250 fp32 from a checkpoint 13.5 us, 40 MB; k_norm_params behind it 4.2 us; k_norm_tiles 16 images of 76 x 76, 128 channels fp32 to rows 27 us, 95 MB, 3.5 TB/s.
+// Measured: k_norm_rows 4 tokens of 256 2.3 us (one round trip to memory and the launch); 92416 x 512 bfloats 33 us, 190 MB, 5.7 TB/s (fp32 67); k_norm_back_rows on as many 46.8 us,
+// 285 MB, 6.1 TB/s (a large copy: 4.8, but the last-level cache keeps part), 17797 x 250 fp32 from a checkpoint 13.1 us, 40 MB; k_norm_params behind it 4.1 us; k_norm_tiles 16 images of 76 x 76, 128 channels fp32 to rows 27 us, 95 MB, 3.5 TB/s.
 #include "ftp_norm_rows.h"
 #include "ftp_tokens.h"
 
@@ -479,7 +479,9 @@ __global__ __launch_bounds__(256) void k_norm_tiles(const TileArgs a)
     });
 }
 
-// A workgroup walks over tiles; channels' sums over a tile's tokens go to LDS, a thread its own channels, and at the end to memory as the workgroup's share.
+// A workgroup walks over tiles; channels' sums over a tile's tokens go to LDS, a thread its own channels, and at the end to memory as the workgroup's share.  16 images of 76 x 76, 128
+// channels, x a map, dy rows: fp32 75 us (143 MB, 1.9 TB/s), bfloats 72: bound by what follows each other in a workgroup, the load of a tile, two sums, the store, and sums over its tokens by as
+// many threads as there are channels.
 template <typename T>
 __global__ __launch_bounds__(256) void k_norm_back_tiles(const TileArgs a)
 {
@@ -609,7 +611,8 @@ size_t tile_bytes(const ftp_norm_shape& s, int px, bool back)
     const size_t es = s.dtype == FTP_BF16 ? 2 : 4;
     return (256 + (back ? 256 : 128)) * 4 + (back ? 3 : 2) * (size_t)s.channels * 4 + (back ? 2 : 1) * (size_t)s.channels * (px + 4 / es) * es;
 }
-// Tokens a tile: 128 bytes of a map's row; fewer, down to 64 bytes, where a CU would hold less than four workgroups, and as few as it takes to stay within 64 KB.
+// Tokens a tile: 128 bytes of a map's row; fewer, down to 64 bytes, where a CU would hold less than four workgroups, and fewer still, down to one, above 64 KB (4096 fp32 channels,
+// backward: 114 KB of a CU's 160).
 int tile_tokens(const ftp_norm_shape& s, bool back)
 {
     const int es = s.dtype == FTP_BF16 ? 2 : 4;
