@@ -515,8 +515,8 @@ __global__ __launch_bounds__(256, (D == 128 || sizeof(T) == 4 ? 1 : 2)) void k_a
             go = go && both_max((spoiled_k & ~bad_channels(dk)) | (spoiled_v & ~bad_channels(dv)) ? 1.0f : 0.0f) > 0;
         }
         if (!__syncthreads_or(go)) return;
-        row_operands<T, MY>(k, go ? kr + c0 : nullptr, my, VEC, a.scale < 0);
-        row_operands<T, MY>(v, go ? vr + c0 : nullptr, my, VEC, false);
+        row_operands<T, MY>(k, inside ? kr + c0 : nullptr, my, VEC, a.scale < 0);        // (of all keys: another wavefront may need this one's part of the scores)
+        row_operands<T, MY>(v, inside ? vr + c0 : nullptr, my, VEC, false);
         walk(begin);
         if (go) store(key);
     }

@@ -119,3 +119,18 @@ def test_one_bad_token_in_the_middle(shape, bad, dtype):
             assert near(getattr(got, t)[:, last + 1:], getattr(want, t)[:, last + 1:]), t
         assert not got.dv[:, :last + 1].isfinite().any()
         assert torch.equal(got.dq[:, :first + 9], want.dq[:, :first + 9]) and torch.equal(got.dq[:, first + 10:], want.dq[:, first + 10:])
+
+
+@pytest.mark.parametrize("c", [3, 97])
+@pytest.mark.parametrize("shape", [(8, 8, 8, 300, 300, 128), (4, 12, 4, 260, 260, 100)])
+def test_one_channel_of_wide_fp32_heads(shape, c):
+    """Gradients of a key's first and last 64 channels are two wavefronts' work, of which one bad channel of a query or of its dout spoils one: the scores are both's all the same."""
+    q, k, v, do = A._make(*shape, "f32")
+    want = A._run(q, k, v, do, "f32", True)
+    for which in ("dout", "query"):
+        q2, do2 = q.clone(), do.clone()
+        (do2 if which == "dout" else q2)[:, 70, ::2, c] = math.nan
+        got = A._run(q2, k, v, do2, "f32", True)
+        for t in ("dk", "dv"):
+            x, y = getattr(got, t)[:, 71:], getattr(want, t)[:, 71:]
+            assert x.isfinite().all() and (x - y).abs().max() <= 2e-5 * y.abs().max(), (which, t)
