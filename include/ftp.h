@@ -305,7 +305,7 @@ int ftp_checkpoint_wgrad(const ftp_checkpoint_shape* shape, const int8_t* codes,
  * 0 .. q_len / kv_len are cut to that); query i sees the keys j < kv_lens[b], and with `causal` only
  * j <= i + kv_lens[b] - q_lens[b] (the last query sees the last key).  A query that sees no key, and one beyond
  * q_lens[b], has out = 0, lse = -infinity and dq = 0; a key that no query sees has dk = dv = 0; a query that sees one key has probability 1
- * there and dq = 0, exactly.  Keys, values and queries that are not seen do not reach any result, whatever they hold (causal calls where they are not
+ * there and dq = 0, exactly (of a score that is a number).  Keys, values and queries that are not seen do not reach any result, whatever they hold (causal calls where they are not
  * finite may take a second walk over the keys, whose results are rounded a little differently).  fp32 numbers are multiplied as three bfloats each: a seen infinity, or number above the largest bfloat, gives NaN, and numbers
  * below 2^-110 lose low bits.  Where the tensors are bfloats, probabilities and their gradients are rounded to bfloats as
  * operands of the products behind them, and dout . out takes the rounded out for queries among more than 256 keys.

@@ -19,6 +19,9 @@ namespace {
 
 template <typename T, int D> constexpr int kKeys = sizeof(T) == 4 ? 32 : 64;       // keys of a tile
 
+// The gradient of a row's scores where it sees one key, from its log-sum, which is that key's score: 0, or NaN where the score is no number.
+__device__ __forceinline__ float one_key(float lse) { return lse - lse; }
+
 // A workgroup is 128 rows against tiles of 64 keys (fp32: 32), two tiles in LDS.  The compiler's order of a tile's instructions is kept: by hand as in k_attention_dkv it was slower here (0.80 -> 0.93 ms).
 //
 // HALVES 2, bfloats: 64 rows, each by two wavefronts that take a unit of every tile and add up their rows through LDS at the end (attention_halves(): 4 x 12 heads x 577 tokens 52.6 -> 45.3 us the pass,
@@ -176,12 +179,14 @@ __global__ __launch_bounds__(256, (kPerCu<T, D>)) void k_attention_dq(const Atte
             return;
         }
         const int i = query_of(a, row), head = kvh * a.group + row - i * a.group;
+        const float zero = seen ? one_key(lse) : 0.0f;
+        const f32x4 none = {zero, zero, zero, zero};
         T* p = (T*)a.dq + b * a.dqs[0] + i * a.dqs[1] + head * a.dqs[2];
 #pragma unroll
         for (int d = 0; d < DT; ++d)
 #pragma unroll
             for (int r = 0; r < 16; r += 4) {
-                const f32x4 v = seen > 1 ? f32x4{dq[d][r], dq[d][r + 1], dq[d][r + 2], dq[d][r + 3]} * a.scale : f32x4{0, 0, 0, 0};      // (one key: probability 1, no gradient)
+                const f32x4 v = seen > 1 ? f32x4{dq[d][r], dq[d][r + 1], dq[d][r + 2], dq[d][r + 3]} * a.scale : none;
                 store4(p, 32 * d + 8 * (r >> 2) + 4 * h, a.d, a.vec, v[0], v[1], v[2], v[3]);
             }
     };
@@ -279,7 +284,7 @@ __global__ __launch_bounds__(256, (D == 128 || sizeof(T) == 4 ? 1 : 2)) void k_a
     };
     sq.init([&](int r) { return offset(a.qs, r); }, a.d);
     sg.init([&](int r) { return offset(a.gs, r); }, a.d);
-    // Rows one0 .. one1 - 1 see one key, the first: their probability is 1 and their ds 0, exactly.  They come in with q = 0 and a log-sum of 0.
+    // Rows one0 .. one1 - 1 see one key, the first: their probability is 1 and their ds 0, exactly.  They come in with q = 0 and a log-sum of 0 (or NaN).
     const int first_seeing = a.causal ? min(max(0, -len.off), len.q) : 0;
     const int one0 = first_seeing * a.group, one1 = len.k == 1 ? rows : a.causal && len.off <= 0 ? min(one0 + a.group, rows) : one0;
     const int queries = a.group <= BM ? each / a.group : 0;
@@ -290,7 +295,8 @@ __global__ __launch_bounds__(256, (D == 128 || sizeof(T) == 4 ? 1 : 2)) void k_a
         sg.fetch(to.tile[1], gp + i0 * a.gs[1] + j0 * a.gs[2], there);
         if (threadIdx.x < BM) {
             ss = tr < there ? len.seen(a, i0 + ti) : 0;
-            sl = ss > 1 ? lsep[(long long)(j0 + tj) * a.q_len + i0 + ti] * kLog2e : ss ? 0.0f : INFINITY;
+            sl = ss ? lsep[(long long)(j0 + tj) * a.q_len + i0 + ti] : INFINITY;
+            sl = ss == 1 ? one_key(sl) : sl * kLog2e;
             sd = ss ? -deltap[t * each + tr] : 0.0f;
         }
     };
@@ -505,9 +511,12 @@ __global__ __launch_bounds__(256, (D == 128 || sizeof(T) == 4 ? 1 : 2)) void k_a
             if (go && sees > key) {
                 const T* qr = row_of(qp, a.qs, row);
                 const T* gr = row_of(gp, a.gs, row);
-                if (sees == 1) add_row<T, DT>(dv, 1.0f, gr + c0, my);
-                else {
-                    const float s = dot_of(qr, kr, a.d), p = __builtin_amdgcn_exp2f(fmaf(a.scale < 0 ? -s : s, a.c, -lsep[(long long)(row - i * a.group) * a.q_len + i] * kLog2e));
+                const float lse = lsep[(long long)(row - i * a.group) * a.q_len + i];
+                if (sees == 1) {
+                    add_row<T, DT>(dv, 1.0f + one_key(lse), gr + c0, my);
+                    add_row<T, DT>(dk, one_key(lse), qr + c0, my);
+                } else {
+                    const float s = dot_of(qr, kr, a.d), p = __builtin_amdgcn_exp2f(fmaf(a.scale < 0 ? -s : s, a.c, -lse * kLog2e));
                     add_row<T, DT>(dv, p, gr + c0, my);
                     add_row<T, DT>(dk, p * (dot_of(gr, vr, a.d) - deltap[row]), qr + c0, my);
                 }
@@ -538,15 +547,17 @@ __global__ __launch_bounds__(256) void k_attention_add(const AttentionArgs a, lo
     const Lengths len(a, b);
     T* p;
     bool any;
+    float none = 0;
     if constexpr (KEYS) {
         p = blockIdx.y ? (T*)a.dv + b * a.dvs[0] + row * a.dvs[1] + kvh * a.dvs[2] : (T*)a.dk + b * a.dks[0] + row * a.dks[1] + kvh * a.dks[2];
         any = row < len.k;
     } else {
-        const int i = query_of(a, row);
-        p = (T*)a.dq + b * a.dqs[0] + i * a.dqs[1] + (kvh * a.group + row - i * a.group) * a.dqs[2];
-        any = len.seen(a, i) > 1;
+        const int i = query_of(a, row), head = kvh * a.group + row - i * a.group, seen = len.seen(a, i);
+        p = (T*)a.dq + b * a.dqs[0] + i * a.dqs[1] + head * a.dqs[2];
+        any = seen > 1;
+        if (seen == 1) none = one_key(a.lse[((long long)b * a.heads + head) * a.q_len + i]);
     }
-    v = any ? v * (blockIdx.y ? 1.0f : a.scale) : f32x4{0, 0, 0, 0};
+    v = any ? v * (blockIdx.y ? 1.0f : a.scale) : f32x4{none, none, none, none};
     store4(p, d0, a.d, a.vec, v[0], v[1], v[2], v[3]);
 }
 

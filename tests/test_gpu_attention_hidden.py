@@ -134,3 +134,28 @@ def test_one_channel_of_wide_fp32_heads(shape, c):
         for t in ("dk", "dv"):
             x, y = getattr(got, t)[:, 71:], getattr(want, t)[:, 71:]
             assert x.isfinite().all() and (x - y).abs().max() <= 2e-5 * y.abs().max(), (which, t)
+
+
+# (rows split over workgroups in the last one's dq, keys' gradients of many rows in the one before)
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape,causal", [((2, 4, 2, 90, 90, 64), True), ((1, 2, 2, 60, 50, 128), True), ((2, 2, 1, 70, 1, 40), False), ((1, 2, 2, 1500, 1, 64), False),
+                                          ((1, 2, 2, 40, 1500, 32), True)])
+def test_one_key_of_a_score_that_is_not_finite(shape, causal, dtype):
+    """A query that sees one key: probability 1 whatever the score, but NaN if it is none, forward and backward."""
+    b, h, kv, ql, kl, d = shape
+    q, k, v, do = A._make(*shape, dtype)
+    lens = torch.tensor([ql] * b, dtype=torch.int32, device="cuda"), torch.tensor([1 if kl == 1500 else kl] * b, dtype=torch.int32, device="cuda")
+    want = A._run(q, k, v, do, dtype, causal, None, *lens)
+    row = max(0, ql - int(lens[1][0])) if causal else 7         # (the first one that sees a key; not causal: any)
+    for bad in (math.nan, math.inf):
+        q2 = q.clone()
+        q2[:, row, 0, 3] = bad
+        got = A._run(q2, k, v, do, dtype, causal, None, *lens)
+        for t in ("out", "dq"):
+            x, y = getattr(got, t), getattr(want, t)
+            assert x[:, row, 0].isnan().all(), t
+            assert torch.equal(x[:, row, 1:], y[:, row, 1:]) and torch.equal(x[:, :row], y[:, :row]) and torch.equal(x[:, row + 1:], y[:, row + 1:]), t
+        for t in ("dk", "dv"):
+            x, y = getattr(got, t), getattr(want, t)
+            assert x[:, 0, 0].isnan().all() and torch.equal(x[:, 0, 1:], y[:, 0, 1:]), t
+            assert x[:, 1:].isfinite().all() and (x[:, 1:] - y[:, 1:]).abs().sum() <= 0.03 * y[:, 1:].abs().sum(), t
