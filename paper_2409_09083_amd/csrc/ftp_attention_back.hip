@@ -327,8 +327,20 @@ __global__ __launch_bounds__(256, (D == 128 || sizeof(T) == 4 ? 1 : 2)) void k_a
             lse[r >> 2][r & 3] = hidden ? 0.0f : lse[r >> 2][r & 3];
         }
     };
-    // whether some row of the tile does not see all of the wavefront's keys
-    const auto hides = [&](int t) { return a.causal && len.seen(a, first_query(t)) < mine + 32; };     // (a tile's first row sees the fewest keys)
+    // Whether some row of the tile does not see all of the wavefront's keys.  Rows that there are not are zeros, whose product with a key that is not finite is no number: they are hidden from such ones.
+    bool odd_keys = false;
+    const auto look_at_keys = [&]() __attribute__((always_inline)) {
+        if constexpr (sizeof(T) == 2) {             // (a seen infinity of fp32 is NaN anyway)
+            uint32_t carry = 0;                     // out of an exponent of all ones
+#pragma unroll
+            for (int s = 0; s < KS; ++s)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    carry |= ((__builtin_bit_cast(u32x4, k[s])[j] & 0x7F807F80u) + 0x00800080u) | ((__builtin_bit_cast(u32x4, v[s])[j] & 0x7F807F80u) + 0x00800080u);
+            odd_keys = __any((carry & 0x80008000u) != 0);
+        }
+    };
+    const auto hides = [&](int t) { return odd_keys || (a.causal && len.seen(a, first_query(t)) < mine + 32); };       // (a tile's first row sees the fewest keys)
     const auto walk = [&](int begin) __attribute__((always_inline)) {
         if constexpr (HALVES == 2) {
             static_assert(UNITS == 1, "a tile is a unit");
@@ -438,6 +450,7 @@ __global__ __launch_bounds__(256, (D == 128 || sizeof(T) == 4 ? 1 : 2)) void k_a
                 fetch(begin, r0);
                 land(r0);
                 if (begin + 1 < hi) fetch(begin + 1, r1);
+                look_at_keys();
                 start(r0, 0, s0, p0);
 #pragma unroll
                 for (int c = 0; c < KS; ++c) {

@@ -159,3 +159,23 @@ def test_one_key_of_a_score_that_is_not_finite(shape, causal, dtype):
             x, y = getattr(got, t), getattr(want, t)
             assert x[:, 0, 0].isnan().all() and torch.equal(x[:, 0, 1:], y[:, 0, 1:]), t
             assert x[:, 1:].isfinite().all() and (x[:, 1:] - y[:, 1:]).abs().sum() <= 0.03 * y[:, 1:].abs().sum(), t
+
+
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("shape", [(2, 3, 1, 50, 50, 64), (1, 2, 2, 200, 300, 128), (40, 6, 6, 100, 90, 40)])
+def test_bfloat_keys_at_minus_infinity(shape, causal):
+    """A key whose scores all are -infinity has probability 0: it is as a key that nobody sees, its own gradients 0 (lengths and groups leave rows of tiles empty)."""
+    b, h, kv, ql, kl, d = shape
+    q, k, v, do = A._make(*shape, "bf16")
+    q[..., 5] = q[..., 5].abs() + 0.5
+    lens = torch.tensor([ql - 7] * b, dtype=torch.int32, device="cuda"), torch.tensor([kl - 3] * b, dtype=torch.int32, device="cuda")
+    far = k.clone()
+    far[:, 10, :, 5] = -1e30                                    # (as good as -infinity)
+    want = A._run(q, far, v, do, "bf16", causal, None, *lens)
+    k[:, 10, :, 5] = -math.inf
+    got = A._run(q, k, v, do, "bf16", causal, None, *lens)
+    for t in ("out", "lse"):
+        assert torch.equal(getattr(got, t), getattr(want, t)), t
+    assert torch.equal(got.dv, want.dv)
+    others = [j for j in range(kl) if j != 10]
+    assert torch.equal(got.dk[:, others], want.dk[:, others]) and (got.dk[:, 10] == 0).all()
