@@ -6,7 +6,7 @@
 // atomics, in an order that changes.  In dq S^T and dP^T have a row per lane, in dkv S and dP a key per lane, so that P and dS again are operands as they lie
 // (ftp_attention.h).  Where 128-row (key) blocks are too few for the CUs, the other axis is split and the parts are added up by a third kernel.
 //
-// Measured, 64 heads x 5776 tokens of 64, bfloats (1.91 TFLOP in seven products, 1.37 in five): dq 0.80-0.87 ms (940-1020 TFLOP/s of its three products), dk and dv 1.20-1.30 ms (840-910 of their four); a large
+// Measured, 64 heads x 5776 tokens of 64, bfloats (1.91 TFLOP in seven products, 1.37 in five): dq 0.78-0.87 ms (940-1050 TFLOP/s of its three products), dk and dv 1.20-1.30 ms (840-910 of their four); a large
 // library product reaches 1265 on the same card.  Matrix cores busy 58 and 43-49 % of the cycles, at a clock that the load lowers to 1.9-2.05 GHz; LDS 30-37 %, without bank conflicts; without any load from
 // memory the two took 0.78 and 0.99 ms.  577 x 701 tokens of 40, fp32, 3 x 2 key heads: dq 25 us, dk and dv 39, sums of the splits 5 + 5: a workgroup's chain of 4 to 8 tiles.
 #include "ftp_attention.h"
