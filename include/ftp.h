@@ -337,6 +337,87 @@ int ftp_attention_backward(const ftp_attention_shape* shape, const void* dout, c
                            const int32_t* q_lens, const int32_t* kv_lens, const void* out, const float* lse,
                            void* dq, void* dk, void* dv, void* workspace, void* stream);
 
+/* ---- operators of training on a vocabulary ---------------------------------------------------------------------------
+ * Rows of an embedding table looked up by id with their gradient, the softmax cross entropy of a linear layer over a vocabulary
+ * without its logits, and the orthogonal part of a weight's update.  Called as the token block's operators: a shape by
+ * pointer, device pointers, the caller's scratch and stream; nothing allocated, nothing waited for, no second stream;
+ * equal calls give equal bits.  Ids and labels outside 0 .. vocab - 1 (-1, say) mean that a row has none. */
+typedef enum { FTP_I32 = 0, FTP_I64 = 1 } ftp_id_type;
+
+/* out[r] = scale * table[ids[r]], rounded once; a row without an id is zero.  rows may be 0.
+ * Backward: dtable[v] = scale * the sum of dy[r] over the rows with ids[r] = v, in 32 bits and in the order of the rows (runs of
+ * 32 neighbours in the list sorted by id first); rows of dtable whose id does not occur are set to zero. */
+typedef struct {
+    int64_t rows;                  /* at most 2^26 */
+    int32_t vocab, channels;       /* >= 1; at most 2^26 and 2^20 */
+    int32_t dtype;                 /* ftp_dtype of table, out and dy */
+    int32_t id_type;               /* ftp_id_type of ids [rows] */
+    float scale;                   /* finite */
+    int32_t reserved;
+    int64_t table_stride;          /* elements between rows of the table (forward) */
+    int64_t row_stride;            /* ... of out (forward; >= channels), of dy (backward; may be 0) */
+} ftp_embedding_shape;
+
+int ftp_embedding_forward(const ftp_embedding_shape* shape, const void* ids, const void* table, void* out, void* stream);
+
+/* Bytes of scratch of ftp_embedding_backward. */
+int ftp_embedding_workspace(const ftp_embedding_shape* shape, size_t* bytes);
+
+/* dtable: fp32 [vocab][channels], contiguous. */
+int ftp_embedding_backward(const ftp_embedding_shape* shape, const void* ids, const void* dy, float* dtable, void* workspace,
+                           void* stream);
+
+/* Logits s[r][v] = scale * x[r] . weight[v], which are never kept.  For rows with a label:
+ * lse[r] = log sum_v exp(s[r][v]), loss[r] = lse[r] - s[r][label], mean = the mean of loss over them; other rows have loss = lse = 0, and
+ * nothing that x (or dloss) holds there reaches any result.  mean is 0 where no row has a label.  A row with a logit that is NaN or
+ * +infinity has NaN.  fp32 numbers are multiplied as three bfloats each: an infinity, or a number above the largest bfloat, gives NaN,
+ * and numbers below 2^-110 lose low bits.
+ * Backward: gradients of sum_r dloss[r] * loss[r], or of the mean where dloss is null, with lse as the forward pass left it:
+ * g[r][v] = dloss[r] * scale * (exp(s[r][v] - lse[r]) - [v = label]), dx = g weight, dweight = g^T x.  Where the tensors are bfloats g is rounded
+ * to them as an operand of those products; all sums are fp32.  Rows without a label have dx = 0. */
+typedef struct {
+    int64_t rows;                  /* may be 0; at most 2^22 */
+    int32_t vocab, channels;       /* >= 1; at most 2^24 and 2^14, and blocks of 256 x 256 logits fewer than 2^21 */
+    int32_t dtype;                 /* ftp_dtype of x, weight, dx and dweight */
+    int32_t id_type;               /* ftp_id_type of labels [rows] */
+    float scale;                   /* finite */
+    int32_t reserved;
+    int64_t x_stride, w_stride, dx_stride, dw_stride;          /* elements between rows; inputs may be broadcast (0) */
+} ftp_token_loss_shape;
+
+/* Bytes of scratch of the two passes (either pointer may be null). */
+int ftp_token_loss_workspace(const ftp_token_loss_shape* shape, size_t* forward_bytes, size_t* backward_bytes);
+
+/* loss, lse: fp32 [rows], or null; mean: one fp32 number, or null. */
+int ftp_token_loss_forward(const ftp_token_loss_shape* shape, const void* x, const void* weight, const void* labels, float* loss,
+                           float* lse, float* mean, void* workspace, void* stream);
+
+/* dloss: fp32 [rows], or null.  dx, dweight: either may be null. */
+int ftp_token_loss_backward(const ftp_token_loss_shape* shape, const void* x, const void* weight, const void* labels,
+                            const float* lse, const float* dloss, void* dx, void* dweight, void* workspace, void* stream);
+
+/* The orthogonal part of a matrix, nearly, by Newton-Schulz steps: with X = x / (|x| + eps), |x| the root of the sum of its squares,
+ * `steps` times X <- a X + (b S + c S^2) X, S = X X^T (with rows > cols the same as X (b S + c S^2), S = X^T X).  With (a, b, c) =
+ * (3.4445, -4.775, 2.0315) and 5 steps singular values above a thousandth of |x| end between 0.6 and 1.3.
+ * Products, their sums and the norm are held in 32 bits or more; between them FTP_F32 keeps 24 bits of a number (three bfloats), FTP_BF16 16 (two).  One
+ * call takes `count` matrices of one size.  A matrix with an infinity or a NaN becomes NaN. */
+typedef struct {
+    int32_t count;                 /* may be 0 */
+    int32_t rows, cols;            /* 1 .. 32768 */
+    int32_t dtype;                 /* ftp_dtype of x and out */
+    int32_t steps;                 /* 1 .. 64 */
+    float a, b, c;                 /* finite */
+    float eps;                     /* >= 0 */
+    int32_t reserved;
+    int64_t matrix_stride, row_stride;     /* elements between matrices and rows of x; may be 0 */
+} ftp_orthogonal_shape;
+
+/* Bytes of scratch of ftp_orthogonal. */
+int ftp_orthogonal_workspace(const ftp_orthogonal_shape* shape, size_t* bytes);
+
+/* out: [count][rows][cols], contiguous; may be x itself if that is too. */
+int ftp_orthogonal(const ftp_orthogonal_shape* shape, const void* x, void* out, void* workspace, void* stream);
+
 const char* ftp_strerror(int code);
 
 /* hipError_t value of the last failed HIP call on this thread (0 if none). */

@@ -53,6 +53,26 @@ class ftp_attention_shape(ctypes.Structure):
         (n + "_stride", _I64x3) for n in ("q", "k", "v", "out", "dout", "dq", "dk", "dv")]
 
 
+FTP_I32, FTP_I64 = 0, 1
+
+
+class ftp_embedding_shape(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("vocab", ctypes.c_int32), ("channels", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("id_type", ctypes.c_int32), ("scale", ctypes.c_float), ("reserved", ctypes.c_int32), ("table_stride", ctypes.c_int64),
+                ("row_stride", ctypes.c_int64)]
+
+
+class ftp_token_loss_shape(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("vocab", ctypes.c_int32), ("channels", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("id_type", ctypes.c_int32), ("scale", ctypes.c_float), ("reserved", ctypes.c_int32)] + [
+        (n + "_stride", ctypes.c_int64) for n in ("x", "w", "dx", "dw")]
+
+
+class ftp_orthogonal_shape(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("count", "rows", "cols", "dtype", "steps")] + [
+        (n, ctypes.c_float) for n in ("a", "b", "c", "eps")] + [("reserved", ctypes.c_int32), ("matrix_stride", ctypes.c_int64), ("row_stride", ctypes.c_int64)]
+
+
 PASS_NAMES = {0: "conv_fwd", 1: "conv_bwd_data", 2: "wgrad", 3: "reduce", 4: "pool_fwd", 5: "pool_bwd", 6: "scale_dy", 7: "update", 8: "wgrad_sum"}
 
 
@@ -68,6 +88,8 @@ class FtpError(RuntimeError):
 TOKEN_EXPORTS = ("ftp_norm_forward", "ftp_norm_workspace", "ftp_norm_backward", "ftp_checkpoint_pack", "ftp_checkpoint_unpack",
                  "ftp_checkpoint_act_backward", "ftp_checkpoint_workspace", "ftp_checkpoint_wgrad", "ftp_attention_workspace",
                  "ftp_attention_forward", "ftp_attention_backward")
+TRAINING_EXPORTS = ("ftp_embedding_forward", "ftp_embedding_workspace", "ftp_embedding_backward", "ftp_token_loss_workspace",
+                    "ftp_token_loss_forward", "ftp_token_loss_backward", "ftp_orthogonal_workspace", "ftp_orthogonal")
 
 
 def _load():
@@ -119,12 +141,21 @@ def _load():
     lib.ftp_attention_workspace.argtypes = [ats, psz, psz]
     lib.ftp_attention_forward.argtypes = [ats] + [vp] * 9
     lib.ftp_attention_backward.argtypes = [ats] + [vp] * 13
+    es, ls = ctypes.POINTER(ftp_embedding_shape), ctypes.POINTER(ftp_token_loss_shape)
+    lib.ftp_embedding_forward.argtypes = [es] + [vp] * 4
+    lib.ftp_embedding_workspace.argtypes = [es, psz]
+    lib.ftp_embedding_backward.argtypes = [es] + [vp] * 5
+    lib.ftp_token_loss_workspace.argtypes = [ls, psz, psz]
+    lib.ftp_token_loss_forward.argtypes = [ls] + [vp] * 8
+    lib.ftp_token_loss_backward.argtypes = [ls] + [vp] * 9
+    lib.ftp_orthogonal_workspace.argtypes = [ctypes.POINTER(ftp_orthogonal_shape), psz]
+    lib.ftp_orthogonal.argtypes = [ctypes.POINTER(ftp_orthogonal_shape)] + [vp] * 4
     lib.ftp_strerror.argtypes = [ctypes.c_int]
     lib.ftp_strerror.restype = ctypes.c_char_p
     lib.ftp_last_hip_error.restype = ctypes.c_int
     lib.ftp_joint_launches.restype = ctypes.c_longlong
     for f in ("ftp_profile", "ftp_profile_read", "ftp_set_overlap", "ftp_plan_buffer", "ftp_plan_rect", "ftp_plan_map_shape", "ftp_plan_sizes", "ftp_plan_work", "ftp_forward",
-              "ftp_forward_static", "ftp_backward", "ftp_reduce_wgrad", "ftp_sgd_step") + TOKEN_EXPORTS:
+              "ftp_forward_static", "ftp_backward", "ftp_reduce_wgrad", "ftp_sgd_step") + TOKEN_EXPORTS + TRAINING_EXPORTS:
         getattr(lib, f).restype = ctypes.c_int
     return lib
 
@@ -133,7 +164,7 @@ _lib = _load()
 
 EXPORTS = ("ftp_profile", "ftp_profile_read", "ftp_set_overlap", "ftp_plan", "ftp_plan_destroy", "ftp_plan_buffer", "ftp_plan_rect", "ftp_plan_map_shape", "ftp_plan_sizes", "ftp_plan_work",
            "ftp_forward", "ftp_forward_static", "ftp_backward", "ftp_reduce_wgrad", "ftp_sgd_step", "ftp_strerror", "ftp_last_hip_error",
-           "ftp_joint_launches") + TOKEN_EXPORTS
+           "ftp_joint_launches") + TOKEN_EXPORTS + TRAINING_EXPORTS
 
 
 def _check(rc, where):
@@ -305,6 +336,47 @@ def ftp_attention_forward(shape, q, k, v, q_lens, kv_lens, out, lse, workspace, 
 def ftp_attention_backward(shape, dout, q, k, v, q_lens, kv_lens, out, lse, dq, dk, dv, workspace, stream=0):
     _check(_lib.ftp_attention_backward(shape, dout, q, k, v, q_lens, kv_lens, out, lse, dq, dk, dv, workspace, stream),
            "ftp_attention_backward")
+
+
+# ---- operators of training on a vocabulary ----
+def ftp_embedding_forward(shape, ids, table, out, stream=0):
+    rc = _lib.ftp_embedding_forward(shape, ids, table, out, stream)
+    if rc:
+        _check(rc, "ftp_embedding_forward")
+
+
+def ftp_embedding_workspace(shape):
+    n = ctypes.c_size_t()
+    _check(_lib.ftp_embedding_workspace(shape, n), "ftp_embedding_workspace")
+    return n.value
+
+
+def ftp_embedding_backward(shape, ids, dy, dtable, workspace, stream=0):
+    _check(_lib.ftp_embedding_backward(shape, ids, dy, dtable, workspace, stream), "ftp_embedding_backward")
+
+
+def ftp_token_loss_workspace(shape):
+    f, b = ctypes.c_size_t(), ctypes.c_size_t()
+    _check(_lib.ftp_token_loss_workspace(shape, f, b), "ftp_token_loss_workspace")
+    return f.value, b.value
+
+
+def ftp_token_loss_forward(shape, x, weight, labels, loss, lse, mean, workspace, stream=0):
+    _check(_lib.ftp_token_loss_forward(shape, x, weight, labels, loss, lse, mean, workspace, stream), "ftp_token_loss_forward")
+
+
+def ftp_token_loss_backward(shape, x, weight, labels, lse, dloss, dx, dweight, workspace, stream=0):
+    _check(_lib.ftp_token_loss_backward(shape, x, weight, labels, lse, dloss, dx, dweight, workspace, stream), "ftp_token_loss_backward")
+
+
+def ftp_orthogonal_workspace(shape):
+    n = ctypes.c_size_t()
+    _check(_lib.ftp_orthogonal_workspace(shape, n), "ftp_orthogonal_workspace")
+    return n.value
+
+
+def ftp_orthogonal(shape, x, out, workspace, stream=0):
+    _check(_lib.ftp_orthogonal(shape, x, out, workspace, stream), "ftp_orthogonal")
 
 
 def ftp_strerror(code):

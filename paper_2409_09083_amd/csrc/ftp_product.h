@@ -1,0 +1,252 @@
+// Products of bfloat matrices, D[a][b] = sum over k of A(a, k) B(b, k), as the training operators use them: a workgroup's block of D in registers, stages of both operands in LDS.
+//
+// An operand lies either along the contraction (element (i, k) at i * stride + k) or across it (k * stride + i); the latter is read through the transposing LDS load.  An fp32 matrix is PLANES
+// matrices whose sum it is (three hold its 24 bits, two 16), a product of two the sum of the products of planes that are above 2^-24 (2^-16) of it, smallest first: six (three).  So there is one kernel, whose
+// contraction is as many times longer.
+//
+// Stages of 32 are fetched straight into LDS three to four ahead (buffer loads; what is past the end of an operand arrives as zeros), one barrier a stage.  A wavefront has 128 x 64 of a block of 256 x 256: 8 products of
+// 32 x 32 x 16 to 6 operands of 1 KB, three quarters of what the LDS delivers in that time.
+#pragma once
+#include "ftp_tokens.h"
+
+#include <type_traits>
+
+namespace ftp {
+
+typedef __bf16 b16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+// A matrix in bfloats, 16-byte aligned, its stride a multiple of 8 elements.  along: rows are indices, cols the contraction (a multiple of 32, the part that is none in zeros); across: rows the contraction.
+struct Matrix {
+    const bf16_t* p;
+    long long stride, plane;                        // elements between rows, between planes
+    long long rows;
+    int cols;
+};
+
+// A workgroup's block BA x BB by WA x WB wavefronts; XA, XB: the operand lies across.
+template <int BA_, int BB_, int WA_, int WB_, bool XA_, bool XB_, int KS_ = 32>
+struct Product {
+    static constexpr int BA = BA_, BB = BB_, WA = WA_, WB = WB_, kThreads = WA * WB * 64, KS = KS_, kAhead = 3;
+    static constexpr bool XA = XA_, XB = XB_;
+    static constexpr int IA = BA / WA / 32, IB = BB / WB / 32;                     // 32 x 32 blocks of a wavefront
+    static constexpr int kBytesA = BA * KS * 2, kBytesB = BB * KS * 2;
+    static constexpr int kLoadsA = kBytesA / 16 / kThreads, kLoadsB = kBytesB / 16 / kThreads, kLoads = kLoadsA + kLoadsB;
+    static_assert(kLoadsA * kThreads * 16 == kBytesA && kLoadsB * kThreads * 16 == kBytesB, "whole loads a thread");
+    static_assert(kAhead * kLoads < 64, "what vmcnt counts");
+    struct Stage { char a[kBytesA], b[kBytesB]; };
+
+    // Which 16 bytes of a row lie where: rows of 64 or 128 bytes (along) so that 16 rows' equal chunks meet no bank twice, longer ones (across) so that 4 rows x 64 bytes do not.
+    template <int B, bool X>
+    static __device__ __forceinline__ int mix(int row)
+    {
+        if constexpr (!X) return KS == 32 ? (row >> 2) & 3 : (row >> 1) & 7;
+        else return B >= 128 ? ((row & 3) << 2) | ((row >> 2) & 3) : ((row & 2) << 1) | ((row >> 2) & 3);
+    }
+    // operand (index i0 + lane % 32; contraction 16 s + 8 h + j)
+    template <int B, bool X>
+    static __device__ __forceinline__ b16x8 operand(const char* t, int i0, int s)
+    {
+        const int l = threadIdx.x & 63, h = l >> 5;
+        if constexpr (!X) {
+            const int row = i0 + (l & 31);
+            return *(const b16x8*)(t + row * (KS * 2) + (((2 * s + h) ^ mix<B, X>(row)) << 4));
+        } else {
+            // each 16 lanes: 4 rows x 16 columns, lane i brings 8 bytes of row i / 4 and takes column i of the four rows
+            const int i = l & 15, col = i0 + (l & 16) + (i & 3) * 4;
+            s16x4 v[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int row = 16 * s + 8 * h + 4 * j + (i >> 2);
+                v[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                    (s16x4 __attribute__((address_space(3)))*)(t + row * (B * 2) + (((col >> 3) ^ mix<B, X>(row)) << 4) + (col & 7) * 2));
+            }
+            return __builtin_bit_cast(b16x8, __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7));
+        }
+    }
+    // an operand's block on its way to LDS
+    template <int B, bool X, int N>
+    struct Source {
+        const char* base;                           // of the stage to come, in plane 0
+        long long plane, left;                      // bytes between planes, from the base to the end
+        long long step;                             // bytes a stage
+        int at[N];                                  // this thread's chunks, bytes from the base
+        __device__ __forceinline__ void init(const Matrix& m, long long i0, long long k0)
+        {
+            const long long first = X ? k0 * m.stride + i0 : i0 * m.stride + k0;
+            base = (const char*)(m.p + first);
+            plane = m.plane * 2;
+            left = ((m.rows - 1) * m.stride + m.cols - first) * 2;
+            step = X ? KS * m.stride * 2 : KS * 2;
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                constexpr int kRow = X ? B / 8 : KS / 8;                            // chunks of a row
+                const int u = threadIdx.x + kThreads * i, row = u / kRow, chunk = (u % kRow) ^ mix<B, X>(row);
+                at[i] = (int)(row * m.stride * 2) + chunk * 16;
+            }
+        }
+        __device__ __forceinline__ void fetch(char* to, long long stage, int p, bool any) const
+        {
+            const long long off = stage * step;
+            const int n = any ? (int)min(max(left - off, 0ll), 0x7FFFFFF0ll) : 0;
+            const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)(base + off + p * plane), (short)0, n, 0x00020000);
+            const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x & ~63);
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)(to + (wave + kThreads * i) * 16), 16, at[i], 0, 0, 0);
+        }
+    };
+
+    static __device__ __forceinline__ int wave_a() { return (__builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % WA) * (IA * 32); }
+    static __device__ __forceinline__ int wave_b() { return (__builtin_amdgcn_readfirstlane(threadIdx.x >> 6) / WA) * (IB * 32); }
+
+    // acc[i][j] += the block at (a0, b0) over the stages [lo, hi) of the contraction.  planes: of both operands.  The stages s are distinct objects, so that loads into one are no reason to wait for those
+    // into another.  At the end all of this wavefront's loads have landed.
+    static __device__ __forceinline__ void run(f32x16 (&acc)[IA][IB], const Matrix& a, const Matrix& b, long long a0, long long b0, int lo, int hi, int planes, Stage& s0, Stage& s1, Stage& s2,
+                                               Stage& s3)
+    {
+        Source<BA, XA, kLoadsA> fa;
+        Source<BB, XB, kLoadsB> fb;
+        fa.init(a, a0, (long long)lo * KS);
+        fb.init(b, b0, (long long)lo * KS);
+        const int wa = wave_a(), wb = wave_b(), per = hi - lo, terms = planes == 1 ? 1 : planes == 2 ? 3 : 6, total = per * terms;
+        // planes of the terms, two bits each: (2, 0) (0, 2) (1, 1) (1, 0) (0, 1) (0, 0)
+        uint32_t pa = planes == 3 ? 0x52u : planes == 2 ? 0x1u : 0u, pb = planes == 3 ? 0x118u : planes == 2 ? 0x4u : 0u;
+        int k = 0, fetched = 0;
+        const auto fetch = [&](Stage& to) __attribute__((always_inline)) {
+            const bool any = fetched < total;
+            fa.fetch(to.a, k, pa & 3, any);
+            fb.fetch(to.b, k, pb & 3, any);
+            ++fetched;
+            if (++k == per) { k = 0; pa >>= 2; pb >>= 2; }
+        };
+        if (total == 0) return;
+        b16x8 x[2][IA], y[2][IB];
+        const auto read = [&](auto to, const Stage& from, int s) __attribute__((always_inline)) {
+#pragma unroll
+            for (int i = 0; i < IA; ++i) x[to][i] = operand<BA, XA>(from.a, wa + 32 * i, s);
+#pragma unroll
+            for (int j = 0; j < IB; ++j) y[to][j] = operand<BB, XB>(from.b, wb + 32 * j, s);
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        const auto multiply = [&](auto from) __attribute__((always_inline)) {
+#pragma unroll
+            for (int i = 0; i < IA; ++i)
+#pragma unroll
+                for (int j = 0; j < IB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[from][i], y[from][j], acc[i][j], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        // this wavefront's loads of the next stage have landed (`kAhead` are on their way, a load more or less each), its reads of this one too; behind the barrier everybody's
+        const auto landed = [&](auto ahead) __attribute__((always_inline)) {
+            constexpr int n = ahead * kLoads;
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_s_waitcnt((n & 15) | (n >> 4) << 14 | 0x70);
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+        };
+        constexpr std::integral_constant<int, 0> even{};
+        constexpr std::integral_constant<int, 1> odd{};
+        constexpr int N = KS / 16;
+        static_assert(N % 2 == 0, "operands alternate");
+        // Operands are read one product block ahead, over the barrier too: the first ones of a stage while the last block of the one before is multiplied, when that stage's place is free already.
+        const auto step = [&](Stage& now, Stage& next) __attribute__((always_inline)) {
+#pragma unroll
+            for (int s = 0; s + 1 < N; s += 2) {
+                read(odd, now, s + 1);
+                multiply(even);
+                if (s + 2 < N) {
+                    read(even, now, s + 2);
+                    multiply(odd);
+                }
+            }
+            landed(std::integral_constant<int, kAhead - 1>{});
+            fetch(now);
+            read(even, next, 0);
+            multiply(odd);
+        };
+        fetch(s0);
+        fetch(s1);
+        fetch(s2);
+        fetch(s3);
+        landed(std::integral_constant<int, kAhead>{});
+        read(even, s0, 0);
+        // (one way through the loop: where ways meet, the compiler waits for all loads)
+        for (int s = total >> 2; s; --s) {
+            step(s0, s1);
+            step(s1, s2);
+            step(s2, s3);
+            step(s3, s0);
+        }
+        if (total & 3) {
+            step(s0, s1);
+            if ((total & 3) > 1) {
+                step(s1, s2);
+                if ((total & 3) > 2) step(s2, s3);
+            }
+        }
+        __builtin_amdgcn_s_waitcnt(0x70);
+        asm volatile("" ::: "memory");
+    }
+
+    // f(a, b, v): index of the first of four neighbours along a, index along b, values; of this wavefront, from the block's corner
+    template <class F>
+    static __device__ __forceinline__ void each(const f32x16 (&acc)[IA][IB], F f)
+    {
+        const int l = threadIdx.x & 63, h = l >> 5, wa = wave_a(), wb = wave_b();
+#pragma unroll
+        for (int j = 0; j < IB; ++j)
+#pragma unroll
+            for (int i = 0; i < IA; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; r += 4) f(wa + 32 * i + 2 * r + 4 * h, wb + 32 * j + (l & 31), f32x4{acc[i][j][r], acc[i][j][r + 1], acc[i][j][r + 2], acc[i][j][r + 3]});
+    }
+};
+
+// The places of a launch's workgroups: XCD x takes the x-th eighth of the blocks in an order where neighbours share operands, four rows of blocks side by side.
+__device__ __forceinline__ bool block_of(int index, int ablocks, int bblocks, int& ia, int& ib)
+{
+    const int total = ablocks * bblocks, per = (total + 7) >> 3, slot = index >> 3, t = (index & 7) * per + slot;
+    if (slot >= per || t >= total) return false;
+    const int wide = 4 * ablocks, band = t / wide, in = t - band * wide, high = min(4, bblocks - 4 * band);
+    ia = in / high;
+    ib = 4 * band + in - ia * high;
+    return true;
+}
+inline long long block_grid(long long ablocks, long long bblocks) { return ceil_div(ablocks * bblocks, 8) * 8; }
+
+// Blocks (256, 128 or 64 results squared, not below `least`) and shares of the contraction of a product of a x b results over `stages` stages of 32: the choice that should end first.  A CU holds one
+// workgroup of the large blocks, two or four of the others, which then share it.
+struct Split { int block, shares; };
+inline Split split_of(long long a, long long b, long long stages, int least, int most, long long count = 1)
+{
+    Split best = {256, 1};
+    double time = 1e300;
+    for (int block = 256; block >= least; block /= 2) {
+        const int per_cu = block == 256 ? 1 : block == 128 ? 2 : 4;
+        const double stage = block == 256 ? 1.1 : block == 128 ? 0.31 : 0.12;      // microseconds, of a workgroup by itself
+        const long long blocks = ceil_div(a, block) * ceil_div(b, block) * count;
+        for (int s = 1; s <= most && (s == 1 || stages / s >= 8); ++s) {
+            const long long n = blocks * s, rounds = ceil_div(n, 256 * per_cu), beside = n >= 256 * per_cu ? per_cu : ceil_div(n, 256);
+            // start and end of a workgroup; the shares' sum, a launch that reads them
+            const double t = (double)rounds * ((double)ceil_div(stages, s) * stage * (double)beside + 4) + (s > 1 ? 4 + 8e-6 * (double)(a * b * count) * s / 4 : 0);
+            if (t < time) { time = t; best = {block, s}; }
+        }
+    }
+    return best;
+}
+
+// 2 neighbouring numbers as PLANES bfloats each whose sum they are: exactly (3, as split3) or to 16 bits (2; the numbers are known to that only where two planes are used)
+template <int PLANES>
+__device__ __forceinline__ void planes_of(float a, float b, uint32_t (&w)[PLANES])
+{
+    if constexpr (PLANES == 3) split3(a, b, w[0], w[1], w[2]);
+    else {
+        w[0] = pack_bf16(a, b);
+        if constexpr (PLANES == 2) w[1] = pack_bf16(a - __uint_as_float(w[0] << 16), b - __uint_as_float(w[0] & 0xFFFF0000u));
+    }
+}
+
+}  // namespace ftp

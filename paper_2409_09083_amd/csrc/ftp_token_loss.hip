@@ -1,0 +1,552 @@
+// Softmax cross entropy over a vocabulary, from the inputs x and the weight W of the linear layer that makes the logits s = scale W x:
+//   loss = log sum_v exp(s_v) - s_label,   G = dloss scale (exp(s - log sum) - [v = label]),   dx = G W,   dW = G^T x.
+// No logit is kept.  Forward, a block of logits leaves its registers as one maximum and one sum of powers a row; backward, the logits are computed again and leave as G, rounded to the operands of the
+// two products behind it (bfloats, or three of them), for a piece of the vocabulary at a time.
+//
+// Rows without a label have no part in any of it: the others are gathered first (their number stays on the device), so that what the rows left out hold, NaN included, reaches nothing, and costs nothing.
+#include "ftp_training.h"
+#include "ftp_product.h"
+
+#include <algorithm>
+#include <cmath>
+
+namespace ftp {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr int kChunk = 64;                          // rows whose labels one wavefront looks at
+constexpr int kFew = 32;                            // most rows of the forward pass that reads W at the memory's rate
+
+template <bool XA, bool XB> using Big = Product<256, 256, 2, 4, XA, XB>;
+template <bool XA, bool XB> using Mid = Product<128, 128, 2, 2, XA, XB>;
+typedef Product<128, 32, 4, 1, false, false, 64> Few;
+
+// ---- the labelled rows ---------------------------------------------------------------------------------------------
+// How many of each 64 rows have labels.
+__global__ __launch_bounds__(256) void k_labelled(const void* ids, int wide, long long rows, int vocab, int* counts)
+{
+    const long long chunk = (long long)blockIdx.x * 4 + (threadIdx.x >> 6), row = chunk * kChunk + (threadIdx.x & 63);
+    const bool there = row < rows && id_of(ids, wide, row, vocab) >= 0;
+    const unsigned long long all = __ballot(there);
+    if ((threadIdx.x & 63) == 0 && chunk * kChunk < std::max(rows, 1ll)) counts[chunk] = (int)__popcll(all);
+}
+
+// 8 neighbours c0 .. c0 + 7 of a row of C as planes; zeros past its end
+template <typename T, int P>
+__device__ __forceinline__ void copy8(const T* row, int c0, int C, bf16_t* to, long long plane)
+{
+    Pack<T, 8> v;
+    if (c0 + 8 <= C) v.load_any(row + c0);
+    else {
+        T e[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) e[j] = c0 + j < C ? row[c0 + j] : (T)0;
+        __builtin_memcpy(v.w, e, sizeof(e));
+    }
+    if constexpr (P == 1) __builtin_memcpy(to + c0, v.w, 16);
+    else {
+        uint32_t q[4][P];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) planes_of<P>(v.get(2 * j), v.get(2 * j + 1), q[j]);
+#pragma unroll
+        for (int p = 0; p < P; ++p) *(uint4*)(to + p * plane + c0) = uint4{q[0][p], q[1][p], q[2][p], q[3][p]};
+    }
+}
+
+struct GatherArgs {
+    const void* ids; const void* x; const int* counts;
+    bf16_t* xc; int* index; int* label; int* place; int* count;
+    long long rows, stride, plane;
+    int wide, vocab, C, Cp;
+};
+
+// The labelled rows one behind the other: row place[r] of xc is row r of x, index and label say which.  Zeros up to the next multiple of 64 rows.
+template <typename T, int P>
+__global__ __launch_bounds__(256) void k_gather(const GatherArgs a)
+{
+    __shared__ int sums[2][4];
+    __shared__ int where[kChunk];
+    const long long chunk = blockIdx.x, row0 = chunk * kChunk, chunks = gridDim.x;
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+    int before = 0, all = 0;
+    for (long long i = tid; i < chunks; i += 256) {
+        const int n = a.counts[i];
+        all += n;
+        before += i < chunk ? n : 0;
+    }
+#pragma unroll
+    for (int n = 32; n; n >>= 1) { before += __shfl_xor(before, n); all += __shfl_xor(all, n); }
+    if (lane == 0) { sums[0][wave] = before; sums[1][wave] = all; }
+    __syncthreads();
+    before = sums[0][0] + sums[0][1] + sums[0][2] + sums[0][3];
+    all = sums[1][0] + sums[1][1] + sums[1][2] + sums[1][3];
+    if (wave == 0) {
+        const long long row = row0 + lane;
+        const int id = row < a.rows ? id_of(a.ids, a.wide, row, a.vocab) : -1;
+        const unsigned long long there = __ballot(id >= 0);
+        const int to = before + (int)__popcll(there & ((1ull << lane) - 1));
+        where[lane] = id >= 0 ? to : -1;
+        if (row < a.rows) a.place[row] = id >= 0 ? to : -1;
+        if (id >= 0) { a.index[to] = (int)row; a.label[to] = id; }
+    }
+    __syncthreads();
+    const int per = a.Cp >> 3;                      // vectors of a row
+    const int here = (int)std::min<long long>(kChunk, a.rows - row0);
+    for (int u = tid; u < here * per; u += 256) {
+        const int r = u / per, c0 = (u - r * per) * 8;
+        if (where[r] >= 0) copy8<T, P>((const T*)a.x + (row0 + r) * a.stride, c0, a.C, a.xc + (long long)where[r] * a.Cp, a.plane);
+    }
+    if (chunk == 0) {
+        const int end = (all + 63) & ~63;
+        if (tid == 0) *a.count = all;
+        for (int u = tid; u < (end - all) * per; u += 256)
+#pragma unroll
+            for (int p = 0; p < P; ++p) *(uint4*)(a.xc + p * a.plane + (long long)all * a.Cp + 8ll * u) = uint4{0, 0, 0, 0};
+    }
+}
+
+// Rows of W as planes, their length rounded up with zeros.
+template <typename T, int P>
+__global__ __launch_bounds__(256) void k_pack_rows(const T* w, long long stride, long long rows, int C, int Cp, bf16_t* to, long long plane)
+{
+    const int per = Cp >> 3;
+    for (long long u = (long long)blockIdx.x * 256 + threadIdx.x; u < rows * per; u += (long long)gridDim.x * 256) {
+        const long long r = u / per;
+        copy8<T, P>(w + r * stride, (int)(u - r * per) * 8, C, to + r * Cp, plane);
+    }
+}
+
+// ---- logits --------------------------------------------------------------------------------------------------------
+struct LogitArgs {
+    Matrix w, x;                                    // a piece of the vocabulary, the labelled rows
+    const int* count;                               // rows of x (null: all)
+    const int* label;                               // of them (null: ids)
+    const void* ids;
+    int wide, planes, stages, vocab, ablocks, bblocks;
+    int piece0;                                     // the piece's first id
+    float c;                                        // scale * log2(e)
+    float2* part; float* target;                    // forward: [row][ablocks] maximum and sum of a block's powers of 2; the labels' logits times log2(e)
+    const int* index; const float* lse; const float* dloss;     // backward
+    bf16_t* g; long long gstride, gplane;
+};
+
+// What a block of logits leaves: STATS, of each row its maximum m (in powers of 2) and the sum of the others' powers above it, and the label's logit; else PLANES of G.
+template <class L, int PLANES, bool STATS>
+__global__ __launch_bounds__(L::kThreads, 2) void k_logits(const LogitArgs a)
+{
+    __shared__ __align__(16) typename L::Stage s0, s1, s2, s3;
+    __shared__ float2 red[L::WA][L::BB];
+    int ia, ib;
+    if (!block_of((int)blockIdx.x, a.ablocks, a.bblocks, ia, ib)) return;
+    const int a0 = ia * L::BA, b0 = ib * L::BB, rows = a.count ? *a.count : (int)a.x.rows;
+    if (b0 >= rows) return;
+    f32x16 acc[L::IA][L::IB] = {};
+    L::run(acc, a.w, a.x, a0, b0, 0, a.stages, a.planes, s0, s1, s2, s3);
+    const int l = threadIdx.x & 63, h = l >> 5, wa = L::wave_a(), wb = L::wave_b();
+    const int left = (int)a.w.rows - a0 - wa - 4 * h;              // ids of the piece from this lane's first one on
+#pragma unroll
+    for (int j = 0; j < L::IB; ++j) {
+        const int row = b0 + wb + 32 * j + (l & 31);
+        const bool there = row < rows;
+        const int id = !there ? -1 : a.label ? a.label[row] : id_of(a.ids, a.wide, row, a.vocab);
+        const int mine = id < 0 ? -1 : id - a.piece0 - a0 - wa - 4 * h;         // the label, counted from this lane's first id
+        if constexpr (STATS) {
+            float m = -INFINITY, sum = 0;
+#pragma unroll
+            for (int i = 0; i < L::IA; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int at = 32 * i + 8 * (r >> 2) + (r & 3);
+                    acc[i][j][r] = at < left ? acc[i][j][r] * a.c : -INFINITY;
+                    if (mine == at && there) a.target[row] = acc[i][j][r];
+                    m = fmaxf(m, acc[i][j][r]);
+                }
+            m = fmaxf(m, __shfl_xor(m, 32));
+            const float ref = m == -INFINITY ? 0.0f : m;            // (a block of nothing but -infinity sums up to 0)
+#pragma unroll
+            for (int i = 0; i < L::IA; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) sum += __builtin_amdgcn_exp2f(acc[i][j][r] - ref);
+            sum += __shfl_xor(sum, 32);
+            if (h == 0) red[wa / (L::IA * 32)][wb + 32 * j + l] = float2{m, sum};
+        } else {
+            float lse2 = 0, weight = 0;
+            if (there) {
+                const int from = a.index[row];
+                lse2 = a.lse[from] * kLog2e;
+                weight = a.dloss ? a.dloss[from] : 1.0f;
+            }
+            if (row < ((rows + 63) & ~63)) {
+                bf16_t* to = a.g + (long long)row * a.gstride + a0 + wa + 4 * h;
+#pragma unroll
+                for (int i = 0; i < L::IA; ++i)
+#pragma unroll
+                    for (int r = 0; r < 16; r += 4) {
+                        float v[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const int at = 32 * i + 2 * r + e;
+                            const float p = __builtin_amdgcn_exp2f(fmaf(acc[i][j][r + e], a.c, -lse2));
+                            v[e] = there && at < left ? (mine == at ? p - 1.0f : p) * weight : 0.0f;
+                        }
+                        uint32_t x[PLANES], y[PLANES];
+                        planes_of<PLANES>(v[0], v[1], x);
+                        planes_of<PLANES>(v[2], v[3], y);
+#pragma unroll
+                        for (int p = 0; p < PLANES; ++p) *(uint2*)(to + p * a.gplane + 32 * i + 2 * r) = uint2{x[p], y[p]};
+                    }
+            }
+        }
+    }
+    if constexpr (STATS) {
+        __syncthreads();
+        for (int b = threadIdx.x; b < L::BB; b += L::kThreads) {
+            if (b0 + b >= rows) break;
+            float2 v = red[0][b];
+#pragma unroll
+            for (int w = 1; w < L::WA; ++w) {
+                const float2 o = red[w][b];
+                const float m = fmaxf(v.x, o.x), ref = m == -INFINITY ? 0.0f : m;
+                v = float2{m, v.y * __builtin_amdgcn_exp2f(v.x - ref) + o.y * __builtin_amdgcn_exp2f(o.x - ref)};
+            }
+            a.part[(long long)(b0 + b) * a.ablocks + ia] = v;
+        }
+    }
+}
+
+// The blocks' statistics joined: a wavefront a row, its lanes' blocks in turn.  Losses and log-sums of all rows (0 where there is no label), and each workgroup's sum of losses and labelled rows.
+__global__ __launch_bounds__(256) void k_loss_join(const float2* part, const float* target, const int* place, const void* ids, int wide, long long rows, int vocab, int blocks, float* loss,
+                                                   float* lse, double* sums, float* mean)
+{
+    __shared__ double total[4];
+    __shared__ int known[4];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    double sum = 0;
+    int n = 0;
+    for (long long row = (long long)blockIdx.x * 4 + wave; row < rows; row += 4ll * gridDim.x) {
+        const long long at = place ? place[row] : id_of(ids, wide, row, vocab) >= 0 ? row : -1;
+        float one = 0, two = 0;
+        if (at >= 0) {
+            const float2* p = part + at * blocks;
+            float m = -INFINITY;
+            for (int i = lane; i < blocks; i += 64) m = fmaxf(m, p[i].x);
+#pragma unroll
+            for (int k = 32; k; k >>= 1) m = fmaxf(m, __shfl_xor(m, k));
+            const float ref = m == -INFINITY ? 0.0f : m;
+            float s = 0;
+            for (int i = lane; i < blocks; i += 64) s = fmaf(p[i].y, __builtin_amdgcn_exp2f(p[i].x - ref), s);
+#pragma unroll
+            for (int k = 32; k; k >>= 1) s += __shfl_xor(s, k);
+            two = fmaf(ref, kLn2, logf(s));
+            one = fmaf(ref - target[at], kLn2, logf(s));         // (one word alone has loss 0)
+            sum += one;
+            ++n;
+        }
+        if (lane == 0) {
+            if (loss) loss[row] = one;
+            if (lse) lse[row] = two;
+        }
+    }
+    if (lane == 0) { total[wave] = sum; known[wave] = n; }
+    __syncthreads();
+    if (threadIdx.x) return;
+    sum = total[0] + total[1] + total[2] + total[3];
+    n = known[0] + known[1] + known[2] + known[3];
+    if (gridDim.x == 1) { if (mean) *mean = n ? (float)(sum / n) : 0.0f; }
+    else if (mean) { sums[2 * blockIdx.x] = sum; sums[2 * blockIdx.x + 1] = n; }
+}
+__global__ __launch_bounds__(256) void k_loss_mean(const double* sums, int n, float* mean)
+{
+    __shared__ double t[2][4];
+    double a = 0, b = 0;
+    for (int i = threadIdx.x; i < n; i += 256) { a += sums[2 * i]; b += sums[2 * i + 1]; }
+#pragma unroll
+    for (int k = 32; k; k >>= 1) { a += __shfl_xor(a, k); b += __shfl_xor(b, k); }
+    if ((threadIdx.x & 63) == 0) { t[0][threadIdx.x >> 6] = a; t[1][threadIdx.x >> 6] = b; }
+    __syncthreads();
+    if (threadIdx.x) return;
+    a = t[0][0] + t[0][1] + t[0][2] + t[0][3];
+    b = t[1][0] + t[1][1] + t[1][2] + t[1][3];
+    *mean = b > 0 ? (float)(a / b) : 0.0f;
+}
+
+// ---- gradients -----------------------------------------------------------------------------------------------------
+struct GradArgs {
+    Matrix a, b;
+    const int* count;
+    int planes, stages, shares, ablocks, bblocks, add;
+    float* part; long long pstride, pshare;         // [share][index of b][pstride]
+    void* out; long long ostride; int C; float scale; int mean;     // dw alone, without shares
+};
+
+__device__ __forceinline__ float gradient_scale(float scale, int mean, const int* count)
+{
+    return !mean ? scale : *count ? scale / (float)*count : 0.0f;
+}
+
+// dx's block: channels x rows over the piece's ids, added to what the pieces before left
+template <class L>
+__global__ __launch_bounds__(L::kThreads, 2) void k_loss_dx(const GradArgs a)
+{
+    __shared__ __align__(16) typename L::Stage s0, s1, s2, s3;
+    int ia, ib;
+    const int blocks = a.bblocks * a.shares;
+    if (!block_of((int)blockIdx.x, a.ablocks, blocks, ia, ib)) return;
+    const int share = ib / a.bblocks, rows = *a.count, a0 = ia * L::BA, b0 = (ib - share * a.bblocks) * L::BB;
+    if (b0 >= rows) return;
+    f32x16 acc[L::IA][L::IB] = {};
+    const int lo = (int)((long long)a.stages * share / a.shares), hi = (int)((long long)a.stages * (share + 1) / a.shares);
+    L::run(acc, a.a, a.b, a0, b0, lo, hi, a.planes, s0, s1, s2, s3);
+    L::each(acc, [&](int i, int j, f32x4 v) __attribute__((always_inline)) {
+        if (a0 + i >= a.pstride || b0 + j >= rows) return;
+        f32x4* p = (f32x4*)(a.part + share * a.pshare + (long long)(b0 + j) * a.pstride + a0 + i);
+        *p = a.add ? *p + v : v;
+    });
+}
+
+// dW's block: channels x ids over the labelled rows
+template <class L, typename T>
+__global__ __launch_bounds__(L::kThreads, 2) void k_loss_dw(const GradArgs a)
+{
+    __shared__ __align__(16) typename L::Stage s0, s1, s2, s3;
+    int ia, ib;
+    const int blocks = a.bblocks * a.shares;
+    if (!block_of((int)blockIdx.x, a.ablocks, blocks, ia, ib)) return;
+    const int share = ib / a.bblocks, a0 = ia * L::BA, b0 = (ib - share * a.bblocks) * L::BB, stages = (*a.count + L::KS - 1) / L::KS;
+    f32x16 acc[L::IA][L::IB] = {};
+    const int lo = (int)((long long)stages * share / a.shares), hi = (int)((long long)stages * (share + 1) / a.shares);
+    L::run(acc, a.a, a.b, a0, b0, lo, hi, a.planes, s0, s1, s2, s3);
+    const float f = gradient_scale(a.scale, a.mean, a.count);
+    L::each(acc, [&](int i, int j, f32x4 v) __attribute__((always_inline)) {
+        const long long id = b0 + j;
+        if (a0 + i >= a.pstride || id >= a.add) return;             // (here: the piece's ids)
+        if (a.shares > 1) {
+            *(f32x4*)(a.part + share * a.pshare + id * a.pstride + a0 + i) = v;
+            return;
+        }
+        T* p = (T*)a.out + id * a.ostride + a0 + i;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) if (a0 + i + e < a.C) st(p + e, v[e] * f);
+    });
+}
+
+// Sums of the shares, in their order, as gradients: row r of out is row place[r] of them (place null: r), or zeros.
+template <typename T>
+__global__ __launch_bounds__(256) void k_loss_sum(const float* part, long long pstride, long long pshare, int shares, const int* place, long long rows, void* out, long long ostride, int C, float scale,
+                                                  int mean, const int* count)
+{
+    const int per = (C + 3) >> 2;
+    const float f = gradient_scale(scale, mean, count);
+    for (long long u = (long long)blockIdx.x * 256 + threadIdx.x; u < rows * per; u += (long long)gridDim.x * 256) {
+        const long long r = u / per, from = place ? place[r] : r;
+        const int c = (int)(u - r * per) * 4;
+        f32x4 v = {0, 0, 0, 0};
+        if (from >= 0) {
+            const float* p = part + from * pstride + c;
+#pragma unroll 4
+            for (int s = 0; s < shares; ++s) v += *(const f32x4*)(p + s * pshare);
+            v *= f;
+        }
+        T* to = (T*)out + r * ostride + c;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) if (c + e < C) st(to + e, v[e]);
+    }
+}
+
+// ---- plans ---------------------------------------------------------------------------------------------------------
+int planes_of_type(int dtype) { return dtype == FTP_BF16 ? 1 : 3; }
+int padded(int c) { return (c + 63) & ~63; }
+long long round_up(long long v, long long to) { return ceil_div(v, to) * to; }
+
+struct Plan {
+    int planes, Cp, blocks, pack_w, gather, few;
+    long long Np, chunks, piece, ids;               // ids: of a piece, rounded up to whole blocks
+    Split logits, dx, dw;
+    int joins;
+};
+Plan plan_of(const ftp_token_loss_shape& s, bool back)
+{
+    Plan p = {};
+    p.planes = planes_of_type(s.dtype);
+    p.Cp = padded(s.channels);
+    p.Np = round_up(std::max<long long>(s.rows, 1), 64);
+    p.chunks = ceil_div(std::max<long long>(s.rows, 1), kChunk);
+    const long long terms = p.planes == 1 ? 1 : 6;
+    // whether W, and few rows of x, can be read as they lie (their addresses are looked at by the call: scratch is there for both ways)
+    p.few = !back && s.rows <= kFew;
+    if (!back) {
+        p.logits = split_of(s.vocab, s.rows, p.Cp / 32 * terms, 128, 1);
+        p.blocks = (int)ceil_div(s.vocab, p.few ? Few::BA : p.logits.block);
+        p.joins = (int)std::min<long long>(ceil_div(std::max<long long>(s.rows, 1), 4), s.rows <= 64 ? 1 : 1024);
+        return p;
+    }
+    // a piece's G in at most 512 MiB and rows of 2^20, whole blocks
+    const long long fits = std::min((512ll << 20) / (2 * p.planes * p.Np) / 256 * 256, 1ll << 20), all = round_up(s.vocab, 256);
+    const long long pieces = ceil_div(all, std::max(256ll, fits));
+    p.piece = round_up(ceil_div(s.vocab, pieces), 256);
+    p.ids = p.piece;
+    p.logits = split_of(p.piece, s.rows, p.Cp / 32 * terms, 128, 1);
+    p.dx = split_of(s.channels, s.rows, p.piece / 32 * terms, 128, 16);
+    p.dw = split_of(s.channels, p.piece, p.Np / 32 * terms, 128, 16);
+    return p;
+}
+
+struct Buffers {
+    int *counts, *index, *label, *place, *count;
+    bf16_t *xc, *wc, *g;
+    float2* part; float *target, *dx, *dw; double* sums;
+    size_t bytes;
+};
+Buffers buffers_of(const ftp_token_loss_shape& s, const Plan& p, bool back, char* ws)
+{
+    Buffers b = {};
+    Parts t(ws);
+    b.counts = t.take<int>(p.chunks);
+    b.index = t.take<int>(p.Np);
+    b.label = t.take<int>(p.Np);
+    b.place = t.take<int>(p.Np);
+    b.count = t.take<int>(1);
+    b.xc = t.take<bf16_t>(p.planes * p.Np * p.Cp);
+    b.wc = t.take<bf16_t>((size_t)p.planes * s.vocab * p.Cp);
+    if (!back) {
+        b.part = t.take<float2>((size_t)p.Np * p.blocks);
+        b.target = t.take<float>(p.Np);
+        b.sums = t.take<double>(2 * 1024);
+    } else {
+        b.g = t.take<bf16_t>((size_t)p.planes * p.Np * p.ids);
+        b.dx = t.take<float>((size_t)p.dx.shares * p.Np * p.Cp);
+        b.dw = t.take<float>(p.dw.shares > 1 ? (size_t)p.dw.shares * p.piece * p.Cp : 0);
+    }
+    b.bytes = t.used;
+    return b;
+}
+
+unsigned pass_grid(long long n) { return (unsigned)std::min<long long>(std::max<long long>(ceil_div(n, 256), 1), 4096); }
+
+template <int P>
+void gather(const ftp_token_loss_shape& s, const Plan& p, const Buffers& b, const void* x, const void* labels, hipStream_t st)
+{
+    k_labelled<<<(unsigned)ceil_div(p.chunks, 4), 256, 0, st>>>(labels, s.id_type, s.rows, s.vocab, b.counts);
+    GatherArgs g = {};
+    g.ids = labels; g.x = x; g.counts = b.counts; g.xc = b.xc; g.index = b.index; g.label = b.label; g.place = b.place; g.count = b.count;
+    g.rows = s.rows; g.stride = s.x_stride; g.plane = p.Np * p.Cp; g.wide = s.id_type; g.vocab = s.vocab; g.C = s.channels; g.Cp = p.Cp;
+    if constexpr (P == 1) k_gather<bf16_t, 1><<<(unsigned)p.chunks, 256, 0, st>>>(g);
+    else k_gather<float, 3><<<(unsigned)p.chunks, 256, 0, st>>>(g);
+}
+
+// W as the products read it
+template <int P>
+Matrix weight(const ftp_token_loss_shape& s, const Plan& p, const Buffers& b, const void* w, hipStream_t st)
+{
+    if (P == 1 && s.channels % 64 == 0 && s.w_stride % 8 == 0 && s.w_stride < (1 << 20) && aligned(w, 16)) return Matrix{(const bf16_t*)w, s.w_stride, 0, s.vocab, p.Cp};
+    const long long plane = (long long)s.vocab * p.Cp;
+    const unsigned grid = pass_grid(plane / 8);
+    if constexpr (P == 1) k_pack_rows<bf16_t, 1><<<grid, 256, 0, st>>>((const bf16_t*)w, s.w_stride, s.vocab, s.channels, p.Cp, b.wc, plane);
+    else k_pack_rows<float, 3><<<grid, 256, 0, st>>>((const float*)w, s.w_stride, s.vocab, s.channels, p.Cp, b.wc, plane);
+    return Matrix{b.wc, p.Cp, plane, s.vocab, p.Cp};
+}
+
+template <class L, int P, bool STATS>
+void logits(LogitArgs& a, long long rows, hipStream_t st)
+{
+    a.stages = a.w.cols / L::KS;
+    a.ablocks = (int)ceil_div(a.w.rows, L::BA);
+    a.bblocks = (int)ceil_div(rows, L::BB);
+    if (rows) k_logits<L, P, STATS><<<(unsigned)block_grid(a.ablocks, a.bblocks), L::kThreads, 0, st>>>(a);
+}
+
+template <int P>
+void forward(const ftp_token_loss_shape& s, const void* x, const void* w, const void* labels, float* loss, float* lse, float* mean, char* ws, hipStream_t st)
+{
+    const Plan p = plan_of(s, false);
+    const Buffers b = buffers_of(s, p, false, ws);
+    LogitArgs a = {};
+    a.planes = P; a.wide = s.id_type; a.vocab = s.vocab; a.c = s.scale * kLog2e; a.part = b.part; a.target = b.target; a.ids = labels;
+    const bool plain = p.few && P == 1 && s.channels % 64 == 0 && (s.x_stride % 8 == 0 || s.rows <= 1) && s.x_stride < (1 << 20) && aligned(x, 16);
+    a.w = weight<P>(s, p, b, w, st);
+    if (plain) a.x = Matrix{(const bf16_t*)x, s.x_stride, 0, s.rows, p.Cp};
+    else {
+        gather<P>(s, p, b, x, labels, st);
+        a.x = Matrix{b.xc, p.Cp, p.Np * p.Cp, p.Np, p.Cp};
+        a.count = b.count; a.label = b.label;
+    }
+    if (p.few) logits<Few, P, true>(a, s.rows, st);
+    else if (p.logits.block == 256) logits<Big<false, false>, P, true>(a, s.rows, st);
+    else logits<Mid<false, false>, P, true>(a, s.rows, st);
+    k_loss_join<<<p.joins, 256, 0, st>>>(b.part, b.target, plain ? nullptr : b.place, labels, s.id_type, s.rows, s.vocab, a.ablocks, loss, lse, b.sums, mean);
+    if (p.joins > 1 && mean) k_loss_mean<<<1, 256, 0, st>>>(b.sums, p.joins, mean);
+}
+
+template <class L, typename T>
+void dw_pass(GradArgs& a, hipStream_t st) { k_loss_dw<L, T><<<(unsigned)block_grid(a.ablocks, (long long)a.bblocks * a.shares), L::kThreads, 0, st>>>(a); }
+template <class L>
+void dx_pass(GradArgs& a, hipStream_t st) { k_loss_dx<L><<<(unsigned)block_grid(a.ablocks, (long long)a.bblocks * a.shares), L::kThreads, 0, st>>>(a); }
+
+template <int P, typename T>
+void backward(const ftp_token_loss_shape& s, const void* x, const void* w, const void* labels, const float* lse, const float* dloss, void* dx, void* dw, char* ws, hipStream_t st)
+{
+    const Plan p = plan_of(s, true);
+    const Buffers b = buffers_of(s, p, true, ws);
+    gather<P>(s, p, b, x, labels, st);
+    const Matrix all = weight<P>(s, p, b, w, st), xc = {b.xc, p.Cp, p.Np * p.Cp, p.Np, p.Cp};
+    for (long long v0 = 0; v0 < s.vocab; v0 += p.piece) {
+        const int n = (int)std::min<long long>(p.piece, s.vocab - v0);
+        Matrix wp = all;
+        wp.p += v0 * all.stride;
+        wp.rows = n;
+        const Matrix g = {b.g, p.ids, p.Np * p.ids, p.Np, (int)p.ids};
+        LogitArgs a = {};
+        a.w = wp; a.x = xc; a.count = b.count; a.label = b.label; a.planes = P; a.vocab = s.vocab; a.piece0 = (int)v0; a.c = s.scale * kLog2e;
+        a.index = b.index; a.lse = lse; a.dloss = dloss; a.g = b.g; a.gstride = p.ids; a.gplane = p.Np * p.ids;
+        if (p.logits.block == 256) logits<Big<false, false>, P, false>(a, s.rows, st);
+        else logits<Mid<false, false>, P, false>(a, s.rows, st);
+        GradArgs k = {};
+        k.count = b.count; k.planes = P; k.C = s.channels; k.scale = s.scale; k.mean = !dloss; k.pstride = p.Cp;
+        if (dx && s.rows) {
+            const int block = p.dx.block;
+            k.a = wp; k.b = g; k.stages = (int)ceil_div(n, 32); k.shares = p.dx.shares; k.add = v0 > 0;
+            k.ablocks = (int)ceil_div(p.Cp, block); k.bblocks = (int)ceil_div(s.rows, block);
+            k.part = b.dx; k.pshare = p.Np * p.Cp;
+            if (p.dx.block == 256) dx_pass<Big<true, false>>(k, st);
+            else dx_pass<Mid<true, false>>(k, st);
+        }
+        if (dw) {
+            const int block = p.dw.block;
+            k.a = xc; k.b = g; k.shares = p.dw.shares; k.add = n;
+            k.ablocks = (int)ceil_div(p.Cp, block); k.bblocks = (int)ceil_div(n, block);
+            k.part = b.dw; k.pshare = p.piece * p.Cp;
+            T* out = (T*)dw + v0 * s.dw_stride;
+            k.out = out; k.ostride = s.dw_stride;
+            if (p.dw.block == 256) dw_pass<Big<true, true>, T>(k, st);
+            else dw_pass<Mid<true, true>, T>(k, st);
+            if (k.shares > 1)
+                k_loss_sum<T><<<pass_grid(n * ceil_div(s.channels, 4)), 256, 0, st>>>(b.dw, p.Cp, k.pshare, k.shares, nullptr, n, out, s.dw_stride, s.channels, s.scale, !dloss, b.count);
+        }
+    }
+    if (dx && s.rows)
+        k_loss_sum<T><<<pass_grid(s.rows * ceil_div(s.channels, 4)), 256, 0, st>>>(b.dx, p.Cp, p.Np * p.Cp, p.dx.shares, b.place, s.rows, dx, s.dx_stride, s.channels, s.scale, !dloss, b.count);
+}
+
+}  // namespace
+
+bool token_loss_fits(const ftp_token_loss_shape& s)
+{
+    // rows, ids and blocks are 32-bit numbers, and a launch has fewer than 2^32 threads
+    return s.rows <= (1ll << 22) && s.vocab <= (1 << 24) && s.channels <= (1 << 14) && ceil_div(s.rows, 256) * ceil_div(s.vocab, 256) < (1 << 21);
+}
+size_t token_loss_forward_workspace(const ftp_token_loss_shape& s) { return buffers_of(s, plan_of(s, false), false, nullptr).bytes; }
+size_t token_loss_backward_workspace(const ftp_token_loss_shape& s) { return buffers_of(s, plan_of(s, true), true, nullptr).bytes; }
+
+void token_loss_forward(const ftp_token_loss_shape& s, const void* x, const void* w, const void* labels, float* loss, float* lse, float* mean, char* ws, hipStream_t st)
+{
+    if (s.dtype == FTP_BF16) forward<1>(s, x, w, labels, loss, lse, mean, ws, st);
+    else forward<3>(s, x, w, labels, loss, lse, mean, ws, st);
+}
+void token_loss_backward(const ftp_token_loss_shape& s, const void* x, const void* w, const void* labels, const float* lse, const float* dloss, void* dx, void* dw, char* ws,
+                         hipStream_t st)
+{
+    if (s.dtype == FTP_BF16) backward<1, bf16_t>(s, x, w, labels, lse, dloss, dx, dw, ws, st);
+    else backward<3, float>(s, x, w, labels, lse, dloss, dx, dw, ws, st);
+}
+
+}  // namespace ftp
