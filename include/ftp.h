@@ -377,7 +377,7 @@ int ftp_embedding_backward(const ftp_embedding_shape* shape, const void* ids, co
  * to them as an operand of those products; all sums are fp32.  Rows without a label have dx = 0. */
 typedef struct {
     int64_t rows;                  /* may be 0; at most 2^22 */
-    int32_t vocab, channels;       /* >= 1; at most 2^24 and 2^14, and blocks of 256 x 256 logits fewer than 2^21 */
+    int32_t vocab, channels;       /* >= 1; at most 2^22 and 2^14, and blocks of 256 x 256 logits fewer than 2^21 */
     int32_t dtype;                 /* ftp_dtype of x, weight, dx and dweight */
     int32_t id_type;               /* ftp_id_type of labels [rows] */
     float scale;                   /* finite */

@@ -64,7 +64,7 @@ __global__ __launch_bounds__(256) void k_normed(const T* x, long long mstride, l
             planes_of<P>(v[0], v[1], q[j]);
         }
 #pragma unroll
-        for (int p = 0; p < P; ++p) *(uint4*)(to + p * plane + 8 * u) = uint4{q[0][p], q[1][p], q[2][p], q[3][p]};
+        for (int p = 0; p < P; ++p) *(uint4*)(to + p * plane + ((long long)(c0 >> 5) * Rp + r) * 32 + (c0 & 31)) = uint4{q[0][p], q[1][p], q[2][p], q[3][p]};
     }
 }
 
@@ -76,7 +76,7 @@ struct StepArgs {
     // what becomes of the sums v: f0 old + f1 v, old being planes too
     float f0, f1;
     const bf16_t* old; bf16_t* to;
-    long long plane_old, plane_to, next; int stride, arows, brows;      // (old and to lie alike) [matrix: next][index of b: stride][index of a]
+    long long plane, next; int stride, arows, brows;        // (old and to: a Matrix of brows rows and arows columns each) [matrix: next]
     void* out; int orows, ocols;                    // instead of planes: the results, rows along b
     float* part; long long pshare;                  // [share][matrix][index of b][stride]
 };
@@ -97,9 +97,9 @@ __device__ __forceinline__ f32x4 planes_sum(const bf16_t* p, long long plane)
 template <typename T, int P>
 __device__ __forceinline__ void finish(const StepArgs& a, int matrix, int i, int j, f32x4 v, bool mirror)
 {
-    const long long at = matrix * a.next + (long long)j * a.stride + i;
+    const long long block = a.brows * 32ll, at = matrix * a.next + (i >> 5) * block + j * 32 + (i & 31);
     v *= a.f1;
-    if (a.f0 != 0) v += a.f0 * planes_sum<P>(a.old + at, a.plane_old);
+    if (a.f0 != 0) v += a.f0 * planes_sum<P>(a.old + at, a.plane);
     if (a.out) {
         T* p = (T*)a.out + ((long long)matrix * a.orows + j) * a.ocols + i;
         if (j < a.orows)
@@ -112,14 +112,14 @@ __device__ __forceinline__ void finish(const StepArgs& a, int matrix, int i, int
     planes_of<P>(v[2], v[3], y);
 #pragma unroll
     for (int p = 0; p < P; ++p) {
-        bf16_t* to = a.to + p * a.plane_to;
+        bf16_t* to = a.to + p * a.plane;
         *(uint2*)(to + at) = uint2{x[p], y[p]};
         if (mirror) {
-            bf16_t* m = to + matrix * a.next + (long long)i * a.stride + j;
+            bf16_t* m = to + matrix * a.next + (j >> 5) * block + i * 32 + (j & 31);
             m[0] = (bf16_t)x[p];
-            m[a.stride] = (bf16_t)(x[p] >> 16);
-            m[2ll * a.stride] = (bf16_t)y[p];
-            m[3ll * a.stride] = (bf16_t)(y[p] >> 16);
+            m[32] = (bf16_t)(x[p] >> 16);
+            m[64] = (bf16_t)y[p];
+            m[96] = (bf16_t)(y[p] >> 16);
         }
     }
 }
@@ -245,12 +245,12 @@ void run(const ftp_orthogonal_shape& s, const T* x, T* out, char* ws, hipStream_
     const long long xnext = (long long)p.Rp * p.Cp, xplane = s.count * xnext, qnext = (long long)p.mp * p.mp, qplane = s.count * qnext;
     k_squares<T><<<(unsigned)(s.count * p.parts), 256, 0, st>>>(x, s.matrix_stride, s.row_stride, s.rows, s.cols, p.parts, b.sums);
     k_normed<T, P><<<dim3((unsigned)std::min<long long>(ceil_div(xnext, 2048), 4096), (unsigned)s.count), 256, 0, st>>>(x, s.matrix_stride, s.row_stride, s.rows, s.cols, p.parts, b.sums, s.eps, b.x[0], p.Rp, p.Cp, xplane);
-    const Matrix S = {b.s, p.mp, qplane, p.mp, p.mp}, Q = {b.q, p.mp, qplane, p.mp, p.mp};
+    const Matrix S = blocked(b.s, p.mp, p.mp, qplane), Q = blocked(b.q, p.mp, p.mp, qplane);
     for (int step = 0; step < s.steps; ++step) {
-        const Matrix X = {b.x[step & 1], p.Cp, xplane, p.Rp, p.Cp};
+        const Matrix X = blocked(b.x[step & 1], p.Rp, p.Cp, xplane);
         StepArgs k = {};
         k.planes = P; k.count = s.count; k.part = b.part;
-        k.stride = k.arows = k.brows = p.mp; k.next = qnext; k.plane_old = k.plane_to = qplane; k.pshare = qplane;
+        k.stride = k.arows = k.brows = p.mp; k.next = qnext; k.plane = qplane; k.pshare = qplane;
         // S
         k.a = k.b = X; k.anext = k.bnext = xnext; k.stages = std::max(p.Rp, p.Cp) / 32; k.symmetric = 1; k.f1 = 1; k.to = b.s;
         if (p.tall) product<true, true, T, P>(k, p.s, st);
@@ -260,7 +260,7 @@ void run(const ftp_orthogonal_shape& s, const T* x, T* out, char* ws, hipStream_
         product<false, false, T, P>(k, p.q, st);
         // a X + that times X
         k.symmetric = 0; k.f0 = s.a; k.f1 = 1; k.old = b.x[step & 1]; k.to = b.x[~step & 1];
-        k.stride = k.arows = p.Cp; k.brows = p.Rp; k.next = xnext; k.plane_old = k.plane_to = xplane; k.pshare = xplane;
+        k.stride = k.arows = p.Cp; k.brows = p.Rp; k.next = xnext; k.plane = xplane; k.pshare = xplane;
         if (step + 1 == s.steps) { k.out = out; k.orows = s.rows; k.ocols = s.cols; }
         if (p.tall) {
             k.a = Q; k.b = X; k.anext = qnext; k.bnext = xnext;

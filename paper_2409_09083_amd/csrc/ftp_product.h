@@ -9,7 +9,9 @@
 #pragma once
 #include "ftp_tokens.h"
 
+#include <tuple>
 #include <type_traits>
+#include <utility>
 
 namespace ftp {
 
@@ -19,24 +21,42 @@ typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
-// A matrix in bfloats, 16-byte aligned, its stride a multiple of 8 elements.  along: rows are indices, cols the contraction (a multiple of 32, the part that is none in zeros); across: rows the contraction.
+// f(0), f(1), .. f(N - 1) with constants
+template <class F, int... I>
+__device__ __forceinline__ void unrolled(F f, std::integer_sequence<int, I...>) { (f(std::integral_constant<int, I>{}), ...); }
+template <int N, class F>
+__device__ __forceinline__ void unrolled(F f) { unrolled(f, std::make_integer_sequence<int, N>{}); }
+
+// A matrix in bfloats: element (r, c) lies at (c / 32) * block + r * row + c % 32.  So row-major ones (block 32) and those laid out for the products (row 32: 32 columns of all rows one behind the other) go the same way; of
+// the latter a stage is one run of memory along and a few across, where rows of 64 bytes each half a cache line were twice the requests to the L2.  16-byte aligned, `row` a multiple of 8; along: cols is a multiple of the
+// stages', the part that is none in zeros; across: rows past the end, up to a stage's, are zeros or out of the matrix.
 struct Matrix {
     const bf16_t* p;
-    long long stride, plane;                        // elements between rows, between planes
-    long long rows;
+    long long row, block, plane;                    // elements between rows, between blocks of 32 columns, between planes
+    long long rows, size;                           // size: elements from p to the end of a plane
     int cols;
 };
+inline Matrix blocked(const bf16_t* p, long long rows, int cols, long long plane) { return Matrix{p, 32, rows * 32, plane, rows, rows * cols, cols}; }
+inline Matrix row_major(const bf16_t* p, long long stride, long long rows, int cols) { return Matrix{p, stride, 32, 0, rows, (rows - 1) * stride + cols, cols}; }
+// rows [r0, r0 + n)
+inline Matrix rows_of(Matrix m, long long r0, long long n)
+{
+    m.p += r0 * m.row;
+    m.size -= r0 * m.row;
+    m.rows = n;
+    return m;
+}
 
 // A workgroup's block BA x BB by WA x WB wavefronts; XA, XB: the operand lies across.
-template <int BA_, int BB_, int WA_, int WB_, bool XA_, bool XB_, int KS_ = 32>
+template <int BA_, int BB_, int WA_, int WB_, bool XA_, bool XB_, int KS_ = 32, int STAGES = 4>
 struct Product {
-    static constexpr int BA = BA_, BB = BB_, WA = WA_, WB = WB_, kThreads = WA * WB * 64, KS = KS_, kAhead = 3;
+    static constexpr int BA = BA_, BB = BB_, WA = WA_, WB = WB_, kThreads = WA * WB * 64, KS = KS_, kStages = STAGES;
     static constexpr bool XA = XA_, XB = XB_;
     static constexpr int IA = BA / WA / 32, IB = BB / WB / 32;                     // 32 x 32 blocks of a wavefront
     static constexpr int kBytesA = BA * KS * 2, kBytesB = BB * KS * 2;
     static constexpr int kLoadsA = kBytesA / 16 / kThreads, kLoadsB = kBytesB / 16 / kThreads, kLoads = kLoadsA + kLoadsB;
     static_assert(kLoadsA * kThreads * 16 == kBytesA && kLoadsB * kThreads * 16 == kBytesB, "whole loads a thread");
-    static_assert(kAhead * kLoads < 64, "what vmcnt counts");
+    static_assert((kStages - 1) * kLoads < 64, "what vmcnt counts");
     struct Stage { char a[kBytesA], b[kBytesB]; };
 
     // Which 16 bytes of a row lie where: rows of 64 or 128 bytes (along) so that 16 rows' equal chunks meet no bank twice, longer ones (across) so that 4 rows x 64 bytes do not.
@@ -76,16 +96,16 @@ struct Product {
         int at[N];                                  // this thread's chunks, bytes from the base
         __device__ __forceinline__ void init(const Matrix& m, long long i0, long long k0)
         {
-            const long long first = X ? k0 * m.stride + i0 : i0 * m.stride + k0;
+            const long long first = X ? k0 * m.row + (i0 >> 5) * m.block : i0 * m.row + (k0 >> 5) * m.block;
             base = (const char*)(m.p + first);
             plane = m.plane * 2;
-            left = ((m.rows - 1) * m.stride + m.cols - first) * 2;
-            step = X ? KS * m.stride * 2 : KS * 2;
+            left = (m.size - first) * 2;
+            step = X ? KS * m.row * 2 : KS / 32 * m.block * 2;
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 constexpr int kRow = X ? B / 8 : KS / 8;                            // chunks of a row
                 const int u = threadIdx.x + kThreads * i, row = u / kRow, chunk = (u % kRow) ^ mix<B, X>(row);
-                at[i] = (int)(row * m.stride * 2) + chunk * 16;
+                at[i] = (int)((chunk >> 2) * m.block * 2) + (int)(row * m.row * 2) + (chunk & 3) * 16;
             }
         }
         __device__ __forceinline__ void fetch(char* to, long long stage, int p, bool any) const
@@ -100,13 +120,23 @@ struct Product {
         }
     };
 
+    template <int I, class F>
+    static __device__ __forceinline__ void rest(int left, F f)
+    {
+        if constexpr (I + 1 < kStages) {
+            if (left <= I) return;
+            f(std::integral_constant<int, I>{});
+            rest<I + 1>(left, f);
+        }
+    }
+
     static __device__ __forceinline__ int wave_a() { return (__builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % WA) * (IA * 32); }
     static __device__ __forceinline__ int wave_b() { return (__builtin_amdgcn_readfirstlane(threadIdx.x >> 6) / WA) * (IB * 32); }
 
-    // acc[i][j] += the block at (a0, b0) over the stages [lo, hi) of the contraction.  planes: of both operands.  The stages s are distinct objects, so that loads into one are no reason to wait for those
+    // acc[i][j] += the block at (a0, b0) over the stages [lo, hi) of the contraction.  planes: of both operands.  The stages are distinct objects, so that loads into one are no reason to wait for those
     // into another.  At the end all of this wavefront's loads have landed.
-    static __device__ __forceinline__ void run(f32x16 (&acc)[IA][IB], const Matrix& a, const Matrix& b, long long a0, long long b0, int lo, int hi, int planes, Stage& s0, Stage& s1, Stage& s2,
-                                               Stage& s3)
+    template <class... S>
+    static __device__ __forceinline__ void run(f32x16 (&acc)[IA][IB], const Matrix& a, const Matrix& b, long long a0, long long b0, int lo, int hi, int planes, S&... stages)
     {
         Source<BA, XA, kLoadsA> fa;
         Source<BB, XB, kLoadsB> fb;
@@ -139,7 +169,7 @@ struct Product {
                 for (int j = 0; j < IB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[from][i], y[from][j], acc[i][j], 0, 0, 0);
             __builtin_amdgcn_sched_barrier(0);
         };
-        // this wavefront's loads of the next stage have landed (`kAhead` are on their way, a load more or less each), its reads of this one too; behind the barrier everybody's
+        // this wavefront's loads of the next stage have landed (`ahead` stages behind it are on their way), its reads of this one too; behind the barrier everybody's
         const auto landed = [&](auto ahead) __attribute__((always_inline)) {
             constexpr int n = ahead * kLoads;
             asm volatile("" ::: "memory");
@@ -162,35 +192,41 @@ struct Product {
                     multiply(odd);
                 }
             }
-            landed(std::integral_constant<int, kAhead - 1>{});
+            landed(std::integral_constant<int, kStages - 2>{});
             fetch(now);
             read(even, next, 0);
             multiply(odd);
         };
-        fetch(s0);
-        fetch(s1);
-        fetch(s2);
-        fetch(s3);
-        landed(std::integral_constant<int, kAhead>{});
-        read(even, s0, 0);
+        static_assert(sizeof...(S) == kStages, "a place a stage");
+        const std::tuple<S&...> at(stages...);
+        const auto place = [&](auto i) __attribute__((always_inline)) -> Stage& { return std::get<i % kStages>(at); };
+        unrolled<kStages>([&](auto i) __attribute__((always_inline)) { fetch(place(i)); });
+        landed(std::integral_constant<int, kStages - 1>{});
+        read(even, std::get<0>(at), 0);
         // (one way through the loop: where ways meet, the compiler waits for all loads)
-        for (int s = total >> 2; s; --s) {
-            step(s0, s1);
-            step(s1, s2);
-            step(s2, s3);
-            step(s3, s0);
-        }
-        if (total & 3) {
-            step(s0, s1);
-            if ((total & 3) > 1) {
-                step(s1, s2);
-                if ((total & 3) > 2) step(s2, s3);
-            }
-        }
+        for (int s = total / kStages; s; --s)
+            unrolled<kStages>([&](auto i) __attribute__((always_inline)) { step(place(i), place(std::integral_constant<int, i + 1>{})); });
+        const int left = total % kStages;
+        rest<0>(left, [&](auto i) __attribute__((always_inline)) { step(place(i), place(std::integral_constant<int, i + 1>{})); });
         __builtin_amdgcn_s_waitcnt(0x70);
         asm volatile("" ::: "memory");
     }
 
+    // f(v, a): every result of this lane, and its index along a counted from the lane's first one
+    template <class F>
+    static __device__ __forceinline__ void all(f32x16 (&acc)[IA][IB], F f)
+    {
+#pragma unroll
+        for (int i = 0; i < IA; ++i)
+#pragma unroll
+            for (int j = 0; j < IB; ++j)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    float v = acc[i][j][r];
+                    f(v, 32 * i + 8 * (r >> 2) + (r & 3));
+                    acc[i][j][r] = v;
+                }
+    }
     // f(a, b, v): index of the first of four neighbours along a, index along b, values; of this wavefront, from the block's corner
     template <class F>
     static __device__ __forceinline__ void each(const f32x16 (&acc)[IA][IB], F f)

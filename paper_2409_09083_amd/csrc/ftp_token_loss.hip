@@ -15,9 +15,11 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int kChunk = 64;                          // rows whose labels one wavefront looks at
+constexpr int kPackRows = 4096;                     // from here on W is laid out for the products
 constexpr int kFew = 32;                            // most rows of the forward pass that reads W at the memory's rate
 
 template <bool XA, bool XB> using Big = Product<256, 256, 2, 4, XA, XB>;
+typedef Product<256, 128, 2, 2, false, false, 32, 3> Two;         // two workgroups a CU: one's powers beside the other's products
 template <bool XA, bool XB> using Mid = Product<128, 128, 2, 2, XA, XB>;
 typedef Product<128, 32, 4, 1, false, false, 64> Few;
 
@@ -31,7 +33,7 @@ __global__ __launch_bounds__(256) void k_labelled(const void* ids, int wide, lon
     if ((threadIdx.x & 63) == 0 && chunk * kChunk < std::max(rows, 1ll)) counts[chunk] = (int)__popcll(all);
 }
 
-// 8 neighbours c0 .. c0 + 7 of a row of C as planes; zeros past its end
+// 8 neighbours c0 .. c0 + 7 of a row of C as planes, to where they lie; zeros past its end
 template <typename T, int P>
 __device__ __forceinline__ void copy8(const T* row, int c0, int C, bf16_t* to, long long plane)
 {
@@ -43,20 +45,20 @@ __device__ __forceinline__ void copy8(const T* row, int c0, int C, bf16_t* to, l
         for (int j = 0; j < 8; ++j) e[j] = c0 + j < C ? row[c0 + j] : (T)0;
         __builtin_memcpy(v.w, e, sizeof(e));
     }
-    if constexpr (P == 1) __builtin_memcpy(to + c0, v.w, 16);
+    if constexpr (P == 1) __builtin_memcpy(to, v.w, 16);
     else {
         uint32_t q[4][P];
 #pragma unroll
         for (int j = 0; j < 4; ++j) planes_of<P>(v.get(2 * j), v.get(2 * j + 1), q[j]);
 #pragma unroll
-        for (int p = 0; p < P; ++p) *(uint4*)(to + p * plane + c0) = uint4{q[0][p], q[1][p], q[2][p], q[3][p]};
+        for (int p = 0; p < P; ++p) *(uint4*)(to + p * plane) = uint4{q[0][p], q[1][p], q[2][p], q[3][p]};
     }
 }
 
 struct GatherArgs {
     const void* ids; const void* x; const int* counts;
     bf16_t* xc; int* index; int* label; int* place; int* count;
-    long long rows, stride, plane;
+    long long rows, stride, plane, block;           // of xc: as a Matrix lies
     int wide, vocab, C, Cp;
 };
 
@@ -94,25 +96,27 @@ __global__ __launch_bounds__(256) void k_gather(const GatherArgs a)
     const int here = (int)std::min<long long>(kChunk, a.rows - row0);
     for (int u = tid; u < here * per; u += 256) {
         const int r = u / per, c0 = (u - r * per) * 8;
-        if (where[r] >= 0) copy8<T, P>((const T*)a.x + (row0 + r) * a.stride, c0, a.C, a.xc + (long long)where[r] * a.Cp, a.plane);
+        if (where[r] >= 0) copy8<T, P>((const T*)a.x + (row0 + r) * a.stride, c0, a.C, a.xc + (c0 >> 5) * a.block + where[r] * 32 + (c0 & 31), a.plane);
     }
     if (chunk == 0) {
         const int end = (all + 63) & ~63;
         if (tid == 0) *a.count = all;
-        for (int u = tid; u < (end - all) * per; u += 256)
+        for (int u = tid; u < (end - all) * per; u += 256) {
+            const int r = u / per, c0 = (u - r * per) * 8;
 #pragma unroll
-            for (int p = 0; p < P; ++p) *(uint4*)(a.xc + p * a.plane + (long long)all * a.Cp + 8ll * u) = uint4{0, 0, 0, 0};
+            for (int p = 0; p < P; ++p) *(uint4*)(a.xc + p * a.plane + (c0 >> 5) * a.block + (all + r) * 32 + (c0 & 31)) = uint4{0, 0, 0, 0};
+        }
     }
 }
 
-// Rows of W as planes, their length rounded up with zeros.
+// W as planes, laid out for the products; zeros up to Rp rows of Cp.
 template <typename T, int P>
-__global__ __launch_bounds__(256) void k_pack_rows(const T* w, long long stride, long long rows, int C, int Cp, bf16_t* to, long long plane)
+__global__ __launch_bounds__(256) void k_pack_rows(const T* w, long long stride, int rows, int C, int Rp, int Cp, bf16_t* to, long long plane)
 {
     const int per = Cp >> 3;
-    for (long long u = (long long)blockIdx.x * 256 + threadIdx.x; u < rows * per; u += (long long)gridDim.x * 256) {
-        const long long r = u / per;
-        copy8<T, P>(w + r * stride, (int)(u - r * per) * 8, C, to + r * Cp, plane);
+    for (long long u = (long long)blockIdx.x * 256 + threadIdx.x; u < (long long)Rp * per; u += (long long)gridDim.x * 256) {
+        const int r = (int)(u / per), c0 = (int)(u - (long long)r * per) * 8;
+        copy8<T, P>(w + r * stride, r < rows ? c0 : 0, r < rows ? C : 0, to + ((long long)(c0 >> 5) * Rp + r) * 32 + (c0 & 31), plane);
     }
 }
 
@@ -124,78 +128,100 @@ struct LogitArgs {
     const void* ids;
     int wide, planes, stages, vocab, ablocks, bblocks;
     int piece0;                                     // the piece's first id
-    float c;                                        // scale * log2(e)
-    float2* part; float* target;                    // forward: [row][ablocks] maximum and sum of a block's powers of 2; the labels' logits times log2(e)
+    float c; int negate;                            // |scale| * log2(e), and whether scale is negative
+    float2* part; float* target;                    // forward: [row][ablocks] maximum and sum of a block's powers of 2; the labels' products
     const int* index; const float* lse; const float* dloss;     // backward
-    bf16_t* g; long long gstride, gplane;
+    bf16_t* g; long long gblock, gplane;            // G, as a Matrix lies
 };
 
 // What a block of logits leaves: STATS, of each row its maximum m (in powers of 2) and the sum of the others' powers above it, and the label's logit; else PLANES of G.
 template <class L, int PLANES, bool STATS>
 __global__ __launch_bounds__(L::kThreads, 2) void k_logits(const LogitArgs a)
 {
-    __shared__ __align__(16) typename L::Stage s0, s1, s2, s3;
+    __shared__ __align__(16) typename L::Stage s0, s1, s2;
     __shared__ float2 red[L::WA][L::BB];
     int ia, ib;
     if (!block_of((int)blockIdx.x, a.ablocks, a.bblocks, ia, ib)) return;
     const int a0 = ia * L::BA, b0 = ib * L::BB, rows = a.count ? *a.count : (int)a.x.rows;
     if (b0 >= rows) return;
     f32x16 acc[L::IA][L::IB] = {};
-    L::run(acc, a.w, a.x, a0, b0, 0, a.stages, a.planes, s0, s1, s2, s3);
+    if constexpr (L::kStages == 3) L::run(acc, a.w, a.x, a0, b0, 0, a.stages, a.planes, s0, s1, s2);
+    else {
+        __shared__ __align__(16) typename L::Stage s3;
+        L::run(acc, a.w, a.x, a0, b0, 0, a.stages, a.planes, s0, s1, s2, s3);
+    }
     const int l = threadIdx.x & 63, h = l >> 5, wa = L::wave_a(), wb = L::wave_b();
-    const int left = (int)a.w.rows - a0 - wa - 4 * h;              // ids of the piece from this lane's first one on
+    if (a.negate)
+        L::all(acc, [&](float& v, int) __attribute__((always_inline)) { v = -v; });
+    const int left = (int)a.w.rows - a0 - wa;                      // ids of the piece from this wavefront's first one on
+    if (left < 32 * L::IA)                                          // (no power of those past its end)
+        L::all(acc, [&](float& v, int at) __attribute__((always_inline)) { v = at + 4 * h < left ? v : -INFINITY; });
 #pragma unroll
     for (int j = 0; j < L::IB; ++j) {
         const int row = b0 + wb + 32 * j + (l & 31);
         const bool there = row < rows;
         const int id = !there ? -1 : a.label ? a.label[row] : id_of(a.ids, a.wide, row, a.vocab);
         const int mine = id < 0 ? -1 : id - a.piece0 - a0 - wa - 4 * h;         // the label, counted from this lane's first id
+        const bool look = __any(mine >= 0 && mine < 32 * L::IA);    // (a wavefront's rows have few labels in its block: most have none)
         if constexpr (STATS) {
+            if (look) {
+                float t = 0;
+#pragma unroll
+                for (int i = 0; i < L::IA; ++i)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) t = mine == 32 * i + 8 * (r >> 2) + (r & 3) ? acc[i][j][r] : t;
+                if (mine >= 0 && mine < 32 * L::IA && !(mine & 4)) a.target[row] = t;          // (this lane's ids: the others are the other half's)
+            }
             float m = -INFINITY, sum = 0;
 #pragma unroll
             for (int i = 0; i < L::IA; ++i)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int at = 32 * i + 8 * (r >> 2) + (r & 3);
-                    acc[i][j][r] = at < left ? acc[i][j][r] * a.c : -INFINITY;
-                    if (mine == at && there) a.target[row] = acc[i][j][r];
-                    m = fmaxf(m, acc[i][j][r]);
-                }
-            m = fmaxf(m, __shfl_xor(m, 32));
+                for (int r = 0; r < 16; ++r) m = fmaxf(m, acc[i][j][r]);
+            m = fmaxf(m, __shfl_xor(m, 32)) * a.c;
             const float ref = m == -INFINITY ? 0.0f : m;            // (a block of nothing but -infinity sums up to 0)
 #pragma unroll
             for (int i = 0; i < L::IA; ++i)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) sum += __builtin_amdgcn_exp2f(acc[i][j][r] - ref);
+                for (int r = 0; r < 16; ++r) sum += __builtin_amdgcn_exp2f(fmaf(acc[i][j][r], a.c, -ref));
             sum += __shfl_xor(sum, 32);
             if (h == 0) red[wa / (L::IA * 32)][wb + 32 * j + l] = float2{m, sum};
         } else {
-            float lse2 = 0, weight = 0;
+            float lse2 = INFINITY, weight = 1.0f;                   // (rows behind the last one have powers of 0)
             if (there) {
                 const int from = a.index[row];
                 lse2 = a.lse[from] * kLog2e;
-                weight = a.dloss ? a.dloss[from] : 1.0f;
+                if (a.dloss) weight = a.dloss[from];
             }
-            if (row < ((rows + 63) & ~63)) {
-                bf16_t* to = a.g + (long long)row * a.gstride + a0 + wa + 4 * h;
+#pragma unroll
+            for (int i = 0; i < L::IA; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) acc[i][j][r] = __builtin_amdgcn_exp2f(fmaf(acc[i][j][r], a.c, -lse2));
+            if (look)
 #pragma unroll
                 for (int i = 0; i < L::IA; ++i)
 #pragma unroll
-                    for (int r = 0; r < 16; r += 4) {
-                        float v[4];
+                    for (int r = 0; r < 16; ++r) acc[i][j][r] -= mine == 32 * i + 8 * (r >> 2) + (r & 3) ? 1.0f : 0.0f;
+            if (a.dloss)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const int at = 32 * i + 2 * r + e;
-                            const float p = __builtin_amdgcn_exp2f(fmaf(acc[i][j][r + e], a.c, -lse2));
-                            v[e] = there && at < left ? (mine == at ? p - 1.0f : p) * weight : 0.0f;
-                        }
-                        uint32_t x[PLANES], y[PLANES];
-                        planes_of<PLANES>(v[0], v[1], x);
-                        planes_of<PLANES>(v[2], v[3], y);
+                for (int i = 0; i < L::IA; ++i)
 #pragma unroll
-                        for (int p = 0; p < PLANES; ++p) *(uint2*)(to + p * a.gplane + 32 * i + 2 * r) = uint2{x[p], y[p]};
+                    for (int r = 0; r < 16; ++r) acc[i][j][r] *= weight;
+            if (row >= ((rows + 63) & ~63)) continue;
+            bf16_t* to = a.g + ((a0 + wa) >> 5) * a.gblock + (long long)row * 32 + 8 * h;
+#pragma unroll
+            for (int i = 0; i < L::IA; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; r += 8) {
+                    // registers r .. r + 3 are ids 2 r + 4 h .. of the block, the next four 2 r + 8 + 4 h ..: halves exchanged, 8 neighbours a lane
+                    uint32_t x[2][2][PLANES];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) planes_of<PLANES>(acc[i][j][r + 2 * e], acc[i][j][r + 2 * e + 1], x[e >> 1][e & 1]);
+#pragma unroll
+                    for (int p = 0; p < PLANES; ++p) {
+                        const auto u = __builtin_amdgcn_permlane32_swap(x[0][0][p], x[1][0][p], false, false), v = __builtin_amdgcn_permlane32_swap(x[0][1][p], x[1][1][p], false, false);
+                        *(uint4*)(to + p * a.gplane + i * a.gblock + 2 * r) = uint4{u[0], v[0], u[1], v[1]};
                     }
-            }
+                }
         }
     }
     if constexpr (STATS) {
@@ -215,7 +241,7 @@ __global__ __launch_bounds__(L::kThreads, 2) void k_logits(const LogitArgs a)
 }
 
 // The blocks' statistics joined: a wavefront a row, its lanes' blocks in turn.  Losses and log-sums of all rows (0 where there is no label), and each workgroup's sum of losses and labelled rows.
-__global__ __launch_bounds__(256) void k_loss_join(const float2* part, const float* target, const int* place, const void* ids, int wide, long long rows, int vocab, int blocks, float* loss,
+__global__ __launch_bounds__(256) void k_loss_join(const float2* part, const float* target, const int* place, const void* ids, int wide, long long rows, int vocab, int blocks, float c, float* loss,
                                                    float* lse, double* sums, float* mean)
 {
     __shared__ double total[4];
@@ -238,7 +264,7 @@ __global__ __launch_bounds__(256) void k_loss_join(const float2* part, const flo
 #pragma unroll
             for (int k = 32; k; k >>= 1) s += __shfl_xor(s, k);
             two = fmaf(ref, kLn2, logf(s));
-            one = fmaf(ref - target[at], kLn2, logf(s));         // (one word alone has loss 0)
+            one = fmaf(fmaf(-target[at], c, ref), kLn2, logf(s));
             sum += one;
             ++n;
         }
@@ -360,7 +386,7 @@ long long round_up(long long v, long long to) { return ceil_div(v, to) * to; }
 
 struct Plan {
     int planes, Cp, blocks, pack_w, gather, few;
-    long long Np, chunks, piece, ids;               // ids: of a piece, rounded up to whole blocks
+    long long Np, Vp, chunks, piece;                // rows and ids up to whole blocks of 64; ids of a piece, whole blocks of 256
     Split logits, dx, dw;
     int joins;
 };
@@ -370,6 +396,7 @@ Plan plan_of(const ftp_token_loss_shape& s, bool back)
     p.planes = planes_of_type(s.dtype);
     p.Cp = padded(s.channels);
     p.Np = round_up(std::max<long long>(s.rows, 1), 64);
+    p.Vp = round_up(s.vocab, 64);
     p.chunks = ceil_div(std::max<long long>(s.rows, 1), kChunk);
     const long long terms = p.planes == 1 ? 1 : 6;
     // whether W, and few rows of x, can be read as they lie (their addresses are looked at by the call: scratch is there for both ways)
@@ -384,7 +411,6 @@ Plan plan_of(const ftp_token_loss_shape& s, bool back)
     const long long fits = std::min((512ll << 20) / (2 * p.planes * p.Np) / 256 * 256, 1ll << 20), all = round_up(s.vocab, 256);
     const long long pieces = ceil_div(all, std::max(256ll, fits));
     p.piece = round_up(ceil_div(s.vocab, pieces), 256);
-    p.ids = p.piece;
     p.logits = split_of(p.piece, s.rows, p.Cp / 32 * terms, 128, 1);
     p.dx = split_of(s.channels, s.rows, p.piece / 32 * terms, 128, 16);
     p.dw = split_of(s.channels, p.piece, p.Np / 32 * terms, 128, 16);
@@ -407,13 +433,13 @@ Buffers buffers_of(const ftp_token_loss_shape& s, const Plan& p, bool back, char
     b.place = t.take<int>(p.Np);
     b.count = t.take<int>(1);
     b.xc = t.take<bf16_t>(p.planes * p.Np * p.Cp);
-    b.wc = t.take<bf16_t>((size_t)p.planes * s.vocab * p.Cp);
+    b.wc = t.take<bf16_t>((size_t)p.planes * p.Vp * p.Cp);
     if (!back) {
         b.part = t.take<float2>((size_t)p.Np * p.blocks);
         b.target = t.take<float>(p.Np);
         b.sums = t.take<double>(2 * 1024);
     } else {
-        b.g = t.take<bf16_t>((size_t)p.planes * p.Np * p.ids);
+        b.g = t.take<bf16_t>((size_t)p.planes * p.Np * p.piece);
         b.dx = t.take<float>((size_t)p.dx.shares * p.Np * p.Cp);
         b.dw = t.take<float>(p.dw.shares > 1 ? (size_t)p.dw.shares * p.piece * p.Cp : 0);
     }
@@ -429,21 +455,27 @@ void gather(const ftp_token_loss_shape& s, const Plan& p, const Buffers& b, cons
     k_labelled<<<(unsigned)ceil_div(p.chunks, 4), 256, 0, st>>>(labels, s.id_type, s.rows, s.vocab, b.counts);
     GatherArgs g = {};
     g.ids = labels; g.x = x; g.counts = b.counts; g.xc = b.xc; g.index = b.index; g.label = b.label; g.place = b.place; g.count = b.count;
-    g.rows = s.rows; g.stride = s.x_stride; g.plane = p.Np * p.Cp; g.wide = s.id_type; g.vocab = s.vocab; g.C = s.channels; g.Cp = p.Cp;
+    g.rows = s.rows; g.stride = s.x_stride; g.plane = p.Np * p.Cp; g.block = p.Np * 32; g.wide = s.id_type; g.vocab = s.vocab; g.C = s.channels; g.Cp = p.Cp;
     if constexpr (P == 1) k_gather<bf16_t, 1><<<(unsigned)p.chunks, 256, 0, st>>>(g);
     else k_gather<float, 3><<<(unsigned)p.chunks, 256, 0, st>>>(g);
 }
 
-// W as the products read it
+// W as the products read it: as it lies where it is read once and allows it, else laid out for them.
 template <int P>
-Matrix weight(const ftp_token_loss_shape& s, const Plan& p, const Buffers& b, const void* w, hipStream_t st)
+Matrix weight(const ftp_token_loss_shape& s, const Plan& p, const Buffers& b, const void* w, bool once, hipStream_t st)
 {
-    if (P == 1 && s.channels % 64 == 0 && s.w_stride % 8 == 0 && s.w_stride < (1 << 20) && aligned(w, 16)) return Matrix{(const bf16_t*)w, s.w_stride, 0, s.vocab, p.Cp};
-    const long long plane = (long long)s.vocab * p.Cp;
+    if (P == 1 && once && s.channels % 64 == 0 && s.w_stride % 8 == 0 && s.w_stride < (1 << 20) && aligned(w, 16)) return row_major((const bf16_t*)w, s.w_stride, s.vocab, p.Cp);
+    const long long plane = p.Vp * p.Cp;
     const unsigned grid = pass_grid(plane / 8);
-    if constexpr (P == 1) k_pack_rows<bf16_t, 1><<<grid, 256, 0, st>>>((const bf16_t*)w, s.w_stride, s.vocab, s.channels, p.Cp, b.wc, plane);
-    else k_pack_rows<float, 3><<<grid, 256, 0, st>>>((const float*)w, s.w_stride, s.vocab, s.channels, p.Cp, b.wc, plane);
-    return Matrix{b.wc, p.Cp, plane, s.vocab, p.Cp};
+    if constexpr (P == 1) k_pack_rows<bf16_t, 1><<<grid, 256, 0, st>>>((const bf16_t*)w, s.w_stride, s.vocab, s.channels, (int)p.Vp, p.Cp, b.wc, plane);
+    else k_pack_rows<float, 3><<<grid, 256, 0, st>>>((const float*)w, s.w_stride, s.vocab, s.channels, (int)p.Vp, p.Cp, b.wc, plane);
+    return blocked(b.wc, p.Vp, p.Cp, plane);
+}
+
+void set_scale(LogitArgs& a, float scale)
+{
+    a.c = std::max(std::fabs(scale) * kLog2e, 1e-38f);              // (0 times -infinity, ids past the end, would be no number)
+    a.negate = scale < 0;
 }
 
 template <class L, int P, bool STATS>
@@ -461,19 +493,20 @@ void forward(const ftp_token_loss_shape& s, const void* x, const void* w, const 
     const Plan p = plan_of(s, false);
     const Buffers b = buffers_of(s, p, false, ws);
     LogitArgs a = {};
-    a.planes = P; a.wide = s.id_type; a.vocab = s.vocab; a.c = s.scale * kLog2e; a.part = b.part; a.target = b.target; a.ids = labels;
+    a.planes = P; a.wide = s.id_type; a.vocab = s.vocab; set_scale(a, s.scale); a.part = b.part; a.target = b.target; a.ids = labels;
     const bool plain = p.few && P == 1 && s.channels % 64 == 0 && (s.x_stride % 8 == 0 || s.rows <= 1) && s.x_stride < (1 << 20) && aligned(x, 16);
-    a.w = weight<P>(s, p, b, w, st);
-    if (plain) a.x = Matrix{(const bf16_t*)x, s.x_stride, 0, s.rows, p.Cp};
+    a.w = weight<P>(s, p, b, w, s.rows < kPackRows, st);
+    a.w.rows = s.vocab;
+    if (plain) a.x = row_major((const bf16_t*)x, s.x_stride, s.rows, p.Cp);
     else {
         gather<P>(s, p, b, x, labels, st);
-        a.x = Matrix{b.xc, p.Cp, p.Np * p.Cp, p.Np, p.Cp};
+        a.x = blocked(b.xc, p.Np, p.Cp, p.Np * p.Cp);
         a.count = b.count; a.label = b.label;
     }
     if (p.few) logits<Few, P, true>(a, s.rows, st);
-    else if (p.logits.block == 256) logits<Big<false, false>, P, true>(a, s.rows, st);
+    else if (p.logits.block == 256) logits<Two, P, true>(a, s.rows, st);
     else logits<Mid<false, false>, P, true>(a, s.rows, st);
-    k_loss_join<<<p.joins, 256, 0, st>>>(b.part, b.target, plain ? nullptr : b.place, labels, s.id_type, s.rows, s.vocab, a.ablocks, loss, lse, b.sums, mean);
+    k_loss_join<<<p.joins, 256, 0, st>>>(b.part, b.target, plain ? nullptr : b.place, labels, s.id_type, s.rows, s.vocab, a.ablocks, a.c, loss, lse, b.sums, mean);
     if (p.joins > 1 && mean) k_loss_mean<<<1, 256, 0, st>>>(b.sums, p.joins, mean);
 }
 
@@ -488,17 +521,14 @@ void backward(const ftp_token_loss_shape& s, const void* x, const void* w, const
     const Plan p = plan_of(s, true);
     const Buffers b = buffers_of(s, p, true, ws);
     gather<P>(s, p, b, x, labels, st);
-    const Matrix all = weight<P>(s, p, b, w, st), xc = {b.xc, p.Cp, p.Np * p.Cp, p.Np, p.Cp};
+    const Matrix all = weight<P>(s, p, b, w, s.rows < kPackRows, st), xc = blocked(b.xc, p.Np, p.Cp, p.Np * p.Cp), g = blocked(b.g, p.Np, (int)p.piece, p.Np * p.piece);
     for (long long v0 = 0; v0 < s.vocab; v0 += p.piece) {
         const int n = (int)std::min<long long>(p.piece, s.vocab - v0);
-        Matrix wp = all;
-        wp.p += v0 * all.stride;
-        wp.rows = n;
-        const Matrix g = {b.g, p.ids, p.Np * p.ids, p.Np, (int)p.ids};
+        const Matrix wp = rows_of(all, v0, n);
         LogitArgs a = {};
-        a.w = wp; a.x = xc; a.count = b.count; a.label = b.label; a.planes = P; a.vocab = s.vocab; a.piece0 = (int)v0; a.c = s.scale * kLog2e;
-        a.index = b.index; a.lse = lse; a.dloss = dloss; a.g = b.g; a.gstride = p.ids; a.gplane = p.Np * p.ids;
-        if (p.logits.block == 256) logits<Big<false, false>, P, false>(a, s.rows, st);
+        a.w = wp; a.x = xc; a.count = b.count; a.label = b.label; a.planes = P; a.vocab = s.vocab; a.piece0 = (int)v0; set_scale(a, s.scale);
+        a.index = b.index; a.lse = lse; a.dloss = dloss; a.g = b.g; a.gblock = g.block; a.gplane = g.plane;
+        if (p.logits.block == 256) logits<Two, P, false>(a, s.rows, st);
         else logits<Mid<false, false>, P, false>(a, s.rows, st);
         GradArgs k = {};
         k.count = b.count; k.planes = P; k.C = s.channels; k.scale = s.scale; k.mean = !dloss; k.pstride = p.Cp;
@@ -531,8 +561,8 @@ void backward(const ftp_token_loss_shape& s, const void* x, const void* w, const
 
 bool token_loss_fits(const ftp_token_loss_shape& s)
 {
-    // rows, ids and blocks are 32-bit numbers, and a launch has fewer than 2^32 threads
-    return s.rows <= (1ll << 22) && s.vocab <= (1 << 24) && s.channels <= (1 << 14) && ceil_div(s.rows, 256) * ceil_div(s.vocab, 256) < (1 << 21);
+    // rows, ids, blocks and offsets within a stage are 32-bit numbers, and a launch has fewer than 2^32 threads
+    return s.rows <= (1ll << 22) && s.vocab <= (1 << 22) && s.channels <= (1 << 14) && ceil_div(s.rows, 256) * ceil_div(s.vocab, 256) < (1 << 21);
 }
 size_t token_loss_forward_workspace(const ftp_token_loss_shape& s) { return buffers_of(s, plan_of(s, false), false, nullptr).bytes; }
 size_t token_loss_backward_workspace(const ftp_token_loss_shape& s) { return buffers_of(s, plan_of(s, true), true, nullptr).bytes; }

@@ -146,9 +146,10 @@ def test_large_and_equal_logits(dtype):
     zero = torch.zeros_like(x)
     assert abs(float(head.forward(zero, w, labels)) - math.log(500)) <= 1e-5
     one = vocabulary.TokenLoss(100, 1, 64, dtype)
-    assert float(one.forward(x, w[:1], torch.zeros_like(labels))) == 0
+    # the one logit, |s| < 64, and the log-sum are the same number but for 4 u |s|
+    assert abs(float(one.forward(x, w[:1], torch.zeros_like(labels)))) <= 256 * U
     dx, dw = one.backward(x, w[:1], torch.zeros_like(labels))
-    # exp(s - lse) of the one word is 1 up to the rounding of lse's product with log2(e): |s| < 64
+    # exp(s - lse) of the one word is 1 up to the rounding of lse's product with log2(e)
     assert float(dx.abs().max()) <= 1e-4 and float(dw.abs().max()) <= 1e-4
 
 
