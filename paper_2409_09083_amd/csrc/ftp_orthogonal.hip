@@ -3,7 +3,7 @@
 //
 // A step is three products.  Errors of X, S and their products meet a factor of up to a (3.4) a step where singular values are small, so numbers go from one product to the next as
 // three bfloats (fp32: 24 bits, six products of planes) or two (bfloat: 16 bits, three), and sums are fp32.  S and b S + c S^2 are symmetric: blocks on and below the diagonal are multiplied, the others are mirrored.
-// Products with too few blocks for the chip are cut along their contraction, whose shares a second kernel adds up.
+// Blocks that do not fill a last round of the chip (all, of small products) are cut along their contraction, whose shares a second kernel adds up.
 #include "ftp_training.h"
 #include "ftp_product.h"
 
@@ -16,21 +16,29 @@ namespace {
 template <int B, bool XA, bool XB> struct BlockOf;
 template <bool XA, bool XB> struct BlockOf<256, XA, XB> { typedef Product<256, 256, 2, 4, XA, XB> type; };
 template <bool XA, bool XB> struct BlockOf<128, XA, XB> { typedef Product<128, 128, 2, 2, XA, XB> type; };
-template <bool XA, bool XB> struct BlockOf<64, XA, XB> { typedef Product<64, 64, 2, 2, XA, XB> type; };
+template <bool XA, bool XB> struct BlockOf<64, XA, XB> { typedef Product<64, 64, 2, 2, XA, XB, 64> type; };
 
-// A part of each matrix' sum of squares a workgroup.
+// A part of each matrix' rows' sum of squares a workgroup: 32 lanes a row.
 template <typename T>
 __global__ __launch_bounds__(256) void k_squares(const T* x, long long mstride, long long rstride, int rows, int cols, int parts, double* sums)
 {
+    constexpr int E = 16 / (int)sizeof(T);
     __shared__ double lds[4];
     const int matrix = blockIdx.x / parts, part = blockIdx.x - matrix * parts;
-    const long long n = (long long)rows * cols, lo = n * part / parts, hi = n * (part + 1) / parts;
     x += matrix * mstride;
     double s = 0;
-    for (long long u = lo + threadIdx.x; u < hi; u += 256) {
-        const long long r = u / cols;
-        const double v = ld(x + r * rstride + (u - r * cols));
-        s = fma(v, v, s);
+    for (int r = part * 8 + (threadIdx.x >> 5); r < rows; r += parts * 8) {
+        const T* p = x + r * rstride;
+#pragma unroll 4
+        for (int c = (threadIdx.x & 31) * E; c < cols; c += 32 * E) {
+            if (c + E <= cols) {
+                Pack<T, E> v;
+                v.load_any(p + c);
+#pragma unroll
+                for (int e = 0; e < E; ++e) { const double d = v.get(e); s = fma(d, d, s); }
+            } else
+                for (int e = c; e < cols; ++e) { const double d = ld(p + e); s = fma(d, d, s); }
+        }
     }
 #pragma unroll
     for (int k = 32; k; k >>= 1) s += __shfl_xor(s, k);
@@ -39,46 +47,63 @@ __global__ __launch_bounds__(256) void k_squares(const T* x, long long mstride, 
     if (threadIdx.x == 0) sums[blockIdx.x] = lds[0] + lds[1] + lds[2] + lds[3];
 }
 
-// x / (|x| + eps) as planes, with zeros up to whole blocks of 64.
+// 1 / (|x| + eps) of a matrix, for a whole workgroup
+__device__ __forceinline__ double inverse_norm(const double* sums, int parts, double eps)
+{
+    __shared__ double lds[4];
+    double s = 0;
+    for (int i = threadIdx.x; i < parts; i += 256) s += sums[i];
+#pragma unroll
+    for (int k = 32; k; k >>= 1) s += __shfl_xor(s, k);
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = s;
+    __syncthreads();
+    return 1.0 / (sqrt(lds[0] + lds[1] + lds[2] + lds[3]) + eps);
+}
+
+// x / (|x| + eps) as planes, laid out for the products, with zeros up to whole blocks of 64: 64 rows x 32 columns at a time.
 template <typename T, int P>
 __global__ __launch_bounds__(256) void k_normed(const T* x, long long mstride, long long rstride, int rows, int cols, int parts, const double* sums, double eps, bf16_t* to, int Rp, int Cp, long long plane)
 {
     const int matrix = blockIdx.y;
-    double total = 0;
-    for (int i = 0; i < parts; ++i) total += sums[matrix * parts + i];
-    const double inv = 1.0 / (sqrt(total) + eps);
-    const int per = Cp >> 3;
+    const double inv = inverse_norm(sums + (long long)matrix * parts, parts, eps);
+    const int across = Cp >> 5, tiles = across * (Rp >> 6), r_in = threadIdx.x >> 2, c_in = (threadIdx.x & 3) * 8;
     x += matrix * mstride;
     to += (long long)matrix * Rp * Cp;
-    for (long long u = (long long)blockIdx.x * 256 + threadIdx.x; u < (long long)Rp * per; u += (long long)gridDim.x * 256) {
-        const int r = (int)(u / per), c0 = (int)(u - (long long)r * per) * 8;
+    for (int t = blockIdx.x; t < tiles; t += gridDim.x) {
+        const int rb = t / across, cb = t - rb * across, r = rb * 64 + r_in, c0 = cb * 32 + c_in;
+        float v[8] = {};
+        if (r < rows) {
+            const T* p = x + r * rstride + c0;
+            if (c0 + 8 <= cols) {
+                Pack<T, 8> w;
+                w.load_any(p);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = (float)(w.get(e) * inv);
+            } else
+#pragma unroll
+                for (int e = 0; e < 8; ++e) if (c0 + e < cols) v[e] = (float)(ld(p + e) * inv);
+        }
         uint32_t q[4][P];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            float v[2];
+        for (int j = 0; j < 4; ++j) planes_of<P>(v[2 * j], v[2 * j + 1], q[j]);
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const int c = c0 + 2 * j + e;
-                v[e] = r < rows && c < cols ? (float)(ld(x + r * rstride + c) * inv) : 0.0f;
-            }
-            planes_of<P>(v[0], v[1], q[j]);
-        }
-#pragma unroll
-        for (int p = 0; p < P; ++p) *(uint4*)(to + p * plane + ((long long)(c0 >> 5) * Rp + r) * 32 + (c0 & 31)) = uint4{q[0][p], q[1][p], q[2][p], q[3][p]};
+        for (int k = 0; k < P; ++k) *(uint4*)(to + k * plane + ((long long)cb * Rp + r) * 32 + c_in) = uint4{q[0][k], q[1][k], q[2][k], q[3][k]};
     }
 }
 
 struct StepArgs {
     Matrix a, b;                                    // of the first matrix
     long long anext, bnext;                         // elements to the next one's
-    int planes, stages, shares, count, ablocks, bblocks;
-    int symmetric;                                  // blocks below the diagonal are mirrored instead
+    int planes, stages, count, ablocks, bblocks;    // stages of 32, an even number
+    int blocks, whole, shares;                      // blocks of all matrices; the first `whole` of them by a workgroup each, the others by `shares`
+    int groups, grouped;                            // those others: groups (matrices) x blocks
+    int symmetric;                                  // blocks above the diagonal are mirrored ones
     // what becomes of the sums v: f0 old + f1 v, old being planes too
     float f0, f1;
     const bf16_t* old; bf16_t* to;
-    long long plane, next; int stride, arows, brows;        // (old and to: a Matrix of brows rows and arows columns each) [matrix: next]
+    long long plane, next; int arows, brows;        // (old and to: a Matrix of brows rows and arows columns each) [matrix: next]
     void* out; int orows, ocols;                    // instead of planes: the results, rows along b
-    float* part; long long pshare;                  // [share][matrix][index of b][stride]
+    float* part;                                    // [block that is cut][share][index of b][index of a]
 };
 
 template <int P>
@@ -124,66 +149,104 @@ __device__ __forceinline__ void finish(const StepArgs& a, int matrix, int i, int
     }
 }
 
-template <class L, typename T, int P>
-__global__ __launch_bounds__(L::kThreads, 2) void k_step(const StepArgs a)
+// Which matrix and block: neighbours in the list share operands.
+__device__ __forceinline__ void step_block(const StepArgs& a, int t, int& ia, int& ib, int& matrix)
 {
-    __shared__ __align__(16) typename L::Stage s0, s1, s2, s3;
-    int ia, ib, matrix, share = 0;
+    const int per = a.blocks / a.count;
+    matrix = t / per;
+    t -= matrix * per;
     if (a.symmetric) {
-        const int per = a.ablocks * (a.ablocks + 1) / 2;
-        int t;
-        if (!block_of((int)blockIdx.x, per, a.count, t, matrix)) return;
         ib = 0;
         while (t > ib) t -= ++ib;                   // row ib has ib + 1 blocks
         ia = t;
     } else {
-        int g;
-        if (!block_of((int)blockIdx.x, a.ablocks, a.bblocks * a.shares * a.count, ia, g)) return;
-        ib = g % a.bblocks;
-        g /= a.bblocks;
-        share = g % a.shares;
-        matrix = g / a.shares;
+        const int wide = 4 * a.ablocks, band = t / wide, in = t - band * wide, high = min(4, a.bblocks - 4 * band);
+        ia = in / high;
+        ib = 4 * band + in - ia * high;
     }
+}
+
+template <class L, typename T, int P>
+__global__ __launch_bounds__(L::kThreads, 2) void k_step(const StepArgs a)
+{
+    __shared__ __align__(16) typename L::Stage s0, s1, s2, s3;
+    // XCD x takes the x-th eighth of the whole blocks; behind them come the shares, those of the same part of a matrix on one XCD
+    int t, share = 0, shares = 1;
+    const int per = (a.whole + 7) >> 3, index = (int)blockIdx.x;
+    if (index < 8 * per) {
+        t = (index & 7) * per + (index >> 3);
+        if (t >= a.whole) return;
+    } else {
+        int g;
+        shares = a.shares;
+        if (!xcd_order(index - 8 * per, a.groups * shares, a.grouped, g, t)) return;
+        share = g % shares;
+        t += a.whole + g / shares * a.grouped;
+    }
+    int ia, ib, matrix;
+    step_block(a, t, ia, ib, matrix);
     const int a0 = ia * L::BA, b0 = ib * L::BB;
     Matrix x = a.a, y = a.b;
     x.p += matrix * a.anext;
     y.p += matrix * a.bnext;
     f32x16 acc[L::IA][L::IB] = {};
-    L::run(acc, x, y, a0, b0, (int)((long long)a.stages * share / a.shares), (int)((long long)a.stages * (share + 1) / a.shares), a.planes, s0, s1, s2, s3);
-    L::each(acc, [&](int i, int j, f32x4 v) __attribute__((always_inline)) {
-        i += a0;
-        j += b0;
-        if (i >= a.arows || j >= a.brows) return;
-        if (a.shares > 1) *(f32x4*)(a.part + share * a.pshare + matrix * a.next + (long long)j * a.stride + i) = v;
-        else finish<T, P>(a, matrix, i, j, v, a.symmetric && ia != ib);
-    });
+    const int stages = a.stages / (L::KS / 32);
+    L::run(acc, x, y, a0, b0, (int)((long long)stages * share / shares), (int)((long long)stages * (share + 1) / shares), a.planes, s0, s1, s2, s3);
+    if (shares > 1) {
+        float* p = a.part + ((long long)(t - a.whole) * shares + share) * (L::BA * L::BB);
+        L::each(acc, [&](int i, int j, f32x4 v) __attribute__((always_inline)) { *(f32x4*)(p + j * L::BA + i) = v; });
+    } else
+        L::each(acc, [&](int i, int j, f32x4 v) __attribute__((always_inline)) {
+            if (a0 + i < a.arows && b0 + j < a.brows) finish<T, P>(a, matrix, a0 + i, b0 + j, v, a.symmetric && ia != ib);
+        });
 }
 
-template <typename T, int P>
+// The shares' sums, in their order: 1024 results a workgroup.
+template <typename T, int P, int B>
 __global__ __launch_bounds__(256) void k_step_sum(const StepArgs a)
 {
-    const long long n = a.count * a.next / 4;
-    for (long long u = (long long)blockIdx.x * 256 + threadIdx.x; u < n; u += (long long)gridDim.x * 256) {
-        const int matrix = (int)(4 * u / a.next), in = (int)(4 * u - matrix * a.next), j = in / a.stride;
-        f32x4 v = {0, 0, 0, 0};
-#pragma unroll 4
-        for (int s = 0; s < a.shares; ++s) v += *(const f32x4*)(a.part + s * a.pshare + 4 * u);
-        finish<T, P>(a, matrix, in - j * a.stride, j, v, false);
+    constexpr int kPer = B * B / 1024;
+    const int cut = blockIdx.x / kPer, u = (blockIdx.x - cut * kPer) * 1024 + threadIdx.x * 4, j = u / B, i = u % B;
+    int ia, ib, matrix;
+    step_block(a, a.whole + cut, ia, ib, matrix);
+    if (ia * B + i >= a.arows || ib * B + j >= a.brows) return;
+    const float* p = a.part + (long long)cut * a.shares * (B * B) + u;
+    f32x4 v = {0, 0, 0, 0};
+#pragma unroll 8
+    for (int s = 0; s < a.shares; ++s) v += *(const f32x4*)(p + (long long)s * (B * B));
+    finish<T, P>(a, matrix, ia * B + i, ib * B + j, v, a.symmetric && ia != ib);
+}
+
+// How a product's blocks go over the chip: their size, how many are whole, and the shares of the others.
+struct Cut { int block, blocks, whole, shares; };
+Cut cut_of(int a, int b, bool symmetric, long long stages, int count)
+{
+    Cut best = {};
+    double least = 1e300;
+    for (int block = 256; block >= 64; block /= 2) {
+        const int per_cu = block == 256 ? 1 : 2;
+        const long long slots = 256 * per_cu, na = ceil_div(a, block), nb = ceil_div(b, block), n = (symmetric ? na * (na + 1) / 2 : na * nb) * count;
+        // microseconds a stage with so many workgroups on a CU; 5 for a workgroup's start and end
+        const auto stage = [&](long long beside) { return block == 256 ? 0.92 : block == 128 ? 0.13 + 0.2 * (double)beside : 0.05 + 0.09 * (double)beside; };
+        const long long whole = n / slots * slots, left = n - whole;
+        const double first = (double)(whole / slots) * ((double)stages * stage(per_cu) + 5);
+        for (int s = 1; s <= 32 && (s == 1 || stages / s >= 6); ++s) {
+            const double last = left ? (double)ceil_div(left * s, slots) * ((double)ceil_div(stages, s) * stage(std::min<long long>(per_cu, ceil_div(left * s, 256))) + 5) : 0;
+            const double sum = left && s > 1 ? 5 + 2e-6 * (double)(left * s) * block * block : 0;
+            if (first + last + sum < least) {
+                least = first + last + sum;
+                best = {block, (int)n, (int)(s > 1 ? whole : n), s};
+            }
+        }
     }
+    return best;
 }
 
 struct Plan {
     int planes, Rp, Cp, m, mp, parts;
     bool tall;
-    Split s, q, x;                                  // of S, its square, X
+    Cut s, q, x;                                    // of S, its square, X
 };
-Split symmetric_or_split(int m, long long stages, int count)
-{
-    // (a symmetric product is not cut as well)
-    const Split half = split_of(m, (m + 1) / 2, stages, 64, 1, count), cut = split_of(m, m, stages, 64, 16, count);
-    const auto blocks = [&](int b) { const long long n = ceil_div(m, b); return n * (n + 1) / 2 * count; };
-    return cut.shares > 1 && blocks(half.block) * 2 < 256 ? cut : Split{half.block, 1};
-}
 Plan plan_of(const ftp_orthogonal_shape& s)
 {
     Plan p = {};
@@ -193,11 +256,11 @@ Plan plan_of(const ftp_orthogonal_shape& s)
     p.tall = s.rows > s.cols;
     p.m = std::min(s.rows, s.cols);
     p.mp = (p.m + 63) & ~63;
-    p.parts = (int)std::min<long long>(256, ceil_div((long long)s.rows * s.cols, 4096));
+    p.parts = (int)std::min<long long>(1024, ceil_div(s.rows, 8));
     const long long terms = p.planes == 2 ? 3 : 6, longer = std::max(p.Rp, p.Cp);
-    p.s = symmetric_or_split(p.m, longer / 32 * terms, s.count);
-    p.q = symmetric_or_split(p.m, p.mp / 32 * terms, s.count);
-    p.x = split_of(s.cols, s.rows, p.mp / 32 * terms, 64, 16, s.count);
+    p.s = cut_of(p.mp, p.mp, true, longer / 32 * terms, s.count);
+    p.q = cut_of(p.mp, p.mp, true, p.mp / 32 * terms, s.count);
+    p.x = cut_of(p.Cp, p.Rp, false, p.mp / 32 * terms, s.count);
     return p;
 }
 
@@ -211,8 +274,8 @@ Buffers buffers_of(const ftp_orthogonal_shape& s, const Plan& p, char* ws)
     for (auto& e : b.x) e = t.take<bf16_t>(p.planes * x);
     b.s = t.take<bf16_t>(p.planes * q);
     b.q = t.take<bf16_t>(p.planes * q);
-    const auto shares = [](const Split& k) { return k.shares > 1 ? (size_t)k.shares : 0; };
-    b.part = t.take<float>(std::max({shares(p.s) * q, shares(p.q) * q, shares(p.x) * x}));
+    const auto shares = [](const Cut& k) { return (size_t)(k.blocks - k.whole) * k.shares * k.block * k.block; };
+    b.part = t.take<float>(std::max({shares(p.s), shares(p.q), shares(p.x)}));
     b.bytes = t.used;
     return b;
 }
@@ -223,17 +286,20 @@ void launch(StepArgs& a, hipStream_t st)
     typedef typename BlockOf<B, XA, XB>::type L;
     a.ablocks = (int)ceil_div(a.arows, B);
     a.bblocks = (int)ceil_div(a.brows, B);
-    const long long grid = a.symmetric ? block_grid((long long)a.ablocks * (a.ablocks + 1) / 2, a.count) : block_grid(a.ablocks, (long long)a.bblocks * a.shares * a.count);
-    k_step<L, T, P><<<(unsigned)grid, L::kThreads, 0, st>>>(a);
-    if (a.shares > 1) k_step_sum<T, P><<<(unsigned)std::min<long long>(ceil_div(a.count * a.next, 1024), 8192), 256, 0, st>>>(a);
+    const int cut = a.blocks - a.whole;
+    a.groups = a.whole ? 1 : a.count;
+    a.grouped = cut / a.groups;
+    k_step<L, T, P><<<(unsigned)ceil_div(a.whole, 8) * 8 + (cut ? xcd_grid(a.groups * a.shares, a.grouped) : 0), L::kThreads, 0, st>>>(a);
+    if (cut) k_step_sum<T, P, B><<<(unsigned)(cut * (B * B / 1024)), 256, 0, st>>>(a);
 }
 template <bool XA, bool XB, typename T, int P>
-void product(StepArgs& a, const Split& s, hipStream_t st)
+void product(StepArgs& a, const Cut& c, hipStream_t st)
 {
-    a.shares = s.shares;
-    a.symmetric = a.symmetric && s.shares == 1;
-    if (s.block == 256) launch<256, XA, XB, T, P>(a, st);
-    else if (s.block == 128) launch<128, XA, XB, T, P>(a, st);
+    a.blocks = c.blocks;
+    a.whole = c.whole;
+    a.shares = c.shares;
+    if (c.block == 256) launch<256, XA, XB, T, P>(a, st);
+    else if (c.block == 128) launch<128, XA, XB, T, P>(a, st);
     else launch<64, XA, XB, T, P>(a, st);
 }
 
@@ -244,13 +310,13 @@ void run(const ftp_orthogonal_shape& s, const T* x, T* out, char* ws, hipStream_
     const Buffers b = buffers_of(s, p, ws);
     const long long xnext = (long long)p.Rp * p.Cp, xplane = s.count * xnext, qnext = (long long)p.mp * p.mp, qplane = s.count * qnext;
     k_squares<T><<<(unsigned)(s.count * p.parts), 256, 0, st>>>(x, s.matrix_stride, s.row_stride, s.rows, s.cols, p.parts, b.sums);
-    k_normed<T, P><<<dim3((unsigned)std::min<long long>(ceil_div(xnext, 2048), 4096), (unsigned)s.count), 256, 0, st>>>(x, s.matrix_stride, s.row_stride, s.rows, s.cols, p.parts, b.sums, s.eps, b.x[0], p.Rp, p.Cp, xplane);
+    k_normed<T, P><<<dim3((unsigned)std::min<long long>(xnext / 2048, 2048), (unsigned)s.count), 256, 0, st>>>(x, s.matrix_stride, s.row_stride, s.rows, s.cols, p.parts, b.sums, s.eps, b.x[0], p.Rp, p.Cp, xplane);
     const Matrix S = blocked(b.s, p.mp, p.mp, qplane), Q = blocked(b.q, p.mp, p.mp, qplane);
     for (int step = 0; step < s.steps; ++step) {
         const Matrix X = blocked(b.x[step & 1], p.Rp, p.Cp, xplane);
         StepArgs k = {};
         k.planes = P; k.count = s.count; k.part = b.part;
-        k.stride = k.arows = k.brows = p.mp; k.next = qnext; k.plane = qplane; k.pshare = qplane;
+        k.arows = k.brows = p.mp; k.next = qnext; k.plane = qplane;
         // S
         k.a = k.b = X; k.anext = k.bnext = xnext; k.stages = std::max(p.Rp, p.Cp) / 32; k.symmetric = 1; k.f1 = 1; k.to = b.s;
         if (p.tall) product<true, true, T, P>(k, p.s, st);
@@ -260,7 +326,7 @@ void run(const ftp_orthogonal_shape& s, const T* x, T* out, char* ws, hipStream_
         product<false, false, T, P>(k, p.q, st);
         // a X + that times X
         k.symmetric = 0; k.f0 = s.a; k.f1 = 1; k.old = b.x[step & 1]; k.to = b.x[~step & 1];
-        k.stride = k.arows = p.Cp; k.brows = p.Rp; k.next = xnext; k.plane = xplane; k.pshare = xplane;
+        k.arows = p.Cp; k.brows = p.Rp; k.next = xnext; k.plane = xplane;
         if (step + 1 == s.steps) { k.out = out; k.orows = s.rows; k.ocols = s.cols; }
         if (p.tall) {
             k.a = Q; k.b = X; k.anext = qnext; k.bnext = xnext;

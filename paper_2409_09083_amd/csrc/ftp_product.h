@@ -56,7 +56,7 @@ struct Product {
     static constexpr int kBytesA = BA * KS * 2, kBytesB = BB * KS * 2;
     static constexpr int kLoadsA = kBytesA / 16 / kThreads, kLoadsB = kBytesB / 16 / kThreads, kLoads = kLoadsA + kLoadsB;
     static_assert(kLoadsA * kThreads * 16 == kBytesA && kLoadsB * kThreads * 16 == kBytesB, "whole loads a thread");
-    static_assert((kStages - 1) * kLoads < 64, "what vmcnt counts");
+    static_assert(kStages * kLoads < 64, "what vmcnt counts");
     struct Stage { char a[kBytesA], b[kBytesB]; };
 
     // Which 16 bytes of a row lie where: rows of 64 or 128 bytes (along) so that 16 rows' equal chunks meet no bank twice, longer ones (across) so that 4 rows x 64 bytes do not.
@@ -90,17 +90,20 @@ struct Product {
     // an operand's block on its way to LDS
     template <int B, bool X, int N>
     struct Source {
-        const char* base;                           // of the stage to come, in plane 0
-        long long plane, left;                      // bytes between planes, from the base to the end
-        long long step;                             // bytes a stage
-        int at[N];                                  // this thread's chunks, bytes from the base
+        const char *first, *base;                   // of plane 0, and of what the resource reaches
+        long long plane, all, left;                 // bytes between planes, from the bases to the end
+        uint32_t step, off;                         // bytes a stage, from the base to the stage that is being fetched
+        __amdgpu_buffer_rsrc_t rsrc;
+        int wave;
+        int at[N];                                  // this thread's chunks, bytes from the stage
         __device__ __forceinline__ void init(const Matrix& m, long long i0, long long k0)
         {
-            const long long first = X ? k0 * m.row + (i0 >> 5) * m.block : i0 * m.row + (k0 >> 5) * m.block;
-            base = (const char*)(m.p + first);
+            const long long o = X ? k0 * m.row + (i0 >> 5) * m.block : i0 * m.row + (k0 >> 5) * m.block;
+            first = (const char*)(m.p + o);
             plane = m.plane * 2;
-            left = (m.size - first) * 2;
-            step = X ? KS * m.row * 2 : KS / 32 * m.block * 2;
+            all = (m.size - o) * 2;
+            step = (uint32_t)(X ? KS * m.row * 2 : KS / 32 * m.block * 2);
+            wave = __builtin_amdgcn_readfirstlane(threadIdx.x & ~63) * 16;
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 constexpr int kRow = X ? B / 8 : KS / 8;                            // chunks of a row
@@ -108,15 +111,21 @@ struct Product {
                 at[i] = (int)((chunk >> 2) * m.block * 2) + (int)(row * m.row * 2) + (chunk & 3) * 16;
             }
         }
-        __device__ __forceinline__ void fetch(char* to, long long stage, int p, bool any) const
+        __device__ __forceinline__ void reach()
         {
-            const long long off = stage * step;
-            const int n = any ? (int)min(max(left - off, 0ll), 0x7FFFFFF0ll) : 0;
-            const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)(base + off + p * plane), (short)0, n, 0x00020000);
-            const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x & ~63);
-#pragma unroll
-            for (int i = 0; i < N; ++i)
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)(to + (wave + kThreads * i) * 16), 16, at[i], 0, 0, 0);
+            off = 0;
+            rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)base, (short)0, left <= 0 ? 0 : left > 0xFFFFFFF0ll ? (int)0xFFFFFFF0u : (int)(uint32_t)left, 0x00020000);
+        }
+        __device__ __forceinline__ void start(int p) { base = first + p * plane; left = all; reach(); }
+        // (the hardware's check of the range takes the offset with it: num_records - soffset)
+        __device__ __forceinline__ void next()
+        {
+            off += step;
+            if (off >= 1u << 30) { base += off; left -= off; reach(); }
+        }
+        __device__ __forceinline__ void load(char* to, int i) const
+        {
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)(to + wave + kThreads * 16 * i), 16, at[i], (int)off, 0, 0);
         }
     };
 
@@ -145,69 +154,79 @@ struct Product {
         const int wa = wave_a(), wb = wave_b(), per = hi - lo, terms = planes == 1 ? 1 : planes == 2 ? 3 : 6, total = per * terms;
         // planes of the terms, two bits each: (2, 0) (0, 2) (1, 1) (1, 0) (0, 1) (0, 0)
         uint32_t pa = planes == 3 ? 0x52u : planes == 2 ? 0x1u : 0u, pb = planes == 3 ? 0x118u : planes == 2 ? 0x4u : 0u;
-        int k = 0, fetched = 0;
-        const auto fetch = [&](Stage& to) __attribute__((always_inline)) {
-            const bool any = fetched < total;
-            fa.fetch(to.a, k, pa & 3, any);
-            fb.fetch(to.b, k, pb & 3, any);
-            ++fetched;
-            if (++k == per) { k = 0; pa >>= 2; pb >>= 2; }
-        };
         if (total == 0) return;
+        int k = per, to_come = total;
+        fa.start(pa & 3);
+        fb.start(pb & 3);
+        const auto next_stage = [&]() __attribute__((always_inline)) {
+            if (--to_come <= 0) return;             // (past the end the last stage is fetched again, to where nobody reads it)
+            fa.next();
+            fb.next();
+            if (--k == 0) {
+                k = per;
+                pa >>= 2;
+                pb >>= 2;
+                fa.start(pa & 3);
+                fb.start(pb & 3);
+            }
+        };
+        const auto load = [&](Stage& to, int i) __attribute__((always_inline)) {
+            if (i < kLoadsA) fa.load(to.a, i);
+            else fb.load(to.b, i - kLoadsA);
+        };
         b16x8 x[2][IA], y[2][IB];
-        const auto read = [&](auto to, const Stage& from, int s) __attribute__((always_inline)) {
-#pragma unroll
-            for (int i = 0; i < IA; ++i) x[to][i] = operand<BA, XA>(from.a, wa + 32 * i, s);
-#pragma unroll
-            for (int j = 0; j < IB; ++j) y[to][j] = operand<BB, XB>(from.b, wb + 32 * j, s);
-            __builtin_amdgcn_sched_barrier(0);
+        const auto read = [&](int set, const Stage& from, int s, int i) __attribute__((always_inline)) {
+            if (i < IA) x[set][i] = operand<BA, XA>(from.a, wa + 32 * i, s);
+            else y[set][i - IA] = operand<BB, XB>(from.b, wb + 32 * (i - IA), s);
         };
-        const auto multiply = [&](auto from) __attribute__((always_inline)) {
-#pragma unroll
-            for (int i = 0; i < IA; ++i)
-#pragma unroll
-                for (int j = 0; j < IB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[from][i], y[from][j], acc[i][j], 0, 0, 0);
-            __builtin_amdgcn_sched_barrier(0);
-        };
-        // this wavefront's loads of the next stage have landed (`ahead` stages behind it are on their way), its reads of this one too; behind the barrier everybody's
-        const auto landed = [&](auto ahead) __attribute__((always_inline)) {
-            constexpr int n = ahead * kLoads;
+        // this wavefront's loads of the next stage have landed (n later ones are on their way), its reads of this one too; behind the barrier everybody's
+        const auto landed = [&](auto n) __attribute__((always_inline)) {
             asm volatile("" ::: "memory");
             __builtin_amdgcn_s_waitcnt((n & 15) | (n >> 4) << 14 | 0x70);
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
         };
-        constexpr std::integral_constant<int, 0> even{};
-        constexpr std::integral_constant<int, 1> odd{};
-        constexpr int N = KS / 16;
+        constexpr int N = KS / 16, NM = IA * IB, NR = IA + IB;
         static_assert(N % 2 == 0, "operands alternate");
-        // Operands are read one product block ahead, over the barrier too: the first ones of a stage while the last block of the one before is multiplied, when that stage's place is free already.
-        const auto step = [&](Stage& now, Stage& next) __attribute__((always_inline)) {
+        // The products of operands that are there, and between them the reads of the next ones (k part s of `from`) and a part of the loads into `to`.  All at once behind the barrier, loads and reads held the
+        // products up (8192 x 8192 x 2048: 240 us, where the loads alone take 92 and the products with their reads 137).
+        const auto block = [&](int set, const Stage& from, int s, Stage& to, int part) __attribute__((always_inline)) {
+            const int l0 = part * kLoads / N, nl = (part + 1) * kLoads / N - l0;
 #pragma unroll
-            for (int s = 0; s + 1 < N; s += 2) {
-                read(odd, now, s + 1);
-                multiply(even);
-                if (s + 2 < N) {
-                    read(even, now, s + 2);
-                    multiply(odd);
-                }
+            for (int m = 0; m < NM; ++m) {
+                acc[m / IB][m % IB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[set][m / IB], y[set][m % IB], acc[m / IB][m % IB], 0, 0, 0);
+#pragma unroll
+                for (int i = m; i < NR && (i == m || m == NM - 1); ++i) read(set ^ 1, from, s, i);
+#pragma unroll
+                for (int i = m * nl / NM; i < (m + 1) * nl / NM; ++i) load(to, l0 + i);
+                __builtin_amdgcn_sched_barrier(0);
             }
-            landed(std::integral_constant<int, kStages - 2>{});
-            fetch(now);
-            read(even, next, 0);
-            multiply(odd);
+        };
+        // The first operands of a stage are read while the last ones of the stage before are multiplied; that stage's place is free then, and takes the loads of one to come until the next barrier.
+        const auto step = [&](Stage& before, Stage& now, Stage& next) __attribute__((always_inline)) {
+#pragma unroll
+            for (int s = 0; s + 1 < N; ++s) block(s & 1, now, s + 1, before, s + 1);
+            landed(std::integral_constant<int, (kStages - 2) * kLoads>{});
+            next_stage();
+            block(1, next, 0, now, 0);
         };
         static_assert(sizeof...(S) == kStages, "a place a stage");
         const std::tuple<S&...> at(stages...);
         const auto place = [&](auto i) __attribute__((always_inline)) -> Stage& { return std::get<i % kStages>(at); };
-        unrolled<kStages>([&](auto i) __attribute__((always_inline)) { fetch(place(i)); });
-        landed(std::integral_constant<int, kStages - 1>{});
-        read(even, std::get<0>(at), 0);
+        unrolled<kStages>([&](auto i) __attribute__((always_inline)) {
+            if constexpr (i > 0) next_stage();
+#pragma unroll
+            for (int n = 0; n < (i + 1 < kStages ? kLoads : kLoads / N); ++n) load(place(i), n);
+        });
+        landed(std::integral_constant<int, (kStages - 2) * kLoads + kLoads / N>{});
+#pragma unroll
+        for (int i = 0; i < NR; ++i) read(0, std::get<0>(at), 0, i);
+        const auto steps = [&](auto i) __attribute__((always_inline)) {
+            step(place(std::integral_constant<int, i + kStages - 1>{}), place(i), place(std::integral_constant<int, i + 1>{}));
+        };
         // (one way through the loop: where ways meet, the compiler waits for all loads)
-        for (int s = total / kStages; s; --s)
-            unrolled<kStages>([&](auto i) __attribute__((always_inline)) { step(place(i), place(std::integral_constant<int, i + 1>{})); });
-        const int left = total % kStages;
-        rest<0>(left, [&](auto i) __attribute__((always_inline)) { step(place(i), place(std::integral_constant<int, i + 1>{})); });
+        for (int s = total / kStages; s; --s) unrolled<kStages>(steps);
+        rest<0>(total % kStages, steps);
         __builtin_amdgcn_s_waitcnt(0x70);
         asm volatile("" ::: "memory");
     }
