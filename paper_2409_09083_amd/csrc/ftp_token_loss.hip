@@ -68,7 +68,8 @@ __global__ __launch_bounds__(256) void k_gather(const GatherArgs a)
 {
     __shared__ int sums[2][4];
     __shared__ int where[kChunk];
-    const long long chunk = blockIdx.x, row0 = chunk * kChunk, chunks = gridDim.x;
+    const long long chunk = blockIdx.x >> 2, row0 = chunk * kChunk, chunks = gridDim.x >> 2;
+    const int sub = blockIdx.x & 3;                 // which 16 rows of the chunk this workgroup copies
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
     int before = 0, all = 0;
     for (long long i = tid; i < chunks; i += 256) {
@@ -88,35 +89,35 @@ __global__ __launch_bounds__(256) void k_gather(const GatherArgs a)
         const unsigned long long there = __ballot(id >= 0);
         const int to = before + (int)__popcll(there & ((1ull << lane) - 1));
         where[lane] = id >= 0 ? to : -1;
-        if (row < a.rows) a.place[row] = id >= 0 ? to : -1;
-        if (id >= 0) { a.index[to] = (int)row; a.label[to] = id; }
+        if (row < a.rows && sub == 0) a.place[row] = id >= 0 ? to : -1;
+        if (id >= 0 && sub == 0) { a.index[to] = (int)row; a.label[to] = id; }
     }
     __syncthreads();
-    const int per = a.Cp >> 3;                      // vectors of a row
-    const int here = (int)std::min<long long>(kChunk, a.rows - row0);
-    for (int u = tid; u < here * per; u += 256) {
-        const int r = u / per, c0 = (u - r * per) * 8;
-        if (where[r] >= 0) copy8<T, P>((const T*)a.x + (row0 + r) * a.stride, c0, a.C, a.xc + (c0 >> 5) * a.block + where[r] * 32 + (c0 & 31), a.plane);
-    }
-    if (chunk == 0) {
-        const int end = (all + 63) & ~63;
-        if (tid == 0) *a.count = all;
-        for (int u = tid; u < (end - all) * per; u += 256) {
-            const int r = u / per, c0 = (u - r * per) * 8;
+    // a wavefront has 16 rows x 32 columns, 1 KB where they go
+    const int r_in = lane >> 2, c_in = (lane & 3) * 8, across = a.Cp >> 5, end = (all + 63) & ~63;
+    const int r = sub * 16 + r_in, to = where[r];
+    const T* from = (const T*)a.x + (row0 + r) * a.stride;
+    if (to >= 0)
+#pragma unroll 4
+        for (int cb = wave; cb < across; cb += 4) copy8<T, P>(from, cb * 32 + c_in, a.C, a.xc + cb * a.block + to * 32 + c_in, a.plane);
+    if (blockIdx.x) return;
+    if (tid == 0) *a.count = all;
+    for (int row = all + r_in; row < end; row += 16)
+        for (int cb = wave; cb < across; cb += 4)
 #pragma unroll
-            for (int p = 0; p < P; ++p) *(uint4*)(a.xc + p * a.plane + (c0 >> 5) * a.block + (all + r) * 32 + (c0 & 31)) = uint4{0, 0, 0, 0};
-        }
-    }
+            for (int p = 0; p < P; ++p) *(uint4*)(a.xc + p * a.plane + cb * a.block + row * 32 + c_in) = uint4{0, 0, 0, 0};
 }
 
 // W as planes, laid out for the products; zeros up to Rp rows of Cp.
 template <typename T, int P>
 __global__ __launch_bounds__(256) void k_pack_rows(const T* w, long long stride, int rows, int C, int Rp, int Cp, bf16_t* to, long long plane)
 {
-    const int per = Cp >> 3;
-    for (long long u = (long long)blockIdx.x * 256 + threadIdx.x; u < (long long)Rp * per; u += (long long)gridDim.x * 256) {
-        const int r = (int)(u / per), c0 = (int)(u - (long long)r * per) * 8;
-        copy8<T, P>(w + r * stride, r < rows ? c0 : 0, r < rows ? C : 0, to + ((long long)(c0 >> 5) * Rp + r) * 32 + (c0 & 31), plane);
+    // a wavefront has 16 rows x 32 columns, 1 KB where they go
+    const int lane = threadIdx.x & 63, across = Cp >> 5, c_in = (lane & 3) * 8;
+    const long long tiles = (long long)(Rp >> 4) * across;
+    for (long long t = (long long)blockIdx.x * 4 + (threadIdx.x >> 6); t < tiles; t += 4ll * gridDim.x) {
+        const int rb = (int)(t / across), cb = (int)(t - (long long)rb * across), r = rb * 16 + (lane >> 2);
+        copy8<T, P>(w + r * stride, r < rows ? cb * 32 + c_in : 0, r < rows ? C : 0, to + ((long long)cb * Rp + r) * 32 + c_in, plane);
     }
 }
 
@@ -300,7 +301,7 @@ __global__ __launch_bounds__(256) void k_loss_mean(const double* sums, int n, fl
 struct GradArgs {
     Matrix a, b;
     const int* count;
-    int planes, stages, shares, ablocks, bblocks, add;
+    int planes, stages, shares, ablocks, bblocks, add;         // dx: shares and blocks for all rows; fewer rows have more shares (dx_shares())
     float* part; long long pstride, pshare;         // [share][index of b][pstride]
     void* out; long long ostride; int C; float scale; int mean;     // dw alone, without shares
 };
@@ -310,22 +311,25 @@ __device__ __forceinline__ float gradient_scale(float scale, int mean, const int
     return !mean ? scale : *count ? scale / (float)*count : 0.0f;
 }
 
+// Shares of the contraction where `rows` of the rows that the launch is made for have labels: as many blocks as the launch has workgroups for.  Share s of row r is row s * dx_rows() + r of the scratch.
+__device__ __forceinline__ int dx_blocks(int rows, int block) { return max((rows + block - 1) / block, 1); }
+__device__ __forceinline__ int dx_shares(int rows, int block, int all) { return all / dx_blocks(rows, block); }
+
 // dx's block: channels x rows over the piece's ids, added to what the pieces before left
 template <class L>
 __global__ __launch_bounds__(L::kThreads, 2) void k_loss_dx(const GradArgs a)
 {
     __shared__ __align__(16) typename L::Stage s0, s1, s2, s3;
     int ia, ib;
-    const int blocks = a.bblocks * a.shares;
-    if (!block_of((int)blockIdx.x, a.ablocks, blocks, ia, ib)) return;
-    const int share = ib / a.bblocks, rows = *a.count, a0 = ia * L::BA, b0 = (ib - share * a.bblocks) * L::BB;
-    if (b0 >= rows) return;
+    const int rows = *a.count, bblocks = dx_blocks(rows, L::BB), shares = dx_shares(rows, L::BB, a.bblocks * a.shares);
+    if (rows == 0 || !block_of((int)blockIdx.x, a.ablocks, bblocks * shares, ia, ib)) return;
+    const int share = ib / bblocks, a0 = ia * L::BA, b0 = (ib - share * bblocks) * L::BB;
     f32x16 acc[L::IA][L::IB] = {};
-    const int lo = (int)((long long)a.stages * share / a.shares), hi = (int)((long long)a.stages * (share + 1) / a.shares);
+    const int lo = (int)((long long)a.stages * share / shares), hi = (int)((long long)a.stages * (share + 1) / shares);
     L::run(acc, a.a, a.b, a0, b0, lo, hi, a.planes, s0, s1, s2, s3);
     L::each(acc, [&](int i, int j, f32x4 v) __attribute__((always_inline)) {
         if (a0 + i >= a.pstride || b0 + j >= rows) return;
-        f32x4* p = (f32x4*)(a.part + share * a.pshare + (long long)(b0 + j) * a.pstride + a0 + i);
+        f32x4* p = (f32x4*)(a.part + ((long long)share * bblocks * L::BB + b0 + j) * a.pstride + a0 + i);
         *p = a.add ? *p + v : v;
     });
 }
@@ -358,11 +362,15 @@ __global__ __launch_bounds__(L::kThreads, 2) void k_loss_dw(const GradArgs a)
 
 // Sums of the shares, in their order, as gradients: row r of out is row place[r] of them (place null: r), or zeros.
 template <typename T>
-__global__ __launch_bounds__(256) void k_loss_sum(const float* part, long long pstride, long long pshare, int shares, const int* place, long long rows, void* out, long long ostride, int C, float scale,
+__global__ __launch_bounds__(256) void k_loss_sum(const float* part, long long pstride, long long pshare, int shares, int block, const int* place, long long rows, void* out, long long ostride, int C, float scale,
                                                   int mean, const int* count)
 {
     const int per = (C + 3) >> 2;
     const float f = gradient_scale(scale, mean, count);
+    if (block) {                                    // of dx: shares for all rows
+        pshare = (long long)dx_blocks(*count, block) * block * pstride;
+        shares = dx_shares(*count, block, shares);
+    }
     for (long long u = (long long)blockIdx.x * 256 + threadIdx.x; u < rows * per; u += (long long)gridDim.x * 256) {
         const long long r = u / per, from = place ? place[r] : r;
         const int c = (int)(u - r * per) * 4;
@@ -407,8 +415,8 @@ Plan plan_of(const ftp_token_loss_shape& s, bool back)
         p.joins = (int)std::min<long long>(ceil_div(std::max<long long>(s.rows, 1), 4), s.rows <= 64 ? 1 : 1024);
         return p;
     }
-    // a piece's G in at most 512 MiB and rows of 2^20, whole blocks
-    const long long fits = std::min((512ll << 20) / (2 * p.planes * p.Np) / 256 * 256, 1ll << 20), all = round_up(s.vocab, 256);
+    // a piece's G in at most 1 GiB and rows of 2^20, whole blocks
+    const long long fits = std::min((1024ll << 20) / (2 * p.planes * p.Np) / 256 * 256, 1ll << 20), all = round_up(s.vocab, 256);
     const long long pieces = ceil_div(all, std::max(256ll, fits));
     p.piece = round_up(ceil_div(s.vocab, pieces), 256);
     p.logits = split_of(p.piece, s.rows, p.Cp / 32 * terms, 128, 1);
@@ -440,7 +448,7 @@ Buffers buffers_of(const ftp_token_loss_shape& s, const Plan& p, bool back, char
         b.sums = t.take<double>(2 * 1024);
     } else {
         b.g = t.take<bf16_t>((size_t)p.planes * p.Np * p.piece);
-        b.dx = t.take<float>((size_t)p.dx.shares * p.Np * p.Cp);
+        b.dx = t.take<float>((size_t)p.dx.shares * round_up(p.Np, p.dx.block) * p.Cp);
         b.dw = t.take<float>(p.dw.shares > 1 ? (size_t)p.dw.shares * p.piece * p.Cp : 0);
     }
     b.bytes = t.used;
@@ -456,8 +464,8 @@ void gather(const ftp_token_loss_shape& s, const Plan& p, const Buffers& b, cons
     GatherArgs g = {};
     g.ids = labels; g.x = x; g.counts = b.counts; g.xc = b.xc; g.index = b.index; g.label = b.label; g.place = b.place; g.count = b.count;
     g.rows = s.rows; g.stride = s.x_stride; g.plane = p.Np * p.Cp; g.block = p.Np * 32; g.wide = s.id_type; g.vocab = s.vocab; g.C = s.channels; g.Cp = p.Cp;
-    if constexpr (P == 1) k_gather<bf16_t, 1><<<(unsigned)p.chunks, 256, 0, st>>>(g);
-    else k_gather<float, 3><<<(unsigned)p.chunks, 256, 0, st>>>(g);
+    if constexpr (P == 1) k_gather<bf16_t, 1><<<(unsigned)p.chunks * 4, 256, 0, st>>>(g);
+    else k_gather<float, 3><<<(unsigned)p.chunks * 4, 256, 0, st>>>(g);
 }
 
 // W as the products read it: as it lies where it is read once and allows it, else laid out for them.
@@ -466,7 +474,7 @@ Matrix weight(const ftp_token_loss_shape& s, const Plan& p, const Buffers& b, co
 {
     if (P == 1 && once && s.channels % 64 == 0 && s.w_stride % 8 == 0 && s.w_stride < (1 << 20) && aligned(w, 16)) return row_major((const bf16_t*)w, s.w_stride, s.vocab, p.Cp);
     const long long plane = p.Vp * p.Cp;
-    const unsigned grid = pass_grid(plane / 8);
+    const unsigned grid = (unsigned)std::min<long long>(ceil_div(p.Vp / 16 * (p.Cp / 32), 4), 8192);
     if constexpr (P == 1) k_pack_rows<bf16_t, 1><<<grid, 256, 0, st>>>((const bf16_t*)w, s.w_stride, s.vocab, s.channels, (int)p.Vp, p.Cp, b.wc, plane);
     else k_pack_rows<float, 3><<<grid, 256, 0, st>>>((const float*)w, s.w_stride, s.vocab, s.channels, (int)p.Vp, p.Cp, b.wc, plane);
     return blocked(b.wc, p.Vp, p.Cp, plane);
@@ -536,7 +544,7 @@ void backward(const ftp_token_loss_shape& s, const void* x, const void* w, const
             const int block = p.dx.block;
             k.a = wp; k.b = g; k.stages = (int)ceil_div(n, 32); k.shares = p.dx.shares; k.add = v0 > 0;
             k.ablocks = (int)ceil_div(p.Cp, block); k.bblocks = (int)ceil_div(s.rows, block);
-            k.part = b.dx; k.pshare = p.Np * p.Cp;
+            k.part = b.dx;
             if (p.dx.block == 256) dx_pass<Big<true, false>>(k, st);
             else dx_pass<Mid<true, false>>(k, st);
         }
@@ -550,11 +558,11 @@ void backward(const ftp_token_loss_shape& s, const void* x, const void* w, const
             if (p.dw.block == 256) dw_pass<Big<true, true>, T>(k, st);
             else dw_pass<Mid<true, true>, T>(k, st);
             if (k.shares > 1)
-                k_loss_sum<T><<<pass_grid(n * ceil_div(s.channels, 4)), 256, 0, st>>>(b.dw, p.Cp, k.pshare, k.shares, nullptr, n, out, s.dw_stride, s.channels, s.scale, !dloss, b.count);
+                k_loss_sum<T><<<pass_grid(n * ceil_div(s.channels, 4)), 256, 0, st>>>(b.dw, p.Cp, k.pshare, k.shares, 0, nullptr, n, out, s.dw_stride, s.channels, s.scale, !dloss, b.count);
         }
     }
     if (dx && s.rows)
-        k_loss_sum<T><<<pass_grid(s.rows * ceil_div(s.channels, 4)), 256, 0, st>>>(b.dx, p.Cp, p.Np * p.Cp, p.dx.shares, b.place, s.rows, dx, s.dx_stride, s.channels, s.scale, !dloss, b.count);
+        k_loss_sum<T><<<pass_grid(s.rows * ceil_div(s.channels, 4)), 256, 0, st>>>(b.dx, p.Cp, 0, (int)ceil_div(s.rows, p.dx.block) * p.dx.shares, p.dx.block, b.place, s.rows, dx, s.dx_stride, s.channels, s.scale, !dloss, b.count);
 }
 
 }  // namespace
