@@ -1,11 +1,11 @@
-// Newton-Schulz steps towards the orthogonal part of a matrix: X <- a X + (b S + c S^2) X with S = X X^T, or, where X is taller than wide, X <- a X + X (b S + c S^2) with S = X^T X.  Neither needs a transposed copy: a product's
+// Newton-Schulz steps towards the orthogonal part of a matrix: X <- (a I + b S + c S^2) X with S = X X^T, or, where X is taller than wide, X <- X (a I + b S + c S^2) with S = X^T X.  Neither needs a transposed copy: a product's
 // operand may lie either way (ftp_product.h).
 //
 // A step is three products.  Errors of X, S and their products meet a factor of up to a (3.4) a step where singular values are small, so numbers go from one product to the next as
-// three bfloats (fp32: 24 bits, six products of planes) or two (bfloat: 16 bits, three), and sums are fp32.  S and b S + c S^2 are symmetric: blocks on and below the diagonal are multiplied, the others are mirrored.
+// three bfloats (fp32: 24 bits, six products of planes) or two (bfloat: 16 bits, three), and sums are fp32.  a goes into the second one's diagonal, so that the third needs no more than its sums.  S and its polynomial are symmetric: blocks on and below the diagonal are multiplied, the others are mirrored.
 // Blocks that do not fill a last round of the chip (all, of small products) are cut along their contraction, whose shares a second kernel adds up.
 #include "ftp_training.h"
-#include "ftp_product.h"
+#include "ftp_orthogonal.h"
 
 #include <algorithm>
 #include <cmath>
@@ -47,19 +47,6 @@ __global__ __launch_bounds__(256) void k_squares(const T* x, long long mstride, 
     if (threadIdx.x == 0) sums[blockIdx.x] = lds[0] + lds[1] + lds[2] + lds[3];
 }
 
-// 1 / (|x| + eps) of a matrix, for a whole workgroup
-__device__ __forceinline__ double inverse_norm(const double* sums, int parts, double eps)
-{
-    __shared__ double lds[4];
-    double s = 0;
-    for (int i = threadIdx.x; i < parts; i += 256) s += sums[i];
-#pragma unroll
-    for (int k = 32; k; k >>= 1) s += __shfl_xor(s, k);
-    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = s;
-    __syncthreads();
-    return 1.0 / (sqrt(lds[0] + lds[1] + lds[2] + lds[3]) + eps);
-}
-
 // x / (|x| + eps) as planes, laid out for the products, with zeros up to whole blocks of 64: 64 rows x 32 columns at a time.
 template <typename T, int P>
 __global__ __launch_bounds__(256) void k_normed(const T* x, long long mstride, long long rstride, int rows, int cols, int parts, const double* sums, double eps, bf16_t* to, int Rp, int Cp, long long plane)
@@ -98,8 +85,9 @@ struct StepArgs {
     int blocks, whole, shares;                      // blocks of all matrices; the first `whole` of them by a workgroup each, the others by `shares`
     int groups, grouped;                            // those others: groups (matrices) x blocks
     int symmetric;                                  // blocks above the diagonal are mirrored ones
-    // what becomes of the sums v: f0 old + f1 v, old being planes too
+    // what becomes of the sums v: diagonal I + f0 old + f1 v, old being planes too (f0 = 0: none)
     float f0, f1;
+    float diagonal, spare;                          // (three floats in a row had the compiler keep a copy of them in LDS: 4 x 512 x 2048 468 -> 600 us)
     const bf16_t* old; bf16_t* to;
     long long plane, next; int arows, brows;        // (old and to: a Matrix of brows rows and arows columns each) [matrix: next]
     void* out; int orows, ocols;                    // instead of planes: the results, rows along b
@@ -125,6 +113,8 @@ __device__ __forceinline__ void finish(const StepArgs& a, int matrix, int i, int
     const long long block = a.brows * 32ll, at = matrix * a.next + (i >> 5) * block + j * 32 + (i & 31);
     v *= a.f1;
     if (a.f0 != 0) v += a.f0 * planes_sum<P>(a.old + at, a.plane);
+    const int on = j - i;                           // which of the four lies on the diagonal
+    v += f32x4{on == 0 ? 1.0f : 0.0f, on == 1 ? 1.0f : 0.0f, on == 2 ? 1.0f : 0.0f, on == 3 ? 1.0f : 0.0f} * a.diagonal;
     if (a.out) {
         T* p = (T*)a.out + ((long long)matrix * a.orows + j) * a.ocols + i;
         if (j < a.orows)
@@ -247,6 +237,7 @@ struct Plan {
     bool tall;
     Cut s, q, x;                                    // of S, its square, X
 };
+int parts_of(const ftp_orthogonal_shape& s) { return (int)std::min<long long>(1024, ceil_div(s.rows, 8)); }
 Plan plan_of(const ftp_orthogonal_shape& s)
 {
     Plan p = {};
@@ -256,7 +247,7 @@ Plan plan_of(const ftp_orthogonal_shape& s)
     p.tall = s.rows > s.cols;
     p.m = std::min(s.rows, s.cols);
     p.mp = (p.m + 63) & ~63;
-    p.parts = (int)std::min<long long>(1024, ceil_div(s.rows, 8));
+    p.parts = parts_of(s);
     const long long terms = p.planes == 2 ? 3 : 6, longer = std::max(p.Rp, p.Cp);
     p.s = cut_of(p.mp, p.mp, true, longer / 32 * terms, s.count);
     p.q = cut_of(p.mp, p.mp, true, p.mp / 32 * terms, s.count);
@@ -306,6 +297,14 @@ void product(StepArgs& a, const Cut& c, hipStream_t st)
 template <typename T, int P>
 void run(const ftp_orthogonal_shape& s, const T* x, T* out, char* ws, hipStream_t st)
 {
+    if (orthogonal_is_small(s)) {
+        Parts t(ws);
+        const int parts = parts_of(s);
+        double* sums = t.take<double>((size_t)s.count * parts);
+        k_squares<T><<<(unsigned)(s.count * parts), 256, 0, st>>>(x, s.matrix_stride, s.row_stride, s.rows, s.cols, parts, sums);
+        orthogonal_small(s, x, out, sums, parts, t, st);
+        return;
+    }
     const Plan p = plan_of(s);
     const Buffers b = buffers_of(s, p, ws);
     const long long xnext = (long long)p.Rp * p.Cp, xplane = s.count * xnext, qnext = (long long)p.mp * p.mp, qplane = s.count * qnext;
@@ -321,11 +320,11 @@ void run(const ftp_orthogonal_shape& s, const T* x, T* out, char* ws, hipStream_
         k.a = k.b = X; k.anext = k.bnext = xnext; k.stages = std::max(p.Rp, p.Cp) / 32; k.symmetric = 1; k.f1 = 1; k.to = b.s;
         if (p.tall) product<true, true, T, P>(k, p.s, st);
         else product<false, false, T, P>(k, p.s, st);
-        // b S + c S^2
-        k.a = k.b = S; k.anext = k.bnext = qnext; k.stages = p.mp / 32; k.symmetric = 1; k.f0 = s.b; k.f1 = s.c; k.old = b.s; k.to = b.q;
+        // a I + b S + c S^2
+        k.a = k.b = S; k.anext = k.bnext = qnext; k.stages = p.mp / 32; k.symmetric = 1; k.diagonal = s.a; k.f0 = s.b; k.f1 = s.c; k.old = b.s; k.to = b.q;
         product<false, false, T, P>(k, p.q, st);
-        // a X + that times X
-        k.symmetric = 0; k.f0 = s.a; k.f1 = 1; k.old = b.x[step & 1]; k.to = b.x[~step & 1];
+        // that times X
+        k.symmetric = 0; k.diagonal = k.f0 = 0; k.f1 = 1; k.to = b.x[~step & 1];
         k.arows = p.Cp; k.brows = p.Rp; k.next = xnext; k.plane = xplane;
         if (step + 1 == s.steps) { k.out = out; k.orows = s.rows; k.ocols = s.cols; }
         if (p.tall) {
@@ -346,7 +345,13 @@ bool orthogonal_fits(const ftp_orthogonal_shape& s)
     // launches of fewer than 2^32 threads
     return (double)s.count * (double)ceil_div(s.rows, 64) * (double)ceil_div(s.cols, 64) < (1 << 23);
 }
-size_t orthogonal_workspace(const ftp_orthogonal_shape& s) { return buffers_of(s, plan_of(s), nullptr).bytes; }
+size_t orthogonal_workspace(const ftp_orthogonal_shape& s)
+{
+    if (!orthogonal_is_small(s)) return buffers_of(s, plan_of(s), nullptr).bytes;
+    Parts t(nullptr);
+    t.take<double>((size_t)s.count * parts_of(s));
+    return orthogonal_small_workspace(s, t);
+}
 void orthogonal(const ftp_orthogonal_shape& s, const void* x, void* out, char* ws, hipStream_t st)
 {
     if (s.dtype == FTP_BF16) run<bf16_t, 2>(s, (const bf16_t*)x, (bf16_t*)out, ws, st);

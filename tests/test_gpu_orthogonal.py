@@ -1,7 +1,7 @@
 """Newton-Schulz steps against the formula in 64 bits.
 
 Bounds of one step, element by element, u = 2^-24: a number between two products is held to h of itself (three bfloats h = u, two 2^-16), products of such numbers are off by 3 h each beside the sum's
-(K + 8) u, whatever its order; the bound follows the formula from X (3 u for the norm and the product with its inverse) over S and b S + c S^2 to the result, each absolute value in the place of its number.
+(K + 8) u, whatever its order; the bound follows the formula from X (3 u for the norm and the product with its inverse) over S and Q = a I + b S + c S^2 to the result Q X, each absolute value in the place of its number.
 
 Bound of several steps: such errors go through the steps that follow, by factors that depend on the matrix.  So the formula runs in 64 bits with every held number and every product's result changed by random parts of
 that size (uniform within +-h, the sums' by +-sqrt(K) u of their absolute values' sum), which makes an error of the size that the kernel's roundings make; the kernel's norm of the error may be 8 times that, and the type's rounding."""
@@ -40,8 +40,8 @@ def _steps(x, steps, eps=1e-7, abc=ABC, noise=None):
     x = keep(x / (torch.linalg.vector_norm(x) + eps))
     for _ in range(steps):
         s = keep(_mm(x, x.t()), x.shape[1], _mm(x.abs(), x.t().abs()))
-        q = keep(b * s + c * _mm(s, s), s.shape[0], abs(c) * _mm(s.abs(), s.abs()))
-        x = keep(a * x + _mm(q, x), s.shape[0], _mm(q.abs(), x.abs()))
+        q = keep(a * torch.eye(len(s), dtype=s.dtype, device=s.device) + b * s + c * _mm(s, s), s.shape[0], abs(c) * _mm(s.abs(), s.abs()))
+        x = keep(_mm(q, x), s.shape[0], _mm(q.abs(), x.abs()))
     return x.t().contiguous() if turned else x
 
 
@@ -58,9 +58,9 @@ def _one_step_bound(x, dtype, eps=1e-7):
     s = _mm(x, x.t()).abs()
     es = es + (h + U) * (s + es)
     ss = _mm(s, s)
-    q = b * s + c * ss
+    q = b * s + c * ss + a * torch.eye(n, dtype=torch.float64, device=x.device)
     eq = b * es + c * (_mm(es, s) + _mm(s, es) + _mm(es, es)) + (c * ((n + 8) * U + 3 * h)) * _mm(s + es, s + es) + (h + 4 * U) * (q + b * es)
-    e = a * ex + _mm(eq, ax + ex) + _mm(q, ex) + ((n + 8) * U + 3 * h) * _mm(q + eq, ax + ex) + 4 * U * (a * ax + _mm(q, ax))
+    e = _mm(eq, ax + ex) + _mm(q, ex) + ((n + 8) * U + 3 * h) * _mm(q + eq, ax + ex)
     return e.t().contiguous() if turned else e
 
 
