@@ -81,7 +81,8 @@ __global__ __launch_bounds__(256) void k_normed(const T* x, long long mstride, l
 struct StepArgs {
     Matrix a, b;                                    // of the first matrix
     long long anext, bnext;                         // elements to the next one's
-    int planes, stages, count, ablocks, bblocks;    // stages of 32, an even number
+    Terms terms;
+    int stages, count, ablocks, bblocks;            // stages of 32, an even number
     int blocks, whole, shares;                      // blocks of all matrices; the first `whole` of them by a workgroup each, the others by `shares`
     int groups, grouped;                            // those others: groups (matrices) x blocks
     int symmetric;                                  // blocks above the diagonal are mirrored ones
@@ -181,7 +182,7 @@ __global__ __launch_bounds__(L::kThreads, 2) void k_step(const StepArgs a)
     y.p += matrix * a.bnext;
     f32x16 acc[L::IA][L::IB] = {};
     const int stages = a.stages / (L::KS / 32);
-    L::run(acc, x, y, a0, b0, (int)((long long)stages * share / shares), (int)((long long)stages * (share + 1) / shares), a.planes, s0, s1, s2, s3);
+    L::run(acc, x, y, a0, b0, (int)((long long)stages * share / shares), (int)((long long)stages * (share + 1) / shares), a.terms, s0, s1, s2, s3);
     if (shares > 1) {
         float* p = a.part + ((long long)(t - a.whole) * shares + share) * (L::BA * L::BB);
         L::each(acc, [&](int i, int j, f32x4 v) __attribute__((always_inline)) { *(f32x4*)(p + j * L::BA + i) = v; });
@@ -314,7 +315,7 @@ void run(const ftp_orthogonal_shape& s, const T* x, T* out, char* ws, hipStream_
     for (int step = 0; step < s.steps; ++step) {
         const Matrix X = blocked(b.x[step & 1], p.Rp, p.Cp, xplane);
         StepArgs k = {};
-        k.planes = P; k.count = s.count; k.part = b.part;
+        k.terms = terms_of(P); k.count = s.count; k.part = b.part;
         k.arows = k.brows = p.mp; k.next = qnext; k.plane = qplane;
         // S
         k.a = k.b = X; k.anext = k.bnext = xnext; k.stages = std::max(p.Rp, p.Cp) / 32; k.symmetric = 1; k.f1 = 1; k.to = b.s;

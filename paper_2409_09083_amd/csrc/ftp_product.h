@@ -47,6 +47,16 @@ inline Matrix rows_of(Matrix m, long long r0, long long n)
     return m;
 }
 
+// The products of planes that a product is the sum of, smallest first: planes of the two operands, two bits each.
+struct Terms { int n; uint32_t a, b; };
+inline Terms terms_of(int planes)
+{
+    // (0, 0);  (1, 0) (0, 1) (0, 0);  (2, 0) (0, 2) (1, 1) (1, 0) (0, 1) (0, 0)
+    return planes == 1 ? Terms{1, 0, 0} : planes == 2 ? Terms{3, 0x1, 0x4} : Terms{6, 0x52, 0x118};
+}
+// ... of one plane with two: (0, 1) (0, 0)
+inline Terms terms_one_two() { return Terms{2, 0, 0x1}; }
+
 // A workgroup's block BA x BB by WA x WB wavefronts; XA, XB: the operand lies across.
 template <int BA_, int BB_, int WA_, int WB_, bool XA_, bool XB_, int KS_ = 32, int STAGES = 4>
 struct Product {
@@ -142,18 +152,17 @@ struct Product {
     static __device__ __forceinline__ int wave_a() { return (__builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % WA) * (IA * 32); }
     static __device__ __forceinline__ int wave_b() { return (__builtin_amdgcn_readfirstlane(threadIdx.x >> 6) / WA) * (IB * 32); }
 
-    // acc[i][j] += the block at (a0, b0) over the stages [lo, hi) of the contraction.  planes: of both operands.  The stages are distinct objects, so that loads into one are no reason to wait for those
+    // acc[i][j] += the block at (a0, b0) over the stages [lo, hi) of the contraction, for all terms.  The stages are distinct objects, so that loads into one are no reason to wait for those
     // into another.  At the end all of this wavefront's loads have landed.
     template <class... S>
-    static __device__ __forceinline__ void run(f32x16 (&acc)[IA][IB], const Matrix& a, const Matrix& b, long long a0, long long b0, int lo, int hi, int planes, S&... stages)
+    static __device__ __forceinline__ void run(f32x16 (&acc)[IA][IB], const Matrix& a, const Matrix& b, long long a0, long long b0, int lo, int hi, Terms terms, S&... stages)
     {
         Source<BA, XA, kLoadsA> fa;
         Source<BB, XB, kLoadsB> fb;
         fa.init(a, a0, (long long)lo * KS);
         fb.init(b, b0, (long long)lo * KS);
-        const int wa = wave_a(), wb = wave_b(), per = hi - lo, terms = planes == 1 ? 1 : planes == 2 ? 3 : 6, total = per * terms;
-        // planes of the terms, two bits each: (2, 0) (0, 2) (1, 1) (1, 0) (0, 1) (0, 0)
-        uint32_t pa = planes == 3 ? 0x52u : planes == 2 ? 0x1u : 0u, pb = planes == 3 ? 0x118u : planes == 2 ? 0x4u : 0u;
+        const int wa = wave_a(), wb = wave_b(), per = hi - lo, total = per * terms.n;
+        uint32_t pa = terms.a, pb = terms.b;
         if (total == 0) return;
         int k = per, to_come = total;
         fa.start(pa & 3);

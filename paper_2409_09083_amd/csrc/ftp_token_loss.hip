@@ -16,7 +16,9 @@ namespace {
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int kChunk = 64;                          // rows whose labels one wavefront looks at
 constexpr int kPackRows = 4096;                     // from here on W is laid out for the products
-constexpr int kFew = 32;                            // most rows of the forward pass that reads W at the memory's rate
+// Up to so many rows G is two bfloats where the tensors are one: its rounding, which the sums over many rows even out, would be as large as the results' own, and costs nothing to avoid.
+constexpr int kExact = 64;
+constexpr int kFew = 32;                            // most rows of the logits that read W at the memory's rate
 
 template <bool XA, bool XB> using Big = Product<256, 256, 2, 4, XA, XB>;
 typedef Product<256, 128, 2, 2, false, false, 32, 3> Two;         // two workgroups a CU: one's powers beside the other's products
@@ -127,7 +129,8 @@ struct LogitArgs {
     const int* count;                               // rows of x (null: all)
     const int* label;                               // of them (null: ids)
     const void* ids;
-    int wide, planes, stages, vocab, ablocks, bblocks;
+    Terms terms;
+    int wide, stages, vocab, ablocks, bblocks;
     int piece0;                                     // the piece's first id
     float c; int negate;                            // |scale| * log2(e), and whether scale is negative
     float2* part; float* target;                    // forward: [row][ablocks] maximum and sum of a block's powers of 2; the labels' products
@@ -146,10 +149,10 @@ __global__ __launch_bounds__(L::kThreads, 2) void k_logits(const LogitArgs a)
     const int a0 = ia * L::BA, b0 = ib * L::BB, rows = a.count ? *a.count : (int)a.x.rows;
     if (b0 >= rows) return;
     f32x16 acc[L::IA][L::IB] = {};
-    if constexpr (L::kStages == 3) L::run(acc, a.w, a.x, a0, b0, 0, a.stages, a.planes, s0, s1, s2);
+    if constexpr (L::kStages == 3) L::run(acc, a.w, a.x, a0, b0, 0, a.stages, a.terms, s0, s1, s2);
     else {
         __shared__ __align__(16) typename L::Stage s3;
-        L::run(acc, a.w, a.x, a0, b0, 0, a.stages, a.planes, s0, s1, s2, s3);
+        L::run(acc, a.w, a.x, a0, b0, 0, a.stages, a.terms, s0, s1, s2, s3);
     }
     const int l = threadIdx.x & 63, h = l >> 5, wa = L::wave_a(), wb = L::wave_b();
     if (a.negate)
@@ -301,7 +304,8 @@ __global__ __launch_bounds__(256) void k_loss_mean(const double* sums, int n, fl
 struct GradArgs {
     Matrix a, b;
     const int* count;
-    int planes, stages, shares, ablocks, bblocks, add;         // dx: shares and blocks for all rows; fewer rows have more shares (dx_shares())
+    Terms terms;
+    int stages, shares, ablocks, bblocks, add;         // dx: shares and blocks for all rows; fewer rows have more shares (dx_shares())
     float* part; long long pstride, pshare;         // [share][index of b][pstride]
     void* out; long long ostride; int C; float scale; int mean;     // dw alone, without shares
 };
@@ -326,7 +330,7 @@ __global__ __launch_bounds__(L::kThreads, 2) void k_loss_dx(const GradArgs a)
     const int share = ib / bblocks, a0 = ia * L::BA, b0 = (ib - share * bblocks) * L::BB;
     f32x16 acc[L::IA][L::IB] = {};
     const int lo = (int)((long long)a.stages * share / shares), hi = (int)((long long)a.stages * (share + 1) / shares);
-    L::run(acc, a.a, a.b, a0, b0, lo, hi, a.planes, s0, s1, s2, s3);
+    L::run(acc, a.a, a.b, a0, b0, lo, hi, a.terms, s0, s1, s2, s3);
     L::each(acc, [&](int i, int j, f32x4 v) __attribute__((always_inline)) {
         if (a0 + i >= a.pstride || b0 + j >= rows) return;
         f32x4* p = (f32x4*)(a.part + ((long long)share * bblocks * L::BB + b0 + j) * a.pstride + a0 + i);
@@ -345,7 +349,7 @@ __global__ __launch_bounds__(L::kThreads, 2) void k_loss_dw(const GradArgs a)
     const int share = ib / a.bblocks, a0 = ia * L::BA, b0 = (ib - share * a.bblocks) * L::BB, stages = (*a.count + L::KS - 1) / L::KS;
     f32x16 acc[L::IA][L::IB] = {};
     const int lo = (int)((long long)stages * share / a.shares), hi = (int)((long long)stages * (share + 1) / a.shares);
-    L::run(acc, a.a, a.b, a0, b0, lo, hi, a.planes, s0, s1, s2, s3);
+    L::run(acc, a.a, a.b, a0, b0, lo, hi, a.terms, s0, s1, s2, s3);
     const float f = gradient_scale(a.scale, a.mean, a.count);
     L::each(acc, [&](int i, int j, f32x4 v) __attribute__((always_inline)) {
         const long long id = b0 + j;
@@ -393,7 +397,7 @@ int padded(int c) { return (c + 63) & ~63; }
 long long round_up(long long v, long long to) { return ceil_div(v, to) * to; }
 
 struct Plan {
-    int planes, Cp, blocks, pack_w, gather, few;
+    int planes, gplanes, Cp, blocks, few;           // bfloats of an input and of an element of G
     long long Np, Vp, chunks, piece;                // rows and ids up to whole blocks of 64; ids of a piece, whole blocks of 256
     Split logits, dx, dw;
     int joins;
@@ -408,7 +412,8 @@ Plan plan_of(const ftp_token_loss_shape& s, bool back)
     p.chunks = ceil_div(std::max<long long>(s.rows, 1), kChunk);
     const long long terms = p.planes == 1 ? 1 : 6;
     // whether W, and few rows of x, can be read as they lie (their addresses are looked at by the call: scratch is there for both ways)
-    p.few = !back && s.rows <= kFew;
+    p.few = s.rows <= kFew;
+    p.gplanes = p.planes == 1 && s.rows <= kExact ? 2 : p.planes;
     if (!back) {
         p.logits = split_of(s.vocab, s.rows, p.Cp / 32 * terms, 128, 1);
         p.blocks = (int)ceil_div(s.vocab, p.few ? Few::BA : p.logits.block);
@@ -416,12 +421,13 @@ Plan plan_of(const ftp_token_loss_shape& s, bool back)
         return p;
     }
     // a piece's G in at most 1 GiB and rows of 2^20, whole blocks
-    const long long fits = std::min((1024ll << 20) / (2 * p.planes * p.Np) / 256 * 256, 1ll << 20), all = round_up(s.vocab, 256);
+    const long long fits = std::min((1024ll << 20) / (2 * p.gplanes * p.Np) / 256 * 256, 1ll << 20), all = round_up(s.vocab, 256);
     const long long pieces = ceil_div(all, std::max(256ll, fits));
     p.piece = round_up(ceil_div(s.vocab, pieces), 256);
     p.logits = split_of(p.piece, s.rows, p.Cp / 32 * terms, 128, 1);
-    p.dx = split_of(s.channels, s.rows, p.piece / 32 * terms, 128, 16);
-    p.dw = split_of(s.channels, p.piece, p.Np / 32 * terms, 128, 16);
+    const long long gterms = p.planes == 1 ? p.gplanes : 6;
+    p.dx = split_of(s.channels, s.rows, p.piece / 32 * gterms, 128, 16);
+    p.dw = split_of(s.channels, p.piece, p.Np / 32 * gterms, 128, 16);
     return p;
 }
 
@@ -447,7 +453,7 @@ Buffers buffers_of(const ftp_token_loss_shape& s, const Plan& p, bool back, char
         b.target = t.take<float>(p.Np);
         b.sums = t.take<double>(2 * 1024);
     } else {
-        b.g = t.take<bf16_t>((size_t)p.planes * p.Np * p.piece);
+        b.g = t.take<bf16_t>((size_t)p.gplanes * p.Np * p.piece);
         b.dx = t.take<float>((size_t)p.dx.shares * round_up(p.Np, p.dx.block) * p.Cp);
         b.dw = t.take<float>(p.dw.shares > 1 ? (size_t)p.dw.shares * p.piece * p.Cp : 0);
     }
@@ -501,7 +507,7 @@ void forward(const ftp_token_loss_shape& s, const void* x, const void* w, const 
     const Plan p = plan_of(s, false);
     const Buffers b = buffers_of(s, p, false, ws);
     LogitArgs a = {};
-    a.planes = P; a.wide = s.id_type; a.vocab = s.vocab; set_scale(a, s.scale); a.part = b.part; a.target = b.target; a.ids = labels;
+    a.terms = terms_of(P); a.wide = s.id_type; a.vocab = s.vocab; set_scale(a, s.scale); a.part = b.part; a.target = b.target; a.ids = labels;
     const bool plain = p.few && P == 1 && s.channels % 64 == 0 && (s.x_stride % 8 == 0 || s.rows <= 1) && s.x_stride < (1 << 20) && aligned(x, 16);
     a.w = weight<P>(s, p, b, w, s.rows < kPackRows, st);
     a.w.rows = s.vocab;
@@ -534,12 +540,14 @@ void backward(const ftp_token_loss_shape& s, const void* x, const void* w, const
         const int n = (int)std::min<long long>(p.piece, s.vocab - v0);
         const Matrix wp = rows_of(all, v0, n);
         LogitArgs a = {};
-        a.w = wp; a.x = xc; a.count = b.count; a.label = b.label; a.planes = P; a.vocab = s.vocab; a.piece0 = (int)v0; set_scale(a, s.scale);
+        a.w = wp; a.x = xc; a.count = b.count; a.label = b.label; a.terms = terms_of(P); a.vocab = s.vocab; a.piece0 = (int)v0; set_scale(a, s.scale);
         a.index = b.index; a.lse = lse; a.dloss = dloss; a.g = b.g; a.gblock = g.block; a.gplane = g.plane;
-        if (p.logits.block == 256) logits<Two, P, false>(a, s.rows, st);
+        if (p.few) logits<Few, P == 1 ? 2 : 3, false>(a, s.rows, st);
+        else if (p.gplanes != P) logits<Mid<false, false>, P == 1 ? 2 : 3, false>(a, s.rows, st);
+        else if (p.logits.block == 256) logits<Two, P, false>(a, s.rows, st);
         else logits<Mid<false, false>, P, false>(a, s.rows, st);
         GradArgs k = {};
-        k.count = b.count; k.planes = P; k.C = s.channels; k.scale = s.scale; k.mean = !dloss; k.pstride = p.Cp;
+        k.count = b.count; k.terms = p.gplanes == P ? terms_of(P) : terms_one_two(); k.C = s.channels; k.scale = s.scale; k.mean = !dloss; k.pstride = p.Cp;
         if (dx && s.rows) {
             const int block = p.dx.block;
             k.a = wp; k.b = g; k.stages = (int)ceil_div(n, 32); k.shares = p.dx.shares; k.add = v0 > 0;
