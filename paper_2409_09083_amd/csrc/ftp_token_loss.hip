@@ -14,10 +14,11 @@ namespace ftp {
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr int kCountRows = 4096;                    // most rows whose labels every workgroup counts by itself (a launch less)
 constexpr int kChunk = 64;                          // rows whose labels one wavefront looks at
 constexpr int kPackRows = 4096;                     // from here on W is laid out for the products
 // Up to so many rows G is two bfloats where the tensors are one: its rounding, which the sums over many rows even out, would be as large as the results' own, and costs nothing to avoid.
-constexpr int kExact = 64;
+constexpr int kExact = 256;
 constexpr int kFew = 32;                            // most rows of the logits that read W at the memory's rate
 
 template <bool XA, bool XB> using Big = Product<256, 256, 2, 4, XA, XB>;
@@ -57,27 +58,55 @@ __device__ __forceinline__ void copy8(const T* row, int c0, int C, bf16_t* to, l
     }
 }
 
-struct GatherArgs {
-    const void* ids; const void* x; const int* counts;
+struct PrepareArgs {
+    const void* ids; const void* x; const int* counts;         // counts null: of so few rows that each workgroup counts them itself
     bf16_t* xc; int* index; int* label; int* place; int* count;
     long long rows, stride, plane, block;           // of xc: as a Matrix lies
     int wide, vocab, C, Cp;
+    int gathering;                                  // the first workgroups, four a chunk; the others lay W out
+    const void* w; bf16_t* wc; long long wstride, wplane; int Vp;
 };
 
-// The labelled rows one behind the other: row place[r] of xc is row r of x, index and label say which.  Zeros up to the next multiple of 64 rows.
+// W as planes, laid out for the products; zeros up to Vp rows of Cp.  `index` of `groups` workgroups.
 template <typename T, int P>
-__global__ __launch_bounds__(256) void k_gather(const GatherArgs a)
+__device__ __forceinline__ void lay_out(const PrepareArgs& a, int index, int groups)
 {
+    // a wavefront has 16 rows x 32 columns, 1 KB where they go
+    const int lane = threadIdx.x & 63, across = a.Cp >> 5, c_in = (lane & 3) * 8;
+    const long long tiles = (long long)(a.Vp >> 4) * across;
+    for (long long t = (long long)index * 4 + (threadIdx.x >> 6); t < tiles; t += 4ll * groups) {
+        const int rb = (int)(t / across), cb = (int)(t - (long long)rb * across), r = rb * 16 + (lane >> 2);
+        copy8<T, P>((const T*)a.w + r * a.wstride, r < a.vocab ? cb * 32 + c_in : 0, r < a.vocab ? a.C : 0, a.wc + ((long long)cb * a.Vp + r) * 32 + c_in, a.wplane);
+    }
+}
+
+// The labelled rows one behind the other: row place[r] of xc is row r of x, index and label say which.  Zeros up to the next multiple of 64 rows.  And W.
+template <typename T, int P>
+__global__ __launch_bounds__(256) void k_prepare(const PrepareArgs a)
+{
+    if ((int)blockIdx.x >= a.gathering) {
+        lay_out<T, P>(a, blockIdx.x - a.gathering, gridDim.x - a.gathering);
+        return;
+    }
     __shared__ int sums[2][4];
     __shared__ int where[kChunk];
-    const long long chunk = blockIdx.x >> 2, row0 = chunk * kChunk, chunks = gridDim.x >> 2;
+    const long long chunk = blockIdx.x >> 2, row0 = chunk * kChunk, chunks = a.gathering >> 2;
     const int sub = blockIdx.x & 3;                 // which 16 rows of the chunk this workgroup copies
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
     int before = 0, all = 0;
-    for (long long i = tid; i < chunks; i += 256) {
-        const int n = a.counts[i];
-        all += n;
-        before += i < chunk ? n : 0;
+    if (a.counts) {
+        for (long long i = tid; i < chunks; i += 256) {
+            const int n = a.counts[i];
+            all += n;
+            before += i < chunk ? n : 0;
+        }
+    } else {
+#pragma unroll 4
+        for (long long r = tid; r < a.rows; r += 256) {
+            const int n = id_of(a.ids, a.wide, r, a.vocab) >= 0;
+            all += n;
+            before += r < row0 ? n : 0;
+        }
     }
 #pragma unroll
     for (int n = 32; n; n >>= 1) { before += __shfl_xor(before, n); all += __shfl_xor(all, n); }
@@ -108,19 +137,6 @@ __global__ __launch_bounds__(256) void k_gather(const GatherArgs a)
         for (int cb = wave; cb < across; cb += 4)
 #pragma unroll
             for (int p = 0; p < P; ++p) *(uint4*)(a.xc + p * a.plane + cb * a.block + row * 32 + c_in) = uint4{0, 0, 0, 0};
-}
-
-// W as planes, laid out for the products; zeros up to Rp rows of Cp.
-template <typename T, int P>
-__global__ __launch_bounds__(256) void k_pack_rows(const T* w, long long stride, int rows, int C, int Rp, int Cp, bf16_t* to, long long plane)
-{
-    // a wavefront has 16 rows x 32 columns, 1 KB where they go
-    const int lane = threadIdx.x & 63, across = Cp >> 5, c_in = (lane & 3) * 8;
-    const long long tiles = (long long)(Rp >> 4) * across;
-    for (long long t = (long long)blockIdx.x * 4 + (threadIdx.x >> 6); t < tiles; t += 4ll * gridDim.x) {
-        const int rb = (int)(t / across), cb = (int)(t - (long long)rb * across), r = rb * 16 + (lane >> 2);
-        copy8<T, P>(w + r * stride, r < rows ? cb * 32 + c_in : 0, r < rows ? C : 0, to + ((long long)cb * Rp + r) * 32 + c_in, plane);
-    }
 }
 
 // ---- logits --------------------------------------------------------------------------------------------------------
@@ -463,27 +479,26 @@ Buffers buffers_of(const ftp_token_loss_shape& s, const Plan& p, bool back, char
 
 unsigned pass_grid(long long n) { return (unsigned)std::min<long long>(std::max<long long>(ceil_div(n, 256), 1), 4096); }
 
+// The labelled rows and W as the products read it: W as it lies where it is read by few rows and allows it, else laid out for them.  rows: whether the rows are wanted.
 template <int P>
-void gather(const ftp_token_loss_shape& s, const Plan& p, const Buffers& b, const void* x, const void* labels, hipStream_t st)
+Matrix prepare(const ftp_token_loss_shape& s, const Plan& p, const Buffers& b, const void* x, const void* w, const void* labels, bool rows, hipStream_t st)
 {
-    k_labelled<<<(unsigned)ceil_div(p.chunks, 4), 256, 0, st>>>(labels, s.id_type, s.rows, s.vocab, b.counts);
-    GatherArgs g = {};
-    g.ids = labels; g.x = x; g.counts = b.counts; g.xc = b.xc; g.index = b.index; g.label = b.label; g.place = b.place; g.count = b.count;
-    g.rows = s.rows; g.stride = s.x_stride; g.plane = p.Np * p.Cp; g.block = p.Np * 32; g.wide = s.id_type; g.vocab = s.vocab; g.C = s.channels; g.Cp = p.Cp;
-    if constexpr (P == 1) k_gather<bf16_t, 1><<<(unsigned)p.chunks * 4, 256, 0, st>>>(g);
-    else k_gather<float, 3><<<(unsigned)p.chunks * 4, 256, 0, st>>>(g);
-}
-
-// W as the products read it: as it lies where it is read once and allows it, else laid out for them.
-template <int P>
-Matrix weight(const ftp_token_loss_shape& s, const Plan& p, const Buffers& b, const void* w, bool once, hipStream_t st)
-{
-    if (P == 1 && once && s.channels % 64 == 0 && s.w_stride % 8 == 0 && s.w_stride < (1 << 20) && aligned(w, 16)) return row_major((const bf16_t*)w, s.w_stride, s.vocab, p.Cp);
-    const long long plane = p.Vp * p.Cp;
-    const unsigned grid = (unsigned)std::min<long long>(ceil_div(p.Vp / 16 * (p.Cp / 32), 4), 8192);
-    if constexpr (P == 1) k_pack_rows<bf16_t, 1><<<grid, 256, 0, st>>>((const bf16_t*)w, s.w_stride, s.vocab, s.channels, (int)p.Vp, p.Cp, b.wc, plane);
-    else k_pack_rows<float, 3><<<grid, 256, 0, st>>>((const float*)w, s.w_stride, s.vocab, s.channels, (int)p.Vp, p.Cp, b.wc, plane);
-    return blocked(b.wc, p.Vp, p.Cp, plane);
+    const bool plain = P == 1 && s.rows < kPackRows && s.channels % 64 == 0 && s.w_stride % 8 == 0 && s.w_stride < (1 << 20) && aligned(w, 16);
+    PrepareArgs a = {};
+    a.ids = labels; a.x = x; a.xc = b.xc; a.index = b.index; a.label = b.label; a.place = b.place; a.count = b.count;
+    a.rows = s.rows; a.stride = s.x_stride; a.plane = p.Np * p.Cp; a.block = p.Np * 32; a.wide = s.id_type; a.vocab = s.vocab; a.C = s.channels; a.Cp = p.Cp;
+    a.gathering = rows ? (int)p.chunks * 4 : 0;
+    a.w = w; a.wc = b.wc; a.wstride = s.w_stride; a.wplane = p.Vp * p.Cp; a.Vp = (int)p.Vp;
+    const unsigned grid = (unsigned)a.gathering + (plain ? 0 : (unsigned)std::min<long long>(ceil_div(p.Vp / 16 * (p.Cp / 32), 4), 8192));
+    if (rows && s.rows > kCountRows) {
+        k_labelled<<<(unsigned)ceil_div(p.chunks, 4), 256, 0, st>>>(labels, s.id_type, s.rows, s.vocab, b.counts);
+        a.counts = b.counts;
+    }
+    if (grid) {
+        if constexpr (P == 1) k_prepare<bf16_t, 1><<<grid, 256, 0, st>>>(a);
+        else k_prepare<float, 3><<<grid, 256, 0, st>>>(a);
+    }
+    return plain ? row_major((const bf16_t*)w, s.w_stride, s.vocab, p.Cp) : blocked(b.wc, p.Vp, p.Cp, a.wplane);
 }
 
 void set_scale(LogitArgs& a, float scale)
@@ -509,11 +524,10 @@ void forward(const ftp_token_loss_shape& s, const void* x, const void* w, const 
     LogitArgs a = {};
     a.terms = terms_of(P); a.wide = s.id_type; a.vocab = s.vocab; set_scale(a, s.scale); a.part = b.part; a.target = b.target; a.ids = labels;
     const bool plain = p.few && P == 1 && s.channels % 64 == 0 && (s.x_stride % 8 == 0 || s.rows <= 1) && s.x_stride < (1 << 20) && aligned(x, 16);
-    a.w = weight<P>(s, p, b, w, s.rows < kPackRows, st);
+    a.w = prepare<P>(s, p, b, x, w, labels, !plain, st);
     a.w.rows = s.vocab;
     if (plain) a.x = row_major((const bf16_t*)x, s.x_stride, s.rows, p.Cp);
     else {
-        gather<P>(s, p, b, x, labels, st);
         a.x = blocked(b.xc, p.Np, p.Cp, p.Np * p.Cp);
         a.count = b.count; a.label = b.label;
     }
@@ -534,8 +548,7 @@ void backward(const ftp_token_loss_shape& s, const void* x, const void* w, const
 {
     const Plan p = plan_of(s, true);
     const Buffers b = buffers_of(s, p, true, ws);
-    gather<P>(s, p, b, x, labels, st);
-    const Matrix all = weight<P>(s, p, b, w, s.rows < kPackRows, st), xc = blocked(b.xc, p.Np, p.Cp, p.Np * p.Cp), g = blocked(b.g, p.Np, (int)p.piece, p.Np * p.piece);
+    const Matrix all = prepare<P>(s, p, b, x, w, labels, true, st), xc = blocked(b.xc, p.Np, p.Cp, p.Np * p.Cp), g = blocked(b.g, p.Np, (int)p.piece, p.Np * p.piece);
     for (long long v0 = 0; v0 < s.vocab; v0 += p.piece) {
         const int n = (int)std::min<long long>(p.piece, s.vocab - v0);
         const Matrix wp = rows_of(all, v0, n);
