@@ -238,7 +238,8 @@ struct Plan {
     bool tall;
     Cut s, q, x;                                    // of S, its square, X
 };
-int parts_of(const ftp_orthogonal_shape& s) { return (int)std::min<long long>(1024, ceil_div(s.rows, 8)); }
+// Workgroups of a matrix' sum of squares: of 8 rows and more, fewer than 2^23 in all.
+int parts_of(const ftp_orthogonal_shape& s) { return (int)std::min<long long>({1024, ceil_div(s.rows, 8), (1 << 23) / std::max(s.count, 1)}); }
 Plan plan_of(const ftp_orthogonal_shape& s)
 {
     Plan p = {};

@@ -20,7 +20,7 @@ int check(const ftp_embedding_shape* s)
 
 int check(const ftp_token_loss_shape* s)
 {
-    if (!s || !is_type(s->dtype) || !is_id(s->id_type) || s->rows < 0 || s->vocab < 1 || s->channels < 1 || !std::isfinite(s->scale)) return FTP_EINVAL;
+    if (!s || !is_type(s->dtype) || !is_id(s->id_type) || s->rows < 0 || s->vocab < 1 || s->channels < 1 || !(std::fabs(s->scale) <= 1e38f)) return FTP_EINVAL;
     if (s->x_stride < 0 || s->w_stride < 0 || s->dx_stride < 0 || s->dw_stride < 0) return FTP_EINVAL;
     return token_loss_fits(*s) ? FTP_OK : FTP_EUNSUPPORTED;
 }
