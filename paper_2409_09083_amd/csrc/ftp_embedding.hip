@@ -109,16 +109,17 @@ __device__ __forceinline__ void first_places(int (&n)[kSortWaves][kBins], int (&
     __syncthreads();
 }
 
+constexpr int kHeld = 4;                            // keys that a lane keeps from the count
+
 // A wavefront's keys [lo, hi) to their places, 64 after the other, each behind the lanes of its digit before it.
 template <class Get, class Put>
-__device__ __forceinline__ void place_keys(int* first, int lo, int hi, int shift, int bits, Get get, Put put)
+__device__ __forceinline__ void place_keys(int* first, int lo, int hi, int shift, int bits, const Pair (&held)[kHeld], Get get, Put put)
 {
     const int lane = threadIdx.x & 63, mask = (1 << bits) - 1;
     volatile int* at = first;
-    for (int i0 = lo; i0 < hi; i0 += 64) {
+    const auto round = [&](int i0, Pair p) __attribute__((always_inline)) {
         const bool there = i0 + lane < hi;
-        Pair p = {0, 0};
-        if (there) p = get(i0 + lane);
+        if (!there) p = Pair{0, 0};
         const int digit = (p.key >> shift) & mask;
         unsigned long long same = __ballot(there);
         for (int k = 0; k < bits; ++k) {
@@ -132,7 +133,10 @@ __device__ __forceinline__ void place_keys(int* first, int lo, int hi, int shift
             put(to, p);
         }
         __builtin_amdgcn_wave_barrier();
-    }
+    };
+#pragma unroll
+    for (int k = 0; k < kHeld; ++k) if (lo + 64 * k < hi) round(lo + 64 * k, held[k]);
+    for (int i0 = lo + 64 * kHeld; i0 < hi; i0 += 64) round(i0, i0 + lane < hi ? get(i0 + lane) : Pair{0, 0});
 }
 
 // One pass over a list of many workgroups: each key to its place, behind all keys of smaller digits, those of its digit in earlier workgroups, wavefronts and lanes.
@@ -153,10 +157,17 @@ __global__ __launch_bounds__(kSortThreads) void k_place(const SortArgs a)
     for (int i = tid; i < kSortWaves * kBins; i += kSortThreads) (&n[0][0])[i] = 0;
     __syncthreads();
     const int part = a.per / kSortWaves, lo = blockIdx.x * a.per + wave * part, hi = min(lo + part, a.rows);
-    for (int i = lo + lane; i < hi; i += 64) atomicAdd(&n[wave][(pair_of(a, i).key >> a.shift) & mask], 1);
+    Pair held[kHeld];
+#pragma unroll
+    for (int k = 0; k < kHeld; ++k) {
+        const int i = lo + 64 * k + lane;
+        held[k] = i < hi ? pair_of(a, i) : Pair{0, 0};
+        if (i < hi) atomicAdd(&n[wave][(held[k].key >> a.shift) & mask], 1);
+    }
+    for (int i = lo + 64 * kHeld + lane; i < hi; i += 64) atomicAdd(&n[wave][(pair_of(a, i).key >> a.shift) & mask], 1);
     __syncthreads();
     first_places(n, wsum, all, before);
-    place_keys(n[wave], lo, hi, a.shift, a.bits, [&](int i) { return pair_of(a, i); }, [&](int to, Pair p) { a.out[to] = p; });
+    place_keys(n[wave], lo, hi, a.shift, a.bits, held, [&](int i) { return pair_of(a, i); }, [&](int to, Pair p) { a.out[to] = p; });
 }
 
 // All passes over a short list, in one workgroup's LDS (4995 keys of 10 bits: 41 us a backward pass with two launches a pass, 24 so).
@@ -178,14 +189,21 @@ __global__ __launch_bounds__(kSortThreads) void k_sort(const SortArgs a)
         __syncthreads();
         for (int i = tid; i < kSortWaves * kBins; i += kSortThreads) (&n[0][0])[i] = 0;
         __syncthreads();
-        for (int i = lo + lane; i < hi; i += 64) atomicAdd(&n[wave][(list[now][i].key >> shift) & mask], 1);
+        Pair held[kHeld];
+#pragma unroll
+        for (int k = 0; k < kHeld; ++k) {
+            const int i = lo + 64 * k + lane;
+            held[k] = i < hi ? list[now][i] : Pair{0, 0};
+            if (i < hi) atomicAdd(&n[wave][(held[k].key >> shift) & mask], 1);
+        }
+        for (int i = lo + 64 * kHeld + lane; i < hi; i += 64) atomicAdd(&n[wave][(list[now][i].key >> shift) & mask], 1);
         __syncthreads();
         int all = 0;
         if (tid < kBins)
 #pragma unroll
             for (int w = 0; w < kSortWaves; ++w) all += n[w][tid];
         first_places(n, wsum, all, 0);
-        place_keys(n[wave], lo, hi, shift, a.digit, [&](int i) { return list[now][i]; }, [&](int to, Pair p) { list[now ^ 1][to] = p; });
+        place_keys(n[wave], lo, hi, shift, a.digit, held, [&](int i) { return list[now][i]; }, [&](int to, Pair p) { list[now ^ 1][to] = p; });
     }
     __syncthreads();
     for (int i = tid; i < a.rows; i += kSortThreads) a.out[i] = list[now][i];

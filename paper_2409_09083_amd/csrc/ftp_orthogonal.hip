@@ -86,57 +86,53 @@ struct StepArgs {
     int blocks, whole, shares;                      // blocks of all matrices; the first `whole` of them by a workgroup each, the others by `shares`
     int groups, grouped;                            // those others: groups (matrices) x blocks
     int symmetric;                                  // blocks above the diagonal are mirrored ones
-    // what becomes of the sums v: diagonal I + f0 old + f1 v, old being planes too (f0 = 0: none)
+    // what becomes of the sums v: themselves, or (old not null) diagonal I + f0 old + f1 v, old being planes too
     float f0, f1;
     float diagonal, spare;                          // (three floats in a row had the compiler keep a copy of them in LDS: 4 x 512 x 2048 468 -> 600 us)
     const bf16_t* old; bf16_t* to;
     long long plane, next; int arows, brows;        // (old and to: a Matrix of brows rows and arows columns each) [matrix: next]
-    void* out; int orows, ocols;                    // instead of planes: the results, rows along b
+    void* out; int orows, ocols, vec;               // instead of planes: the results, rows along b
     float* part;                                    // [block that is cut][share][index of b][index of a]
 };
 
-template <int P>
-__device__ __forceinline__ f32x4 planes_sum(const bf16_t* p, long long plane)
-{
-    f32x4 v = {0, 0, 0, 0};
-#pragma unroll
-    for (int k = P - 1; k >= 0; --k) {
-        const uint2 w = *(const uint2*)(p + k * plane);
-        v += f32x4{__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xFFFF0000u), __uint_as_float(w.y << 16), __uint_as_float(w.y & 0xFFFF0000u)};
-    }
-    return v;
-}
-
-// Four neighbouring results: (matrix, j: index along b, i: first index along a)
+// Eight neighbouring results: (matrix, j: index along b, i: first index along a)
 template <typename T, int P>
-__device__ __forceinline__ void finish(const StepArgs& a, int matrix, int i, int j, f32x4 v, bool mirror)
+__device__ __forceinline__ void finish(const StepArgs& a, int matrix, int i, int j, float (&v)[8], bool mirror)
 {
     const long long block = a.brows * 32ll, at = matrix * a.next + (i >> 5) * block + j * 32 + (i & 31);
-    v *= a.f1;
-    if (a.f0 != 0) v += a.f0 * planes_sum<P>(a.old + at, a.plane);
-    const int on = j - i;                           // which of the four lies on the diagonal
-    v += f32x4{on == 0 ? 1.0f : 0.0f, on == 1 ? 1.0f : 0.0f, on == 2 ? 1.0f : 0.0f, on == 3 ? 1.0f : 0.0f} * a.diagonal;
-    if (a.out) {
-        T* p = (T*)a.out + ((long long)matrix * a.orows + j) * a.ocols + i;
-        if (j < a.orows)
+    if (a.old) {
+        uint4 w[P];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) if (i + e < a.ocols) st(p + e, v[e]);
+        for (int p = 0; p < P; ++p) w[p] = *(const uint4*)(a.old + at + p * a.plane);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            float old = 0;
+#pragma unroll
+            for (int p = P - 1; p >= 0; --p) {
+                const uint32_t x = e < 2 ? w[p].x : e < 4 ? w[p].y : e < 6 ? w[p].z : w[p].w;
+                old += __uint_as_float(e & 1 ? x & 0xFFFF0000u : x << 16);
+            }
+            v[e] = fmaf(a.f1, v[e], a.f0 * old) + (i + e == j ? a.diagonal : 0.0f);
+        }
+    }
+    if (a.out) {
+        if (j < a.orows) store8((T*)a.out + ((long long)matrix * a.orows + j) * a.ocols + i, a.ocols - i, a.vec, v);
         return;
     }
-    uint32_t x[P], y[P];
-    planes_of<P>(v[0], v[1], x);
-    planes_of<P>(v[2], v[3], y);
+    bf16_t* to = a.to + at;
+    if (!mirror) {
+        store_planes<P>(to, a.plane, v);
+        return;
+    }
+    uint32_t x[4][P];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) planes_of<P>(v[2 * e], v[2 * e + 1], x[e]);
 #pragma unroll
     for (int p = 0; p < P; ++p) {
-        bf16_t* to = a.to + p * a.plane;
-        *(uint2*)(to + at) = uint2{x[p], y[p]};
-        if (mirror) {
-            bf16_t* m = to + matrix * a.next + (j >> 5) * block + i * 32 + (j & 31);
-            m[0] = (bf16_t)x[p];
-            m[32] = (bf16_t)(x[p] >> 16);
-            m[64] = (bf16_t)y[p];
-            m[96] = (bf16_t)(y[p] >> 16);
-        }
+        *(uint4*)(to + p * a.plane) = uint4{x[0][p], x[1][p], x[2][p], x[3][p]};
+        bf16_t* m = a.to + p * a.plane + matrix * a.next + (j >> 5) * block + i * 32 + (j & 31);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) m[32 * e] = (bf16_t)(x[e >> 1][p] >> (16 * (e & 1)));
     }
 }
 
@@ -185,26 +181,31 @@ __global__ __launch_bounds__(L::kThreads, 2) void k_step(const StepArgs a)
     L::run(acc, x, y, a0, b0, (int)((long long)stages * share / shares), (int)((long long)stages * (share + 1) / shares), a.terms, s0, s1, s2, s3);
     if (shares > 1) {
         float* p = a.part + ((long long)(t - a.whole) * shares + share) * (L::BA * L::BB);
-        L::each(acc, [&](int i, int j, f32x4 v) __attribute__((always_inline)) { *(f32x4*)(p + j * L::BA + i) = v; });
+        L::quads(acc, [&](int i, int j, f32x4 v) __attribute__((always_inline)) { *(f32x4*)(p + j * L::BA + i) = v; });
     } else
-        L::each(acc, [&](int i, int j, f32x4 v) __attribute__((always_inline)) {
+        L::each(acc, [&](int i, int j, float (&v)[8]) __attribute__((always_inline)) {
             if (a0 + i < a.arows && b0 + j < a.brows) finish<T, P>(a, matrix, a0 + i, b0 + j, v, a.symmetric && ia != ib);
         });
 }
 
-// The shares' sums, in their order: 1024 results a workgroup.
+// The shares' sums, in their order: 2048 results a workgroup.
 template <typename T, int P, int B>
 __global__ __launch_bounds__(256) void k_step_sum(const StepArgs a)
 {
-    constexpr int kPer = B * B / 1024;
-    const int cut = blockIdx.x / kPer, u = (blockIdx.x - cut * kPer) * 1024 + threadIdx.x * 4, j = u / B, i = u % B;
+    constexpr int kPer = B * B / 2048;
+    const int cut = blockIdx.x / kPer, u = (blockIdx.x - cut * kPer) * 2048 + threadIdx.x * 8, j = u / B, i = u % B;
     int ia, ib, matrix;
     step_block(a, a.whole + cut, ia, ib, matrix);
     if (ia * B + i >= a.arows || ib * B + j >= a.brows) return;
     const float* p = a.part + (long long)cut * a.shares * (B * B) + u;
-    f32x4 v = {0, 0, 0, 0};
+    f32x4 sum[2] = {};
 #pragma unroll 8
-    for (int s = 0; s < a.shares; ++s) v += *(const f32x4*)(p + (long long)s * (B * B));
+    for (int s = 0; s < a.shares; ++s)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) sum[k] += *(const f32x4*)(p + (long long)s * (B * B) + 4 * k);
+    float v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = sum[e >> 2][e & 3];
     finish<T, P>(a, matrix, ia * B + i, ib * B + j, v, a.symmetric && ia != ib);
 }
 
@@ -283,7 +284,7 @@ void launch(StepArgs& a, hipStream_t st)
     a.groups = a.whole ? 1 : a.count;
     a.grouped = cut / a.groups;
     k_step<L, T, P><<<(unsigned)ceil_div(a.whole, 8) * 8 + (cut ? xcd_grid(a.groups * a.shares, a.grouped) : 0), L::kThreads, 0, st>>>(a);
-    if (cut) k_step_sum<T, P, B><<<(unsigned)(cut * (B * B / 1024)), 256, 0, st>>>(a);
+    if (cut) k_step_sum<T, P, B><<<(unsigned)(cut * (B * B / 2048)), 256, 0, st>>>(a);
 }
 template <bool XA, bool XB, typename T, int P>
 void product(StepArgs& a, const Cut& c, hipStream_t st)
@@ -319,16 +320,16 @@ void run(const ftp_orthogonal_shape& s, const T* x, T* out, char* ws, hipStream_
         k.terms = terms_of(P); k.count = s.count; k.part = b.part;
         k.arows = k.brows = p.mp; k.next = qnext; k.plane = qplane;
         // S
-        k.a = k.b = X; k.anext = k.bnext = xnext; k.stages = std::max(p.Rp, p.Cp) / 32; k.symmetric = 1; k.f1 = 1; k.to = b.s;
+        k.a = k.b = X; k.anext = k.bnext = xnext; k.stages = std::max(p.Rp, p.Cp) / 32; k.symmetric = 1; k.to = b.s;
         if (p.tall) product<true, true, T, P>(k, p.s, st);
         else product<false, false, T, P>(k, p.s, st);
         // a I + b S + c S^2
         k.a = k.b = S; k.anext = k.bnext = qnext; k.stages = p.mp / 32; k.symmetric = 1; k.diagonal = s.a; k.f0 = s.b; k.f1 = s.c; k.old = b.s; k.to = b.q;
         product<false, false, T, P>(k, p.q, st);
         // that times X
-        k.symmetric = 0; k.diagonal = k.f0 = 0; k.f1 = 1; k.to = b.x[~step & 1];
+        k.symmetric = 0; k.old = nullptr; k.to = b.x[~step & 1];
         k.arows = p.Cp; k.brows = p.Rp; k.next = xnext; k.plane = xplane;
-        if (step + 1 == s.steps) { k.out = out; k.orows = s.rows; k.ocols = s.cols; }
+        if (step + 1 == s.steps) { k.out = out; k.orows = s.rows; k.ocols = s.cols; k.vec = aligned(out, 16) && s.cols % 8 == 0; }
         if (p.tall) {
             k.a = Q; k.b = X; k.anext = qnext; k.bnext = xnext;
             product<false, false, T, P>(k, p.x, st);

@@ -14,7 +14,7 @@ namespace ftp {
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr int kCountRows = 4096;                    // most rows whose labels every workgroup counts by itself (a launch less)
+constexpr int kCountRows = 4096;                     // most rows whose labels every workgroup counts by itself (a launch less)
 constexpr int kChunk = 64;                          // rows whose labels one wavefront looks at
 constexpr int kPackRows = 4096;                     // from here on W is laid out for the products
 // Up to so many rows G is two bfloats where the tensors are one: its rounding, which the sums over many rows even out, would be as large as the results' own, and costs nothing to avoid.
@@ -226,23 +226,13 @@ __global__ __launch_bounds__(L::kThreads, 2) void k_logits(const LogitArgs a)
                 for (int i = 0; i < L::IA; ++i)
 #pragma unroll
                     for (int r = 0; r < 16; ++r) acc[i][j][r] *= weight;
-            if (row >= ((rows + 63) & ~63)) continue;
-            bf16_t* to = a.g + ((a0 + wa) >> 5) * a.gblock + (long long)row * 32 + 8 * h;
-#pragma unroll
-            for (int i = 0; i < L::IA; ++i)
-#pragma unroll
-                for (int r = 0; r < 16; r += 8) {
-                    // registers r .. r + 3 are ids 2 r + 4 h .. of the block, the next four 2 r + 8 + 4 h ..: halves exchanged, 8 neighbours a lane
-                    uint32_t x[2][2][PLANES];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) planes_of<PLANES>(acc[i][j][r + 2 * e], acc[i][j][r + 2 * e + 1], x[e >> 1][e & 1]);
-#pragma unroll
-                    for (int p = 0; p < PLANES; ++p) {
-                        const auto u = __builtin_amdgcn_permlane32_swap(x[0][0][p], x[1][0][p], false, false), v = __builtin_amdgcn_permlane32_swap(x[0][1][p], x[1][1][p], false, false);
-                        *(uint4*)(to + p * a.gplane + i * a.gblock + 2 * r) = uint4{u[0], v[0], u[1], v[1]};
-                    }
-                }
         }
+    }
+    if constexpr (!STATS) {
+        const int all = (rows + 63) & ~63;
+        L::each(acc, [&](int i, int j, const float (&v)[8]) __attribute__((always_inline)) {
+            if (b0 + j < all) store_planes<PLANES>(a.g + ((a0 + i) >> 5) * a.gblock + (b0 + j) * 32ll + (i & 31), a.gplane, v);
+        });
     }
     if constexpr (STATS) {
         __syncthreads();
@@ -323,7 +313,7 @@ struct GradArgs {
     Terms terms;
     int stages, shares, ablocks, bblocks, add;         // dx: shares and blocks for all rows; fewer rows have more shares (dx_shares())
     float* part; long long pstride, pshare;         // [share][index of b][pstride]
-    void* out; long long ostride; int C; float scale; int mean;     // dw alone, without shares
+    void* out; long long ostride; int C, vec; float scale; int mean;        // dw alone, without shares
 };
 
 __device__ __forceinline__ float gradient_scale(float scale, int mean, const int* count)
@@ -347,7 +337,7 @@ __global__ __launch_bounds__(L::kThreads, 2) void k_loss_dx(const GradArgs a)
     f32x16 acc[L::IA][L::IB] = {};
     const int lo = (int)((long long)a.stages * share / shares), hi = (int)((long long)a.stages * (share + 1) / shares);
     L::run(acc, a.a, a.b, a0, b0, lo, hi, a.terms, s0, s1, s2, s3);
-    L::each(acc, [&](int i, int j, f32x4 v) __attribute__((always_inline)) {
+    L::quads(acc, [&](int i, int j, f32x4 v) __attribute__((always_inline)) {
         if (a0 + i >= a.pstride || b0 + j >= rows) return;
         f32x4* p = (f32x4*)(a.part + ((long long)share * bblocks * L::BB + b0 + j) * a.pstride + a0 + i);
         *p = a.add ? *p + v : v;
@@ -367,25 +357,28 @@ __global__ __launch_bounds__(L::kThreads, 2) void k_loss_dw(const GradArgs a)
     const int lo = (int)((long long)stages * share / a.shares), hi = (int)((long long)stages * (share + 1) / a.shares);
     L::run(acc, a.a, a.b, a0, b0, lo, hi, a.terms, s0, s1, s2, s3);
     const float f = gradient_scale(a.scale, a.mean, a.count);
-    L::each(acc, [&](int i, int j, f32x4 v) __attribute__((always_inline)) {
+    if (a.shares > 1) {
+        L::quads(acc, [&](int i, int j, f32x4 v) __attribute__((always_inline)) {
+            if (a0 + i < a.pstride && b0 + j < a.add) *(f32x4*)(a.part + share * a.pshare + (long long)(b0 + j) * a.pstride + a0 + i) = v;         // (add: here the piece's ids)
+        });
+        return;
+    }
+    L::each(acc, [&](int i, int j, const float (&v)[8]) __attribute__((always_inline)) {
         const long long id = b0 + j;
-        if (a0 + i >= a.pstride || id >= a.add) return;             // (here: the piece's ids)
-        if (a.shares > 1) {
-            *(f32x4*)(a.part + share * a.pshare + id * a.pstride + a0 + i) = v;
-            return;
-        }
-        T* p = (T*)a.out + id * a.ostride + a0 + i;
+        if (a0 + i >= a.C || id >= a.add) return;
+        float w[8];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) if (a0 + i + e < a.C) st(p + e, v[e] * f);
+        for (int e = 0; e < 8; ++e) w[e] = v[e] * f;
+        store8((T*)a.out + id * a.ostride + a0 + i, a.C - a0 - i, a.vec, w);
     });
 }
 
 // Sums of the shares, in their order, as gradients: row r of out is row place[r] of them (place null: r), or zeros.
 template <typename T>
-__global__ __launch_bounds__(256) void k_loss_sum(const float* part, long long pstride, long long pshare, int shares, int block, const int* place, long long rows, void* out, long long ostride, int C, float scale,
-                                                  int mean, const int* count)
+__global__ __launch_bounds__(256) void k_loss_sum(const float* part, long long pstride, long long pshare, int shares, int block, const int* place, long long rows, void* out, long long ostride, int C, int vec,
+                                                  float scale, int mean, const int* count)
 {
-    const int per = (C + 3) >> 2;
+    const int per = (C + 7) >> 3;
     const float f = gradient_scale(scale, mean, count);
     if (block) {                                    // of dx: shares for all rows
         pshare = (long long)dx_blocks(*count, block) * block * pstride;
@@ -393,17 +386,20 @@ __global__ __launch_bounds__(256) void k_loss_sum(const float* part, long long p
     }
     for (long long u = (long long)blockIdx.x * 256 + threadIdx.x; u < rows * per; u += (long long)gridDim.x * 256) {
         const long long r = u / per, from = place ? place[r] : r;
-        const int c = (int)(u - r * per) * 4;
-        f32x4 v = {0, 0, 0, 0};
+        const int c = (int)(u - r * per) * 8;
+        f32x4 v[2] = {};
         if (from >= 0) {
             const float* p = part + from * pstride + c;
 #pragma unroll 4
-            for (int s = 0; s < shares; ++s) v += *(const f32x4*)(p + s * pshare);
-            v *= f;
+            for (int s = 0; s < shares; ++s) {
+                v[0] += *(const f32x4*)(p + s * pshare);
+                v[1] += *(const f32x4*)(p + s * pshare + 4);
+            }
         }
-        T* to = (T*)out + r * ostride + c;
+        float w[8];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) if (c + e < C) st(to + e, v[e]);
+        for (int e = 0; e < 8; ++e) w[e] = v[e >> 2][e & 3] * f;
+        store8((T*)out + r * ostride + c, C - c, vec, w);
     }
 }
 
@@ -548,6 +544,7 @@ void backward(const ftp_token_loss_shape& s, const void* x, const void* w, const
 {
     const Plan p = plan_of(s, true);
     const Buffers b = buffers_of(s, p, true, ws);
+    const auto vectors = [](const void* p, long long stride) { return aligned(p, 16) && stride % 8 == 0; };        // rows whose 8 neighbours can be stored at once
     const Matrix all = prepare<P>(s, p, b, x, w, labels, true, st), xc = blocked(b.xc, p.Np, p.Cp, p.Np * p.Cp), g = blocked(b.g, p.Np, (int)p.piece, p.Np * p.piece);
     for (long long v0 = 0; v0 < s.vocab; v0 += p.piece) {
         const int n = (int)std::min<long long>(p.piece, s.vocab - v0);
@@ -575,15 +572,15 @@ void backward(const ftp_token_loss_shape& s, const void* x, const void* w, const
             k.ablocks = (int)ceil_div(p.Cp, block); k.bblocks = (int)ceil_div(n, block);
             k.part = b.dw; k.pshare = p.piece * p.Cp;
             T* out = (T*)dw + v0 * s.dw_stride;
-            k.out = out; k.ostride = s.dw_stride;
+            k.out = out; k.ostride = s.dw_stride; k.vec = vectors(dw, s.dw_stride);
             if (p.dw.block == 256) dw_pass<Big<true, true>, T>(k, st);
             else dw_pass<Mid<true, true>, T>(k, st);
             if (k.shares > 1)
-                k_loss_sum<T><<<pass_grid(n * ceil_div(s.channels, 4)), 256, 0, st>>>(b.dw, p.Cp, k.pshare, k.shares, 0, nullptr, n, out, s.dw_stride, s.channels, s.scale, !dloss, b.count);
+                k_loss_sum<T><<<pass_grid(n * ceil_div(s.channels, 8)), 256, 0, st>>>(b.dw, p.Cp, k.pshare, k.shares, 0, nullptr, n, out, s.dw_stride, s.channels, k.vec, s.scale, !dloss, b.count);
         }
     }
     if (dx && s.rows)
-        k_loss_sum<T><<<pass_grid(s.rows * ceil_div(s.channels, 4)), 256, 0, st>>>(b.dx, p.Cp, 0, (int)ceil_div(s.rows, p.dx.block) * p.dx.shares, p.dx.block, b.place, s.rows, dx, s.dx_stride, s.channels, s.scale, !dloss, b.count);
+        k_loss_sum<T><<<pass_grid(s.rows * ceil_div(s.channels, 8)), 256, 0, st>>>(b.dx, p.Cp, 0, (int)ceil_div(s.rows, p.dx.block) * p.dx.shares, p.dx.block, b.place, s.rows, dx, s.dx_stride, s.channels, vectors(dx, s.dx_stride), s.scale, !dloss, b.count);
 }
 
 }  // namespace

@@ -121,6 +121,20 @@ def test_singular_values_and_vectors(rows, cols, dtype):
     assert float((p - p.t()).norm()) <= (2 * LAST[dtype] + 1e-5) * float(p.norm()) * 2
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("abc", [(1.5, -0.5, 0.0), (0.0, 1.0, 0.0), (2.0, 0.0, -1.0), (1.0, 0.0, 0.0), (0.0, 0.0, 1.0)])
+def test_other_coefficients(abc, dtype):
+    """Also those that are 0; x's largest singular value is below 1, so that no bound is larger than (1 + |a| + |b| + |c|) times what one step's operands are held to."""
+    from paper_2409_09083_amd import orthogonal
+    for rows, cols in ((30, 50), (90, 200), (200, 90)):
+        x = _matrix(1, rows, cols, dtype, seed=9)[0]
+        got = orthogonal.Orthogonal(rows, cols, dtype, steps=1, coefficients=abc).forward(x).double()
+        want = _steps(x, 1, abc=abc)
+        n = max(rows, cols)
+        # norms: |X| = 1, |S| <= 1, |S^2| <= 1; each is off by (n + 8) u + 4 h of the absolute values' product, of norm at most |X|^2 = 1, at most 8 such errors behind each other
+        assert float((got - want).norm()) <= 8 * (sum(map(abs, abc)) + 1) * ((n + 8) * U + 4 * HELD[dtype]) + LAST[dtype] * float(want.norm())
+
+
 def test_special_matrices():
     from paper_2409_09083_amd import orthogonal
     x = _matrix(4, 40, 70, "f32", seed=3)
