@@ -346,7 +346,7 @@ typedef enum { FTP_I32 = 0, FTP_I64 = 1 } ftp_id_type;
 
 /* out[r] = scale * table[ids[r]], rounded once; a row without an id is zero.  rows may be 0.
  * Backward: dtable[v] = scale * the sum of dy[r] over the rows with ids[r] = v, in 32 bits and in the order of the rows (runs of
- * 32 neighbours in the list sorted by id first); rows of dtable whose id does not occur are set to zero. */
+ * 8 or 32 neighbours in the list sorted by id first); rows of dtable whose id does not occur are set to zero. */
 typedef struct {
     int64_t rows;                  /* at most 2^26 */
     int32_t vocab, channels;       /* >= 1; at most 2^26 and 2^20 */

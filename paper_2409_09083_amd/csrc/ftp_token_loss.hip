@@ -230,9 +230,22 @@ __global__ __launch_bounds__(L::kThreads, 2) void k_logits(const LogitArgs a)
     }
     if constexpr (!STATS) {
         const int all = (rows + 63) & ~63;
-        L::each(acc, [&](int i, int j, const float (&v)[8]) __attribute__((always_inline)) {
-            if (b0 + j < all) store_planes<PLANES>(a.g + ((a0 + i) >> 5) * a.gblock + (b0 + j) * 32ll + (i & 31), a.gplane, v);
-        });
+        const auto to = [&](int i, int j) __attribute__((always_inline)) { return a.g + ((a0 + i) >> 5) * a.gblock + (b0 + j) * 32ll + (i & 31); };
+        if constexpr (PLANES == 1) {
+            // (the halves exchange what is rounded already: half the registers)
+#pragma unroll
+            for (int j = 0; j < L::IB; ++j)
+#pragma unroll
+                for (int i = 0; i < L::IA; ++i)
+#pragma unroll
+                    for (int r = 0; r < 16; r += 8) {
+                        const auto pair = [&](int k) __attribute__((always_inline)) { return pack_bf16(acc[i][j][r + k], acc[i][j][r + k + 1]); };
+                        const auto x = __builtin_amdgcn_permlane32_swap(pair(0), pair(4), false, false), y = __builtin_amdgcn_permlane32_swap(pair(2), pair(6), false, false);
+                        const int at = wb + 32 * j + (l & 31);
+                        if (b0 + at < all) *(uint4*)to(wa + 32 * i + 2 * r + 8 * h, at) = uint4{x[0], y[0], x[1], y[1]};
+                    }
+        } else
+            L::each(acc, [&](int i, int j, const float (&v)[8]) __attribute__((always_inline)) { if (b0 + j < all) store_planes<PLANES>(to(i, j), a.gplane, v); });
     }
     if constexpr (STATS) {
         __syncthreads();
@@ -311,7 +324,7 @@ struct GradArgs {
     Matrix a, b;
     const int* count;
     Terms terms;
-    int stages, shares, ablocks, bblocks, add;         // dx: shares and blocks for all rows; fewer rows have more shares (dx_shares())
+    int stages, shares, most, ablocks, bblocks, add;         // dx: shares and blocks for all rows; fewer rows have more shares (dx_shares())
     float* part; long long pstride, pshare;         // [share][index of b][pstride]
     void* out; long long ostride; int C, vec; float scale; int mean;        // dw alone, without shares
 };
@@ -321,9 +334,10 @@ __device__ __forceinline__ float gradient_scale(float scale, int mean, const int
     return !mean ? scale : *count ? scale / (float)*count : 0.0f;
 }
 
-// Shares of the contraction where `rows` of the rows that the launch is made for have labels: as many blocks as the launch has workgroups for.  Share s of row r is row s * dx_rows() + r of the scratch.
+// Shares of the contraction where `rows` of the rows that the launch is made for have labels: as many as the launch has workgroups (all) for, at most `most`.  Share s of row r is row
+// s * dx_blocks() * block + r of the scratch.
 __device__ __forceinline__ int dx_blocks(int rows, int block) { return max((rows + block - 1) / block, 1); }
-__device__ __forceinline__ int dx_shares(int rows, int block, int all) { return all / dx_blocks(rows, block); }
+__device__ __forceinline__ int dx_shares(int rows, int block, int all, int most) { return min(all / dx_blocks(rows, block), most); }
 
 // dx's block: channels x rows over the piece's ids, added to what the pieces before left
 template <class L>
@@ -331,7 +345,7 @@ __global__ __launch_bounds__(L::kThreads, 2) void k_loss_dx(const GradArgs a)
 {
     __shared__ __align__(16) typename L::Stage s0, s1, s2, s3;
     int ia, ib;
-    const int rows = *a.count, bblocks = dx_blocks(rows, L::BB), shares = dx_shares(rows, L::BB, a.bblocks * a.shares);
+    const int rows = *a.count, bblocks = dx_blocks(rows, L::BB), shares = dx_shares(rows, L::BB, a.bblocks * a.shares, a.most);
     if (rows == 0 || !block_of((int)blockIdx.x, a.ablocks, bblocks * shares, ia, ib)) return;
     const int share = ib / bblocks, a0 = ia * L::BA, b0 = (ib - share * bblocks) * L::BB;
     f32x16 acc[L::IA][L::IB] = {};
@@ -375,14 +389,14 @@ __global__ __launch_bounds__(L::kThreads, 2) void k_loss_dw(const GradArgs a)
 
 // Sums of the shares, in their order, as gradients: row r of out is row place[r] of them (place null: r), or zeros.
 template <typename T>
-__global__ __launch_bounds__(256) void k_loss_sum(const float* part, long long pstride, long long pshare, int shares, int block, const int* place, long long rows, void* out, long long ostride, int C, int vec,
+__global__ __launch_bounds__(256) void k_loss_sum(const float* part, long long pstride, long long pshare, int shares, int block, int most, const int* place, long long rows, void* out, long long ostride, int C, int vec,
                                                   float scale, int mean, const int* count)
 {
     const int per = (C + 7) >> 3;
     const float f = gradient_scale(scale, mean, count);
     if (block) {                                    // of dx: shares for all rows
         pshare = (long long)dx_blocks(*count, block) * block * pstride;
-        shares = dx_shares(*count, block, shares);
+        shares = dx_shares(*count, block, shares, most);
     }
     for (long long u = (long long)blockIdx.x * 256 + threadIdx.x; u < rows * per; u += (long long)gridDim.x * 256) {
         const long long r = u / per, from = place ? place[r] : r;
@@ -412,7 +426,7 @@ struct Plan {
     int planes, gplanes, Cp, blocks, few;           // bfloats of an input and of an element of G
     long long Np, Vp, chunks, piece;                // rows and ids up to whole blocks of 64; ids of a piece, whole blocks of 256
     Split logits, dx, dw;
-    int joins;
+    int joins, most;
 };
 Plan plan_of(const ftp_token_loss_shape& s, bool back)
 {
@@ -439,6 +453,7 @@ Plan plan_of(const ftp_token_loss_shape& s, bool back)
     p.logits = split_of(p.piece, s.rows, p.Cp / 32 * terms, 128, 1);
     const long long gterms = p.planes == 1 ? p.gplanes : 6;
     p.dx = split_of(s.channels, s.rows, p.piece / 32 * gterms, 128, 16);
+    p.most = (int)std::max<long long>(p.dx.shares, p.piece / 32 * gterms / 24);
     p.dw = split_of(s.channels, p.piece, p.Np / 32 * gterms, 128, 16);
     return p;
 }
@@ -560,7 +575,7 @@ void backward(const ftp_token_loss_shape& s, const void* x, const void* w, const
         k.count = b.count; k.terms = p.gplanes == P ? terms_of(P) : terms_one_two(); k.C = s.channels; k.scale = s.scale; k.mean = !dloss; k.pstride = p.Cp;
         if (dx && s.rows) {
             const int block = p.dx.block;
-            k.a = wp; k.b = g; k.stages = (int)ceil_div(n, 32); k.shares = p.dx.shares; k.add = v0 > 0;
+            k.a = wp; k.b = g; k.stages = (int)ceil_div(n, 32); k.shares = p.dx.shares; k.most = p.most; k.add = v0 > 0;
             k.ablocks = (int)ceil_div(p.Cp, block); k.bblocks = (int)ceil_div(s.rows, block);
             k.part = b.dx;
             if (p.dx.block == 256) dx_pass<Big<true, false>>(k, st);
@@ -576,11 +591,11 @@ void backward(const ftp_token_loss_shape& s, const void* x, const void* w, const
             if (p.dw.block == 256) dw_pass<Big<true, true>, T>(k, st);
             else dw_pass<Mid<true, true>, T>(k, st);
             if (k.shares > 1)
-                k_loss_sum<T><<<pass_grid(n * ceil_div(s.channels, 8)), 256, 0, st>>>(b.dw, p.Cp, k.pshare, k.shares, 0, nullptr, n, out, s.dw_stride, s.channels, k.vec, s.scale, !dloss, b.count);
+                k_loss_sum<T><<<pass_grid(n * ceil_div(s.channels, 8)), 256, 0, st>>>(b.dw, p.Cp, k.pshare, k.shares, 0, 0, nullptr, n, out, s.dw_stride, s.channels, k.vec, s.scale, !dloss, b.count);
         }
     }
     if (dx && s.rows)
-        k_loss_sum<T><<<pass_grid(s.rows * ceil_div(s.channels, 8)), 256, 0, st>>>(b.dx, p.Cp, 0, (int)ceil_div(s.rows, p.dx.block) * p.dx.shares, p.dx.block, b.place, s.rows, dx, s.dx_stride, s.channels, vectors(dx, s.dx_stride), s.scale, !dloss, b.count);
+        k_loss_sum<T><<<pass_grid(s.rows * ceil_div(s.channels, 8)), 256, 0, st>>>(b.dx, p.Cp, 0, (int)ceil_div(s.rows, p.dx.block) * p.dx.shares, p.dx.block, p.most, b.place, s.rows, dx, s.dx_stride, s.channels, vectors(dx, s.dx_stride), s.scale, !dloss, b.count);
 }
 
 }  // namespace
