@@ -92,7 +92,7 @@ struct StepArgs {
     const bf16_t* old; bf16_t* to;
     long long plane, next; int arows, brows;        // (old and to: a Matrix of brows rows and arows columns each) [matrix: next]
     void* out; int orows, ocols, vec;               // instead of planes: the results, rows along b
-    float* part;                                    // [block that is cut][share][index of b][index of a]
+    float* part;                                    // sums: [block that is cut][share]
 };
 
 // Eight neighbouring results: (matrix, j: index along b, i: first index along a)
@@ -157,18 +157,20 @@ template <class L, typename T, int P>
 __global__ __launch_bounds__(L::kThreads, 2) void k_step(const StepArgs a)
 {
     __shared__ __align__(16) typename L::Stage s0, s1, s2, s3;
-    // XCD x takes the x-th eighth of the whole blocks; behind them come the shares, those of the same part of a matrix on one XCD
-    int t, share = 0, shares = 1;
-    const int per = (a.whole + 7) >> 3, index = (int)blockIdx.x;
+    // XCD x takes the x-th eighth of the whole blocks; behind them come the shares, in eighths too, those of the same part of a matrix one behind the other
+    int t, share = 0, shares = 1, index = (int)blockIdx.x;
+    const int per = (a.whole + 7) >> 3;
     if (index < 8 * per) {
         t = (index & 7) * per + (index >> 3);
         if (t >= a.whole) return;
     } else {
-        int g;
         shares = a.shares;
-        if (!xcd_order(index - 8 * per, a.groups * shares, a.grouped, g, t)) return;
+        index -= 8 * per;
+        const int all = a.groups * shares * a.grouped, each = (all + 7) >> 3, at = (index & 7) * each + (index >> 3);
+        if ((index >> 3) >= each || at >= all) return;
+        const int g = at / a.grouped;
         share = g % shares;
-        t += a.whole + g / shares * a.grouped;
+        t = a.whole + g / shares * a.grouped + at - g * a.grouped;
     }
     int ia, ib, matrix;
     step_block(a, t, ia, ib, matrix);
@@ -179,34 +181,25 @@ __global__ __launch_bounds__(L::kThreads, 2) void k_step(const StepArgs a)
     f32x16 acc[L::IA][L::IB] = {};
     const int stages = a.stages / (L::KS / 32);
     L::run(acc, x, y, a0, b0, (int)((long long)stages * share / shares), (int)((long long)stages * (share + 1) / shares), a.terms, s0, s1, s2, s3);
-    if (shares > 1) {
-        float* p = a.part + ((long long)(t - a.whole) * shares + share) * (L::BA * L::BB);
-        L::quads(acc, [&](int i, int j, f32x4 v) __attribute__((always_inline)) { *(f32x4*)(p + j * L::BA + i) = v; });
-    } else
+    if (shares > 1) L::put(acc, a.part + ((long long)(t - a.whole) * shares + share) * L::kSums, false);
+    else
         L::each(acc, [&](int i, int j, float (&v)[8]) __attribute__((always_inline)) {
             if (a0 + i < a.arows && b0 + j < a.brows) finish<T, P>(a, matrix, a0 + i, b0 + j, v, a.symmetric && ia != ib);
         });
 }
 
-// The shares' sums, in their order: 2048 results a workgroup.
-template <typename T, int P, int B>
+// The shares' sums, in their order.
+template <class L, typename T, int P>
 __global__ __launch_bounds__(256) void k_step_sum(const StepArgs a)
 {
-    constexpr int kPer = B * B / 2048;
-    const int cut = blockIdx.x / kPer, u = (blockIdx.x - cut * kPer) * 2048 + threadIdx.x * 8, j = u / B, i = u % B;
+    const int cut = blockIdx.x / L::kParts;
     int ia, ib, matrix;
     step_block(a, a.whole + cut, ia, ib, matrix);
-    if (ia * B + i >= a.arows || ib * B + j >= a.brows) return;
-    const float* p = a.part + (long long)cut * a.shares * (B * B) + u;
-    f32x4 sum[2] = {};
-#pragma unroll 8
-    for (int s = 0; s < a.shares; ++s)
-#pragma unroll
-        for (int k = 0; k < 2; ++k) sum[k] += *(const f32x4*)(p + (long long)s * (B * B) + 4 * k);
-    float v[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = sum[e >> 2][e & 3];
-    finish<T, P>(a, matrix, ia * B + i, ib * B + j, v, a.symmetric && ia != ib);
+    L::take(a.part + (long long)cut * a.shares * L::kSums, L::kSums, a.shares, blockIdx.x - cut * L::kParts, [&](int i, int j, float (&v)[8]) __attribute__((always_inline)) {
+        i += ia * L::BA;
+        j += ib * L::BB;
+        if (i < a.arows && j < a.brows) finish<T, P>(a, matrix, i, j, v, a.symmetric && ia != ib);
+    });
 }
 
 // How a product's blocks go over the chip: their size, how many are whole, and the shares of the others.
@@ -283,8 +276,8 @@ void launch(StepArgs& a, hipStream_t st)
     const int cut = a.blocks - a.whole;
     a.groups = a.whole ? 1 : a.count;
     a.grouped = cut / a.groups;
-    k_step<L, T, P><<<(unsigned)ceil_div(a.whole, 8) * 8 + (cut ? xcd_grid(a.groups * a.shares, a.grouped) : 0), L::kThreads, 0, st>>>(a);
-    if (cut) k_step_sum<T, P, B><<<(unsigned)(cut * (B * B / 2048)), 256, 0, st>>>(a);
+    k_step<L, T, P><<<(unsigned)(ceil_div(a.whole, 8) * 8 + ceil_div((long long)cut * a.shares, 8) * 8), L::kThreads, 0, st>>>(a);
+    if (cut) k_step_sum<L, T, P><<<(unsigned)(cut * L::kParts), 256, 0, st>>>(a);
 }
 template <bool XA, bool XB, typename T, int P>
 void product(StepArgs& a, const Cut& c, hipStream_t st)

@@ -255,19 +255,46 @@ struct Product {
                     acc[i][j][r] = v;
                 }
     }
-    // f(a, b, v): index of the first of four neighbours along a, index along b, values; of this wavefront, from the block's corner
-    template <class F>
-    static __device__ __forceinline__ void quads(const f32x16 (&acc)[IA][IB], F f)
+    // A share's sums as they lie in the registers, 1 KB a store (as rows of results 32 bytes of each went at once, and 247 MB of them took as long as the products), added to what is there or not.
+    static constexpr int kUnits = IA * IB, kSums = BA * BB;
+    static __device__ __forceinline__ void put(const f32x16 (&acc)[IA][IB], float* to, bool add)
     {
-        const int l = threadIdx.x & 63, h = l >> 5, wa = wave_a(), wb = wave_b();
 #pragma unroll
-        for (int j = 0; j < IB; ++j)
+        for (int u = 0; u < kUnits; ++u)
 #pragma unroll
-            for (int i = 0; i < IA; ++i)
-#pragma unroll
-                for (int r = 0; r < 16; r += 4) f(wa + 32 * i + 2 * r + 4 * h, wb + 32 * j + (l & 31), f32x4{acc[i][j][r], acc[i][j][r + 1], acc[i][j][r + 2], acc[i][j][r + 3]});
+            for (int q = 0; q < 4; ++q) {
+                const f32x16& x = acc[u % IA][u / IA];
+                f32x4* p = (f32x4*)to + (u * 4 + q) * kThreads + threadIdx.x;
+                const f32x4 v = {x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]};
+                *p = add ? *p + v : v;
+            }
     }
-    // f(a, b, v): index of the first of eight neighbours along a, index along b, values.  (A lane's registers are four neighbours; the halves exchange every other four: 16 bytes of bfloats a store instead
+    // ... added up, `next` floats from one share to the next, by 256 threads: part `index` of kParts.  f as for each().
+    static constexpr int kParts = kUnits * (kThreads / 256);
+    template <class F>
+    static __device__ __forceinline__ void take(const float* from, long long next, int shares, int index, F f)
+    {
+        const int u = index / (kThreads / 256), tid = (index % (kThreads / 256)) * 256 + threadIdx.x, l = tid & 63, h = l >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+        const f32x4* p = (const f32x4*)from + u * 4 * kThreads + tid;
+        f32x4 s[4] = {};
+#pragma unroll 4
+        for (int k = 0; k < shares; ++k, p += next / 4)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) s[q] += p[q * kThreads];
+#pragma unroll
+        for (int q = 0; q < 4; q += 2) {
+            float v[8];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(s[q][e]), __float_as_uint(s[q + 1][e]), false, false);
+                v[e] = __uint_as_float(x[0]);
+                v[4 + e] = __uint_as_float(x[1]);
+            }
+            f((wave % WA) * (IA * 32) + 32 * (u % IA) + 8 * q + 8 * h, (wave / WA) * (IB * 32) + 32 * (u / IA) + (l & 31), v);
+        }
+    }
+
+    // f(a, b, v): index of the first of eight neighbours along a, index along b, values; of this wavefront, from the block's corner.  (A lane's registers are four neighbours; the halves exchange every other four: 16 bytes of bfloats a store instead
     // of 8 or less.  32768 x 1024 of them from 11552 rows: 712 -> 636 us.)
     template <class F>
     static __device__ __forceinline__ void each(const f32x16 (&acc)[IA][IB], F f)

@@ -324,9 +324,11 @@ struct GradArgs {
     Matrix a, b;
     const int* count;
     Terms terms;
-    int stages, shares, most, ablocks, bblocks, add;         // dx: shares and blocks for all rows; fewer rows have more shares (dx_shares())
-    float* part; long long pstride, pshare;         // [share][index of b][pstride]
-    void* out; long long ostride; int C, vec; float scale; int mean;        // dw alone, without shares
+    int stages, shares, most, ablocks, bblocks, add;           // dx: shares and blocks for all rows; fewer rows have more shares (dx_shares())
+    float* part;                                    // sums: [share][block along b][block along a]
+    void* out; long long ostride; int C, vec; float scale; int mean;
+    int ids;                                        // dw: of the piece
+    const int* place; const int* index; int rows, summing;     // dx
 };
 
 __device__ __forceinline__ float gradient_scale(float scale, int mean, const int* count)
@@ -334,8 +336,7 @@ __device__ __forceinline__ float gradient_scale(float scale, int mean, const int
     return !mean ? scale : *count ? scale / (float)*count : 0.0f;
 }
 
-// Shares of the contraction where `rows` of the rows that the launch is made for have labels: as many as the launch has workgroups (all) for, at most `most`.  Share s of row r is row
-// s * dx_blocks() * block + r of the scratch.
+// Shares of the contraction where `rows` of the rows that the launch is made for have labels: as many as the launch has workgroups (all) for, at most `most`.
 __device__ __forceinline__ int dx_blocks(int rows, int block) { return max((rows + block - 1) / block, 1); }
 __device__ __forceinline__ int dx_shares(int rows, int block, int all, int most) { return min(all / dx_blocks(rows, block), most); }
 
@@ -351,11 +352,7 @@ __global__ __launch_bounds__(L::kThreads, 2) void k_loss_dx(const GradArgs a)
     f32x16 acc[L::IA][L::IB] = {};
     const int lo = (int)((long long)a.stages * share / shares), hi = (int)((long long)a.stages * (share + 1) / shares);
     L::run(acc, a.a, a.b, a0, b0, lo, hi, a.terms, s0, s1, s2, s3);
-    L::quads(acc, [&](int i, int j, f32x4 v) __attribute__((always_inline)) {
-        if (a0 + i >= a.pstride || b0 + j >= rows) return;
-        f32x4* p = (f32x4*)(a.part + ((long long)share * bblocks * L::BB + b0 + j) * a.pstride + a0 + i);
-        *p = a.add ? *p + v : v;
-    });
+    L::put(acc, a.part + ((long long)ib * a.ablocks + ia) * L::kSums, a.add);
 }
 
 // dW's block: channels x ids over the labelled rows
@@ -372,14 +369,12 @@ __global__ __launch_bounds__(L::kThreads, 2) void k_loss_dw(const GradArgs a)
     L::run(acc, a.a, a.b, a0, b0, lo, hi, a.terms, s0, s1, s2, s3);
     const float f = gradient_scale(a.scale, a.mean, a.count);
     if (a.shares > 1) {
-        L::quads(acc, [&](int i, int j, f32x4 v) __attribute__((always_inline)) {
-            if (a0 + i < a.pstride && b0 + j < a.add) *(f32x4*)(a.part + share * a.pshare + (long long)(b0 + j) * a.pstride + a0 + i) = v;         // (add: here the piece's ids)
-        });
+        L::put(acc, a.part + ((long long)ib * a.ablocks + ia) * L::kSums, false);
         return;
     }
     L::each(acc, [&](int i, int j, const float (&v)[8]) __attribute__((always_inline)) {
         const long long id = b0 + j;
-        if (a0 + i >= a.C || id >= a.add) return;
+        if (a0 + i >= a.C || id >= a.ids) return;
         float w[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) w[e] = v[e] * f;
@@ -387,34 +382,44 @@ __global__ __launch_bounds__(L::kThreads, 2) void k_loss_dw(const GradArgs a)
     });
 }
 
-// Sums of the shares, in their order, as gradients: row r of out is row place[r] of them (place null: r), or zeros.
-template <typename T>
-__global__ __launch_bounds__(256) void k_loss_sum(const float* part, long long pstride, long long pshare, int shares, int block, int most, const int* place, long long rows, void* out, long long ostride, int C, int vec,
-                                                  float scale, int mean, const int* count)
+// dx from the shares' sums, each in its row's place; rows without a label are zeros (the workgroups from `summing` on).
+template <class L, typename T>
+__global__ __launch_bounds__(256) void k_loss_dx_sum(const GradArgs a)
 {
-    const int per = (C + 7) >> 3;
-    const float f = gradient_scale(scale, mean, count);
-    if (block) {                                    // of dx: shares for all rows
-        pshare = (long long)dx_blocks(*count, block) * block * pstride;
-        shares = dx_shares(*count, block, shares, most);
-    }
-    for (long long u = (long long)blockIdx.x * 256 + threadIdx.x; u < rows * per; u += (long long)gridDim.x * 256) {
-        const long long r = u / per, from = place ? place[r] : r;
-        const int c = (int)(u - r * per) * 8;
-        f32x4 v[2] = {};
-        if (from >= 0) {
-            const float* p = part + from * pstride + c;
-#pragma unroll 4
-            for (int s = 0; s < shares; ++s) {
-                v[0] += *(const f32x4*)(p + s * pshare);
-                v[1] += *(const f32x4*)(p + s * pshare + 4);
-            }
+    if ((int)blockIdx.x >= a.summing) {
+        const int per = (a.C + 7) >> 3;
+        const long long n = (long long)a.rows * per, step = (long long)(gridDim.x - a.summing) * 256;
+        const float zeros[8] = {};
+        for (long long u = (long long)(blockIdx.x - a.summing) * 256 + threadIdx.x; u < n; u += step) {
+            const long long r = u / per;
+            const int c = (int)(u - r * per) * 8;
+            if (a.place[r] < 0) store8((T*)a.out + r * a.ostride + c, a.C - c, a.vec, zeros);
         }
-        float w[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) w[e] = v[e >> 2][e & 3] * f;
-        store8((T*)out + r * ostride + c, C - c, vec, w);
+        return;
     }
+    const int rows = *a.count, bblocks = dx_blocks(rows, L::BB), shares = dx_shares(rows, L::BB, a.bblocks * a.shares, a.most);
+    const int t = blockIdx.x / L::kParts, ib = t / a.ablocks, ia = t - ib * a.ablocks, a0 = ia * L::BA, b0 = ib * L::BB;
+    if (b0 >= rows) return;
+    const float f = gradient_scale(a.scale, a.mean, a.count);
+    L::take(a.part + (long long)t * L::kSums, (long long)bblocks * a.ablocks * L::kSums, shares, blockIdx.x - t * L::kParts, [&](int i, int j, float (&v)[8]) __attribute__((always_inline)) {
+        if (b0 + j >= rows || a0 + i >= a.C) return;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] *= f;
+        store8((T*)a.out + a.index[b0 + j] * a.ostride + a0 + i, a.C - a0 - i, a.vec, v);
+    });
+}
+
+template <class L, typename T>
+__global__ __launch_bounds__(256) void k_loss_dw_sum(const GradArgs a)
+{
+    const int t = blockIdx.x / L::kParts, ib = t / a.ablocks, ia = t - ib * a.ablocks, a0 = ia * L::BA, b0 = ib * L::BB;
+    const float f = gradient_scale(a.scale, a.mean, a.count);
+    L::take(a.part + (long long)t * L::kSums, (long long)a.bblocks * a.ablocks * L::kSums, a.shares, blockIdx.x - t * L::kParts, [&](int i, int j, float (&v)[8]) __attribute__((always_inline)) {
+        if (b0 + j >= a.ids || a0 + i >= a.C) return;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] *= f;
+        store8((T*)a.out + (long long)(b0 + j) * a.ostride + a0 + i, a.C - a0 - i, a.vec, v);
+    });
 }
 
 // ---- plans ---------------------------------------------------------------------------------------------------------
@@ -481,8 +486,8 @@ Buffers buffers_of(const ftp_token_loss_shape& s, const Plan& p, bool back, char
         b.sums = t.take<double>(2 * 1024);
     } else {
         b.g = t.take<bf16_t>((size_t)p.gplanes * p.Np * p.piece);
-        b.dx = t.take<float>((size_t)p.dx.shares * round_up(p.Np, p.dx.block) * p.Cp);
-        b.dw = t.take<float>(p.dw.shares > 1 ? (size_t)p.dw.shares * p.piece * p.Cp : 0);
+        b.dx = t.take<float>((size_t)p.dx.shares * round_up(p.Np, p.dx.block) * round_up(p.Cp, p.dx.block));
+        b.dw = t.take<float>(p.dw.shares > 1 ? (size_t)p.dw.shares * p.piece * round_up(p.Cp, p.dw.block) : 0);
     }
     b.bytes = t.used;
     return b;
@@ -550,7 +555,17 @@ void forward(const ftp_token_loss_shape& s, const void* x, const void* w, const 
 }
 
 template <class L, typename T>
-void dw_pass(GradArgs& a, hipStream_t st) { k_loss_dw<L, T><<<(unsigned)block_grid(a.ablocks, (long long)a.bblocks * a.shares), L::kThreads, 0, st>>>(a); }
+void dw_pass(GradArgs& a, hipStream_t st)
+{
+    k_loss_dw<L, T><<<(unsigned)block_grid(a.ablocks, (long long)a.bblocks * a.shares), L::kThreads, 0, st>>>(a);
+    if (a.shares > 1) k_loss_dw_sum<L, T><<<(unsigned)(a.ablocks * a.bblocks * L::kParts), 256, 0, st>>>(a);
+}
+template <class L, typename T>
+void dx_sum(GradArgs& a, hipStream_t st)
+{
+    a.summing = a.ablocks * a.bblocks * L::kParts;
+    k_loss_dx_sum<L, T><<<(unsigned)a.summing + std::min<unsigned>(pass_grid(a.rows * ceil_div(a.C, 8)), 1024), 256, 0, st>>>(a);
+}
 template <class L>
 void dx_pass(GradArgs& a, hipStream_t st) { k_loss_dx<L><<<(unsigned)block_grid(a.ablocks, (long long)a.bblocks * a.shares), L::kThreads, 0, st>>>(a); }
 
@@ -572,30 +587,28 @@ void backward(const ftp_token_loss_shape& s, const void* x, const void* w, const
         else if (p.logits.block == 256) logits<Two, P, false>(a, s.rows, st);
         else logits<Mid<false, false>, P, false>(a, s.rows, st);
         GradArgs k = {};
-        k.count = b.count; k.terms = p.gplanes == P ? terms_of(P) : terms_one_two(); k.C = s.channels; k.scale = s.scale; k.mean = !dloss; k.pstride = p.Cp;
+        k.count = b.count; k.terms = p.gplanes == P ? terms_of(P) : terms_one_two(); k.C = s.channels; k.scale = s.scale; k.mean = !dloss;
         if (dx && s.rows) {
-            const int block = p.dx.block;
             k.a = wp; k.b = g; k.stages = (int)ceil_div(n, 32); k.shares = p.dx.shares; k.most = p.most; k.add = v0 > 0;
-            k.ablocks = (int)ceil_div(p.Cp, block); k.bblocks = (int)ceil_div(s.rows, block);
-            k.part = b.dx;
-            if (p.dx.block == 256) dx_pass<Big<true, false>>(k, st);
-            else dx_pass<Mid<true, false>>(k, st);
+            k.ablocks = (int)ceil_div(p.Cp, p.dx.block); k.bblocks = (int)ceil_div(s.rows, p.dx.block);
+            k.part = b.dx; k.out = dx; k.ostride = s.dx_stride; k.vec = vectors(dx, s.dx_stride); k.place = b.place; k.index = b.index; k.rows = (int)s.rows;
+            const bool last = v0 + p.piece >= s.vocab;
+            if (p.dx.block == 256) {
+                dx_pass<Big<true, false>>(k, st);
+                if (last) dx_sum<Big<true, false>, T>(k, st);
+            } else {
+                dx_pass<Mid<true, false>>(k, st);
+                if (last) dx_sum<Mid<true, false>, T>(k, st);
+            }
         }
         if (dw) {
-            const int block = p.dw.block;
-            k.a = xc; k.b = g; k.shares = p.dw.shares; k.add = n;
-            k.ablocks = (int)ceil_div(p.Cp, block); k.bblocks = (int)ceil_div(n, block);
-            k.part = b.dw; k.pshare = p.piece * p.Cp;
-            T* out = (T*)dw + v0 * s.dw_stride;
-            k.out = out; k.ostride = s.dw_stride; k.vec = vectors(dw, s.dw_stride);
+            k.a = xc; k.b = g; k.shares = p.dw.shares; k.ids = n;
+            k.ablocks = (int)ceil_div(p.Cp, p.dw.block); k.bblocks = (int)ceil_div(n, p.dw.block);
+            k.part = b.dw; k.out = (T*)dw + v0 * s.dw_stride; k.ostride = s.dw_stride; k.vec = vectors(dw, s.dw_stride);
             if (p.dw.block == 256) dw_pass<Big<true, true>, T>(k, st);
             else dw_pass<Mid<true, true>, T>(k, st);
-            if (k.shares > 1)
-                k_loss_sum<T><<<pass_grid(n * ceil_div(s.channels, 8)), 256, 0, st>>>(b.dw, p.Cp, k.pshare, k.shares, 0, 0, nullptr, n, out, s.dw_stride, s.channels, k.vec, s.scale, !dloss, b.count);
         }
     }
-    if (dx && s.rows)
-        k_loss_sum<T><<<pass_grid(s.rows * ceil_div(s.channels, 8)), 256, 0, st>>>(b.dx, p.Cp, 0, (int)ceil_div(s.rows, p.dx.block) * p.dx.shares, p.dx.block, p.most, b.place, s.rows, dx, s.dx_stride, s.channels, vectors(dx, s.dx_stride), s.scale, !dloss, b.count);
 }
 
 }  // namespace
