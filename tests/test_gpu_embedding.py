@@ -113,6 +113,24 @@ def test_what_rows_without_an_id_hold_reaches_nothing():
     assert got[4].isinf().all() and torch.equal(got[:4], want[:4]) and torch.equal(got[5:], want[5:])
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_offsets_of_more_than_31_bits(dtype):
+    """A table of 2.9 billion elements, ids at both ends of it."""
+    from paper_2409_09083_amd import vocabulary
+    vocab, c = 700000, 4104
+    ids = torch.tensor([vocab - 1, 0, vocab - 1, 523300, -1, vocab - 2, 0], device="cuda")
+    dy = _normal((7, c), dtype, 1)
+    e = vocabulary.Embedding(7, vocab, c, dtype)
+    table = torch.empty((vocab, c), dtype=TYPES[dtype], device="cuda")
+    for r in (vocab - 1, vocab - 2, 523300, 0):
+        table[r] = r % 97
+    assert e.forward(ids, table)[:, -1].tolist() == [float((r % 97) if r >= 0 else 0) for r in ids.tolist()]
+    del table
+    d = e.backward(ids, dy)
+    assert sorted(torch.count_nonzero(d, dim=1).nonzero().squeeze(1).tolist()) == [0, 523300, vocab - 2, vocab - 1]
+    assert torch.equal(d[vocab - 1], dy[0].float() + dy[2].float()) and torch.equal(d[0], dy[1].float() + dy[6].float()) and torch.equal(d[523300], dy[3].float())
+
+
 def test_gradient_by_differences():
     from paper_2409_09083_amd import vocabulary
     ids, g = _ids(40, 9, "skewed"), _normal((40, 6), "f32", 7)

@@ -200,6 +200,26 @@ def test_pieces_of_the_vocabulary_and_splits(dtype, monkeypatch):
         _check(vocabulary.TokenLoss(rows, vocab, channels, dtype), x, w, labels, 1.0, dtype)
 
 
+@pytest.mark.parametrize("rows,dtype", [(4100, "bf16"), (70, "bf16"), (33, "f32")])
+def test_offsets_of_more_than_31_bits(rows, dtype):
+    """A weight of 2.4 GB (its planes 7.4), G of 1.2 GB where there are many rows; labels at both ends of it."""
+    from paper_2409_09083_amd import vocabulary
+    vocab, channels = 150000, 8192
+    g = torch.Generator(device="cuda").manual_seed(1)
+    w = (torch.randn((vocab, channels), generator=g, device="cuda") * channels ** -0.5).to(TYPES[dtype])
+    labels = torch.randint(0, vocab, (rows,), generator=g, device="cuda")
+    labels[0], labels[1], labels[2] = vocab - 1, 0, -1
+    x = (torch.randn((rows, channels), generator=g, device="cuda") + 8 * w[labels.clamp(min=0)].float()).to(TYPES[dtype])
+    head = vocabulary.TokenLoss(rows, vocab, channels, dtype)
+    mean = float(head.forward(x, w, labels))
+    r = _reference(x, w, labels, 1.0, dtype)
+    there = r["there"]
+    assert _near(head.lse[there], r["lse"]) and _near(head.losses[there], r["loss"])
+    assert abs(mean - float(r["loss"][0].mean())) <= float(r["loss"][1].mean()) + 2 * U * abs(mean)
+    dx, dw = head.backward(x, w, labels)
+    assert _near(dx[there], r["dx"]) and not dx[~there].any() and _near(dw, r["dw"])
+
+
 def test_empty_refusals_streams_and_graph():
     from paper_2409_09083_amd import vocabulary
     e = vocabulary.TokenLoss(0, 50, 8)
