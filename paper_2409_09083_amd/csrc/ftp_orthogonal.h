@@ -8,6 +8,7 @@ namespace ftp {
 // Matrices whose smaller side is at most 64: a launch a step (ftp_orthogonal_small.hip).
 inline bool orthogonal_is_small(const ftp_orthogonal_shape& s) { return (s.rows < s.cols ? s.rows : s.cols) <= 64; }
 size_t orthogonal_small_workspace(const ftp_orthogonal_shape& s, Parts& t);
+bool orthogonal_small_sums(const ftp_orthogonal_shape& s);          // whether it wants the sums
 // sums: `parts` parts of each matrix' sum of squares; t: the scratch behind them
 void orthogonal_small(const ftp_orthogonal_shape& s, const void* x, void* out, const double* sums, int parts, Parts& t, hipStream_t st);
 

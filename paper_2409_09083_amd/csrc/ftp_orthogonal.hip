@@ -297,7 +297,7 @@ void run(const ftp_orthogonal_shape& s, const T* x, T* out, char* ws, hipStream_
         Parts t(ws);
         const int parts = parts_of(s);
         double* sums = t.take<double>((size_t)s.count * parts);
-        k_squares<T><<<(unsigned)(s.count * parts), 256, 0, st>>>(x, s.matrix_stride, s.row_stride, s.rows, s.cols, parts, sums);
+        if (orthogonal_small_sums(s)) k_squares<T><<<(unsigned)(s.count * parts), 256, 0, st>>>(x, s.matrix_stride, s.row_stride, s.rows, s.cols, parts, sums);
         orthogonal_small(s, x, out, sums, parts, t, st);
         return;
     }

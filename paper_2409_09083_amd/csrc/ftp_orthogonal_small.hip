@@ -1,8 +1,8 @@
-// Newton-Schulz steps of matrices with a side of at most 64, one launch a step: a chain of latencies, not of work.
+// Newton-Schulz steps of matrices with a side of at most 64, one launch a step or one for all: a chain of latencies, not of work.
 //
 // X lies as m x L, m <= 64 (a tall matrix transposed), in blocks of 64 columns that belong to one workgroup from step to step.  A step's workgroup adds up the parts of S = X X^T that the workgroups of the step before left, makes
 // a I + b S + c S^2 of it in LDS (each for itself: 24 matrix instructions a wavefront), multiplies its blocks with that, and takes their part of the next S from the result while it is in LDS.
-// 64 x 576, fp32, 5 steps: 134 us as three products a step, SMALL_US us so.
+// 64 x 576, fp32, 5 steps: 134 us as three products a step, 56 so.  Up to 4 blocks stay in one workgroup's LDS, all steps in one launch.
 #include "ftp_orthogonal.h"
 
 #include <algorithm>
@@ -10,6 +10,7 @@
 namespace ftp {
 namespace {
 
+constexpr int kWhole = 4;                           // most blocks that one workgroup takes through all steps
 constexpr int kSide = 64, kTile = kSide * kSide * 2;           // bytes of a plane of 64 x 64
 
 // 16 bytes (8 columns: chunk) of a row: neither 16 rows of one chunk nor the transposing load's 4 rows x 64 bytes meet on the banks.
@@ -172,6 +173,93 @@ __global__ __launch_bounds__(256) void k_small_step(const SmallArgs a)
     for (int q = 0; q < 4; ++q) to[256 * q] = f32x4{next[4 * q], next[4 * q + 1], next[4 * q + 2], next[4 * q + 3]};
 }
 
+// All steps of a matrix of up to NB blocks by one workgroup, X in its LDS: four wavefronts a block.
+template <typename T, int P, int NB>
+__global__ __launch_bounds__(256 * NB) void k_small_all(const SmallArgs a, int steps)
+{
+    constexpr int kJoin = (NB - 1) * kSide * kSide * 4, kWork = kJoin > 2 * P * kTile ? kJoin : 2 * P * kTile;
+    __shared__ __align__(16) char work[kWork], tx[NB][P * kTile];
+    __shared__ double sums[4 * NB];
+    char *const ts = work, *const tq = work + P * kTile;
+    const int matrix = blockIdx.x, block = __builtin_amdgcn_readfirstlane(threadIdx.x >> 8), tid = threadIdx.x & 255, wave = tid >> 6, l = tid & 63, h = l >> 5, a0 = 32 * (wave & 1),
+              b0 = 32 * (wave >> 1), row = b0 + (l & 31);
+    const T* x = (const T*)a.x + matrix * a.mstride;
+    char* const mine = tx[block];
+    // neighbours in memory on neighbouring lanes, whichever way x lies
+    float held[16];
+    double square = 0;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) {
+        const int e = tid + 256 * k, r = a.tall ? e & 63 : e >> 6, at = block * kSide + (a.tall ? e >> 6 : e & 63);
+        held[k] = r < a.m && at < a.len ? (float)ld(x + (a.tall ? at * a.rstride + r : r * a.rstride + at)) : 0.0f;
+        square = fma((double)held[k], (double)held[k], square);
+    }
+#pragma unroll
+    for (int k = 32; k; k >>= 1) square += __shfl_xor(square, k);
+    if (l == 0) sums[4 * block + wave] = square;
+    __syncthreads();
+    square = 0;
+#pragma unroll
+    for (int k = 0; k < 4 * NB; ++k) square += sums[k];
+    const double inv = 1.0 / (sqrt(square) + a.eps);
+#pragma unroll
+    for (int k = 0; k < 16; ++k) {
+        const int e = tid + 256 * k, r = a.tall ? e & 63 : e >> 6, c = a.tall ? e >> 6 : e & 63;
+        uint32_t q[P];
+        planes_of<P>((float)(held[k] * inv), 0.0f, q);
+#pragma unroll
+        for (int p = 0; p < P; ++p) *(bf16_t*)(mine + p * kTile + chunk_at(r, c >> 3) + (c & 7) * 2) = (bf16_t)q[p];
+    }
+    const auto put = [&](char* t, const f32x16& v) __attribute__((always_inline)) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) put4<P>(t, row, a0 + 8 * q + 4 * h, v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+    };
+    for (int step = 0; step < steps; ++step) {
+        __syncthreads();
+        f32x16 s = product<P>(f32x16{}, [&](int p, int k) { return rows_operand(mine + p * kTile, a0, k); }, [&](int p, int k) { return rows_operand(mine + p * kTile, b0, k); });
+        if constexpr (NB > 1) {
+            // the blocks' parts of S, added up in their order by the first one's wavefronts
+            f32x4* part = (f32x4*)work;
+            if (block) {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) part[((block - 1) * 4 + q) * 256 + tid] = f32x4{s[4 * q], s[4 * q + 1], s[4 * q + 2], s[4 * q + 3]};
+            }
+            __syncthreads();
+            if (!block) {
+#pragma unroll
+                for (int n = 0; n < NB - 1; ++n)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const f32x4 v = part[(n * 4 + q) * 256 + tid];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) s[4 * q + e] += v[e];
+                    }
+            }
+            __syncthreads();
+        }
+        if (!block) put(ts, s);
+        __syncthreads();
+        if (!block) {
+            f32x16 q = product<P>(f32x16{}, [&](int p, int k) { return rows_operand(ts + p * kTile, a0, k); }, [&](int p, int k) { return rows_operand(ts + p * kTile, b0, k); });
+#pragma unroll
+            for (int r = 0; r < 16; ++r) q[r] = fmaf(a.c, q[r], a.b * s[r]) + (a0 + 8 * (r >> 2) + 4 * h + (r & 3) == row ? a.a : 0.0f);
+            put(tq, q);
+        }
+        __syncthreads();
+        const f32x16 v = product<P>(f32x16{}, [&](int p, int k) { return columns_operand(mine + p * kTile, a0, k); }, [&](int p, int k) { return rows_operand(tq + p * kTile, b0, k); });
+        __syncthreads();
+        if (step + 1 < steps) {
+            put(mine, v);
+            continue;
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const int at = block * kSide + a0 + 8 * (r >> 2) + 4 * h + (r & 3);
+            if (row < a.m && at < a.len) st((T*)a.out + (long long)matrix * a.m * a.len + (a.tall ? (long long)at * a.m + row : (long long)row * a.len + at), v[r]);
+        }
+    }
+}
+
 // Workgroups of a matrix: one a block up to 32, whose parts of S each of them adds up.
 void shape_of(const ftp_orthogonal_shape& s, SmallArgs& a)
 {
@@ -186,6 +274,12 @@ void shape_of(const ftp_orthogonal_shape& s, SmallArgs& a)
 template <typename T, int P>
 void run(const ftp_orthogonal_shape& s, SmallArgs& a, float* (&parts)[2], hipStream_t st)
 {
+    if (a.blocks <= kWhole) {
+        if (a.blocks == 1) k_small_all<T, P, 1><<<(unsigned)s.count, 256, 0, st>>>(a, s.steps);
+        else if (a.blocks == 2) k_small_all<T, P, 2><<<(unsigned)s.count, 512, 0, st>>>(a, s.steps);
+        else k_small_all<T, P, kWhole><<<(unsigned)s.count, 256 * kWhole, 0, st>>>(a, s.steps);
+        return;
+    }
     const unsigned grid = (unsigned)(s.count * a.groups);
     a.to = parts[0];
     k_small_start<T, P><<<grid, 256, 0, st>>>(a);
@@ -204,6 +298,13 @@ void take(const ftp_orthogonal_shape& s, const SmallArgs& a, Parts& t, bf16_t*& 
 }
 
 }  // namespace
+
+bool orthogonal_small_sums(const ftp_orthogonal_shape& s)
+{
+    SmallArgs a = {};
+    shape_of(s, a);
+    return a.blocks > kWhole;
+}
 
 size_t orthogonal_small_workspace(const ftp_orthogonal_shape& s, Parts& t)
 {
