@@ -91,7 +91,7 @@ struct StepArgs {
     float diagonal, spare;                          // (three floats in a row had the compiler keep a copy of them in LDS: 4 x 512 x 2048 468 -> 600 us)
     const bf16_t* old; bf16_t* to;
     long long plane, next; int arows, brows;        // (old and to: a Matrix of brows rows and arows columns each) [matrix: next]
-    void* out; int orows, ocols, vec;               // instead of planes: the results, rows along b
+    void* out; int orows, ocols;                    // instead of planes: the results, rows along b
     float* part;                                    // sums: [block that is cut][share]
 };
 
@@ -116,7 +116,7 @@ __device__ __forceinline__ void finish(const StepArgs& a, int matrix, int i, int
         }
     }
     if (a.out) {
-        if (j < a.orows) store8((T*)a.out + ((long long)matrix * a.orows + j) * a.ocols + i, a.ocols - i, a.vec, v);
+        if (j < a.orows) store8((T*)a.out + ((long long)matrix * a.orows + j) * a.ocols + i, a.ocols - i, v);
         return;
     }
     bf16_t* to = a.to + at;
@@ -322,7 +322,7 @@ void run(const ftp_orthogonal_shape& s, const T* x, T* out, char* ws, hipStream_
         // that times X
         k.symmetric = 0; k.old = nullptr; k.to = b.x[~step & 1];
         k.arows = p.Cp; k.brows = p.Rp; k.next = xnext; k.plane = xplane;
-        if (step + 1 == s.steps) { k.out = out; k.orows = s.rows; k.ocols = s.cols; k.vec = aligned(out, 16) && s.cols % 8 == 0; }
+        if (step + 1 == s.steps) { k.out = out; k.orows = s.rows; k.ocols = s.cols; }
         if (p.tall) {
             k.a = Q; k.b = X; k.anext = qnext; k.bnext = xnext;
             product<false, false, T, P>(k, p.x, st);

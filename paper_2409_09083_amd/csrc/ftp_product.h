@@ -269,29 +269,34 @@ struct Product {
                 *p = add ? *p + v : v;
             }
     }
-    // ... added up, `next` floats from one share to the next, by 256 threads: part `index` of kParts.  f as for each().
-    static constexpr int kParts = kUnits * (kThreads / 256);
+    // ... added up, `next` floats from one share to the next, by 256 threads: part `index` of kParts, whose four wavefronts take the shares in turn (few blocks have many).  f as for each().
+    static constexpr int kParts = kUnits * (kThreads / 64);
     template <class F>
     static __device__ __forceinline__ void take(const float* from, long long next, int shares, int index, F f)
     {
-        const int u = index / (kThreads / 256), tid = (index % (kThreads / 256)) * 256 + threadIdx.x, l = tid & 63, h = l >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-        const f32x4* p = (const f32x4*)from + u * 4 * kThreads + tid;
+        __shared__ f32x4 sums[4][4][64];
+        const int u = index / (kThreads / 64), wave = index % (kThreads / 64), l = threadIdx.x & 63, h = l >> 5, turn = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const f32x4* p = (const f32x4*)(from + turn * next) + u * 4 * kThreads + wave * 64 + l;
         f32x4 s[4] = {};
 #pragma unroll 4
-        for (int k = 0; k < shares; ++k, p += next / 4)
+        for (int k = turn; k < shares; k += 4, p += next)
 #pragma unroll
             for (int q = 0; q < 4; ++q) s[q] += p[q * kThreads];
 #pragma unroll
-        for (int q = 0; q < 4; q += 2) {
-            float v[8];
+        for (int q = 0; q < 4; ++q) sums[turn][q][l] = s[q];
+        __syncthreads();
+        if (turn >= 2) return;
+        const int q = 2 * turn;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(s[q][e]), __float_as_uint(s[q + 1][e]), false, false);
-                v[e] = __uint_as_float(x[0]);
-                v[4 + e] = __uint_as_float(x[1]);
-            }
-            f((wave % WA) * (IA * 32) + 32 * (u % IA) + 8 * q + 8 * h, (wave / WA) * (IB * 32) + 32 * (u / IA) + (l & 31), v);
+        for (int e = 0; e < 2; ++e) s[e] = (sums[0][q + e][l] + sums[1][q + e][l]) + (sums[2][q + e][l] + sums[3][q + e][l]);
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(s[0][e]), __float_as_uint(s[1][e]), false, false);
+            v[e] = __uint_as_float(x[0]);
+            v[4 + e] = __uint_as_float(x[1]);
         }
+        f((wave % WA) * (IA * 32) + 32 * (u % IA) + 8 * q + 8 * h, (wave / WA) * (IB * 32) + 32 * (u / IA) + (l & 31), v);
     }
 
     // f(a, b, v): index of the first of eight neighbours along a, index along b, values; of this wavefront, from the block's corner.  (A lane's registers are four neighbours; the halves exchange every other four: 16 bytes of bfloats a store instead
@@ -372,17 +377,18 @@ __device__ __forceinline__ void store_planes(bf16_t* to, long long plane, const 
 #pragma unroll
     for (int p = 0; p < PLANES; ++p) *(uint4*)(to + p * plane) = uint4{x[0][p], x[1][p], x[2][p], x[3][p]};
 }
-// The first n of 8 neighbours of a row of results, at once where vec says that their address allows it.
+// The first n of 8 neighbours of a row of results, at any address: all eight at once.
 template <typename T>
-__device__ __forceinline__ void store8(T* to, int n, bool vec, const float (&v)[8])
+__device__ __forceinline__ void store8(T* to, int n, const float (&v)[8])
 {
-    if (vec && n >= 8) {
+    if (n >= 8) {
         Pack<T, 8> w;
         w.put(v);
-        w.store(to);
+        w.store_any(to);
         return;
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) if (e < n) st(to + e, v[e]);
 }
+
 }  // namespace ftp

@@ -326,7 +326,7 @@ struct GradArgs {
     Terms terms;
     int stages, shares, most, ablocks, bblocks, add;           // dx: shares and blocks for all rows; fewer rows have more shares (dx_shares())
     float* part;                                    // sums: [share][block along b][block along a]
-    void* out; long long ostride; int C, vec; float scale; int mean;
+    void* out; long long ostride; int C; float scale; int mean;
     int ids;                                        // dw: of the piece
     const int* place; const int* index; int rows, summing;     // dx
 };
@@ -378,7 +378,7 @@ __global__ __launch_bounds__(L::kThreads, 2) void k_loss_dw(const GradArgs a)
         float w[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) w[e] = v[e] * f;
-        store8((T*)a.out + id * a.ostride + a0 + i, a.C - a0 - i, a.vec, w);
+        store8((T*)a.out + id * a.ostride + a0 + i, a.C - a0 - i, w);
     });
 }
 
@@ -393,7 +393,7 @@ __global__ __launch_bounds__(256) void k_loss_dx_sum(const GradArgs a)
         for (long long u = (long long)(blockIdx.x - a.summing) * 256 + threadIdx.x; u < n; u += step) {
             const long long r = u / per;
             const int c = (int)(u - r * per) * 8;
-            if (a.place[r] < 0) store8((T*)a.out + r * a.ostride + c, a.C - c, a.vec, zeros);
+            if (a.place[r] < 0) store8((T*)a.out + r * a.ostride + c, a.C - c, zeros);
         }
         return;
     }
@@ -405,7 +405,7 @@ __global__ __launch_bounds__(256) void k_loss_dx_sum(const GradArgs a)
         if (b0 + j >= rows || a0 + i >= a.C) return;
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] *= f;
-        store8((T*)a.out + a.index[b0 + j] * a.ostride + a0 + i, a.C - a0 - i, a.vec, v);
+        store8((T*)a.out + a.index[b0 + j] * a.ostride + a0 + i, a.C - a0 - i, v);
     });
 }
 
@@ -418,7 +418,7 @@ __global__ __launch_bounds__(256) void k_loss_dw_sum(const GradArgs a)
         if (b0 + j >= a.ids || a0 + i >= a.C) return;
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] *= f;
-        store8((T*)a.out + (long long)(b0 + j) * a.ostride + a0 + i, a.C - a0 - i, a.vec, v);
+        store8((T*)a.out + (long long)(b0 + j) * a.ostride + a0 + i, a.C - a0 - i, v);
     });
 }
 
@@ -457,7 +457,7 @@ Plan plan_of(const ftp_token_loss_shape& s, bool back)
     p.piece = round_up(ceil_div(s.vocab, pieces), 256);
     p.logits = split_of(p.piece, s.rows, p.Cp / 32 * terms, 128, 1);
     const long long gterms = p.planes == 1 ? p.gplanes : 6;
-    p.dx = split_of(s.channels, s.rows, p.piece / 32 * gterms, 128, 16);
+    p.dx = split_of(s.channels, s.rows, p.piece / 32 * gterms, 128, 64);
     p.most = (int)std::max<long long>(p.dx.shares, p.piece / 32 * gterms / 24);
     p.dw = split_of(s.channels, p.piece, p.Np / 32 * gterms, 128, 16);
     return p;
@@ -574,7 +574,6 @@ void backward(const ftp_token_loss_shape& s, const void* x, const void* w, const
 {
     const Plan p = plan_of(s, true);
     const Buffers b = buffers_of(s, p, true, ws);
-    const auto vectors = [](const void* p, long long stride) { return aligned(p, 16) && stride % 8 == 0; };        // rows whose 8 neighbours can be stored at once
     const Matrix all = prepare<P>(s, p, b, x, w, labels, true, st), xc = blocked(b.xc, p.Np, p.Cp, p.Np * p.Cp), g = blocked(b.g, p.Np, (int)p.piece, p.Np * p.piece);
     for (long long v0 = 0; v0 < s.vocab; v0 += p.piece) {
         const int n = (int)std::min<long long>(p.piece, s.vocab - v0);
@@ -591,7 +590,7 @@ void backward(const ftp_token_loss_shape& s, const void* x, const void* w, const
         if (dx && s.rows) {
             k.a = wp; k.b = g; k.stages = (int)ceil_div(n, 32); k.shares = p.dx.shares; k.most = p.most; k.add = v0 > 0;
             k.ablocks = (int)ceil_div(p.Cp, p.dx.block); k.bblocks = (int)ceil_div(s.rows, p.dx.block);
-            k.part = b.dx; k.out = dx; k.ostride = s.dx_stride; k.vec = vectors(dx, s.dx_stride); k.place = b.place; k.index = b.index; k.rows = (int)s.rows;
+            k.part = b.dx; k.out = dx; k.ostride = s.dx_stride; k.place = b.place; k.index = b.index; k.rows = (int)s.rows;
             const bool last = v0 + p.piece >= s.vocab;
             if (p.dx.block == 256) {
                 dx_pass<Big<true, false>>(k, st);
@@ -604,7 +603,7 @@ void backward(const ftp_token_loss_shape& s, const void* x, const void* w, const
         if (dw) {
             k.a = xc; k.b = g; k.shares = p.dw.shares; k.ids = n;
             k.ablocks = (int)ceil_div(p.Cp, p.dw.block); k.bblocks = (int)ceil_div(n, p.dw.block);
-            k.part = b.dw; k.out = (T*)dw + v0 * s.dw_stride; k.ostride = s.dw_stride; k.vec = vectors(dw, s.dw_stride);
+            k.part = b.dw; k.out = (T*)dw + v0 * s.dw_stride; k.ostride = s.dw_stride;
             if (p.dw.block == 256) dw_pass<Big<true, true>, T>(k, st);
             else dw_pass<Mid<true, true>, T>(k, st);
         }
