@@ -5,7 +5,8 @@
 // contraction is as many times longer.
 //
 // Stages of 32 (64) are fetched straight into LDS three to four ahead (buffer loads; what is past the end of an operand arrives as zeros), one barrier a stage, loads and reads between the matrix instructions.  A wavefront has 128 x 64 of
-// a block of 256 x 256: 8 products of 32 x 32 x 16 to 6 operands of 1 KB.  8192 x 8192 x 2048: 204 us, 1.35 PFLOP/s (256 x 128 1.16, 128 x 128 1.14, 64 x 64 0.65); of zeros, which take less power, 1.65.
+// a block of 256 x 256: 8 products of 32 x 32 x 16 to 6 operands of 1 KB.  8192 x 8192 x 2048: 213 to 232 us, 1.18 to 1.29 PFLOP/s (256 x 128 1.13 to 1.14, 128 x 128
+// 1.03 to 1.12, 64 x 64 0.63 to 0.66); of zeros, which take less power, 1.76 to 1.80.
 #pragma once
 #include "ftp_tokens.h"
 
@@ -198,7 +199,7 @@ struct Product {
         constexpr int N = KS / 16, NM = IA * IB, NR = IA + IB;
         static_assert(N % 2 == 0, "operands alternate");
         // The products of operands that are there, and between them the reads of the next ones (k part s of `from`) and a part of the loads into `to`.  All at once behind the barrier, loads and reads held the
-        // products up (8192 x 8192 x 2048: 240 us, where the loads alone take 92 and the products with their reads 137; so 222).
+        // products up (8192 x 8192 x 2048: 240 us, where the loads alone take 92 and the products with their reads 137; so 222, one run each).
         const auto block = [&](int set, const Stage& from, int s, Stage& to, int part) __attribute__((always_inline)) {
             const int l0 = part * kLoads / N, nl = (part + 1) * kLoads / N - l0;
 #pragma unroll
