@@ -348,7 +348,7 @@ typedef enum { FTP_I32 = 0, FTP_I64 = 1 } ftp_id_type;
  * Backward: dtable[v] = scale * the sum of dy[r] over the rows with ids[r] = v, in 32 bits and in the order of the rows (runs of
  * 8 or 32 neighbours in the list sorted by id first); rows of dtable whose id does not occur are set to zero. */
 typedef struct {
-    int64_t rows;                  /* at most 2^26 */
+    int64_t rows;                  /* at most 2^26; backward, rows * channels at most 2^38 */
     int32_t vocab, channels;       /* >= 1; at most 2^26 and 2^20 */
     int32_t dtype;                 /* ftp_dtype of table, out and dy */
     int32_t id_type;               /* ftp_id_type of ids [rows] */

@@ -383,6 +383,8 @@ void embedding_forward(const ftp_embedding_shape& s, const void* ids, const void
         k_embed<float><<<grid, 256, 0, st>>>(ids, s.id_type, (const float*)table, s.table_stride, (float*)out, s.row_stride, s.rows, s.vocab, s.channels, s.scale, lanes);
 }
 
+// k_runs has a thread for each vector of 4 numbers (or 8) of a piece of 32 rows: fewer than 2^32 (short lists' pieces of 8 rows stay below that)
+bool embedding_backward_fits(const ftp_embedding_shape& s) { return s.rows * s.channels <= 1ll << 38; }
 size_t embedding_workspace(const ftp_embedding_shape& s) { return buffers_of(s, nullptr).bytes; }
 
 void embedding_backward(const ftp_embedding_shape& s, const void* ids, const void* dy, float* dtable, void* ws, hipStream_t st)

@@ -5,6 +5,7 @@
 namespace ftp {
 
 void embedding_forward(const ftp_embedding_shape& s, const void* ids, const void* table, void* out, hipStream_t st);
+bool embedding_backward_fits(const ftp_embedding_shape& s);
 size_t embedding_workspace(const ftp_embedding_shape& s);
 void embedding_backward(const ftp_embedding_shape& s, const void* ids, const void* dy, float* dtable, void* ws, hipStream_t st);
 

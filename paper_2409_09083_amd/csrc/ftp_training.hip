@@ -49,6 +49,7 @@ int ftp_embedding_workspace(const ftp_embedding_shape* shape, size_t* bytes)
 {
     const int rc = check(shape);
     if (rc != FTP_OK) return rc;
+    if (!embedding_backward_fits(*shape)) return FTP_EUNSUPPORTED;
     if (!bytes) return FTP_EINVAL;
     *bytes = embedding_workspace(*shape);
     return FTP_OK;
@@ -58,6 +59,7 @@ int ftp_embedding_backward(const ftp_embedding_shape* shape, const void* ids, co
 {
     const int rc = check(shape);
     if (rc != FTP_OK) return rc;
+    if (!embedding_backward_fits(*shape)) return FTP_EUNSUPPORTED;
     if (!dtable || (shape->rows && (!ids || !dy || !workspace))) return FTP_EINVAL;
     embedding_backward(*shape, ids, dy, dtable, workspace, (hipStream_t)stream);
     return launched();

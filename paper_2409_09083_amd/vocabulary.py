@@ -45,10 +45,10 @@ class Embedding(_Vocabulary):
         self.device = _device(device)
         self.training = training
         self.desc = B.ftp_embedding_shape(rows=rows, vocab=vocab, channels=channels, dtype=code, scale=scale)
-        ws = B.ftp_embedding_workspace(self.desc)
         self._row_shape, self._shape, self._table = torch.Size((rows,)), torch.Size((rows, channels)), torch.Size((vocab, channels))
         self.out = self.dtable = self._ws = None
         if training:
+            ws = B.ftp_embedding_workspace(self.desc)       # (refuses sizes before a buffer is made)
             self.dtable = torch.empty(self._table, dtype=torch.float32, device=self.device)
             self._ws = _scratch(ws, self.device)
 

@@ -108,6 +108,16 @@ def test_orthogonal_pointers(B):
     assert _code(B, B.ftp_orthogonal_workspace, ctypes.POINTER(B.ftp_orthogonal_shape)()) == B.FTP_EINVAL
 
 
+def test_embedding_gradients_of_too_many_threads(B):
+    """2^19 rows (all the same in memory) of 2^20 channels are 2^14 pieces of 32 rows x 2^18 vectors of four numbers, 2^32 threads: refused before anything is launched.  The lookup has
+    a loop for them."""
+    s = _embedding(B, rows=1 << 19, channels=1 << 20, row_stride=0)
+    assert _code(B, B.ftp_embedding_workspace, s) == B.FTP_EUNSUPPORTED
+    assert _code(B, B.ftp_embedding_backward, s, P, P, P, P) == B.FTP_EUNSUPPORTED
+    assert B.ftp_embedding_workspace(_embedding(B, rows=1 << 18, channels=1 << 20, row_stride=0)) > 0
+    assert B.ftp_embedding_workspace(_embedding(B, rows=1 << 26, channels=1 << 12, row_stride=0)) > 0
+
+
 def test_scratch_of_all_sizes(B):
     """The plans of sizes over the whole range come to an end and ask for scratch that a card has, for as much of it as grows with the sizes."""
     r = random.Random(1)
