@@ -17,12 +17,17 @@ namespace ftp {
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr int kCountRows = 4096;                     // most rows whose labels every workgroup counts by itself (a launch less)
+// Most rows whose labels every workgroup counts by itself, a launch less (forward on 512 x 64, itself and with the launch: 577 rows 14.4, 16.1 us; 2048 15.7, 16.6; 4096 17.6, 17.1; 8192 21.9, 18.8).
+constexpr int kCountRows = 4096;
 constexpr int kChunk = 64;                          // rows whose labels one wavefront looks at
-constexpr int kPackRows = 4096;                     // from here on W is laid out for the products
-// Up to so many rows G is two bfloats where the tensors are one: its rounding, which the sums over many rows even out, would be as large as the results' own, and costs nothing to avoid.
+// From so many rows on W is laid out for the products (forward on 16384 x 512, as it lies and laid out: 577 rows 30, 34 us; 2048 53, 54; 4096 90, 86; 11552 215, 200).
+constexpr int kPackRows = 4096;
+// Up to so many rows G is two bfloats where the tensors are one: its rounding, which the sums over many rows even out, would be as large as the results' own.  (Backward pass on 16384 x 512: 64 rows 47 us, 41 with one; 256 rows 55, 45 with one.)
 constexpr int kExact = 256;
-constexpr int kFew = 32;                            // most rows of the logits that read W at the memory's rate
+// Most rows whose statistics one workgroup joins (forward on 32768 x 512: 16 rows 11.0 us, by several and a launch for their mean 12.5; 32 rows 13.7 and 12.5).
+constexpr int kJoin = 16;
+// Most rows of the logits whose blocks have 32 of them, with W read at the memory's rate (forward on 32768 x 512, blocks of 128 x 32 and of 128 x 128: 4 rows 10.5, 17.7 us; 33 16.4, 19.4; 64 16.6, 19.8; 128 24.6, 20.2).
+constexpr int kFew = 64;
 
 template <bool XA, bool XB> using Big = Product<256, 256, 2, 4, XA, XB>;
 typedef Product<256, 128, 2, 2, false, false, 32, 3> Two;         // two workgroups a CU: one's powers beside the other's products
@@ -266,16 +271,17 @@ __global__ __launch_bounds__(L::kThreads, 2) void k_logits(const LogitArgs a)
     }
 }
 
-// The blocks' statistics joined: a wavefront a row, its lanes' blocks in turn.  Losses and log-sums of all rows (0 where there is no label), and each workgroup's sum of losses and labelled rows.
-__global__ __launch_bounds__(256) void k_loss_join(const float2* part, const float* target, const int* place, const void* ids, int wide, long long rows, int vocab, int blocks, float c, float* loss,
+// The blocks' statistics joined: a wavefront a row, its lanes' blocks in turn; up to 16 rows by one workgroup of 16, which needs no launch for the mean.  Losses and log-sums of all rows (0 where there is no label), and each workgroup's sum of losses and labelled rows.
+template <int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void k_loss_join(const float2* part, const float* target, const int* place, const void* ids, int wide, long long rows, int vocab, int blocks, float c, float* loss,
                                                    float* lse, double* sums, float* mean)
 {
-    __shared__ double total[4];
-    __shared__ int known[4];
+    __shared__ double total[WAVES];
+    __shared__ int known[WAVES];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     double sum = 0;
     int n = 0;
-    for (long long row = (long long)blockIdx.x * 4 + wave; row < rows; row += 4ll * gridDim.x) {
+    for (long long row = (long long)blockIdx.x * WAVES + wave; row < rows; row += (long long)WAVES * gridDim.x) {
         const long long at = place ? place[row] : id_of(ids, wide, row, vocab) >= 0 ? row : -1;
         float one = 0, two = 0;
         if (at >= 0) {
@@ -302,8 +308,10 @@ __global__ __launch_bounds__(256) void k_loss_join(const float2* part, const flo
     if (lane == 0) { total[wave] = sum; known[wave] = n; }
     __syncthreads();
     if (threadIdx.x) return;
-    sum = total[0] + total[1] + total[2] + total[3];
-    n = known[0] + known[1] + known[2] + known[3];
+    sum = 0;
+    n = 0;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) { sum += total[w]; n += known[w]; }
     if (gridDim.x == 1) { if (mean) *mean = n ? (float)(sum / n) : 0.0f; }
     else if (mean) { sums[2 * blockIdx.x] = sum; sums[2 * blockIdx.x + 1] = n; }
 }
@@ -451,7 +459,7 @@ Plan plan_of(const ftp_token_loss_shape& s, bool back)
     if (!back) {
         p.logits = split_of(s.vocab, s.rows, p.Cp / 32 * terms, 128, 1);
         p.blocks = (int)ceil_div(s.vocab, p.few ? Few::BA : p.logits.block);
-        p.joins = (int)std::min<long long>(ceil_div(std::max<long long>(s.rows, 1), 4), s.rows <= 64 ? 1 : 1024);
+        p.joins = (int)std::min<long long>(ceil_div(std::max<long long>(s.rows, 1), 4), s.rows <= kJoin ? 1 : 1024);
         return p;
     }
     // a piece's G in at most 1 GiB and rows of 2^20, whole blocks
@@ -553,7 +561,9 @@ void forward(const ftp_token_loss_shape& s, const void* x, const void* w, const 
     if (p.few) logits<Few, P, true>(a, s.rows, st);
     else if (p.logits.block == 256) logits<Two, P, true>(a, s.rows, st);
     else logits<Mid<false, false>, P, true>(a, s.rows, st);
-    k_loss_join<<<p.joins, 256, 0, st>>>(b.part, b.target, plain ? nullptr : b.place, labels, s.id_type, s.rows, s.vocab, a.ablocks, a.c, loss, lse, b.sums, mean);
+    const auto join = [&](auto kernel, int threads) { kernel<<<p.joins, threads, 0, st>>>(b.part, b.target, plain ? nullptr : b.place, labels, s.id_type, s.rows, s.vocab, a.ablocks, a.c, loss, lse, b.sums, mean); };
+    if (s.rows > 4 && p.joins == 1) join(k_loss_join<16>, 1024);
+    else join(k_loss_join<4>, 256);
     if (p.joins > 1 && mean) k_loss_mean<<<1, 256, 0, st>>>(b.sums, p.joins, mean);
 }
 

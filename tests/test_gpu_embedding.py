@@ -44,6 +44,18 @@ def _backward64(ids, dy, vocab, scale):
 SIZES = [(1, 1, 1), (3, 7, 5), (31, 2, 8), (32, 40, 64), (33, 1, 250), (64, 300, 16), (1000, 255, 96), (1025, 256, 33), (4995, 1001, 250), (2049, 65536, 40), (5000, 70000, 8), (700, 90, 1100)]
 
 
+@pytest.mark.parametrize("how", ["skewed", "one"])
+@pytest.mark.parametrize("rows", [8192, 8193, 32768, 32769])
+def test_gradient_around_changes_of_plan(rows, how):
+    """Where the list leaves one workgroup's LDS, and where its pieces become longer."""
+    from paper_2409_09083_amd import vocabulary
+    ids, dy = _ids(rows, 1500, how, torch.int64), _normal((rows, 40), "bf16", 3)
+    e = vocabulary.Embedding(rows, 1500, 40, "bf16", scale=1.7)
+    got = e.backward(ids, dy)
+    want, tol = _backward64(ids, dy, 1500, torch.tensor(1.7).double().item())
+    assert ((got.double() - want).abs() <= tol * 1.01 + 1e-7 * want.abs()).all()
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("how", ["any", "skewed", "one", "none"])
 @pytest.mark.parametrize("rows,vocab,channels", SIZES)

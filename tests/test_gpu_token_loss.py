@@ -94,6 +94,17 @@ def test_all_labelled(rows, vocab, channels, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("missing", [0.0, 0.4])
+@pytest.mark.parametrize("channels", [72, 128])
+@pytest.mark.parametrize("rows", [4, 5, 16, 17, 32, 33, 63, 64, 65])
+def test_few_rows(rows, channels, missing, dtype):
+    """Around the numbers of rows where the blocks' sizes and the joins of their statistics change, with x as it lies and gathered."""
+    from paper_2409_09083_amd import vocabulary
+    x, w, labels = _case(rows, 700, channels, dtype, missing, seed=5)
+    _check(vocabulary.TokenLoss(rows, 700, channels, dtype), x, w, labels, 1.0, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("missing", [0.3, 0.95, 1.1])
 @pytest.mark.parametrize("rows,vocab,channels", [(3, 50, 64), (20, 300, 96), (64, 513, 64), (200, 1000, 130), (1500, 260, 64)])
 def test_some_labelled(rows, vocab, channels, missing, dtype):
