@@ -5,7 +5,7 @@
 //
 // Rows without a label have no part in any of it: the others are gathered first (their number stays on the device), so that what the rows left out hold, NaN included, reaches nothing, and costs nothing.
 //
-// Measured: forward, bfloats, 11552 rows on 16384 x 512 193 us (logits 176: 1.10 PFLOP/s), 4 rows on 32768 x 512 12 (the weight read at 3.8 TB/s); backward, 11552 rows on 32768 x 1024 1.95 and 2.00 ms in two runs (logits 743, dx 653, dweight 599: 1.04,
+// Measured: forward, bfloats, 11552 rows on 16384 x 512 193 us (logits 176: 1.10 PFLOP/s), 4 rows on 32768 x 512 12 (the weight read at 3.8 TB/s); backward, 11552 rows on 32768 x 1024 1.95 to 2.03 ms in three runs (logits 743, dx 653, dweight 599: 1.04,
 // 1.19 and 1.29 PFLOP/s, the clock at 1.6 GHz), fp32, 2997 labelled rows of 4995 on 10007 x 202 369 us.
 #include "ftp_training.h"
 #include "ftp_product.h"
