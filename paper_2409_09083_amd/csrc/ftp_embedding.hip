@@ -4,7 +4,7 @@
 // stable), the sorted list is cut into pieces of 32 rows (8 of short lists), and a group of lanes adds up each run of equal ids inside its piece.  Runs that end inside the piece they began in go to the table; parts of longer ones go to scratch,
 // where a second kernel joins them in their order.  No atomics on sums; a frequent id is as many pieces as it has rows for.  The table is cleared beside the first pass of the sort, which leaves the memory idle.
 //
-// Measured: lookup of 46208 rows of 512 fp32 20.4 us (5.5 TB/s with the table in the caches); gradient of 92416 rows of 512 bfloats on 16384 ids 76 us: sort 32, runs 31, joins 9.5; 4995 rows of 250 fp32 24.
+// Measured: lookup of 46208 rows of 512 fp32 20.4 us (5.5 TB/s with the table in the caches); gradient of 92416 rows of 512 bfloats on 16384 ids 76 us: sort 33, runs 31, joins 7; 4995 rows of 250 fp32 24.
 #include "ftp_training.h"
 
 #include <algorithm>
