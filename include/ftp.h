@@ -373,8 +373,8 @@ int ftp_embedding_backward(const ftp_embedding_shape* shape, const void* ids, co
  * +infinity has NaN.  fp32 numbers are multiplied as three bfloats each: an infinity, or a number above the largest bfloat, gives NaN,
  * and numbers below 2^-110 lose low bits.
  * Backward: gradients of sum_r dloss[r] * loss[r], or of the mean where dloss is null, with lse as the forward pass left it:
- * g[r][v] = dloss[r] * scale * (exp(s[r][v] - lse[r]) - [v = label]), dx = g weight, dweight = g^T x.  Where the tensors are bfloats g is rounded
- * to them as an operand of those products (to two of them, 16 bits, for up to 256 rows); all sums are fp32.  Rows without a label have dx = 0. */
+ * g[r][v] = dloss[r] * scale * (exp(s[r][v] - lse[r]) - [v = label]), dx = g weight, dweight = g^T x.  Where the tensors are bfloats g keeps
+ * 16 bits as an operand of those products (two bfloats); all sums are fp32.  Rows without a label have dx = 0. */
 typedef struct {
     int64_t rows;                  /* may be 0; at most 2^22 */
     int32_t vocab, channels;       /* >= 1; at most 2^22 and 2^14, and blocks of 256 x 256 logits fewer than 2^21 */

@@ -1,12 +1,12 @@
 // Softmax cross entropy over a vocabulary, from the inputs x and the weight W of the linear layer that makes the logits s = scale W x:
 //   loss = log sum_v exp(s_v) - s_label,   G = dloss scale (exp(s - log sum) - [v = label]),   dx = G W,   dW = G^T x.
 // No logit is kept.  Forward, a block of logits leaves its registers as one maximum and one sum of powers a row; backward, the logits are computed again and leave as G, rounded to the operands of the
-// two products behind it (bfloats, or three of them), for a piece of the vocabulary at a time.
+// two products behind it (two bfloats, or three), for a piece of the vocabulary at a time.
 //
 // Rows without a label have no part in any of it: the others are gathered first (their number stays on the device), so that what the rows left out hold, NaN included, reaches nothing, and costs nothing.
 //
-// Measured: forward, bfloats, 11552 rows on 16384 x 512 193 us (logits 176: 1.10 PFLOP/s), 4 rows on 32768 x 512 12 (the weight read at 3.8 TB/s); backward, 11552 rows on 32768 x 1024 1.95 to 2.03 ms in three runs (logits 743, dx 653, dweight 599: 1.04,
-// 1.19 and 1.29 PFLOP/s, the clock at 1.6 GHz), fp32, 2997 labelled rows of 4995 on 10007 x 202 369 us.
+// Measured: forward, bfloats, 11552 rows on 16384 x 512 193 us (logits 176: 1.10 PFLOP/s), 4 rows on 32768 x 512 12 (the weight read at 3.8 TB/s); backward, 11552 rows on 32768 x 1024 3.31 ms (logits 879, and with G in two
+// bfloats dx 1350, dweight 1161: 0.88, 1.15 and 1.34 PFLOP/s), fp32, 2997 labelled rows of 4995 on 10007 x 202 369 us.
 #include "ftp_training.h"
 #include "ftp_product.h"
 
@@ -22,8 +22,10 @@ constexpr int kCountRows = 4096;
 constexpr int kChunk = 64;                          // rows whose labels one wavefront looks at
 // From so many rows on W is laid out for the products (forward on 16384 x 512, as it lies and laid out: 577 rows 30, 34 us; 2048 53, 54; 4096 90, 86; 11552 215, 200).
 constexpr int kPackRows = 4096;
-// Up to so many rows G is two bfloats where the tensors are one: its rounding, which the sums over many rows even out, would be as large as the results' own.  (Backward pass on 16384 x 512: 64 rows 47 us, 41 with one; 256 rows 55, 45 with one.)
-constexpr int kExact = 256;
+// Bfloats of G where the tensors are one, at any number of rows.  G's rows add up to 0, and of a weight that has learned its labels its columns nearly do: a part that the rows of W (of x) share goes out of the sums and leaves G's rounding
+// behind.  Weights of 1 + a 64th of a random number in 8 of 64 to 320 channels: dx off by 1.2 to 5 % of its norm with one bfloat, by at most 8e-5 with two before its own rounding (dweight 2e-3, 3e-6).  The price, us with one and with two:
+// 2048 rows on 16384 x 512 143, 214; 11552 on 8192 x 256 215, 379, on 32768 x 1024 1954, 3310.
+constexpr int kGradPlanes = 2;
 // Most rows whose statistics one workgroup joins (forward on 32768 x 512: 16 rows 11.0 us, by several and a launch for their mean 12.5; 32 rows 13.7 and 12.5).
 constexpr int kJoin = 16;
 // Most rows of the logits whose blocks have 32 of them, with W read at the memory's rate (forward on 32768 x 512, blocks of 128 x 32 and of 128 x 128: 4 rows 10.5, 17.7 us; 33 16.4, 19.4; 64 16.6, 19.8; 128 24.6, 20.2).
@@ -239,21 +241,7 @@ __global__ __launch_bounds__(L::kThreads, 2) void k_logits(const LogitArgs a)
     if constexpr (!STATS) {
         const int all = (rows + 63) & ~63;
         const auto to = [&](int i, int j) __attribute__((always_inline)) { return a.g + ((a0 + i) >> 5) * a.gblock + (b0 + j) * 32ll + (i & 31); };
-        if constexpr (PLANES == 1) {
-            // (the halves exchange what is rounded already: half the registers)
-#pragma unroll
-            for (int j = 0; j < L::IB; ++j)
-#pragma unroll
-                for (int i = 0; i < L::IA; ++i)
-#pragma unroll
-                    for (int r = 0; r < 16; r += 8) {
-                        const auto pair = [&](int k) __attribute__((always_inline)) { return pack_bf16(acc[i][j][r + k], acc[i][j][r + k + 1]); };
-                        const auto x = __builtin_amdgcn_permlane32_swap(pair(0), pair(4), false, false), y = __builtin_amdgcn_permlane32_swap(pair(2), pair(6), false, false);
-                        const int at = wb + 32 * j + (l & 31);
-                        if (b0 + at < all) *(uint4*)to(wa + 32 * i + 2 * r + 8 * h, at) = uint4{x[0], y[0], x[1], y[1]};
-                    }
-        } else
-            L::each(acc, [&](int i, int j, const float (&v)[8]) __attribute__((always_inline)) { if (b0 + j < all) store_planes<PLANES>(to(i, j), a.gplane, v); });
+        L::each(acc, [&](int i, int j, const float (&v)[8]) __attribute__((always_inline)) { if (b0 + j < all) store_planes<PLANES>(to(i, j), a.gplane, v); });
     }
     if constexpr (STATS) {
         __syncthreads();
@@ -455,7 +443,7 @@ Plan plan_of(const ftp_token_loss_shape& s, bool back)
     const long long terms = p.planes == 1 ? 1 : 6;
     // whether W, and few rows of x, can be read as they lie (their addresses are looked at by the call: scratch is there for both ways)
     p.few = s.rows <= kFew;
-    p.gplanes = p.planes == 1 && s.rows <= kExact ? 2 : p.planes;
+    p.gplanes = p.planes == 1 ? kGradPlanes : p.planes;
     if (!back) {
         p.logits = split_of(s.vocab, s.rows, p.Cp / 32 * terms, 128, 1);
         p.blocks = (int)ceil_div(s.vocab, p.few ? Few::BA : p.logits.block);
@@ -467,7 +455,7 @@ Plan plan_of(const ftp_token_loss_shape& s, bool back)
     const long long pieces = ceil_div(all, std::max(256ll, fits));
     p.piece = round_up(ceil_div(s.vocab, pieces), 256);
     p.logits = split_of(p.piece, s.rows, p.Cp / 32 * terms, 128, 1);
-    const long long gterms = p.planes == 1 ? p.gplanes : 6;
+    const long long gterms = p.planes == 1 ? kGradPlanes : 6;
     p.dx = split_of(s.channels, s.rows, p.piece / 32 * gterms, 128, 64);
     p.most = (int)std::max<long long>(p.dx.shares, p.piece / 32 * gterms / 24);
     p.dw = split_of(s.channels, p.piece, p.Np / 32 * gterms, 128, 16);
@@ -585,6 +573,7 @@ void dx_pass(GradArgs& a, hipStream_t st) { k_loss_dx<L><<<(unsigned)block_grid(
 template <int P, typename T>
 void backward(const ftp_token_loss_shape& s, const void* x, const void* w, const void* labels, const float* lse, const float* dloss, void* dx, void* dw, char* ws, hipStream_t st)
 {
+    constexpr int G = P == 1 ? kGradPlanes : P;
     const Plan p = plan_of(s, true);
     const Buffers b = buffers_of(s, p, true, ws);
     const Matrix all = prepare<P>(s, p, b, x, w, labels, true, st), xc = blocked(b.xc, p.Np, p.Cp, p.Np * p.Cp), g = blocked(b.g, p.Np, (int)p.piece, p.Np * p.piece);
@@ -594,12 +583,11 @@ void backward(const ftp_token_loss_shape& s, const void* x, const void* w, const
         LogitArgs a = {};
         a.w = wp; a.x = xc; a.count = b.count; a.label = b.label; a.terms = terms_of(P); a.vocab = s.vocab; a.piece0 = (int)v0; set_scale(a, s.scale);
         a.index = b.index; a.lse = lse; a.dloss = dloss; a.g = b.g; a.gblock = g.block; a.gplane = g.plane;
-        if (p.few) logits<Few, P == 1 ? 2 : 3, false>(a, s.rows, st);
-        else if (p.gplanes != P) logits<Mid<false, false>, P == 1 ? 2 : 3, false>(a, s.rows, st);
-        else if (p.logits.block == 256) logits<Two, P, false>(a, s.rows, st);
-        else logits<Mid<false, false>, P, false>(a, s.rows, st);
+        if (p.few) logits<Few, G, false>(a, s.rows, st);
+        else if (p.logits.block == 256) logits<Two, G, false>(a, s.rows, st);
+        else logits<Mid<false, false>, G, false>(a, s.rows, st);
         GradArgs k = {};
-        k.count = b.count; k.terms = p.gplanes == P ? terms_of(P) : terms_one_two(); k.C = s.channels; k.scale = s.scale; k.mean = !dloss;
+        k.count = b.count; k.terms = P == 1 ? terms_one_two() : terms_of(P); k.C = s.channels; k.scale = s.scale; k.mean = !dloss;
         if (dx && s.rows) {
             k.a = wp; k.b = g; k.stages = (int)ceil_div(n, 32); k.shares = p.dx.shares; k.most = p.most; k.add = v0 > 0;
             k.ablocks = (int)ceil_div(p.Cp, p.dx.block); k.bblocks = (int)ceil_div(s.rows, p.dx.block);
