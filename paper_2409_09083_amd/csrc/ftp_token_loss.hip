@@ -327,7 +327,7 @@ struct GradArgs {
     float* part;                                    // sums: [share][block along b][block along a]
     void* out; long long ostride; int C; float scale; int mean;
     int ids;                                        // dw: of the piece
-    const int* place; const int* index; int rows, summing;     // dx
+    const int* place; const int* index; int rows, first, summing;          // dx; first, summing: parts of a launch of the sums
 };
 
 __device__ __forceinline__ float gradient_scale(float scale, int mean, const int* count)
@@ -381,7 +381,7 @@ __global__ __launch_bounds__(L::kThreads, 2) void k_loss_dw(const GradArgs a)
     });
 }
 
-// dx from the shares' sums, each in its row's place; rows without a label are zeros (the workgroups from `summing` on).
+// dx from the shares' sums, each in its row's place; rows without a label are zeros (the last launch's workgroups from `summing` on).
 template <class L, typename T>
 __global__ __launch_bounds__(256) void k_loss_dx_sum(const GradArgs a)
 {
@@ -397,10 +397,10 @@ __global__ __launch_bounds__(256) void k_loss_dx_sum(const GradArgs a)
         return;
     }
     const int rows = *a.count, bblocks = dx_blocks(rows, L::BB), shares = dx_shares(rows, L::BB, a.bblocks * a.shares, a.most);
-    const int t = blockIdx.x / L::kParts, ib = t / a.ablocks, ia = t - ib * a.ablocks, a0 = ia * L::BA, b0 = ib * L::BB;
+    const int part = a.first + (int)blockIdx.x, t = part / L::kParts, ib = t / a.ablocks, ia = t - ib * a.ablocks, a0 = ia * L::BA, b0 = ib * L::BB;
     if (b0 >= rows) return;
     const float f = gradient_scale(a.scale, a.mean, a.count);
-    L::take(a.part + (long long)t * L::kSums, (long long)bblocks * a.ablocks * L::kSums, shares, blockIdx.x - t * L::kParts, [&](int i, int j, float (&v)[8]) __attribute__((always_inline)) {
+    L::take(a.part + (long long)t * L::kSums, (long long)bblocks * a.ablocks * L::kSums, shares, part - t * L::kParts, [&](int i, int j, float (&v)[8]) __attribute__((always_inline)) {
         if (b0 + j >= rows || a0 + i >= a.C) return;
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] *= f;
@@ -564,8 +564,13 @@ void dw_pass(GradArgs& a, hipStream_t st)
 template <class L, typename T>
 void dx_sum(GradArgs& a, hipStream_t st)
 {
-    a.summing = a.ablocks * a.bblocks * L::kParts;
-    k_loss_dx_sum<L, T><<<(unsigned)a.summing + std::min<unsigned>(pass_grid(a.rows * ceil_div(a.C, 8)), 1024), 256, 0, st>>>(a);
+    // a launch has less than 2^32 threads: from 2^34 results on it takes several, the last of which clears the rows without a label
+    const unsigned clearing = std::min<unsigned>(pass_grid(a.rows * ceil_div(a.C, 8)), 1024);
+    const int all = a.ablocks * a.bblocks * L::kParts, most = (int)(kMostGroups - clearing);
+    for (a.first = 0; a.first < all; a.first += a.summing) {
+        a.summing = std::min(all - a.first, most);
+        k_loss_dx_sum<L, T><<<(unsigned)a.summing + (a.first + a.summing == all ? clearing : 0), 256, 0, st>>>(a);
+    }
 }
 template <class L>
 void dx_pass(GradArgs& a, hipStream_t st) { k_loss_dx<L><<<(unsigned)block_grid(a.ablocks, (long long)a.bblocks * a.shares), L::kThreads, 0, st>>>(a); }

@@ -77,3 +77,29 @@ def test_gradients_that_cancel(rows, vocab, channels, missing, weighted, dtype):
         one = g.float().bfloat16().double()
         assert _outside((one @ w.double()).bfloat16(), want_dx) > 0
         assert _outside((one.t().contiguous() @ x[there].double()).bfloat16(), want_dw) > 0
+
+
+def test_more_results_than_one_launch_sums():
+    """2^21 rows of 8192 channels, one row of x for all of them, and 2^21 * 8192 / 4 = 2^32 threads that add up dx' shares: more than a launch has.  140 GB of dx and scratch.  Rows of one
+    label are equal bit by bit, those of the first 256 are checked against the formula, those without a label are zeros."""
+    from paper_2409_09083_amd import vocabulary
+    rows, vocab, channels, none = 1 << 21, 256, 1 << 13, 7
+    g = torch.Generator().manual_seed(3)
+    x = torch.randn((1, channels), generator=g).bfloat16().cuda().expand(rows, channels)
+    w = (torch.randn((vocab, channels), generator=g) * channels ** -0.5).bfloat16().cuda()
+    labels = torch.arange(rows, device="cuda") % vocab
+    labels[none::vocab] = -1
+    head = vocabulary.TokenLoss(rows, vocab, channels, "bf16")
+    try:
+        head.forward(x, w, labels)
+        for t in head.dx.split(1 << 18):
+            t.fill_(float("nan"))
+        dx, _ = head.backward(x, w, labels, torch.ones(rows, device="cuda"))
+        first = dx[:vocab].clone()
+        there, _, want, _ = _bounds(x[:vocab], w, labels[:vocab], "bf16", torch.ones(vocab, device="cuda"))
+        assert _outside(first[there], want) == 0 and not first[none].any()
+        for t in dx.view(-1, vocab, channels).split(256):
+            assert bool((t == first).all())
+    finally:
+        del head
+        torch.cuda.empty_cache()
