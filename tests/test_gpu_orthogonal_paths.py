@@ -1,0 +1,105 @@
+"""Orthogonal updates on each of the ways that a size may take: all steps in one launch (a side of at most 64, the other at most 256; one, two or four blocks of 64), a launch a step (longer ones; above 2048
+several blocks a workgroup), three products a step (both sides above 64).  What the header promises holds on all of them.  Bounds as in test_gpu_orthogonal.py."""
+import math
+
+import pytest
+import torch
+
+from tests.test_gpu_orthogonal import HELD, LAST, TYPES, U, _matrix, _one_step_bound, _steps
+
+pytestmark = pytest.mark.gpu
+ONE = [(40, 50), (64, 128), (117, 33), (50, 190), (64, 256), (256, 64), (193, 64)]
+EACH = [(64, 257), (576, 50), (64, 2049), (4608, 64), (20, 9000)]
+GENERAL = [(65, 65), (133, 307), (307, 133), (640, 200)]
+PATHS = [(40, 70), (64, 256), (256, 60), (64, 576), (576, 50), (33, 2500), (133, 307), (307, 133)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,cols", ONE + EACH + GENERAL + [(32768, 64), (7, 32768)])
+def test_one_step(rows, cols, dtype):
+    from paper_2409_09083_amd import orthogonal
+    x = _matrix(2, rows, cols, dtype, seed=21)
+    got = orthogonal.Orthogonal(rows, cols, dtype, count=2, steps=1).forward(x)
+    for m in range(2):
+        want, tol = _steps(x[m], 1), _one_step_bound(x[m], dtype)
+        assert ((got[m].double() - want).abs() <= tol + LAST[dtype] * (want.abs() + tol) + 1e-37).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,cols", ONE + EACH + GENERAL)
+def test_several_steps(rows, cols, dtype):
+    from paper_2409_09083_amd import orthogonal
+    x = _matrix(2, rows, cols, dtype, seed=22)
+    h = HELD[dtype]
+    for steps in (2, 5):
+        o = orthogonal.Orthogonal(rows, cols, dtype, count=2, steps=steps)
+        got = o.forward(x).clone()
+        o._ws.fill_(255)                                        # scratch need not be cleared
+        assert torch.equal(o.forward(x), got)
+        for m in range(2):
+            g = torch.Generator(device="cuda").manual_seed(m)
+
+            def some(v):
+                return 2 * torch.rand(v.shape, generator=g, device="cuda", dtype=torch.float64) - 1
+
+            def noise(v, k=0, size=None):
+                if size is not None:
+                    v = v + some(v) * (math.sqrt(k) * U + 2 * h) * size
+                return v * (1 + (h + U) * some(v))
+            want = _steps(x[m], steps)
+            off = max(float((_steps(x[m], steps, noise=noise) - want).norm()) for _ in range(3))
+            assert float((got[m].double() - want).norm()) <= 8 * off + LAST[dtype] * float(want.norm())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,cols", PATHS)
+def test_special_matrices(rows, cols, dtype):
+    """A zero matrix, one with a NaN, one with an infinity among others of a call; scales whose squares 32 bits do not hold."""
+    from paper_2409_09083_amd import orthogonal
+    x = _matrix(5, rows, cols, dtype, seed=23)
+    o = orthogonal.Orthogonal(rows, cols, dtype, count=5)
+    want = o.forward(x).clone()
+    x[1] = 0
+    x[2, rows - 1, cols // 2] = math.nan
+    x[3, 0, cols - 1] = -math.inf
+    got = o.forward(x)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[4], want[4]) and not got[1].any() and got[2].isnan().all() and got[3].isnan().all()
+    one = orthogonal.Orthogonal(rows, cols, dtype, eps=0.0)
+    y = _matrix(1, rows, cols, dtype, seed=24)[0]
+    want = one.forward(y).clone()
+    for scale in (2.0 ** 100, 2.0 ** -90):
+        assert torch.equal(one.forward(y * scale), want)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,cols", PATHS)
+def test_strides_in_place_and_graph(rows, cols, dtype):
+    from paper_2409_09083_amd import binding as B
+    from paper_2409_09083_amd import orthogonal
+    x = _matrix(3, rows, cols, dtype, seed=25)
+    o = orthogonal.Orthogonal(rows, cols, dtype, count=3)
+    want = o.forward(x).clone()
+    around = torch.full((3 * (rows + 3) * (cols + 7) + 1,), math.nan, dtype=x.dtype, device="cuda")
+    v = around[1:].view(3, rows + 3, cols + 7)[:, :rows, :cols]
+    v.copy_(x)
+    assert torch.equal(o.forward(v), want)
+    assert torch.equal(o.forward(x[1:2].expand(3, rows, cols))[2], want[1])
+    same = x[:, :1].expand(3, rows, cols)                       # all rows of a matrix one row of memory
+    assert torch.equal(o.forward(same).clone(), o.forward(same.contiguous()))
+    y = x.clone()
+    B.ftp_orthogonal(o.desc, y.data_ptr(), y.data_ptr(), o._ws.data_ptr(), torch.cuda.current_stream().cuda_stream)
+    assert torch.equal(y, want)
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        o.forward(x)
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=side):
+        o.forward(x)
+    for k in range(4):
+        x.copy_(_matrix(3, rows, cols, dtype, seed=30 + k))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = o.out.clone()
+        assert torch.equal(o.forward(x), got)
+        torch.cuda.synchronize()
