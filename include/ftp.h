@@ -398,7 +398,7 @@ int ftp_token_loss_backward(const ftp_token_loss_shape* shape, const void* x, co
 
 /* The orthogonal part of a matrix, nearly, by Newton-Schulz steps: with X = x / (|x| + eps), |x| the root of the sum of its squares,
  * `steps` times X <- a X + (b S + c S^2) X, S = X X^T (with rows > cols the same as X (b S + c S^2), S = X^T X).  With (a, b, c) =
- * (3.4445, -4.775, 2.0315) and 5 steps singular values above a thousandth of |x| end between 0.6 and 1.3.
+ * (3.4445, -4.775, 2.0315) and 5 steps singular values from 0.0014 of |x| on end between 0.6 and 1.3.
  * Products, their sums and the norm are held in 32 bits or more; between them FTP_F32 keeps 24 bits of a number (three bfloats), FTP_BF16 16 (two).  One
  * call takes `count` matrices of one size.  A matrix with an infinity or a NaN becomes NaN. */
 typedef struct {

@@ -1,11 +1,13 @@
 """Orthogonal updates on each of the ways that a size may take: all steps in one launch (a side of at most 64, the other at most 256; one, two or four blocks of 64), a launch a step (longer ones; above 2048
 several blocks a workgroup), three products a step (both sides above 64).  What the header promises holds on all of them.  Bounds as in test_gpu_orthogonal.py."""
 import math
+import os
+import re
 
 import pytest
 import torch
 
-from tests.test_gpu_orthogonal import HELD, LAST, TYPES, U, _matrix, _one_step_bound, _steps
+from tests.test_gpu_orthogonal import ABC, HELD, LAST, TYPES, U, _matrix, _one_step_bound, _steps
 
 pytestmark = pytest.mark.gpu
 ONE = [(40, 50), (64, 128), (117, 33), (50, 190), (64, 256), (256, 64), (193, 64)]
@@ -103,3 +105,42 @@ def test_strides_in_place_and_graph(rows, cols, dtype):
         got = o.out.clone()
         assert torch.equal(o.forward(x), got)
         torch.cuda.synchronize()
+
+
+def _promise():
+    """The header's words on where singular values end: (smallest share of |x|, least, most)."""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    with open(os.path.join(root, "include", "ftp.h")) as f:
+        return tuple(map(float, re.search(r"singular values from ([\d.]+) of \|x\| on end between ([\d.]+) and ([\d.]+)\.\s", f.read()).groups()))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,cols", [(40, 70), (64, 576), (133, 307), (307, 133)])
+def test_singular_values_at_the_stated_limit(rows, cols, dtype):
+    """One entry a row and column: the singular values are those, down to the smallest number of the type that is not below the limit."""
+    from paper_2409_09083_amd import orthogonal
+    limit, least, most = _promise()
+    n = min(rows, cols)
+    values = torch.logspace(0, -2, n, dtype=torch.float64).to(TYPES[dtype])
+    values[-1] = 0
+    low = (limit * values.double().norm() / math.sqrt(1 - limit ** 2)).to(TYPES[dtype])
+    while float(low) < limit * float(torch.cat((values.double(), low.double()[None])).norm()):
+        low = torch.nextafter(low, torch.tensor(1.0, dtype=TYPES[dtype]))
+    values[-1] = low
+    g = torch.Generator().manual_seed(4)
+    at, to = torch.randperm(rows, generator=g)[:n], torch.randperm(cols, generator=g)[:n]
+    x = torch.zeros((rows, cols), dtype=TYPES[dtype])
+    x[at, to] = values
+    got = orthogonal.Orthogonal(rows, cols, dtype).forward(x.cuda()).double().cpu()
+    ends = got[at, to]
+    rest = got.clone()
+    rest[at, to] = 0
+    assert not rest.any() and least <= float(ends.min()) and float(ends.max()) <= most
+    # and the limit is one: what the polynomial makes of it and of a tenth less
+    a, b, c = ABC
+
+    def end(v):
+        for _ in range(5):
+            v = a * v + b * v ** 3 + c * v ** 5
+        return v
+    assert least <= end(limit) and min(end(limit * 10 ** (k / 1000)) for k in range(2853)) >= least > end(0.9 * limit)
