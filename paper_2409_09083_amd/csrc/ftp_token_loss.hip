@@ -158,7 +158,7 @@ struct LogitArgs {
     Terms terms;
     int wide, stages, vocab, ablocks, bblocks;
     int piece0;                                     // the piece's first id
-    float c; int negate;                            // |scale| * log2(e), and whether scale is negative
+    float c, factor;                                // products become powers of 2 by c, after the factor: 1, or -1 for a negative scale, smaller where c would be too small a number
     float2* part; float* target;                    // forward: [row][ablocks] maximum and sum of a block's powers of 2; the labels' products
     const int* index; const float* lse; const float* dloss;     // backward
     bf16_t* g; long long gblock, gplane;            // G, as a Matrix lies
@@ -181,8 +181,8 @@ __global__ __launch_bounds__(L::kThreads, 2) void k_logits(const LogitArgs a)
         L::run(acc, a.w, a.x, a0, b0, 0, a.stages, a.terms, s0, s1, s2, s3);
     }
     const int l = threadIdx.x & 63, h = l >> 5, wa = L::wave_a(), wb = L::wave_b();
-    if (a.negate)
-        L::all(acc, [&](float& v, int) __attribute__((always_inline)) { v = -v; });
+    if (a.factor != 1.0f)
+        L::all(acc, [&](float& v, int) __attribute__((always_inline)) { v *= a.factor; });
     const int left = (int)a.w.rows - a0 - wa;                      // ids of the piece from this wavefront's first one on
     if (left < 32 * L::IA)                                          // (no power of those past its end)
         L::all(acc, [&](float& v, int at) __attribute__((always_inline)) { v = at + 4 * h < left ? v : -INFINITY; });
@@ -330,9 +330,16 @@ struct GradArgs {
     const int* place; const int* index; int rows, first, summing;          // dx; first, summing: parts of a launch of the sums
 };
 
-__device__ __forceinline__ float gradient_scale(float scale, int mean, const int* count)
+// The factor of the products' sums, as a number below 1 and a power of 2: in one float, a small scale's share of the rows lost its low bits.
+struct Factor {
+    float part; int power;
+    __device__ __forceinline__ float operator()(float v) const { return ldexpf(v * part, power); }
+};
+__device__ __forceinline__ Factor gradient_scale(float scale, int mean, const int* count)
 {
-    return !mean ? scale : *count ? scale / (float)*count : 0.0f;
+    int power;
+    const float part = (float)frexp(!mean ? (double)scale : *count ? (double)scale / *count : 0.0, &power);
+    return Factor{__uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(part))), __builtin_amdgcn_readfirstlane(power)};
 }
 
 // Shares of the contraction where `rows` of the rows that the launch is made for have labels: as many as the launch has workgroups (all) for, at most `most`.
@@ -366,7 +373,7 @@ __global__ __launch_bounds__(L::kThreads, 2) void k_loss_dw(const GradArgs a)
     f32x16 acc[L::IA][L::IB] = {};
     const int lo = (int)((long long)stages * share / a.shares), hi = (int)((long long)stages * (share + 1) / a.shares);
     L::run(acc, a.a, a.b, a0, b0, lo, hi, a.terms, s0, s1, s2, s3);
-    const float f = gradient_scale(a.scale, a.mean, a.count);
+    const Factor f = gradient_scale(a.scale, a.mean, a.count);
     if (a.shares > 1) {
         L::put(acc, a.part + ((long long)ib * a.ablocks + ia) * L::kSums, false);
         return;
@@ -376,7 +383,7 @@ __global__ __launch_bounds__(L::kThreads, 2) void k_loss_dw(const GradArgs a)
         if (a0 + i >= a.C || id >= a.ids) return;
         float w[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) w[e] = v[e] * f;
+        for (int e = 0; e < 8; ++e) w[e] = f(v[e]);
         store8((T*)a.out + id * a.ostride + a0 + i, a.C - a0 - i, w);
     });
 }
@@ -399,11 +406,11 @@ __global__ __launch_bounds__(256) void k_loss_dx_sum(const GradArgs a)
     const int rows = *a.count, bblocks = dx_blocks(rows, L::BB), shares = dx_shares(rows, L::BB, a.bblocks * a.shares, a.most);
     const int part = a.first + (int)blockIdx.x, t = part / L::kParts, ib = t / a.ablocks, ia = t - ib * a.ablocks, a0 = ia * L::BA, b0 = ib * L::BB;
     if (b0 >= rows) return;
-    const float f = gradient_scale(a.scale, a.mean, a.count);
+    const Factor f = gradient_scale(a.scale, a.mean, a.count);
     L::take(a.part + (long long)t * L::kSums, (long long)bblocks * a.ablocks * L::kSums, shares, part - t * L::kParts, [&](int i, int j, float (&v)[8]) __attribute__((always_inline)) {
         if (b0 + j >= rows || a0 + i >= a.C) return;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] *= f;
+        for (int e = 0; e < 8; ++e) v[e] = f(v[e]);
         store8((T*)a.out + a.index[b0 + j] * a.ostride + a0 + i, a.C - a0 - i, v);
     });
 }
@@ -412,11 +419,11 @@ template <class L, typename T>
 __global__ __launch_bounds__(256) void k_loss_dw_sum(const GradArgs a)
 {
     const int t = blockIdx.x / L::kParts, ib = t / a.ablocks, ia = t - ib * a.ablocks, a0 = ia * L::BA, b0 = ib * L::BB;
-    const float f = gradient_scale(a.scale, a.mean, a.count);
+    const Factor f = gradient_scale(a.scale, a.mean, a.count);
     L::take(a.part + (long long)t * L::kSums, (long long)a.bblocks * a.ablocks * L::kSums, a.shares, blockIdx.x - t * L::kParts, [&](int i, int j, float (&v)[8]) __attribute__((always_inline)) {
         if (b0 + j >= a.ids || a0 + i >= a.C) return;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] *= f;
+        for (int e = 0; e < 8; ++e) v[e] = f(v[e]);
         store8((T*)a.out + (long long)(b0 + j) * a.ostride + a0 + i, a.C - a0 - i, v);
     });
 }
@@ -518,8 +525,10 @@ Matrix prepare(const ftp_token_loss_shape& s, const Plan& p, const Buffers& b, c
 
 void set_scale(LogitArgs& a, float scale)
 {
-    a.c = std::max(std::fabs(scale) * kLog2e, 1e-38f);              // (0 times -infinity, ids past the end, would be no number)
-    a.negate = scale < 0;
+    // (c is a normal number and not 0, which times -infinity, ids past the end, would be none)
+    const double c = std::fabs((double)scale) * 1.4426950408889634, least = 1e-30;
+    a.c = (float)std::max(c, least);
+    a.factor = (float)std::copysign(std::min(c / least, 1.0), (double)scale);
 }
 
 template <class L, int P, bool STATS>
