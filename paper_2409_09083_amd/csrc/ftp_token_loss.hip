@@ -547,10 +547,11 @@ void forward(const ftp_token_loss_shape& s, const void* x, const void* w, const 
     const Buffers b = buffers_of(s, p, false, ws);
     LogitArgs a = {};
     a.terms = terms_of(P); a.wide = s.id_type; a.vocab = s.vocab; set_scale(a, s.scale); a.part = b.part; a.target = b.target; a.ids = labels;
-    const bool plain = p.few && P == 1 && s.channels % 64 == 0 && (s.x_stride % 8 == 0 || s.rows <= 1) && s.x_stride < (1 << 20) && aligned(x, 16);
+    const long long x_stride = s.rows > 1 ? s.x_stride : s.channels;        // (one row's is no rows' distance: loads of the rows past it would lie on any address)
+    const bool plain = p.few && P == 1 && s.channels % 64 == 0 && x_stride % 8 == 0 && x_stride < (1 << 20) && aligned(x, 16);
     a.w = prepare<P>(s, p, b, x, w, labels, !plain, st);
     a.w.rows = s.vocab;
-    if (plain) a.x = row_major((const bf16_t*)x, s.x_stride, s.rows, p.Cp);
+    if (plain) a.x = row_major((const bf16_t*)x, x_stride, s.rows, p.Cp);
     else {
         a.x = blocked(b.xc, p.Np, p.Cp, p.Np * p.Cp);
         a.count = b.count; a.label = b.label;
