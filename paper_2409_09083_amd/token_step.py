@@ -129,7 +129,8 @@ class Codes:
     def enter(self, y):
         """The map [batch][channels][places] with the known codes' rows added."""
         b, c = y.shape[:2]
-        return y.view(b, c, -1) + self.embedding.forward(self.ids, self.table).view(b, -1, c).transpose(1, 2)
+        self.map = y.view(b, c, -1) + self.embedding.forward(self.ids, self.table).view(b, -1, c).transpose(1, 2)
+        return self.map
 
     def forward(self, z):
         """The mean cross entropy of the labelled places (a number on the device); z: the block's output rows."""
@@ -148,6 +149,11 @@ class Codes:
     def update(self, lr):
         self.table.add_(self.grad.to(self.table.dtype), alpha=-lr)
 
+    def other_bytes(self):
+        """As TokenBlock.other_bytes: the block's input and output, losses and log-sums; the buffers of rows, gradients and scratch (the loss' is the largest: its gradient by the logits)."""
+        e, h = self.embedding, self.head
+        return sum(t.nbytes for t in (self.map, self.z, h.losses, h.lse, h.mean)), sum(t.nbytes for t in (e.out, e.dtable, e._ws, h.dx, h.dweight, h._ws))
+
 
 class OrthogonalUpdate:
     """Weights [n][k] moved along the orthogonal part of their gradients' running sum (momentum), a step of about lr for every singular direction."""
@@ -161,6 +167,10 @@ class OrthogonalUpdate:
         for n, w in self.weights.items():
             total = self.sums[n].mul_(self.momentum).add_(grads[n])
             w.add_(self.parts[n].forward(total).to(w.dtype), alpha=-lr * max(1.0, w.shape[0] / w.shape[1]) ** 0.5)
+
+    def other_bytes(self):
+        """As TokenBlock.other_bytes: the gradients' sums; the buffers of their orthogonal parts and scratch."""
+        return sum(t.nbytes for t in self.sums.values()), sum(p.out.nbytes + p._ws.nbytes for p in self.parts.values())
 
 
 class TokenStep:
@@ -209,6 +219,11 @@ class TokenStep:
             self.block.update(lr)
         return loss
 
+    def other_bytes(self):
+        """What stays beside the 8-bit checkpoints: of the block, the codes and the orthogonal updates, after a step."""
+        parts = [p.other_bytes() for p in (self.block, self.codes, self.matrices) if p]
+        return tuple(map(sum, zip(*parts)))
+
 
 def main(argv=None):
     p = argparse.ArgumentParser(description=__doc__.split("\n")[0])
@@ -232,8 +247,9 @@ def main(argv=None):
         end.synchronize()
         print("step %d: loss %.5f, %.2f ms" % (i, float(loss), start.elapsed_time(end)))
     held, plain = s.block.kept_bytes()
-    tensors, buffers = s.block.other_bytes()
-    print("kept between the passes: %.1f MB in 8 bits for %.1f MB, and %.1f MB of q, k, v, attention's output and statistics" % (held / 1e6, plain / 1e6, tensors / 1e6))
+    tensors, buffers = s.other_bytes()
+    named = "q, k, v, attention's output and statistics" + (", the block's input and output and the losses" if s.codes else "") + (", the gradients' sums" if s.matrices else "")
+    print("kept between the passes: %.1f MB in 8 bits for %.1f MB, and %.1f MB of %s" % (held / 1e6, plain / 1e6, tensors / 1e6, named))
     print("buffers of gradients and scratch: %.1f MB" % (buffers / 1e6))
 
 
