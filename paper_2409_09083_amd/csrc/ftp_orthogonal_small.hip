@@ -1,4 +1,4 @@
-// Newton-Schulz steps of matrices with a side of at most 64, one launch a step or one for all: a chain of latencies, not of work.
+// Newton-Schulz steps of matrices with a side of at most 64, one launch a step or one for all: a chain of latencies, not of work (which ones: ftp_orthogonal.h).
 //
 // X lies as m x L, m <= 64 (a tall matrix transposed), in blocks of 64 columns that belong to one workgroup from step to step.  A step's workgroup adds up the parts of S = X X^T that the workgroups of the step before left, makes
 // a I + b S + c S^2 of it in LDS (each for itself: 24 matrix instructions a wavefront), multiplies its blocks with that, and takes their part of the next S from the result while it is in LDS.
@@ -10,8 +10,6 @@
 namespace ftp {
 namespace {
 
-// Most blocks that one workgroup takes through all steps (fp32, so and with a launch a step: 60 x 50 20, 43 us; 64 x 128 29, 46; 64 x 256 48.6, 48.9; 8 x 256 x 50 42, 61).
-constexpr int kWhole = 4;
 constexpr int kSide = 64, kTile = kSide * kSide * 2;           // bytes of a plane of 64 x 64
 
 // 16 bytes (8 columns: chunk) of a row: neither 16 rows of one chunk nor the transposing load's 4 rows x 64 bytes meet on the banks.

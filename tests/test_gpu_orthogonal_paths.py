@@ -1,5 +1,5 @@
-"""Orthogonal updates on each of the ways that a size may take: all steps in one launch (a side of at most 64, the other at most 256; one, two or four blocks of 64), a launch a step (longer ones; above 2048
-several blocks a workgroup), three products a step (both sides above 64).  What the header promises holds on all of them.  Bounds as in test_gpu_orthogonal.py."""
+"""Orthogonal updates on each of the ways that a size may take: all steps in one launch (a side of at most 64, the other at most 256; one, two or four blocks of 64), a launch a step (longer ones, where their blocks
+are few, or many and long; several blocks a workgroup above 2048), three products a step (the others).  What the header promises holds on all of them.  Bounds as in test_gpu_orthogonal.py."""
 import math
 import os
 import re
@@ -51,6 +51,42 @@ def test_several_steps(rows, cols, dtype):
             want = _steps(x[m], steps)
             off = max(float((_steps(x[m], steps, noise=noise) - want).norm()) for _ in range(3))
             assert float((got[m].double() - want).norm()) <= 8 * off + LAST[dtype] * float(want.norm())
+
+
+# a launch a step: few blocks in all, up to three a workgroup; many and long, 6 and 16 a workgroup.  Beside them those that go as three products instead
+NUMBERS = [(1, 64, 4608), (1, 6144, 64), (1, 64, 6145), (2, 30, 3072), (2, 3073, 64), (16, 64, 384), (17, 64, 384), (22, 64, 12000), (21, 64, 12000), (8, 32768, 50), (7, 32768, 50)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("count,rows,cols", NUMBERS)
+def test_numbers_of_matrices_where_the_way_turns(count, rows, cols, dtype):
+    from paper_2409_09083_amd import orthogonal
+    x = _matrix(count, rows, cols, dtype, seed=26)
+    one = orthogonal.Orthogonal(rows, cols, dtype, count=count, steps=1).forward(x).clone()
+    o = orthogonal.Orthogonal(rows, cols, dtype, count=count)
+    got = o.forward(x).clone()
+    o._ws.fill_(255)
+    assert torch.equal(o.forward(x), got)
+    x[count - 1, 3, 5] = math.nan
+    o._ws.fill_(255)
+    bad = o.forward(x)
+    assert bad[count - 1].isnan().all() and (count == 1 or torch.equal(bad[:-1], got[:-1]))
+    for m in sorted({0, (count - 1) // 2, max(count - 2, 0)}):
+        y = _matrix(count, rows, cols, dtype, seed=26)[m]
+        want, tol = _steps(y, 1), _one_step_bound(y, dtype)
+        assert ((one[m].double() - want).abs() <= tol + LAST[dtype] * (want.abs() + tol) + 1e-37).all()
+        h, g = HELD[dtype], torch.Generator(device="cuda").manual_seed(m)
+
+        def some(v):
+            return 2 * torch.rand(v.shape, generator=g, device="cuda", dtype=torch.float64) - 1
+
+        def noise(v, k=0, size=None):
+            if size is not None:
+                v = v + some(v) * (math.sqrt(k) * U + 2 * h) * size
+            return v * (1 + (h + U) * some(v))
+        want = _steps(y, 5)
+        off = max(float((_steps(y, 5, noise=noise) - want).norm()) for _ in range(3))
+        assert float((got[m].double() - want).norm()) <= 8 * off + LAST[dtype] * float(want.norm())
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
