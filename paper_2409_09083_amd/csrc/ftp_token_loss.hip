@@ -5,8 +5,8 @@
 //
 // Rows without a label have no part in any of it: the others are gathered first (their number stays on the device), so that what the rows left out hold, NaN included, reaches nothing, and costs nothing.
 //
-// Measured: forward, bfloats, 11552 rows on 16384 x 512 193 us (logits 176: 1.10 PFLOP/s), 4 rows on 32768 x 512 12 (the weight read at 3.8 TB/s); backward, 11552 rows on 32768 x 1024 3.31 ms (logits 879, and with G in two
-// bfloats dx 1350, dweight 1161: 0.88, 1.15 and 1.34 PFLOP/s), fp32, 2997 labelled rows of 4995 on 10007 x 202 369 us.
+// Measured: forward, bfloats, 11552 rows on 16384 x 512 193 us (logits 176: 1.10 PFLOP/s), 4 rows on 32768 x 512 12 (the weight read at 3.8 TB/s); backward, 11552 rows on 32768 x 1024 3.31 to 3.41 ms in three runs (logits 895,
+// and with G in two bfloats dx 1346, dweight 1165: 0.87, 1.15 and 1.33 PFLOP/s), fp32, 2997 labelled rows of 4995 on 10007 x 202 369 us.
 #include "ftp_training.h"
 #include "ftp_product.h"
 
